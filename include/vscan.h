@@ -9,6 +9,12 @@
  *   Stage 2 (Sec. 4.2), at a middle LLM layer, per sequence:
  *     vscan_score (QK mode)         head mean of softmax(q_last . K) over a span   (Eq. 5)
  *     vscan_llm_prune               that score + top-k + compaction of hidden / K / V / position ids
+ * and what the layers around the pruned sequence need to go on from there (no counterpart in the paper, which leaves
+ * "structure and format unchanged" to the model's own code):
+ *     vscan_rope                    rotary positions with several axes, from position planes as vscan_llm_prune keeps them
+ *     vscan_kv_plan                 block tables, slot maps and offsets of a paged KV cache from request lengths
+ *     vscan_kv_write                K / V rows into a cache held in 8 bits with a scale per block of tokens and head
+ *     vscan_kv_attention            attention over that cache
  *
  * Conventions shared by every entry point
  *   - Returns a vscan_status.  Nothing throws, aborts or traps.  Arguments are validated on the
@@ -357,10 +363,170 @@ vscan_status vscan_llm_prune_ragged(const vscan_prune_ragged_desc* desc, void* w
                                     void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * vscan_rope: rotary positions with several axes (time, height, width, ...) on queries and keys.
+ *
+ * Pair i of a head vector, i in [0, rot_dim / 2), is turned by the angle
+ *   a_i = pos_ids[axis[i]][b][s] * inv_freq[i]:   (x, y) -> (x cos a_i - y sin a_i, y cos a_i + x sin a_i);
+ * channels from rot_dim on pass through.  Angles are taken in 64 bits (far positions keep their fraction of a turn),
+ * the rotation in 32, with one rounding to `dtype`.  inverse != 0 turns by -a_i: the gradient of the same call.
+ *   pairing   VSCAN_ROPE_HALVES: pair i = channels (i, i + rot_dim / 2); VSCAN_ROPE_ADJACENT: (2i, 2i + 1)
+ *   pos_ids   [pos_planes][batch][seq_len] int32, the layout of vscan_llm_prune
+ *   inv_freq  [rot_dim / 2] float32;  axis [rot_dim / 2] int32, the plane of each pair (clamped to [0, pos_planes) on the device)
+ *   q, k      [batch][heads][seq_len][head_dim] by strides: element (b, h, s, c) lies at
+ *             b * stride[0] + h * stride[1] + s * stride[2] + c.  Either of q and k may be NULL (with its output).
+ *   q_out, k_out  likewise.  An output may be its own input (the same pointer and strides): then the call works in place.
+ *             Otherwise outputs must not overlap inputs.  The elements of one output must not overlap each other.
+ * head_dim a multiple of 8, at most 512; rot_dim even, 2 .. head_dim; strides multiples of 16 bytes; pos_planes 1 .. 16.
+ * No workspace.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { VSCAN_ROPE_HALVES = 0, VSCAN_ROPE_ADJACENT = 1 } vscan_rope_pairing;
+
+typedef struct {
+  int32_t dtype;   /* vscan_dtype */
+  int32_t pairing; /* vscan_rope_pairing */
+  int32_t inverse;
+  int32_t batch, seq_len, q_heads, k_heads, head_dim, rot_dim, pos_planes;
+  const int32_t* pos_ids;
+  const float* inv_freq;
+  const int32_t* axis;
+  const void* q;
+  void* q_out;
+  const void* k;
+  void* k_out;
+  int64_t q_stride[3], q_out_stride[3], k_stride[3], k_out_stride[3]; /* sequence, head, token; in elements */
+} vscan_rope_desc;
+
+vscan_status vscan_rope(const vscan_rope_desc* desc, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The paged KV cache held in 8 bits.
+ *
+ * A cache is a pool of num_blocks blocks; a block holds block_size consecutive tokens of one sequence:
+ *   k_cache, v_cache  [num_blocks][kv_heads][block_size][head_dim] of `kv_dtype` (one byte an element)
+ *   k_scale, v_scale  [num_blocks][kv_heads] float32; an element stands for code * scale
+ *   block_table       [batch][max_blocks] int32: block of tokens [j * block_size, (j + 1) * block_size) of a sequence
+ *   kv_len            [batch] int32: tokens of each sequence, the new ones of this step included
+ *   row_offset        [batch + 1] int32, from 0, not falling: sequence b has n_b = row_offset[b + 1] - row_offset[b] new
+ *                     rows in this step; they are its last n_b tokens.
+ * Rows (of k, v, q, outputs) are given in one of two layouts, element (row, h, c) at
+ *   packed  (padded = 0)  (row_offset[b] + i) * stride[2] + h * stride[1] + c;  `rows` = rows of the whole buffer
+ *   padded  (padded = 1)  b * stride[0] + i * stride[2] + h * stride[1] + c;    `rows` = rows per sequence
+ * with i in [0, n_b); strides are in elements and multiples of 16 bytes.  The padded layout is the one in which
+ * vscan_llm_prune writes k_out and v_out.
+ * head_dim: a multiple of 16, at most 256.  block_size: 16, 32, 64, 128 or 256.
+ *
+ * vscan_kv_plan: from the lengths of the requests to what the other two calls take, in one launch without the host
+ * seeing any of them.
+ *   past_len  [batch] int32 tokens that each sequence has; new_len [batch] int32 tokens that it gets; a negative
+ *             new_len takes tokens off its end (an ended request: -past_len; survivors of a pruning; rejected drafts).
+ *   free_ring [num_blocks] int32 ring of free blocks, ring_state [2] int64 {head, tail}: entries head .. tail - 1
+ *             (modulo num_blocks) are free.  Blocks are taken at the head, in the order of the sequences, and put back at
+ *             the tail; those put back in a call are not taken in the same call.
+ *   Written:  kv_len [batch], row_offset [batch + 1], ring_state_out [2] (not ring_state itself: a step can be planned
+ *             again), the table columns of the blocks that were taken (all others stay as they are), the ring entries of
+ *             the blocks that were put back; optional slot_map [rows] int64 (block * block_size + place in the block) and
+ *             row_pos [rows] int32 (position in the sequence) of each new row, packed; entries from row_offset[batch] on
+ *             are left as they were.
+ *   report    [4] int32: {code, blocks taken, blocks put back, new rows}.  code 0, or a sum of 1 (the ring has too few
+ *             blocks), 2 (a sequence is longer than max_blocks * block_size), 4 (more new rows than `rows`), 8 (a length
+ *             below zero), 16 (ring_state is not a state of this ring).  Unless code is 0 nothing is planned: kv_len = past_len
+ *             (held between 0 and what the table has room for), row_offset all 0, ring_state_out = ring_state, all else untouched, so the calls
+ *             that follow do nothing for this step; the other figures are then what the step would have needed (at most 2^31 - 1).
+ * Limit of this build: batch <= 8192.  No workspace.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { VSCAN_KV_E4M3 = 0, VSCAN_KV_I8 = 1 } vscan_kv_dtype;
+
+typedef struct {
+  int32_t batch, block_size, num_blocks, max_blocks, rows;
+  const int32_t* past_len;
+  const int32_t* new_len;
+  int32_t* block_table;
+  int32_t* free_ring;
+  const int64_t* ring_state;
+  int32_t* kv_len;
+  int32_t* row_offset;
+  int64_t* slot_map;
+  int32_t* row_pos;
+  int64_t* ring_state_out;
+  int32_t* report;
+} vscan_kv_plan_desc;
+
+vscan_status vscan_kv_plan(const vscan_kv_plan_desc* desc, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * vscan_kv_write: the new rows of K and V into the cache.
+ *
+ * The scale of a (block, head) is 2^e with the least e in [-48, 48] such that every |element| <= qmax * 2^e (qmax 448 for E4M3, 127 for I8;
+ * larger elements saturate); codes are element / 2^e, rounded to nearest, ties to even.  A power of two divides without
+ * rounding, and when a block that already holds tokens gets larger ones its scale grows to the new 2^e and its codes are
+ * divided by the ratio: without loss for E4M3 (but for codes that get below its normal range), with one more rounding for I8.
+ * A block whose first token is written in this call starts afresh, whatever its scale was.  A NaN or an infinity in a
+ * (block, head) makes that scale NaN: all that is read from it is NaN until the block starts afresh.
+ * Places behind a sequence's last token keep what they hold.  Rows of a sequence with kv_len < n_b, tokens behind the
+ * table's last column, and blocks whose table entry is not in [0, num_blocks) are not written.  No two sequences may
+ * write into the same block.  No workspace.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype;    /* vscan_dtype of k and v */
+  int32_t kv_dtype; /* vscan_kv_dtype */
+  int32_t batch, kv_heads, head_dim, block_size, num_blocks, max_blocks, rows, padded;
+  const void* k;
+  const void* v;
+  int64_t k_stride[3], v_stride[3]; /* sequence (padded only), head, row */
+  const int32_t* kv_len;
+  const int32_t* row_offset;
+  const int32_t* block_table;
+  void* k_cache;
+  void* v_cache;
+  float* k_scale;
+  float* v_scale;
+} vscan_kv_write_desc;
+
+vscan_status vscan_kv_write(const vscan_kv_write_desc* desc, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * vscan_kv_attention: out = softmax(scale * q K^T) V over the cache, per sequence and query head; query head h reads KV head
+ * floor(h * kv_heads / q_heads).
+ *   causal != 0: row i of the n_b new rows stands at kv_len - n_b + i and sees the tokens up to itself; else every row sees
+ *   all kv_len tokens (an encoder's states, for instance).  A row that sees nothing gives 0 (and lse -inf).
+ *   q, out    rows of q_heads x head_dim of `dtype` in the layouts above, each with its own strides
+ *   lse       optional float32 output: log of the sum of exp(scale * q k) over the tokens seen, element (row, h) at
+ *             row (packed) or b, i (padded) by lse_stride = {sequence, head, row}
+ *   max_q_len no sequence has more new rows than this (rows behind it are left as they were); 1 for decode steps.  The launch
+ *             and the workspace are chosen from it.
+ * Rows that no sequence owns are left as they were.  Tokens behind the table's last column, and tokens in blocks whose
+ * table entry is not in [0, num_blocks), count as not there; vscan_check then gives VSCAN_ERR_INVALID_ARG.
+ * Scores, softmax statistics and sums are float32.
+ * Workspace: vscan_kv_attention_workspace_bytes(desc), which reads the sizes only.
+ * Limits of this build: q_heads / kv_heads <= 64; batch <= 8192.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype;    /* vscan_dtype of q and out */
+  int32_t kv_dtype; /* vscan_kv_dtype */
+  int32_t batch, q_heads, kv_heads, head_dim, block_size, num_blocks, max_blocks, rows, padded;
+  int32_t max_q_len, causal;
+  float scale;
+  const void* q;
+  void* out;
+  float* lse;
+  int64_t q_stride[3], out_stride[3], lse_stride[3]; /* sequence (padded only), head, row */
+  const int32_t* kv_len;
+  const int32_t* row_offset;
+  const int32_t* block_table;
+  const void* k_cache;
+  const void* v_cache;
+  const float* k_scale;
+  const float* v_scale;
+} vscan_kv_attention_desc;
+
+size_t vscan_kv_attention_workspace_bytes(const vscan_kv_attention_desc* desc);
+vscan_status vscan_kv_attention(const vscan_kv_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Housekeeping.
  * vscan_check: synchronises `stream` and reads the device status word at the start of a workspace
- * that the preceding call used; VSCAN_OK, VSCAN_ERR_TIMEOUT (a bounded wait expired) or
- * VSCAN_ERR_CUDA.  Only calls that take a non-empty workspace write that word.
+ * that the preceding call used; VSCAN_OK, VSCAN_ERR_TIMEOUT (a bounded wait expired),
+ * VSCAN_ERR_INVALID_ARG (vscan_kv_attention met a block or a length that is out of range) or VSCAN_ERR_CUDA.  Only calls that take a non-empty workspace write that word.
  * vscan_last_cuda_error: cudaError_t value of the last failing runtime call on this thread (0 if none).
  * vscan_kernel_launches: number of kernels this library has launched in this process so far.
  * ------------------------------------------------------------------------------------------- */

@@ -82,6 +82,17 @@ extern "C" vscan_status vscan_check(const void* workspace, void* stream) {
   VSCAN_CUDA_TRY(cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost,
                                  static_cast<cudaStream_t>(stream)));
   VSCAN_CUDA_TRY(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
+  if (word & kStatusFlags) {
+    uint32_t flags[1024];
+    const uint32_t n = word & ~kStatusFlags;
+    if (n > 1024) return VSCAN_ERR_INVALID_ARG;   // not a status that any call leaves
+    VSCAN_CUDA_TRY(cudaMemcpyAsync(flags, static_cast<const char*>(workspace) + kStatusBytes, n * sizeof(uint32_t),
+                                   cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream)));
+    VSCAN_CUDA_TRY(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
+    for (uint32_t i = 0; i < n; ++i)
+      if (flags[i]) return VSCAN_ERR_INVALID_ARG;
+    return VSCAN_OK;
+  }
   return word == 0 ? VSCAN_OK : VSCAN_ERR_TIMEOUT;
 }
 

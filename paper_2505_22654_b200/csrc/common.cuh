@@ -82,6 +82,10 @@ inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
 
 // The first 256 bytes of every workspace hold the device status word.
 constexpr size_t kStatusBytes = 256;
+// A status word with this bit set says that as many flag words as its other bits say follow the first kStatusBytes, one
+// for each CTA; a flag that is not 0 is a call that met invalid device-side arguments.  (A single word would need a
+// memset in the stream before every launch.)
+constexpr uint32_t kStatusFlags = 0x80000000u;
 
 // Opt a kernel into more than 48 KB of dynamic shared memory (cached per kernel per device).
 template <typename K>
