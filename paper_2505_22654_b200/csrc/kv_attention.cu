@@ -3,7 +3,7 @@
 // One pass over the keys with a running maximum and sum per query row.  K and V are turned from codes in registers, the
 // block's scale goes onto the scores (K) and onto the weights (V).  Queries of the heads that share a KV head, and of
 // neighbouring new rows, form a tile, so that a key that was read once serves all of them.
-#include "kv_attention.cuh"
+#include "kv_attention_mma.cuh"
 
 namespace vscan {
 namespace kv {
@@ -26,28 +26,15 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
   __shared__ ScheduleShared sched;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dependency_wait();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = kStatusFlags | gridDim.x;
-  long long begin, quota, total;
-  locate<kFmaThreads>(p, sched, begin, quota, total);
+  if (blockIdx.x == 0 && threadIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = 0; }
+  Stretch st = locate<kFmaThreads, false>(p, sched);
   if (threadIdx.x == 0) { p.boundary[blockIdx.x].seg1 = 0; p.flags[blockIdx.x] = 0; }
-  if (begin >= total) return;
-  const long long end = min(begin + quota, total);
-  int b = sched.b;
-  long long seq0 = sched.seq0, w = begin;
   bool bad = false;
-  while (w < end) {
-    const Sequence s = sequence_at(p, b);
-    if (w >= seq0 + s.weight) { seq0 += s.weight; ++b; continue; }
-    const long long seg = (w - seq0) / s.units, seg0 = seq0 + seg * s.units;
-    const int head = static_cast<int>(seg / s.tiles), tile = static_cast<int>(seg - static_cast<long long>(head) * s.tiles);
-    const bool whole = s.units <= kWhole;
-    if (whole && w != seg0) { w = seg0 + s.units; continue; }     // the CTA before this one has it
-    const int u0 = static_cast<int>(w - seg0), u1 = whole ? s.units : static_cast<int>(min(end - seg0, static_cast<long long>(s.units)));
-    if (w == begin && u0 > 0 && threadIdx.x == 0) {
-      Boundary bd = {seg0, seg0 + s.units, quota, b, head, tile, 0};
-      p.boundary[blockIdx.x] = bd;
-    }
-    w += u1 - u0;
+  Piece pc;
+  while (next_piece(p, st, pc)) {
+    const Sequence& s = pc.s;
+    const int b = pc.b, head = pc.head, tile = pc.tile, u0 = pc.u0, u1 = pc.u1;
+    if (u0 > 0 && threadIdx.x == 0) p.boundary[blockIdx.x] = {pc.seg0, pc.seg0 + s.units, st.quota, b, head, tile, 0};
     const int n_rows = min(R, s.n * p.group - tile * R);
     if (p.kv_len[b] > s.len) bad = true;
 
@@ -190,37 +177,62 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------- joining cut segments
-// CTA (c, r): where the stretch of CTA c starts inside a segment that is cut there for the first time, row r of its tile
-// from the pieces: the last piece of CTA c - 1, then the first ones of c, c + 1, ... up to the segment's end.  The pieces
-// are added in that order, so results do not depend on timing.
-constexpr int kJoinThreads = 128;
+// Where the stretch of worker k starts inside a segment that is cut there for the first time, the segment's rows from its
+// pieces: the last piece of worker k - 1, then the first ones of k, k + 1, ... up to the segment's end.  The pieces are
+// added in that order, so results do not depend on timing.  A warp takes a row; where workers are warps (few pieces a
+// segment), a warp takes a boundary.
+constexpr int kJoinThreads = 256;
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
   grid_dependency_wait();
-  const int c = blockIdx.x + 1, r = blockIdx.y;
-  const Boundary bd = p.boundary[c];
-  if (bd.seg1 == 0 || (c - 1) * bd.quota > bd.seg0) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool solo = p.status[1] != 0;
+  if (solo && warp >= kWorkersPerCta) return;
+  const int k0 = solo ? blockIdx.x * kWorkersPerCta + warp : blockIdx.x;
+  if (k0 == 0) return;
+  const Boundary bd = p.boundary[k0];
+  if (bd.seg1 == 0 || (k0 - 1) * bd.quota > bd.seg0) return;
   const Sequence s = sequence_at(p, bd.b);
-  if (r >= min(p.tile_rows, s.n * p.group - bd.tile * p.tile_rows)) return;
-  const int D = p.head_dim, R = p.tile_rows;
+  const int D = p.head_dim, R = p.tile_rows, rows = min(R, s.n * p.group - bd.tile * R);
   const size_t stride = partial_floats(R, D);
-  const int last = static_cast<int>((bd.seg1 - 1) / bd.quota);       // CTA of the segment's last unit
-  auto piece = [&](int k) { return p.partial + (static_cast<size_t>(k) * 2 + (k < c ? 1 : 0)) * stride; };
-  float top = -INFINITY;
-  for (int k = c - 1; k <= last; ++k) top = fmaxf(top, piece(k)[R * D + r]);
-  const float base = top == -INFINITY ? 0.f : top;
-  float den = 0.f;
-  for (int k = c - 1; k <= last; ++k) den = fmaf(ex2(piece(k)[R * D + r] - base), piece(k)[R * D + R + r], den);
-  const RowAt at = row_at(p, bd.tile, bd.head, r);
-  char* out = out_at(p, bd.b, s.first, at);
-  for (int i = threadIdx.x; i < D; i += kJoinThreads) {
-    float o = 0.f;
-#pragma unroll 4
-    for (int k = c - 1; k <= last; ++k) o = fmaf(ex2(piece(k)[R * D + r] - base), piece(k)[r * D + i], o);
-    store_out<T>(out, i, den == 0.f ? 0.f : o / den);
+  const int pieces = static_cast<int>((bd.seg1 - 1) / bd.quota) - k0 + 2;   // up to the worker of the segment's last unit
+  const float* first = p.partial + (static_cast<size_t>(k0) * 2 - 1) * stride;   // slot 1 of k0 - 1; then slot 0 of k0, ...
+  auto piece = [&](int i) { return first + (i == 0 ? 0 : 2 * i - 1) * stride; };
+  for (int r = solo ? 0 : warp; r < rows; r += solo ? 1 : kJoinThreads / 32) {
+    float top = -INFINITY;
+    for (int i = lane; i < pieces; i += 32) top = fmaxf(top, piece(i)[R * D + r]);
+    top = warp_max(top);
+    const float base = top == -INFINITY ? 0.f : top;
+    float den = 0.f, acc[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[c] = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < pieces; ++i) {
+      const float* part = piece(i);
+      const float f = ex2(part[R * D + r] - base);
+      den = fmaf(f, part[R * D + R + r], den);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int c = half * 128 + lane * 4;
+        if (c < D) {
+          const float4 o = *reinterpret_cast<const float4*>(part + r * D + c);
+          acc[half * 4] = fmaf(f, o.x, acc[half * 4]);
+          acc[half * 4 + 1] = fmaf(f, o.y, acc[half * 4 + 1]);
+          acc[half * 4 + 2] = fmaf(f, o.z, acc[half * 4 + 2]);
+          acc[half * 4 + 3] = fmaf(f, o.w, acc[half * 4 + 3]);
+        }
+      }
+    }
+    const RowAt at = row_at(p, bd.tile, bd.head, r);
+    char* out = out_at(p, bd.b, s.first, at);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const int d = (c / 4) * 128 + lane * 4 + c % 4;
+      if (d < D) store_out<T>(out, d, den == 0.f ? 0.f : acc[c] / den);
+    }
+    if (lane == 0 && p.lse) *lse_at(p, bd.b, s.first, at) = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.69314718055994531f;
   }
-  if (threadIdx.x == 0 && p.lse) *lse_at(p, bd.b, s.first, at) = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -263,18 +275,26 @@ static vscan_status validate_attention(const vscan_kv_attention_desc* d) {
 }
 
 // Rows of a tile and CTAs of the launch
-struct Plan { int tile_rows; unsigned ctas; };
+struct Plan { int tile_rows; unsigned ctas; bool mma; };
 
 static Plan plan_launch(const vscan_kv_attention_desc* d) {
   Plan pl;
   const int group = d->q_heads / d->kv_heads;
   const int64_t want = static_cast<int64_t>(group) * d->max_q_len;
-  pl.tile_rows = want <= 1 ? 1 : want <= 2 ? 2 : want <= 4 ? 4 : 8;
+  pl.mma = d->dtype == VSCAN_BF16;
+  int64_t resident;
+  if (pl.mma) {
+    pl.tile_rows = want <= 8 || d->head_dim > 128 ? 8 : 16;   // 16 rows of 256 channels do not fit the registers
+    resident = d->head_dim > 128 || pl.tile_rows > 8 ? 2 : 3;
+  } else {
+    pl.tile_rows = want <= 1 ? 1 : want <= 2 ? 2 : want <= 4 ? 4 : 8;
+    resident = 4;
+  }
   // as many CTAs as fit the SMs at once, no more than there can be units
   const int64_t rows = d->padded ? static_cast<int64_t>(d->batch) * (d->rows < d->max_q_len ? d->rows : d->max_q_len) : d->rows;
   const int64_t tiles = rows * group / pl.tile_rows + d->batch;
   const int64_t units = (static_cast<int64_t>(d->max_blocks) * d->block_size + kUnit - 1) / kUnit;
-  int64_t most = 148 * 4;
+  int64_t most = 148 * resident;
   if (units < 1) { if (tiles * d->kv_heads < most) most = tiles * d->kv_heads; }
   else if (tiles * d->kv_heads <= most / units) most = tiles * d->kv_heads * units;
   pl.ctas = static_cast<unsigned>(most < 1 ? 1 : most);
@@ -283,7 +303,7 @@ static Plan plan_launch(const vscan_kv_attention_desc* d) {
 
 // workspace: status word | a flag per CTA | boundaries | partial results
 static size_t flag_bytes(const Plan& pl) { return round_up(pl.ctas * sizeof(uint32_t), 256); }
-static size_t boundary_bytes(const Plan& pl) { return round_up(pl.ctas * sizeof(Boundary), 256); }
+static size_t boundary_bytes(const Plan& pl) { return round_up(pl.ctas * kWorkersPerCta * sizeof(Boundary), 256); }
 
 static size_t fma_smem(int R, int D) { return (static_cast<size_t>(R) * D * (1 + kFmaWarps) + kFmaWarps * 32 * R + 2 * kFmaWarps * R) * 4; }
 
@@ -306,14 +326,40 @@ static vscan_status launch_fma(const AttnParams& p, const Plan& pl, cudaStream_t
   return VSCAN_OK;
 }
 
+template <int KV, int DP>
+static vscan_status launch_mma(const AttnParams& p, const Plan& pl, cudaStream_t stream) {
+  const size_t smem = (static_cast<size_t>(4) * pl.tile_rows * (DP + 2)) * sizeof(float);
+  constexpr int MT = DP == 256 ? 1 : 2;
+#define VSCAN_MMA_CASE(NT)                                                                                          \
+  if (pl.tile_rows == 8 * NT) {                                                                                     \
+    VSCAN_CUDA_TRY(allow_smem(mma_kernel<KV, DP, NT, MT>, smem));                                                   \
+    prof_before("kv_attention_mma", stream);                                                                        \
+    VSCAN_CUDA_TRY(launch_dependent(mma_kernel<KV, DP, NT, MT>, dim3(pl.ctas), dim3(kMmaThreads), smem, stream, p)); \
+    prof_after(stream);                                                                                             \
+    VSCAN_AFTER_LAUNCH();                                                                                           \
+  }
+  VSCAN_MMA_CASE(1)
+  if constexpr (DP <= 128) { VSCAN_MMA_CASE(2) }
+#undef VSCAN_MMA_CASE
+  return VSCAN_OK;
+}
+
+template <typename T, int KV>
+static vscan_status launch_scores(const AttnParams& p, const Plan& pl, cudaStream_t stream) {
+  if constexpr (sizeof(T) == 2)
+    return p.head_dim <= 64 ? launch_mma<KV, 64>(p, pl, stream) : p.head_dim <= 128 ? launch_mma<KV, 128>(p, pl, stream)
+                                                                                    : launch_mma<KV, 256>(p, pl, stream);
+  else return launch_fma<T, KV>(p, pl, stream);
+}
+
 template <typename T>
 static vscan_status launch_attention(const AttnParams& p, const Plan& pl, int kv_dtype, cudaStream_t stream) {
-  const vscan_status st = kv_dtype == VSCAN_KV_E4M3 ? launch_fma<T, VSCAN_KV_E4M3>(p, pl, stream) : launch_fma<T, VSCAN_KV_I8>(p, pl, stream);
+  const vscan_status st = kv_dtype == VSCAN_KV_E4M3 ? launch_scores<T, VSCAN_KV_E4M3>(p, pl, stream) : launch_scores<T, VSCAN_KV_I8>(p, pl, stream);
   if (st != VSCAN_OK) return st;
   // nothing can have been cut when the table has room for kWhole units only, or when one CTA did it all
   if (static_cast<int64_t>(p.max_blocks) * p.block_size <= kWhole * kUnit || pl.ctas == 1) return VSCAN_OK;
   prof_before("kv_attention_join", stream);
-  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, dim3(pl.ctas - 1, pl.tile_rows), dim3(kJoinThreads), 0, stream, p));
+  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, dim3(pl.ctas), dim3(kJoinThreads), 0, stream, p));
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
   return VSCAN_OK;
@@ -329,7 +375,7 @@ extern "C" size_t vscan_kv_attention_workspace_bytes(const vscan_kv_attention_de
       d->head_dim > 256 || d->q_heads / d->kv_heads > 64)
     return kStatusBytes;
   const kv::Plan pl = kv::plan_launch(d);
-  return kStatusBytes + kv::flag_bytes(pl) + kv::boundary_bytes(pl) + round_up(2 * static_cast<size_t>(pl.ctas) * kv::partial_floats(pl.tile_rows, d->head_dim) * 4, 256);
+  return kStatusBytes + kv::flag_bytes(pl) + kv::boundary_bytes(pl) + round_up(2 * static_cast<size_t>(pl.ctas) * kv::kWorkersPerCta * kv::partial_floats(pl.tile_rows, d->head_dim) * 4, 256);
 }
 
 extern "C" vscan_status vscan_kv_attention(const vscan_kv_attention_desc* d, void* workspace, size_t workspace_bytes, void* stream_) {

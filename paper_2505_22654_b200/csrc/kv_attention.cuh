@@ -30,16 +30,19 @@ struct AttnParams {
 };
 
 // The work is a line of units of kUnit tokens: sequences in order, in a sequence KV head by KV head, tile by tile, in a tile
-// the units of its keys.  Each of the G CTAs of a launch takes an equal stretch, whatever the lengths are, so one long
-// sequence among short ones does not hold up the launch.  A segment (one tile, one KV head) that is not longer than
-// kWhole units stays with the CTA that reaches its start; a longer one may be cut, and its pieces are joined afterwards.
+// the units of its keys.  Each worker of a launch takes an equal stretch, whatever the lengths are, so one long sequence
+// among short ones does not hold up the launch.  A segment (one tile, one KV head) that is not longer than `whole` units
+// stays with the worker that reaches its start; a longer one may be cut, and its pieces are joined afterwards.
+// Workers are CTAs whose warps share the tokens of a segment, or, where there are at least as many segments as CTAs, single
+// warps: then nothing has to be exchanged within a CTA, and the balance is finer.
 constexpr int kUnit = 64;
 constexpr int kWhole = 4;
+constexpr int kWorkersPerCta = 4;
 
-struct Boundary {       // what lies at the start of a CTA's stretch
+struct Boundary {       // what lies at the start of a worker's stretch
   long long seg0, seg1; // the segment that is cut there, as places on the line; seg1 = 0: none
   long long quota;
-  int b, head, tile, pad;
+  int b, head, tile, solo;   // solo: the workers are warps
 };
 
 struct Sequence {       // of one sequence: new rows, keys, tiles, units of a segment
@@ -59,49 +62,99 @@ __device__ __forceinline__ Sequence sequence_at(const AttnParams& p, int b) {
 }
 
 struct ScheduleShared {
-  long long warp_sums[32];
-  long long seq0;
-  int b;
+  long long weight[32], segments[32];
+  long long seq0[kWorkersPerCta];
+  int b[kWorkersPerCta];
 };
 
-// Where this CTA's stretch starts: the sequence and its place on the line.  Called by all THREADS threads.
-template <int THREADS>
-__device__ __forceinline__ void locate(const AttnParams& p, ScheduleShared& sh, long long& begin, long long& quota, long long& total) {
+struct Stretch {          // of a worker: [begin, end) of the line, where its first sequence is
+  long long begin, end, quota, seq0;
+  int b, worker, whole;
+  bool solo;
+};
+
+// The stretch of this thread's worker.  Called by all THREADS threads; SOLO: whether warps may be workers.
+template <int THREADS, bool SOLO>
+__device__ __forceinline__ Stretch locate(const AttnParams& p, ScheduleShared& sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = (p.batch + THREADS - 1) / THREADS, b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
-  long long sum = 0;
-  for (int b = b0; b < b1; ++b) sum += sequence_at(p, b).weight;
+  long long sum = 0, segments = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Sequence s = sequence_at(p, b);
+    sum += s.weight;
+    segments += static_cast<long long>(s.tiles) * p.kv_heads;
+  }
   long long incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const long long t = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += t;
+    if (SOLO) segments += __shfl_xor_sync(0xffffffffu, segments, o);
   }
-  if (lane == 31) sh.warp_sums[warp] = incl;
-  if (threadIdx.x == 0) sh.b = -1;
+  if (lane == 31) { sh.weight[warp] = incl; sh.segments[warp] = segments; }
   __syncthreads();
-  long long before = 0;
-  total = 0;
+  long long before = 0, total = 0, all_segments = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
-    if (w < warp) before += sh.warp_sums[w];
-    total += sh.warp_sums[w];
+    if (w < warp) before += sh.weight[w];
+    total += sh.weight[w];
+    all_segments += sh.segments[w];
   }
-  quota = max((total + gridDim.x - 1) / gridDim.x, 1ll);
-  begin = blockIdx.x * quota;
-  long long at = before + incl - sum;
-  if (at <= begin && begin < at + sum) {
-    for (int b = b0; b < b1; ++b) {
-      const long long w = sequence_at(p, b).weight;
-      if (begin < at + w) { sh.b = b; sh.seq0 = at; break; }
-      at += w;
+  Stretch st;
+  st.solo = SOLO && all_segments >= gridDim.x;
+  const int mine = st.solo ? kWorkersPerCta : 1;
+  st.whole = st.solo && (static_cast<long long>(p.max_blocks) << p.shift) > kWhole * kUnit ? 1 : kWhole;
+  const long long workers = static_cast<long long>(gridDim.x) * mine;
+  st.quota = max((total + workers - 1) / workers, st.solo ? 1ll : 2ll);
+  const long long at = before + incl - sum;
+  for (int k = 0; k < mine; ++k) {
+    const long long begin = (static_cast<long long>(blockIdx.x) * mine + k) * st.quota;
+    if (at <= begin && begin < at + sum) {
+      long long first = at;
+      for (int b = b0; b < b1; ++b) {
+        const long long w = sequence_at(p, b).weight;
+        if (begin < first + w) { sh.b[k] = b; sh.seq0[k] = first; break; }
+        first += w;
+      }
     }
   }
   __syncthreads();
+  const int k = st.solo ? warp : 0;
+  st.worker = blockIdx.x * mine + k;
+  st.begin = min(st.worker * st.quota, total);
+  st.end = min(st.begin + st.quota, total);
+  st.b = sh.b[k];                   // not set, and not used, where the stretch is empty
+  st.seq0 = sh.seq0[k];
+  return st;
 }
 
-// Floats of one partial result: tile_rows x head_dim sums, then their maxima, then their denominators
-__host__ __device__ inline size_t partial_floats(int tile_rows, int head_dim) { return static_cast<size_t>(tile_rows) * (head_dim + 2); }
+// The next piece of a worker's stretch
+struct Piece {
+  Sequence s;
+  long long seg0;
+  int b, head, tile, u0, u1;
+};
+__device__ __forceinline__ bool next_piece(const AttnParams& p, Stretch& st, Piece& pc) {
+  while (st.begin < st.end) {
+    pc.s = sequence_at(p, st.b);
+    if (st.begin >= st.seq0 + pc.s.weight) { st.seq0 += pc.s.weight; ++st.b; continue; }
+    const long long seg = (st.begin - st.seq0) / pc.s.units;
+    pc.seg0 = st.seq0 + seg * pc.s.units;
+    pc.head = static_cast<int>(seg / pc.s.tiles);
+    pc.tile = static_cast<int>(seg - static_cast<long long>(pc.head) * pc.s.tiles);
+    pc.b = st.b;
+    const bool whole = pc.s.units <= st.whole;
+    pc.u0 = static_cast<int>(st.begin - pc.seg0);
+    st.begin = pc.seg0 + pc.s.units;
+    if (whole && pc.u0 > 0) continue;                    // the worker before this one has it
+    pc.u1 = whole ? pc.s.units : static_cast<int>(min(st.end - pc.seg0, static_cast<long long>(pc.s.units)));
+    return true;
+  }
+  return false;
+}
+
+// Floats of one partial result: tile_rows x head_dim sums, then their maxima, then their denominators; a multiple of 16 bytes
+__host__ __device__ inline size_t partial_floats(int tile_rows, int head_dim) { return (static_cast<size_t>(tile_rows) * (head_dim + 2) + 3) & ~size_t{3}; }
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
