@@ -1,5 +1,6 @@
-"""Builds libvscan.so (sm_100a) in-tree with nvcc.  No torch types cross the boundary, so the
-library is a plain shared object loaded with ctypes."""
+"""Builds libvscan.so (sm_100a) in-tree with nvcc, and with the host compiler the module _calls.so that marshals the
+arguments of the calls a decode step makes.  No torch types cross the library's boundary, so it is a plain shared object
+loaded with ctypes; only _calls.so is built against torch."""
 from __future__ import annotations
 
 import hashlib
@@ -12,6 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB_PATH = os.path.join(HERE, "libvscan.so")
+
+CALLS_PATH = os.path.join(HERE, "_calls.so")
 
 STAMP_PATH = LIB_PATH + ".digest"
 
@@ -38,9 +41,9 @@ def source_digest() -> str:
 
 
 def _stale() -> bool:
-    """True when libvscan.so is missing or was built from other sources than the ones on disk.  The
+    """True when libvscan.so or _calls.so is missing or was built from other sources than the ones on disk.  The
     digest recorded next to the library decides, not file times (a copied tree has arbitrary ones)."""
-    if not os.path.exists(LIB_PATH) or not os.path.exists(STAMP_PATH):
+    if not os.path.exists(LIB_PATH) or not os.path.exists(CALLS_PATH) or not os.path.exists(STAMP_PATH):
         return True
     with open(STAMP_PATH) as f:
         return f.read().strip() != source_digest()
@@ -50,8 +53,20 @@ def have_nvcc() -> bool:
     return os.path.exists(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc")
 
 
+def _calls_command():
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    cuda = os.path.dirname(os.path.dirname(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"))
+    dirs = [INCLUDE, *cpp_extension.include_paths(), os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return (["g++", "-shared", "-fPIC", "-O2", "-std=c++17", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+            + [f"-I{d}" for d in dirs] + [os.path.join(CSRC, "calls.cpp"), "-o", CALLS_PATH, f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ into one shared library next to this file."""
+    """Compile every .cu under csrc/ into one shared library next to this file, and calls.cpp into the module beside it."""
     if not force and not _stale():
         return LIB_PATH
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
@@ -62,9 +77,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += sources()
+    calls = subprocess.Popen(_calls_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
+    said = calls.communicate()[0]
     if res.returncode != 0:
         raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+    if calls.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + said)
     with open(STAMP_PATH, "w") as f:
         f.write(digest + "\n")
     if verbose:

@@ -7,6 +7,8 @@ fallback of any kind: if the shared library is missing or a call fails, an excep
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import os
 
 import torch
@@ -391,52 +393,21 @@ def vscan_llm_prune(q_last, k, v, hidden, pos_ids, n_sys, n_vis, n_txt, k_keep, 
 
 
 # ------------------------------------------------------------------------------------------ positions and the 8-bit KV cache
-def _dev(device, *tensors):
-    """Data pointers of tensors that have to be on one GPU; a missing one (None) gives None."""
-    ptrs = []
-    for t in tensors:
-        if t is None:
-            ptrs.append(None)
-            continue
-        if t.device != device:
-            raise ValueError(f"tensors on {device} and {t.device} in one call")
-        ptrs.append(t.data_ptr())
-    return ptrs
+_CALLS = None
 
 
-def _gpu(t):
-    if not t.is_cuda:
-        raise ValueError("tensors must be CUDA tensors")
-    return t.device
-
-
-def _whole(t, dtype, shape, name):
-    """A contiguous tensor of this type and shape (-1: any), or an error that names it."""
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: {dtype} wanted, {t.dtype} given")
-    if t.dim() != len(shape) or any(w >= 0 and w != s for w, s in zip(shape, t.shape)):
-        raise ValueError(f"{name}: shape {tuple(shape)} wanted, {tuple(t.shape)} given")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-
-
-def _enqueue(fn_name, desc, device, *workspace):
-    """Calls the entry point on the current stream of the tensors' device, which becomes the current one for the call."""
-    if device.index == torch.cuda.current_device():
-        st = getattr(lib(), fn_name)(C.byref(desc), *workspace, torch.cuda.current_stream(device).cuda_stream)
-    else:
-        with torch.cuda.device(device):
-            st = getattr(lib(), fn_name)(C.byref(desc), *workspace, torch.cuda.current_stream(device).cuda_stream)
-    if st != OK:
-        raise VScanError(st, fn_name)
-
-
-def _strides(t, order, name):
-    """Strides of the leading dimensions of `t` in the given order; its last dimension must be contiguous."""
-    st = t.stride()
-    if t.shape[-1] > 1 and st[-1] != 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
-    return _i64x3(*[0 if i is None or t.shape[i] <= 1 else st[i] for i in order])
+def _calls():
+    """The module that marshals these calls, with the library's entry points in hand."""
+    global _CALLS
+    if _CALLS is None:
+        L = lib()
+        loader = importlib.machinery.ExtensionFileLoader("_calls", _build.CALLS_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
+        loader.exec_module(module)
+        module.init(*[C.cast(getattr(L, "vscan_" + name), C.c_void_p).value
+                      for name in ("rope", "kv_plan", "kv_write", "kv_attention", "kv_attention_workspace_bytes")])
+        _CALLS = module
+    return _CALLS
 
 
 def rope_table(rot_dim, sections, base=10000.0, layout="blocks", device="cuda"):
@@ -471,131 +442,53 @@ def vscan_rope(q, k, pos_ids, inv_freq, axis, pairing=ROPE_HALVES, inverse=False
     """Rotary positions with several axes.  q [B, Hq, S, d] and k [B, Hk, S, d] (either may be None), any strides with a
     contiguous last dimension, pos_ids [planes, B, S] int32, inv_freq and axis [rot_dim / 2] (see rope_table).  inverse turns
     back: the gradient.  An output may be its input.  -> (q_out, k_out)."""
-    x = q if q is not None else k
-    if x is None:
-        raise ValueError("vscan_rope: q or k is needed")
-    device = _gpu(x)
-    B, _, S, d = x.shape
-    P, n = pos_ids.shape[0], inv_freq.shape[0]
-    _whole(pos_ids, torch.int32, (-1, B, S), "pos_ids")
-    _whole(inv_freq, torch.float32, (n,), "inv_freq")
-    _whole(axis, torch.int32, (n,), "axis")
-    desc = RopeDesc(_dtype_code(x), pairing, 1 if inverse else 0, B, S, 0, 0, d, 2 * n, P)
-    desc.pos_ids, desc.inv_freq, desc.axis = _dev(device, pos_ids, inv_freq, axis)
-    if q is not None:
-        q_out = _rope_side(q, q_out, x, "q")
-        desc.q_heads = q.shape[1]
-        desc.q, desc.q_out = _dev(device, q, q_out)
-        desc.q_stride, desc.q_out_stride = _strides(q, (0, 1, 2), "q"), _strides(q_out, (0, 1, 2), "q_out")
-    if k is not None:
-        k_out = _rope_side(k, k_out, x, "k")
-        desc.k_heads = k.shape[1]
-        desc.k, desc.k_out = _dev(device, k, k_out)
-        desc.k_stride, desc.k_out_stride = _strides(k, (0, 1, 2), "k"), _strides(k_out, (0, 1, 2), "k_out")
-    if x.numel() or (k is not None and k.numel()):
-        _enqueue("vscan_rope", desc, device)
+    if q_out is None and q is not None:
+        q_out = torch.empty_like(q)
+    if k_out is None and k is not None:
+        k_out = torch.empty_like(k)
+    st = (_CALLS or _calls()).rope(q, k, pos_ids, inv_freq, axis, pairing, inverse, q_out, k_out)
+    if st != OK:
+        raise VScanError(st, "vscan_rope")
     return q_out, k_out
 
 
-def _rope_side(t, out, like, name):
-    if t.dim() != 4 or t.dtype != like.dtype or (t.shape[0], t.shape[2], t.shape[3]) != (like.shape[0], like.shape[2], like.shape[3]):
-        raise ValueError(f"{name}: [batch, heads, seq_len, head_dim] of one type and size with the other wanted")
-    if out is None:
-        return torch.empty_like(t)
-    if out.shape != t.shape or out.dtype != t.dtype:
-        raise ValueError(f"{name}_out: shape or type differs from {name}")
-    return out
-
-
-def vscan_kv_plan(past_len, new_len, block_table, free_ring, ring_state, block_size, rows=0, out=None):
+def vscan_kv_plan(past_len, new_len, block_table, free_ring, ring_state, block_size, rows=None, out=None):
     """Block tables, slot maps and offsets from request lengths (see include/vscan.h).  past_len, new_len [B] int32,
     block_table [B, max_blocks] int32 and free_ring [num_blocks] int32 (both updated in place), ring_state [2] int64.
     `out`: a dict of the tensors to write (kv_len, row_offset, ring_state_out, report and, if wanted, slot_map and row_pos);
-    what is missing is made here, slot_map and row_pos with `rows` entries.  -> that dict."""
-    device = _gpu(past_len)
-    B = past_len.shape[0]
+    what is missing is made here, slot_map and row_pos with `rows` entries (None: they are not wanted).  -> that dict."""
     o = {} if out is None else out
-
-    def make(name, dtype, size):
-        if name not in o:
-            o[name] = torch.empty(size, dtype=dtype, device=device)
-        elif o[name] is not None:
-            _whole(o[name], dtype, (size,), name)
-        return o[name]
-
-    _whole(past_len, torch.int32, (B,), "past_len")
-    _whole(new_len, torch.int32, (B,), "new_len")
-    _whole(block_table, torch.int32, (B, -1), "block_table")
-    _whole(free_ring, torch.int32, (-1,), "free_ring")
-    _whole(ring_state, torch.int64, (2,), "ring_state")
-    given = [o[name].shape[0] for name in ("slot_map", "row_pos") if o.get(name) is not None]
-    rows = min(given) if given else rows
-    slot_map, row_pos = make("slot_map", torch.int64, rows), make("row_pos", torch.int32, rows)
-    kv_len, row_offset = make("kv_len", torch.int32, B), make("row_offset", torch.int32, B + 1)
-    state_out, report = make("ring_state_out", torch.int64, 2), make("report", torch.int32, 4)
-    desc = KvPlanDesc(B, block_size, free_ring.shape[0], block_table.shape[1], rows,
-                      *_dev(device, past_len, new_len, block_table, free_ring, ring_state, kv_len, row_offset, slot_map, row_pos,
-                            state_out, report))
-    _enqueue("vscan_kv_plan", desc, device)
+    sized = [o[name].shape[0] for name in ("slot_map", "row_pos") if o.get(name) is not None]
+    if sized:
+        rows = min(sized)
+    elif rows is None:
+        rows = 0x7fffffff
+        o.setdefault("slot_map", None)
+        o.setdefault("row_pos", None)
+    if len(o) < 6:
+        B, device = past_len.shape[0], past_len.device
+        for name, dtype, size in (("kv_len", torch.int32, B), ("row_offset", torch.int32, B + 1), ("slot_map", torch.int64, rows),
+                                  ("row_pos", torch.int32, rows), ("ring_state_out", torch.int64, 2), ("report", torch.int32, 4)):
+            if name not in o:
+                o[name] = torch.empty(size, dtype=dtype, device=device)
+    st = (_CALLS or _calls()).kv_plan(past_len, new_len, block_table, free_ring, ring_state, block_size, rows, o["kv_len"], o["row_offset"],
+                                      o["slot_map"], o["row_pos"], o["ring_state_out"], o["report"])
+    if st != OK:
+        raise VScanError(st, "vscan_kv_plan")
     return o
-
-
-_KV_CODES = {torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_I8}
-
-
-def _check_cache(k_cache, v_cache, k_scale, v_scale):
-    """-> (kv dtype code, num_blocks, kv_heads, block_size, head_dim)"""
-    if k_cache.dtype not in _KV_CODES:
-        raise TypeError(f"k_cache: torch.float8_e4m3fn or torch.int8 wanted, {k_cache.dtype} given")
-    if k_cache.dim() != 4:
-        raise ValueError("k_cache: [num_blocks, kv_heads, block_size, head_dim] wanted")
-    nb, h, bs, d = k_cache.shape
-    _whole(k_cache, k_cache.dtype, (nb, h, bs, d), "k_cache")
-    _whole(v_cache, k_cache.dtype, (nb, h, bs, d), "v_cache")
-    _whole(k_scale, torch.float32, (nb, h), "k_scale")
-    _whole(v_scale, torch.float32, (nb, h), "v_scale")
-    return _KV_CODES[k_cache.dtype], nb, h, bs, d
-
-
-def _check_lengths(kv_len, row_offset, block_table):
-    B = kv_len.shape[0]
-    _whole(kv_len, torch.int32, (B,), "kv_len")
-    _whole(row_offset, torch.int32, (B + 1,), "row_offset")
-    _whole(block_table, torch.int32, (B, -1), "block_table")
-    return B, block_table.shape[1]
-
-
-def _row_layout(t, B, heads, d, name):
-    """(rows, padded, strides) of [rows, heads, d] (packed) or [B, heads, rows, d] (padded)."""
-    if t.dim() == 3 and t.shape[1:] == (heads, d):
-        return t.shape[0], 0, _strides(t, (None, 1, 0), name)
-    if t.dim() == 4 and (t.shape[0], t.shape[1], t.shape[3]) == (B, heads, d):
-        return t.shape[2], 1, _strides(t, (0, 1, 2), name)
-    raise ValueError(f"{name}: [rows, {heads}, {d}] or [{B}, {heads}, rows, {d}] wanted, {tuple(t.shape)} given")
 
 
 def vscan_kv_write(k, v, kv_len, row_offset, block_table, k_cache, v_cache, k_scale, v_scale):
     """The new rows of K and V into the 8-bit cache, which is updated in place.  k, v: [rows, Hkv, d] packed by row_offset, or
     [B, Hkv, rows, d] padded (what vscan_llm_prune returns), any strides with a contiguous last dimension."""
-    device = _gpu(k)
-    code, nb, h, bs, d = _check_cache(k_cache, v_cache, k_scale, v_scale)
-    B, cols = _check_lengths(kv_len, row_offset, block_table)
-    rows, padded, k_st = _row_layout(k, B, h, d, "k")
-    if v.shape != k.shape or v.dtype != k.dtype:
-        raise ValueError("v: shape or type differs from k")
-    _, _, v_st = _row_layout(v, B, h, d, "v")
-    desc = KvWriteDesc(_dtype_code(k), code, B, h, d, bs, nb, cols, rows, padded, *_dev(device, k, v), k_st, v_st,
-                       *_dev(device, kv_len, row_offset, block_table, k_cache, v_cache, k_scale, v_scale))
-    _enqueue("vscan_kv_write", desc, device)
+    st = (_CALLS or _calls()).kv_write(k, v, kv_len, row_offset, block_table, k_cache, v_cache, k_scale, v_scale)
+    if st != OK:
+        raise VScanError(st, "vscan_kv_write")
 
 
 def vscan_kv_attention_workspace(q, block_table, k_cache, max_q_len):
     """A workspace for vscan_kv_attention calls of these sizes."""
-    nb, h, bs, d = k_cache.shape
-    rows, padded, _ = _row_layout(q, block_table.shape[0], q.shape[1], d, "q")
-    desc = KvAttentionDesc(_dtype_code(q), _KV_CODES[k_cache.dtype], block_table.shape[0], q.shape[1], h, d, bs, nb, block_table.shape[1],
-                           rows, padded, max_q_len)
-    return Workspace(lib().vscan_kv_attention_workspace_bytes(C.byref(desc)), q.device)
+    return Workspace((_CALLS or _calls()).kv_attention_bytes(q, block_table, k_cache, max_q_len), q.device)
 
 
 def vscan_kv_attention(q, kv_len, row_offset, block_table, k_cache, v_cache, k_scale, v_scale, scale, max_q_len=1, causal=True,
@@ -603,28 +496,14 @@ def vscan_kv_attention(q, kv_len, row_offset, block_table, k_cache, v_cache, k_s
     """Attention of the new rows over the 8-bit cache.  q: [rows, Hq, d] packed by row_offset, or [B, Hq, rows, d] padded;
     out likewise (made here, zeroed, if not given); lse, if given, [rows, Hq] or [B, Hq, rows] float32 receives the log of the
     sum of exponentials.  max_q_len: no sequence has more new rows.  -> out."""
-    device = _gpu(q)
-    code, nb, h, bs, d = _check_cache(k_cache, v_cache, k_scale, v_scale)
-    B, cols = _check_lengths(kv_len, row_offset, block_table)
-    hq = q.shape[1]
-    rows, padded, q_st = _row_layout(q, B, hq, d, "q")
     if out is None:
         out = torch.zeros_like(q)
-    elif out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("out: shape or type differs from q")
-    _, _, o_st = _row_layout(out, B, hq, d, "out")
-    l_st = _i64x3()
-    if lse is not None:
-        if lse.dtype != torch.float32 or lse.shape != q.shape[:-1]:
-            raise ValueError(f"lse: float32 {tuple(q.shape[:-1])} wanted")
-        st = lse.stride()
-        l_st = _i64x3(st[0], st[1], st[2]) if padded else _i64x3(0, st[1], st[0])
-    desc = KvAttentionDesc(_dtype_code(q), code, B, hq, h, d, bs, nb, cols, rows, padded, max_q_len, 1 if causal else 0, scale,
-                           *_dev(device, q, out, lse), q_st, o_st, l_st,
-                           *_dev(device, kv_len, row_offset, block_table, k_cache, v_cache, k_scale, v_scale))
     if workspace is None:
-        workspace = Workspace(lib().vscan_kv_attention_workspace_bytes(C.byref(desc)), device)
-    _enqueue("vscan_kv_attention", desc, device, workspace.ptr, workspace.nbytes)
+        workspace = vscan_kv_attention_workspace(q, block_table, k_cache, max_q_len)
+    st = (_CALLS or _calls()).kv_attention(q, kv_len, row_offset, block_table, k_cache, v_cache, k_scale, v_scale, scale, max_q_len, causal,
+                                           out, lse, workspace.buf)
+    if st != OK:
+        raise VScanError(st, "vscan_kv_attention")
     return out
 
 
