@@ -90,7 +90,7 @@ extern "C" vscan_status vscan_check(const void* workspace, void* stream) {
                                    cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream)));
     VSCAN_CUDA_TRY(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
     for (uint32_t i = 0; i < n; ++i)
-      if (flags[i]) return VSCAN_ERR_INVALID_ARG;
+      if (flags[i]) return flags[i] == VSCAN_ERR_TIMEOUT ? VSCAN_ERR_TIMEOUT : VSCAN_ERR_INVALID_ARG;
     return VSCAN_OK;
   }
   return word == 0 ? VSCAN_OK : VSCAN_ERR_TIMEOUT;

@@ -3,7 +3,7 @@
 // One pass over the keys with a running maximum and sum per query row.  K and V are turned from codes in registers, the
 // block's scale goes onto the scores (K) and onto the weights (V).  Queries of the heads that share a KV head, and of
 // neighbouring new rows, form a tile, so that a key that was read once serves all of them.
-#include "kv_attention_mma.cuh"
+#include "kv_attention_tc.cuh"
 
 namespace vscan {
 namespace kv {
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
       }
     }
   }
-  if (bad) p.flags[blockIdx.x] = 1;
+  if (bad) p.flags[blockIdx.x] = VSCAN_ERR_INVALID_ARG;
 }
 
 // ---------------------------------------------------------------------------------------------- joining cut segments
@@ -192,14 +192,16 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
   const int k0 = solo ? blockIdx.x * kWorkersPerCta + warp : blockIdx.x;
   if (k0 == 0) return;
   const Boundary bd = p.boundary[k0];
-  if (bd.seg1 == 0 || (k0 - 1) * bd.quota > bd.seg0) return;
+  if (bd.seg1 == 0) return;
+  const Boundary before = p.boundary[k0 - 1];
+  if (before.seg1 != 0 && before.seg0 == bd.seg0) return;                   // the segment's first cut is an earlier one
   const Sequence s = sequence_at(p, bd.b);
   const int D = p.head_dim, R = p.tile_rows, rows = min(R, s.n * p.group - bd.tile * R);
   const size_t stride = partial_floats(R, D);
   const int pieces = static_cast<int>((bd.seg1 - 1) / bd.quota) - k0 + 2;   // up to the worker of the segment's last unit
   const float* first = p.partial + (static_cast<size_t>(k0) * 2 - 1) * stride;   // slot 1 of k0 - 1; then slot 0 of k0, ...
   auto piece = [&](int i) { return first + (i == 0 ? 0 : 2 * i - 1) * stride; };
-  for (int r = solo ? 0 : warp; r < rows; r += solo ? 1 : kJoinThreads / 32) {
+  for (int r = solo ? 0 : blockIdx.y * (kJoinThreads / 32) + warp; r < rows; r += solo ? 1 : gridDim.y * (kJoinThreads / 32)) {
     float top = -INFINITY;
     for (int i = lane; i < pieces; i += 32) top = fmaxf(top, piece(i)[R * D + r]);
     top = warp_max(top);
@@ -275,15 +277,21 @@ static vscan_status validate_attention(const vscan_kv_attention_desc* d) {
 }
 
 // Rows of a tile and CTAs of the launch
-struct Plan { int tile_rows; unsigned ctas; bool mma; };
+struct Plan { int tile_rows; unsigned ctas; bool mma, tensor; };
 
 static Plan plan_launch(const vscan_kv_attention_desc* d) {
   Plan pl;
   const int group = d->q_heads / d->kv_heads;
   const int64_t want = static_cast<int64_t>(group) * d->max_q_len;
   pl.mma = d->dtype == VSCAN_BF16;
+  // 5th-generation tensor cores from 17 query rows of a sequence and KV head on: below that the other kernel reads the cache
+  // once as well
+  pl.tensor = pl.mma && want > 16 && d->head_dim <= 128;
   int64_t resident;
-  if (pl.mma) {
+  if (pl.tensor) {
+    pl.tile_rows = kTcRows;
+    resident = 1;
+  } else if (pl.mma) {
     pl.tile_rows = want <= 8 || d->head_dim > 128 ? 8 : 16;   // 16 rows of 256 channels do not fit the registers
     resident = d->head_dim > 128 || pl.tile_rows > 8 ? 2 : 3;
   } else {
@@ -303,7 +311,8 @@ static Plan plan_launch(const vscan_kv_attention_desc* d) {
 
 // workspace: status word | a flag per CTA | boundaries | partial results
 static size_t flag_bytes(const Plan& pl) { return round_up(pl.ctas * sizeof(uint32_t), 256); }
-static size_t boundary_bytes(const Plan& pl) { return round_up(pl.ctas * kWorkersPerCta * sizeof(Boundary), 256); }
+static size_t workers(const Plan& pl) { return static_cast<size_t>(pl.ctas) * (pl.mma && !pl.tensor ? kWorkersPerCta : 1); }
+static size_t boundary_bytes(const Plan& pl) { return round_up(workers(pl) * sizeof(Boundary), 256); }
 
 static size_t fma_smem(int R, int D) { return (static_cast<size_t>(R) * D * (1 + kFmaWarps) + kFmaWarps * 32 * R + 2 * kFmaWarps * R) * 4; }
 
@@ -344,10 +353,21 @@ static vscan_status launch_mma(const AttnParams& p, const Plan& pl, cudaStream_t
   return VSCAN_OK;
 }
 
+template <int KV, int DP>
+static vscan_status launch_tc(const AttnParams& p, const Plan& pl, cudaStream_t stream) {
+  constexpr size_t smem = 1024 + 6 * static_cast<size_t>(DP / 64) * kChunk;
+  VSCAN_CUDA_TRY(allow_smem(tc_kernel<KV, DP>, smem));
+  prof_before("kv_attention_tc", stream);
+  VSCAN_CUDA_TRY(launch_dependent(tc_kernel<KV, DP>, dim3(pl.ctas), dim3(kTcThreads), smem, stream, p));
+  prof_after(stream);
+  VSCAN_AFTER_LAUNCH();
+  return VSCAN_OK;
+}
+
 template <typename T, int KV>
 static vscan_status launch_scores(const AttnParams& p, const Plan& pl, cudaStream_t stream) {
   if constexpr (sizeof(T) == 2)
-    return p.head_dim <= 64 ? launch_mma<KV, 64>(p, pl, stream) : p.head_dim <= 128 ? launch_mma<KV, 128>(p, pl, stream)
+    return pl.tensor ? (p.head_dim <= 64 ? launch_tc<KV, 64>(p, pl, stream) : launch_tc<KV, 128>(p, pl, stream)) : p.head_dim <= 64 ? launch_mma<KV, 64>(p, pl, stream) : p.head_dim <= 128 ? launch_mma<KV, 128>(p, pl, stream)
                                                                                     : launch_mma<KV, 256>(p, pl, stream);
   else return launch_fma<T, KV>(p, pl, stream);
 }
@@ -356,10 +376,10 @@ template <typename T>
 static vscan_status launch_attention(const AttnParams& p, const Plan& pl, int kv_dtype, cudaStream_t stream) {
   const vscan_status st = kv_dtype == VSCAN_KV_E4M3 ? launch_scores<T, VSCAN_KV_E4M3>(p, pl, stream) : launch_scores<T, VSCAN_KV_I8>(p, pl, stream);
   if (st != VSCAN_OK) return st;
-  // nothing can have been cut when the table has room for kWhole units only, or when one CTA did it all
-  if (static_cast<int64_t>(p.max_blocks) * p.block_size <= kWhole * kUnit || pl.ctas == 1) return VSCAN_OK;
+  // nothing can have been cut when the table has room for kWhole units only (few rows), or when one CTA did it all
+  if ((!pl.tensor && static_cast<int64_t>(p.max_blocks) * p.block_size <= kWhole * kUnit) || pl.ctas == 1) return VSCAN_OK;
   prof_before("kv_attention_join", stream);
-  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, dim3(pl.ctas), dim3(kJoinThreads), 0, stream, p));
+  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, dim3(pl.ctas, pl.tensor ? kTcRows / 16 : 1), dim3(kJoinThreads), 0, stream, p));
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
   return VSCAN_OK;
@@ -375,7 +395,7 @@ extern "C" size_t vscan_kv_attention_workspace_bytes(const vscan_kv_attention_de
       d->head_dim > 256 || d->q_heads / d->kv_heads > 64)
     return kStatusBytes;
   const kv::Plan pl = kv::plan_launch(d);
-  return kStatusBytes + kv::flag_bytes(pl) + kv::boundary_bytes(pl) + round_up(2 * static_cast<size_t>(pl.ctas) * kv::kWorkersPerCta * kv::partial_floats(pl.tile_rows, d->head_dim) * 4, 256);
+  return kStatusBytes + kv::flag_bytes(pl) + kv::boundary_bytes(pl) + round_up(2 * kv::workers(pl) * kv::partial_floats(pl.tile_rows, d->head_dim) * 4, 256);
 }
 
 extern "C" vscan_status vscan_kv_attention(const vscan_kv_attention_desc* d, void* workspace, size_t workspace_bytes, void* stream_) {

@@ -24,7 +24,7 @@ struct AttnParams {
   int tile_rows;        // query rows (new row x head of the group) of a tile
   float scale_log2e;
   uint32_t* status;
-  uint32_t* flags;             // [ctas] 1: the CTA met a block or a length out of range
+  uint32_t* flags;             // [ctas] vscan_status: the CTA met a block or a length out of range, or gave up a wait
   struct Boundary* boundary;   // [ctas]
   float* partial;              // [ctas][2][tile_rows][head_dim + 2]
 };
@@ -158,7 +158,7 @@ __host__ __device__ inline size_t partial_floats(int tile_rows, int head_dim) { 
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 

@@ -433,7 +433,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
       }
     }
   }
-  if (bad) p.flags[blockIdx.x] = 1;
+  if (bad) p.flags[blockIdx.x] = VSCAN_ERR_INVALID_ARG;
 }
 
 }  // namespace kv

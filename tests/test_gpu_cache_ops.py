@@ -357,14 +357,18 @@ def _attend_case(kv, dtype, hq, hk, d, bs, past, new, causal, padded, seed, max_
     (8, 1, 64, 32, [129], [1]), (16, 1, 256, 16, [70, 33], [1, 1]), (2, 1, 80, 128, [200], [1]), (6, 3, 16, 256, [5, 400], [1, 1]),
     (40, 1, 96, 16, [77], [1]), (64, 1, 64, 16, [90], [1]),
     (4, 2, 128, 16, [10, 0, 200], [0, 5, 3]),                           # a sequence without rows, few rows each
-    (7, 1, 128, 16, [50, 3, 0], [16, 1, 33]), (2, 2, 64, 16, [0], [70]), (3, 1, 48, 32, [100], [40])])
+    (7, 1, 128, 16, [50, 3, 0], [16, 1, 33]), (2, 2, 64, 16, [0], [70]), (3, 1, 48, 32, [100], [40]),
+    # many rows: one and two tiles of 128 rows, several of 256, steps of 128 keys that end inside, whole and short sequences mixed
+    (1, 1, 128, 16, [0], [128]), (1, 1, 64, 64, [128], [129]), (7, 1, 128, 64, [300], [75]), (4, 2, 80, 16, [0, 500, 3], [130, 1, 66]),
+    (2, 1, 16, 128, [250], [300]), (12, 2, 96, 32, [77, 0], [24, 50]), (2, 1, 256, 16, [40], [30])])
 def test_attention(kv, dtype, hq, hk, d, bs, past, new):
     for causal in (True, False):
         _attend_case(kv, dtype, hq, hk, d, bs, past, new, causal, padded=(len(past) % 2 == 0), seed=hq + d)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("hq,hk,past,new", [(4, 1, [5000, 3, 700, 1], [1, 1, 1, 1]), (7, 1, [4000], [2]), (2, 2, [1500], [20])])
+@pytest.mark.parametrize("hq,hk,past,new", [(4, 1, [5000, 3, 700, 1], [1, 1, 1, 1]), (7, 1, [4000], [2]), (2, 2, [1500], [20]),
+                                              (1, 1, [3000], [40]), (5, 1, [2600, 0], [60, 90])])
 def test_attention_of_cut_sequences(dtype, hq, hk, past, new):
     _attend_case("e4m3", dtype, hq, hk, 64, 16, past, new, True, padded=False, seed=3)
 
