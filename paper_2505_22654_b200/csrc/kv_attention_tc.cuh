@@ -1,15 +1,16 @@
 // Attention of many query rows (prompts, chunks) for bf16 queries on the 5th-generation tensor cores.
 //
 // A CTA takes 256 query rows (new rows x heads of a group) of one KV head as two tiles of 128 and runs over its stretch of
-// the keys, 128 at a time:
+// the keys, 64 at a time:
 //   warps 0-3, 4-7   one query row a thread of tile 0, 1: scores from tensor memory, running maximum and sum, weights back
 //                    to tensor memory, over the scores that they come from; the results at the end
-//   warps 8-11       K and V from codes to f16 in shared memory (128-byte swizzle), two stages each; a key that was turned
-//                    once serves both tiles
-//   warp 12          issues the products: S[128 x 128] = Q K^T (operands in shared memory), O[128 x d] += P V with P read
+//   warps 8-11       K and V from codes to f16 in shared memory (128-byte swizzle), two stages of 128 keys each; a key that was
+//                    turned once serves both tiles
+//   warp 12          issues the products: S[128 x 64] = Q K^T (operands in shared memory), O[128 x d] += P V with P read
 //                    from tensor memory and V, tokens down and channels across, as the MN-major operand
-// The two tiles take turns: while one's weights are made, the other's products run.  Tensor memory is full: two tiles of
-// scores and two of sums, 128 columns each.
+// Scores of a tile alternate between two buffers, so those of the next step are there when the weights of this one are done
+// (128 keys a step and one buffer: 7300 cycles per 128 keys, of which a tile waited 2000 for its scores).  Tensor memory is
+// full: two tiles x two buffers x 64 columns of scores, two tiles x 128 columns of sums.
 //
 // Roundings as in the kernel for few rows: queries exact in f16 but for a power of two, weights in f16 relative to a
 // reference of the V scales, all else float32.  Per element of S: one fused multiply-add, one exponential, one add, one
@@ -25,18 +26,22 @@ namespace kv {
 
 constexpr int kTcThreads = 416;
 constexpr int kTcRows = 256;          // query rows of a CTA
-constexpr int kTcKeys = 128;          // keys of a step
-constexpr int kTcRing = 4;            // steps whose scales are kept: a converter is at most three steps ahead of a reader
+constexpr int kTcKeys = 128;          // keys of a stage
+constexpr int kTcStep = 64;           // keys of a step
+constexpr int kTcRing = 4;            // stages whose scales are kept: the converters are at most three ahead of a reader
 constexpr int kChunk = 128 * 128;     // bytes of [128 rows x 64 f16]
 
 struct TcShared {
-  uint64_t q_full[2], s_full[2], p_full[2], o_done[2];
+  // of the tiles, and of their score buffers: with one barrier for both buffers a wait could not tell a step from the one
+  // after the next
+  uint64_t q_full[2], s_full[2][2], p_full[2][2], o_done[2][2];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t scale_full[kTcRing];
   uint32_t tmem_base;
   int abort_flag;
-  int missing[kTcRing];
-  float ks[kTcRing][8], vs[kTcRing][8];   // of the 16-token groups of a step
+  float4 group[8][8];                     // per warp: of each 16-token group {K scale, V shift, its inverse factor}
+  uint32_t there[kTcRing];                // of the 16-token groups of a stage: a bit each, not there at all: 0
+  alignas(16) float ks[kTcRing][8], vs[kTcRing][8];
   long long weight[kTcThreads / 32];
   long long seq0;
   int b;
@@ -142,16 +147,49 @@ __device__ __forceinline__ bool tc_next(const AttnParams& p, TcStretch& st, TcPi
   return false;
 }
 
+// Steps of a piece: the last stage may end after its first
+__device__ __forceinline__ int tc_steps(const TcPiece& pc) {
+  return max(1, (min(pc.most, pc.u1 * kTcKeys) - pc.u0 * kTcKeys + kTcStep - 1) / kTcStep);
+}
+
 // ---------------------------------------------------------------------------------------------- instructions
-__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) { tc::umma_bf16(d, a, b, idesc, accumulate); }
-// A operand in tensor memory: row i in lane i, two f16 in a column
-__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+// The issuing warp stays converged: all lanes run its control flow and compute the descriptors, which are warp-uniform, and one
+// elected lane issues.  (Inside a branch of one lane every descriptor has to go through vector registers: 100 cycles a product.)
+// Four products of 16 inner elements each; the operands' descriptors advance by step_a (or columns) and step_b.
+__device__ __forceinline__ void umma_f16_ss_x4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred e, p;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
+      "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, 1;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, 1;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, 1;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+      : "memory");
+}
+// A operand in tensor memory: row i in lane i, two f16 in a column; 16 rows of 128 bytes of B a product
+__device__ __forceinline__ void umma_f16_ts_x4(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred e, p;\n\t.reg .b32 a1, a2, a3;\n\t.reg .b64 b1, b2, b3;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "add.u32 a1, %1, 8;\n\tadd.u32 a2, %1, 16;\n\tadd.u32 a3, %1, 24;\n\t"
+      "add.u64 b1, %2, 128;\n\tadd.u64 b2, %2, 256;\n\tadd.u64 b3, %2, 384;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, 1;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, 1;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, 1;\n\t}"
       ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
       : "memory");
+}
+// Arrives on `bar` when the products that the elected lane has issued so far are done
+__device__ __forceinline__ void umma_commit_warp(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(tc::smem_u32(bar)) : "memory");
 }
 // f16 x f16 -> float32, M = 128; b_mn: the second operand MN-major
 __device__ __forceinline__ uint32_t idesc_f16(int n, bool b_mn) {
@@ -170,7 +208,70 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
         "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// 16 bytes, or zeros: a predicated load, no branch around it
+__device__ __forceinline__ uint4 ld_nc_16_if(const void* p, uint32_t on) {
+  uint4 r;
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+      "@q ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "=&r"(r.x), "=&r"(r.y), "=&r"(r.z), "=&r"(r.w)
+      : "l"(p), "r"(on));
+  return r;
+}
+// Two float32 operations in one instruction
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// Tensor-memory loads with their wait in one statement: between the two the compiler must not move a register, because its
+// value is not there yet
+__device__ __forceinline__ void tmem_read16(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_read64(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+        "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]),
+        "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]),
+        "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]),
+        "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]),
+        "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+      : "r"(taddr)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -192,7 +293,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.q_full[i], 4); mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 4); mbar_init(&sh.o_done[i], 1);
+      mbar_init(&sh.q_full[i], 4);
+      for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[i][k], 1); mbar_init(&sh.p_full[i][k], 4); mbar_init(&sh.o_done[i][k], 1); }
       mbar_init(&sh.k_full[i], 4); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.v_full[i], 4); mbar_init(&sh.v_empty[i], 1);
     }
     for (int i = 0; i < kTcRing; ++i) mbar_init(&sh.scale_full[i], 1);
@@ -206,7 +308,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = sh.tmem_base;              // scores of tile 0, 1 at columns 0, 128; sums at 256, 384
+  const uint32_t tmem = sh.tmem_base;              // scores of tile t, buffer k at column 128 t + 64 k; sums at 256 + 128 t
   grid_dependency_wait();
   TcStretch st = tc_locate(p, sh);
   if (threadIdx.x == 0) {
@@ -225,13 +327,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
     const uint32_t s_addr = tmem + lanes + tile * 128, o_addr = tmem + lanes + 256 + tile * 128;
     unsigned char* q_row = q_sh + tile * kTileBytes + r * 128;
     int n_it = 0;            // steps of this tile so far
-    int step = 0;            // steps of the CTA so far
+    int stage = 0;           // stages of the CTA so far
     bool ok = true;
     while (ok && tc_next(p, st, pc)) {
-      const int steps = pc.u1 - pc.u0;
+      const int stages = pc.u1 - pc.u0, steps = tc_steps(pc);
       if (pc.u0 > 0 && threadIdx.x == 0)
         p.boundary[blockIdx.x] = {pc.seg0, pc.seg1, st.quota, pc.b, pc.head, pc.tile, 0};
-      if (tile * 128 >= pc.n_rows) { step += steps; continue; }
+      if (tile * 128 >= pc.n_rows) { stage += stages; continue; }
       if (p.kv_len[pc.b] > pc.q.s.len) bad = true;
       const int in_tile = tile * 128 + r;
       const bool on = in_tile < pc.n_rows;
@@ -243,27 +345,26 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       float cq;
       {
         const char* src = q_at(p, pc.b, pc.q.s.first, at);
-        uint4 raw[DP / 8];
-#pragma unroll
-        for (int c = 0; c < DP / 8; ++c) {
-          raw[c] = make_uint4(0, 0, 0, 0);
-          if (on && c * 8 < D) raw[c] = ld_nc_16(src + c * 16);
-        }
+        auto load8 = [&](int c, float* f) {
+          uint4 raw = make_uint4(0, 0, 0, 0);
+          if (on && c * 8 < D) raw = *reinterpret_cast<const uint4*>(src + c * 16);
+          Vec16<__nv_bfloat16>::unpack(raw, f);
+        };
         float top = 0.f;
-#pragma unroll
+#pragma unroll 4
         for (int c = 0; c < DP / 8; ++c) {
           float f[8];
-          Vec16<__nv_bfloat16>::unpack(raw[c], f);
+          load8(c, f);
 #pragma unroll
           for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
         }
         const int e = max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100);
         const float up = copysignf(exp2_int(min(14 - e, 127)), p.scale_log2e);   // the factor of a score is kept positive
         cq = exp2_int(max(e - 14, -126)) * fabsf(p.scale_log2e);
-#pragma unroll
-        for (int c = 0; c < DP / 8; ++c) {
+#pragma unroll 4
+        for (int c = 0; c < DP / 8; ++c) {                                       // a second time, from the caches
           float f[8];
-          Vec16<__nv_bfloat16>::unpack(raw[c], f);
+          load8(c, f);
           const uint4 w = make_uint4(pack_f16(f[0] * up, f[1] * up), pack_f16(f[2] * up, f[3] * up), pack_f16(f[4] * up, f[5] * up),
                                      pack_f16(f[6] * up, f[7] * up));
           *reinterpret_cast<uint4*>(q_row + (c >> 3) * kChunk + (((c & 7) ^ (r & 7)) << 4)) = w;
@@ -273,104 +374,137 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         if (lane == 0) mbar_arrive(&sh.q_full[tile]);
       }
 
-      float m = -INFINITY, l = 0.f, ref = 0.f;
-      for (int j = 0; j < steps && ok; ++j, ++n_it, ++step) {
-        const int slot = step & (kTcRing - 1);
-        ok = mbar_wait_warp(&sh.scale_full[slot], (step / kTcRing) & 1, abort_flag) && mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
+      float m = -INFINITY, l = 0.f, ref = 0.f, v_top = 0.f;
+      uint32_t there = 0;
+      bool odd = false;      // a scale of the stage is 0 or NaN
+      for (int j = 0; j < steps && ok; ++j, ++n_it) {
+        const int slot = (stage + j / 2) & (kTcRing - 1), buf = n_it & 1;
+        // A tile that had nothing to do in the piece before may be stages ahead of the converters, and a wait tells a phase from
+        // the next only: the first scores of a piece are waited for before its first scales.
+        if (j == 0) ok = mbar_wait_warp(&sh.s_full[tile][buf], (n_it >> 1) & 1, abort_flag);
+        if (ok && (j & 1) == 0) {    // a new stage: its scales, and what follows from them for all rows alike
+          ok = mbar_wait_warp(&sh.scale_full[slot], ((stage + j / 2) / kTcRing) & 1, abort_flag);
+          if (!ok) break;
+          const float4 va = *reinterpret_cast<const float4*>(sh.vs[slot]), vb = *reinterpret_cast<const float4*>(sh.vs[slot] + 4);
+          v_top = fmaxf(fmaxf(fmaxf(va.x, va.y), fmaxf(va.z, va.w)), fmaxf(fmaxf(vb.x, vb.y), fmaxf(vb.z, vb.w)));
+          there = sh.there[slot];
+          const float k8 = sh.ks[slot][lane & 7], v8 = sh.vs[slot][lane & 7];
+          odd = __any_sync(0xffffffffu, !(k8 > 0.f) || v8 != v8);
+        }
+        // a new reference of the V scales; rare
+        float f = 1.f;
+        const bool moved = v_top > ref || (v_top < 0.125f * ref && v_top > 0.f);
+        if (moved) { f = ref / v_top; ref = v_top; }
+        if (moved || (j & 1) == 0) {
+          // the V scale of a group goes into the exponent, its inverse onto the group's share of the denominator; a group
+          // whose scale is far below the reference (or 0) gives weights that are 0 in f16 and still counts in the denominator
+          __syncwarp();
+          if (lane < 8) {
+            const float fv = ref > 0.f ? sh.vs[slot][lane] * (kWeightScale / ref) : 0.f * sh.vs[slot][lane];
+            const float shift = fv == fv ? fmaxf(__log2f(fv), -60.f) : fv;
+            sh.group[warp][lane] = make_float4(sh.ks[slot][lane], shift, ex2(-shift), 0.f);
+          }
+          __syncwarp();
+        }
+        if (j > 0) ok = mbar_wait_warp(&sh.s_full[tile][buf], (n_it >> 1) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        const float* ks = sh.ks[slot];
-        const float* vs = sh.vs[slot];
-        const int vis = seen - (pc.u0 + j) * kTcKeys;             // columns that this row sees
-        const bool masked = __any_sync(0xffffffffu, vis < kTcKeys) || sh.missing[slot];
-        auto hidden = [&](int g, int c) { return c >= vis || ks[g] < 0.f; };
+        const uint32_t sb_addr = s_addr + buf * kTcStep;
+        const float4* group = sh.group[warp] + (j & 1) * 4;
+        // the columns that this row sees, 32 to a word
+        const int vis = seen - pc.u0 * kTcKeys - j * kTcStep;
+        const uint32_t there4 = (there >> ((j & 1) * 4)) & 15u;
+        const bool masked = __any_sync(0xffffffffu, vis < kTcStep) || there4 != 15u;
+        auto hide = [&](uint32_t* v, int half, uint32_t with) {
+          const int n = vis - half * 32;
+          const uint32_t mask = (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u) &
+                                (((there4 >> (2 * half)) & 1u ? 0xffffu : 0u) | ((there4 >> (2 * half + 1)) & 1u ? 0xffff0000u : 0u));
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (!((mask >> k) & 1u)) v[k] = with;
+        };
 
         // ---- largest score
         float top = -INFINITY;
+        uint32_t v[64];
+        tmem_read64(sb_addr, v);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t v[64];
-          tmem_ld32(s_addr + half * 64, v);
-          tmem_ld32(s_addr + half * 64 + 32, v + 32);
-          tmem_wait_ld();
+        for (int h = 0; h < 2; ++h) {
+          if (masked) hide(v + h * 32, h, 0xff800000u);   // -inf
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            float x = -INFINITY;
-            if (!masked) {
+          for (int g = 0; g < 2; ++g) {
+            float x = __uint_as_float(v[h * 32 + g * 16]);
 #pragma unroll
-              for (int k = 0; k < 16; ++k) x = fmaxf(x, __uint_as_float(v[g * 16 + k]));
-            } else {
-#pragma unroll
-              for (int k = 0; k < 16; ++k)
-                if (!hidden(half * 4 + g, half * 64 + g * 16 + k)) x = fmaxf(x, __uint_as_float(v[g * 16 + k]));
-            }
-            if (x > -INFINITY) top = fmaxf(top, x * (cq * ks[half * 4 + g]));
+            for (int k = 1; k < 15; k += 2) x = fmaxf(fmaxf(x, __uint_as_float(v[h * 32 + g * 16 + k])), __uint_as_float(v[h * 32 + g * 16 + k + 1]));
+            x = fmaxf(x, __uint_as_float(v[h * 32 + g * 16 + 15]));
+            if (x > -INFINITY) top = fmaxf(top, x * group[h * 2 + g].x);
           }
         }
-        // ---- a new maximum or a new reference of the V scales rescales the sums; both are rare
-        float v_top = 0.f;
-#pragma unroll
-        for (int g = 0; g < 8; ++g) v_top = fmaxf(v_top, vs[g]);
-        float f = 1.f;
+        top *= cq;
+        // ---- a new maximum rescales the sums; rare as well
         const bool over = top > m + kLazy;
         if (__any_sync(0xffffffffu, over)) {
-          const float now = fmaxf(m, top);
-          f = now == -INFINITY ? 1.f : ex2(m - now);
+          const float now = fmaxf(m, top), fm = now == -INFINITY ? 1.f : ex2(m - now);
           m = now;
-          l *= f;
+          l *= fm;
+          f *= fm;
         }
-        const bool moved = v_top > ref || (v_top < 0.125f * ref && v_top > 0.f);
-        if (moved) { f *= ref / v_top; ref = v_top; }
         if (j > 0 && __any_sync(0xffffffffu, f != 1.f)) {
-          ok = mbar_wait_warp(&sh.o_done[tile], (n_it - 1) & 1, abort_flag);
+          ok = mbar_wait_warp(&sh.o_done[tile][buf ^ 1], ((n_it - 1) >> 1) & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < DP; c += 16) {
             uint32_t v[16];
-            tmem_ld16(o_addr + c, v);
-            tmem_wait_ld();
+            tmem_read16(o_addr + c, v);
 #pragma unroll
             for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
             tmem_st16(o_addr + c, v);
           }
         }
-        // ---- weights over the scores: the columns a chunk is written to have been read before
-        const float inv_ref = ref > 0.f ? kWeightScale / ref : 0.f, minus_m = m == -INFINITY ? 0.f : -m;
-        float l0 = 0.f, l1 = 0.f;
+        // ---- weights over the scores, which are all in registers.  A masked score is -inf, its weight 0, as long as the scales
+        // are numbers above 0
+        const float minus_m = m == -INFINITY ? 0.f : -m;
 #pragma unroll
-        for (int quarter = 0; quarter < 4; ++quarter) {
-          uint32_t v[32], w[16];
-          tmem_ld32(s_addr + quarter * 32, v);
-          tmem_wait_ld();
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[16];
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const float fk = cq * ks[quarter * 2 + g], fv = vs[quarter * 2 + g] * inv_ref;
+            const float4 gr = group[h * 2 + g];
+            const float fk = cq * gr.x, shifted = minus_m + gr.y;
+            const uint64_t mul = pair(fk, fk), add = pair(shifted, shifted);
 #pragma unroll
-            for (int k = 0; k < 16; k += 2) {
-              float e0 = ex2(fmaf(__uint_as_float(v[g * 16 + k]), fk, minus_m)), e1 = ex2(fmaf(__uint_as_float(v[g * 16 + k + 1]), fk, minus_m));
-              float w0 = e0 * fv, w1 = e1 * fv;
-              if (masked) {
-                const int c = quarter * 32 + g * 16 + k;
-                if (hidden(quarter * 2 + g, c)) e0 = w0 = 0.f;
-                if (hidden(quarter * 2 + g, c + 1)) e1 = w1 = 0.f;
-              }
-              l0 += e0;
-              l1 += e1;
-              w[g * 8 + k / 2] = pack_f16(w0, w1);
+            for (int k = g * 16; k < g * 16 + 16; k += 2) {
+              const float2 x = unpair(fma2(pair(__uint_as_float(v[h * 32 + k]), __uint_as_float(v[h * 32 + k + 1])), mul, add));
+              v[h * 32 + k] = __float_as_uint(ex2(x.x));
+              v[h * 32 + k + 1] = __float_as_uint(ex2(x.y));
             }
           }
-          tmem_st16(s_addr + quarter * 16, w);
+          if (masked && odd) hide(v + h * 32, h, 0u);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            uint64_t sums = 0;
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+              const float w0 = __uint_as_float(v[h * 32 + g * 16 + k]), w1 = __uint_as_float(v[h * 32 + g * 16 + k + 1]);
+              sums = add2(sums, pair(w0, w1));
+              w[g * 8 + k / 2] = pack_f16(w0, w1);
+            }
+            const float2 both = unpair(sums);
+            const float sum = both.x + both.y;
+            if (sum != 0.f) l = fmaf(sum, group[h * 2 + g].z, l);
+          }
+          tmem_st16(sb_addr + h * 16, w);
         }
-        l += l0 + l1;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_full[tile]);
+        if (lane == 0) mbar_arrive(&sh.p_full[tile][buf]);
       }
       if (!ok) break;
+      stage += stages;
       // ---- results
-      ok = mbar_wait_warp(&sh.o_done[tile], (n_it - 1) & 1, abort_flag);
+      ok = mbar_wait_warp(&sh.o_done[tile][(n_it - 1) & 1], ((n_it - 1) >> 1) & 1, abort_flag);
       if (!ok) break;
       tc_fence_after();
       const bool complete = pc.u0 == 0 && pc.u1 == pc.units;
@@ -380,8 +514,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 #pragma unroll 1
       for (int c = 0; c < DP; c += 16) {
         uint32_t v[16];
-        tmem_ld16(o_addr + c, v);
-        tmem_wait_ld();
+        tmem_read16(o_addr + c, v);
         if (on && c < D) {
           float x[16];
 #pragma unroll
@@ -422,19 +555,26 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         }
         return x;
       };
-      uint4 raw[kLoads];
-      auto load = [&](const uint8_t* cache, int blk, int t0) {
+      // codes of a step of K and of V, each on its way while the other is turned
+      uint4 raw_k[kLoads], raw_v[kLoads];
+      const unsigned rows_mask = static_cast<unsigned>(p.block_size - 1);
+      auto load = [&](uint4* raw, const uint8_t* cache, int blk, int t0) {
+        const uint8_t* mine = cache + piece * 16;
+        const unsigned cell = static_cast<unsigned>(blk) * static_cast<unsigned>(p.kv_heads) + static_cast<unsigned>(pc.head);
+        const uint8_t* at[kLoads];
+        uint32_t on[kLoads];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          const int row = row0 + i * kRowsPass, t = t0 + row;
-          const int block = __shfl_sync(0xffffffffu, blk, row >> 4);
-          raw[i] = make_uint4(0, 0, 0, 0);
-          if (in_dim && t < pc.most && block >= 0)
-            raw[i] = ld_nc_16(cache + (static_cast<size_t>(block) * p.kv_heads + pc.head) * cell_bytes +
-                              static_cast<size_t>(t & (p.block_size - 1)) * D + piece * 16);
+        for (int i = 0; i < kLoads; ++i) {       // the 16-token group of a load is the same for all lanes
+          const int row = row0 + i * kRowsPass, group = (warp & 3) * (32 / kPer) / 16 + i * kRowsPass / 16;
+          const unsigned c = __shfl_sync(0xffffffffu, cell, group);
+          const int block = __shfl_sync(0xffffffffu, blk, group);      // by all lanes, whatever they load
+          on[i] = in_dim && t0 + row < pc.most && block >= 0;
+          at[i] = mine + static_cast<size_t>(c) * static_cast<unsigned>(cell_bytes) + ((t0 + row) & rows_mask) * static_cast<unsigned>(D);
         }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) raw[i] = ld_nc_16_if(at[i], on[i]);
       };
-      auto store = [&](unsigned char* dst) {
+      auto store = [&](const uint4* raw, unsigned char* dst) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           const int row = row0 + i * kRowsPass;
@@ -451,83 +591,87 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         __syncwarp();
       };
       int blk = blocks_at(pc.u0 * kTcKeys);
-      load(p.k_cache, blk, pc.u0 * kTcKeys);
+      load(raw_k, p.k_cache, blk, pc.u0 * kTcKeys);
+      load(raw_v, p.v_cache, blk, pc.u0 * kTcKeys);
+      int next = pc.u0 + 1 < pc.u1 ? blocks_at((pc.u0 + 1) * kTcKeys) : -1;
       for (int u = pc.u0; u < pc.u1 && ok; ++u, ++step) {
         const int s = step & 1, slot = step & (kTcRing - 1), t0 = u * kTcKeys;
         if (step >= 2) ok = mbar_wait_warp(&sh.k_empty[s], ((step >> 1) - 1) & 1, abort_flag);
         if (!ok) break;
-        store(k_sh + s * kTileBytes);
-        if (lane == 0) mbar_arrive(&sh.k_full[s]);
-        load(p.v_cache, blk, t0);
+        float scale = 0.f;         // lanes 0-7 K, 8-15 V, of warp 8: on its way while the keys are turned
+        const int b8 = __shfl_sync(0xffffffffu, blk, lane & 7);
         if (warp == 8) {
-          const bool none = lane < 8 && blk < 0 && t0 + lane * 16 < pc.most;
-          if (lane < 8) {
-            const size_t cell = static_cast<size_t>(max(blk, 0)) * p.kv_heads + pc.head;
-            sh.ks[slot][lane] = blk >= 0 ? __ldg(p.k_scale + cell) : none ? -1.f : 0.f;
-            sh.vs[slot][lane] = blk >= 0 ? __ldg(p.v_scale + cell) : 0.f;
-          }
-          const bool any = __any_sync(0xffffffffu, none);
-          if (lane == 0) sh.missing[slot] = any;
+          const size_t cell = static_cast<size_t>(max(b8, 0)) * p.kv_heads + pc.head;
+          if (lane < 16 && b8 >= 0) scale = __ldg((lane < 8 ? p.k_scale : p.v_scale) + cell);
+        }
+        store(raw_k, k_sh + s * kTileBytes);
+        if (lane == 0) mbar_arrive(&sh.k_full[s]);
+        if (warp == 8) {
+          if (lane < 8) sh.ks[slot][lane] = b8 >= 0 ? scale : 1.f;      // (a group that is not there is masked)
+          else if (lane < 16) sh.vs[slot][lane - 8] = scale;
+          const unsigned there = __ballot_sync(0xffffffffu, blk >= 0);
+          if (lane == 0) sh.there[slot] = there & 0xffu;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.scale_full[slot]);
         }
-        const int next = u + 1 < pc.u1 ? blocks_at(t0 + kTcKeys) : -1;
+        if (u + 1 < pc.u1) load(raw_k, p.k_cache, next, t0 + kTcKeys);
         if (step >= 2) ok = mbar_wait_warp(&sh.v_empty[s], ((step >> 1) - 1) & 1, abort_flag);
         if (!ok) break;
-        store(v_sh + s * kTileBytes);
+        store(raw_v, v_sh + s * kTileBytes);
         if (lane == 0) mbar_arrive(&sh.v_full[s]);
+        if (u + 1 < pc.u1) load(raw_v, p.v_cache, next, t0 + kTcKeys);
         blk = next;
-        if (u + 1 < pc.u1) load(p.k_cache, blk, t0 + kTcKeys);
+        next = u + 2 < pc.u1 ? blocks_at(t0 + 2 * kTcKeys) : -1;
       }
     }
   } else {
     // ============================================================ products
-    if (lane == 0) {
-      const uint32_t qk = idesc_f16(kTcKeys, false), pv = idesc_f16(DP, true);
+    {
+      const uint32_t qk = idesc_f16(kTcStep, false), pv = idesc_f16(DP, true);
       const uint32_t q_addr = smem_u32(q_sh), k_addr = smem_u32(k_sh), v_addr = smem_u32(v_sh);
-      int step = 0, n_it[2] = {0, 0}, n_piece[2] = {0, 0};
+      int stage = 0, n0[2] = {0, 0}, n_piece[2] = {0, 0};     // n0: steps of a tile before this piece
       bool ok = true;
-      auto scores = [&](int t, int s) {        // S of tile t from stage s of K
-        // the weights that lie there have been used up, not only issued
-        if (n_it[t] > 0 && !mbar_wait(&sh.o_done[t], (n_it[t] - 1) & 1, abort_flag)) return false;
+      // Scores of step j of the piece for tile t.  The weights that lie in the buffer have to be used up, not only issued.
+      auto scores = [&](int t, int j) {
+        const int n = n0[t] + j, s = (stage + j / 2) & 1;
+        if (n >= 2 && !mbar_wait_warp(&sh.o_done[t][n & 1], ((n - 2) >> 1) & 1, abort_flag)) return false;
         tc_fence_after();
+        const uint32_t d = tmem + t * 128 + (n & 1) * kTcStep;
+        const uint64_t a = smem_desc_sw128(q_addr + t * kTileBytes), b = smem_desc_sw128(k_addr + s * kTileBytes + (j & 1) * kTcStep * 128);
 #pragma unroll
-        for (int c = 0; c < kDChunks; ++c) {
-          const uint64_t a = smem_desc_sw128(q_addr + t * kTileBytes + c * kChunk), b = smem_desc_sw128(k_addr + s * kTileBytes + c * kChunk);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) umma_f16_ss(tmem + t * 128, a + 2u * k, b + 2u * k, qk, c > 0 || k > 0);
-        }
-        umma_commit(&sh.s_full[t]);
+        for (int c = 0; c < kDChunks; ++c) umma_f16_ss_x4(d, a + c * (kChunk >> 4), b + c * (kChunk >> 4), qk, c > 0);
+        umma_commit_warp(&sh.s_full[t][n & 1]);
         return true;
       };
       while (ok && tc_next(p, st, pc)) {
-        const int tiles = pc.n_rows > 128 ? 2 : 1;
-        for (int t = 0; t < tiles && ok; ++t) ok = mbar_wait(&sh.q_full[t], n_piece[t]++ & 1, abort_flag);
-        ok = ok && mbar_wait(&sh.k_full[step & 1], (step >> 1) & 1, abort_flag);
-        for (int t = 0; t < tiles && ok; ++t) ok = scores(t, step & 1);
-        if (!ok) break;
-        umma_commit(&sh.k_empty[step & 1]);
-        for (int u = pc.u0; u < pc.u1 && ok; ++u, ++step) {
-          const int s = step & 1;
-          const bool more = u + 1 < pc.u1;
-          ok = mbar_wait(&sh.v_full[s], (step >> 1) & 1, abort_flag);
-          for (int t = 0; t < tiles && ok; ++t) {
-            ok = mbar_wait(&sh.p_full[t], n_it[t] & 1, abort_flag);
-            if (!ok) break;
+        const int two = pc.n_rows > 128, steps = tc_steps(pc), total = steps << two, ahead = 2 + two;
+        for (int t = 0; t <= two && ok; ++t) ok = mbar_wait_warp(&sh.q_full[t], n_piece[t]++ & 1, abort_flag);
+        // Tiles in turn: i-th products with V, then scores `ahead` of them: of the other tile's next step but one, into a buffer
+        // whose products with V were issued two places before and are done by now.  One loop, its code in one place: it is
+        // fetched anew each time, between the long loops of the other warps.
+#pragma unroll 1
+        for (int i = -ahead; i < total && ok; ++i) {
+          if (i >= 0) {
+            const int t = i & two, j = i >> two, n = n0[t] + j, buf = n & 1, s = (stage + j / 2) & 1;
+            if (t == 0 && (j & 1) == 0 && !mbar_wait_warp(&sh.v_full[s], ((stage + j / 2) >> 1) & 1, abort_flag)) { ok = false; break; }
+            if (!mbar_wait_warp(&sh.p_full[t][buf], (n >> 1) & 1, abort_flag)) { ok = false; break; }
             tc_fence_after();
-#pragma unroll
-            for (int k = 0; k < kTcKeys / 16; ++k)
-              umma_f16_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, desc_mn(v_addr + s * kTileBytes + k * 2048), pv, u > pc.u0 || k > 0);
-            umma_commit(&sh.o_done[t]);
-            if (t == tiles - 1) umma_commit(&sh.v_empty[s]);
-            ++n_it[t];
-            if (more) {
-              if (t == 0) ok = mbar_wait(&sh.k_full[s ^ 1], ((step + 1) >> 1) & 1, abort_flag);
-              ok = ok && scores(t, s ^ 1);
-            }
+            const uint64_t b = desc_mn(v_addr + s * kTileBytes + (j & 1) * kTcStep * 128);
+            const uint32_t d = tmem + 256 + t * 128, a = tmem + t * 128 + buf * kTcStep;
+            static_assert(kTcStep == 64, "four products of 16 keys");
+            umma_f16_ts_x4(d, a, b, pv, j > 0);
+            umma_commit_warp(&sh.o_done[t][buf]);
+            if (t == two && ((j & 1) || j == steps - 1)) umma_commit_warp(&sh.v_empty[s]);
           }
-          if (ok && more) umma_commit(&sh.k_empty[s ^ 1]);
+          if (i + ahead < total) {
+            const int t = (i + ahead) & two, j = (i + ahead) >> two, s = (stage + j / 2) & 1;
+            if (t == 0 && (j & 1) == 0) ok = mbar_wait_warp(&sh.k_full[s], ((stage + j / 2) >> 1) & 1, abort_flag);
+            ok = ok && scores(t, j);
+            if (ok && t == two && ((j & 1) || j == steps - 1)) umma_commit_warp(&sh.k_empty[s]);
+          }
         }
+        for (int t = 0; t <= two; ++t) n0[t] += steps;
+        stage += pc.u1 - pc.u0;
       }
     }
     __syncwarp();
