@@ -1,16 +1,16 @@
 // Attention of many query rows (prompts, chunks) for bf16 queries on the 5th-generation tensor cores.
 //
 // A CTA takes 256 query rows (new rows x heads of a group) of one KV head as two tiles of 128 and runs over its stretch of
-// the keys, 64 at a time:
-//   warps 0-3, 4-7   one query row a thread of tile 0, 1: scores from tensor memory, running maximum and sum, weights back
-//                    to tensor memory, over the scores that they come from; the results at the end
-//   warps 8-11       K and V from codes to f16 in shared memory (128-byte swizzle), two stages of 128 keys each; a key that was
-//                    turned once serves both tiles
-//   warp 12          issues the products: S[128 x 64] = Q K^T (operands in shared memory), O[128 x d] += P V with P read
+// the keys, 128 at a time:
+//   warps 0-7, 8-15  tile 0, 1: two threads a query row, 64 of the step's scores each.  Scores from tensor memory, running
+//                    maximum and sum, weights back to tensor memory, over the scores that they come from; the results at the end
+//   warps 16-19      K and V from codes to f16 in shared memory (128-byte swizzle), two stages each; a key that was turned
+//                    once serves both tiles
+//   warp 20          issues the products: S[128 x 128] = Q K^T (operands in shared memory), O[128 x d] += P V with P read
 //                    from tensor memory and V, tokens down and channels across, as the MN-major operand
-// Scores of a tile alternate between two buffers, so those of the next step are there when the weights of this one are done
-// (128 keys a step and one buffer: 7300 cycles per 128 keys, of which a tile waited 2000 for its scores).  Tensor memory is
-// full: two tiles x two buffers x 64 columns of scores, two tiles x 128 columns of sums.
+// The two tiles take turns: while one's weights are made, the other's products run.  Tensor memory is full: two tiles of
+// scores and two of sums, 128 columns each.  (Scores of 64 keys in two buffers a tile would hide the products behind the
+// weights, but a product 64 columns wide takes as long as one of 128: 70 and 65 cycles measured.)
 //
 // Roundings as in the kernel for few rows: queries exact in f16 but for a power of two, weights in f16 relative to a
 // reference of the V scales, all else float32.  Per element of S: one fused multiply-add, one exponential, one add, one
@@ -24,23 +24,23 @@
 namespace vscan {
 namespace kv {
 
-constexpr int kTcThreads = 416;
+constexpr int kTcThreads = 672;
+constexpr int kTcConverter = 16, kTcIssuer = 20;   // first warp of each role
 constexpr int kTcRows = 256;          // query rows of a CTA
-constexpr int kTcKeys = 128;          // keys of a stage
-constexpr int kTcStep = 64;           // keys of a step
-constexpr int kTcRing = 4;            // stages whose scales are kept: the converters are at most three ahead of a reader
+constexpr int kTcKeys = 128;          // keys of a step
+constexpr int kTcRing = 4;            // steps whose scales are kept: the converters are at most three ahead of a reader
 constexpr int kChunk = 128 * 128;     // bytes of [128 rows x 64 f16]
 
 struct TcShared {
-  // of the tiles, and of their score buffers: with one barrier for both buffers a wait could not tell a step from the one
-  // after the next
-  uint64_t q_full[2], s_full[2][2], p_full[2][2], o_done[2][2];
+  uint64_t q_full[2], s_full[2], p_full[2], o_done[2];   // of the tiles
+  uint64_t pair[2][4];                                   // of the two warps that share 32 rows
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t scale_full[kTcRing];
   uint32_t tmem_base;
   int abort_flag;
-  float4 group[8][8];                     // per warp: of each 16-token group {K scale, V shift, its inverse factor}
-  uint32_t there[kTcRing];                // of the 16-token groups of a stage: a bit each, not there at all: 0
+  float4 group[16][4];                    // per warp: of each of its 16-token groups {K scale, V shift, its inverse factor}
+  float swap[2][2][2][128];               // [step parity][tile][half][row]: what the two threads of a row tell each other
+  uint32_t there[kTcRing];                // of the 16-token groups of a step: a bit each, not there at all: 0
   alignas(16) float ks[kTcRing][8], vs[kTcRing][8];
   long long weight[kTcThreads / 32];
   long long seq0;
@@ -147,11 +147,6 @@ __device__ __forceinline__ bool tc_next(const AttnParams& p, TcStretch& st, TcPi
   return false;
 }
 
-// Steps of a piece: the last stage may end after its first
-__device__ __forceinline__ int tc_steps(const TcPiece& pc) {
-  return max(1, (min(pc.most, pc.u1 * kTcKeys) - pc.u0 * kTcKeys + kTcStep - 1) / kTcStep);
-}
-
 // ---------------------------------------------------------------------------------------------- instructions
 // The issuing warp stays converged: all lanes run its control flow and compute the descriptors, which are warp-uniform, and one
 // elected lane issues.  (Inside a branch of one lane every descriptor has to go through vector registers: 100 cycles a product.)
@@ -253,22 +248,16 @@ __device__ __forceinline__ void tmem_read16(uint32_t taddr, uint32_t* v) {
       : "r"(taddr)
       : "memory");
 }
-__device__ __forceinline__ void tmem_read64(uint32_t taddr, uint32_t* v) {
+__device__ __forceinline__ void tmem_read32(uint32_t taddr, uint32_t* v) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
-      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
-      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
       : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
         "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
         "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
-        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]),
-        "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]),
-        "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]),
-        "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]),
-        "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
       : "r"(taddr)
       : "memory");
 }
@@ -293,22 +282,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.q_full[i], 4);
-      for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[i][k], 1); mbar_init(&sh.p_full[i][k], 4); mbar_init(&sh.o_done[i][k], 1); }
+      mbar_init(&sh.q_full[i], 8); mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 8); mbar_init(&sh.o_done[i], 1);
+      for (int k = 0; k < 4; ++k) mbar_init(&sh.pair[i][k], 2);
       mbar_init(&sh.k_full[i], 4); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.v_full[i], 4); mbar_init(&sh.v_empty[i], 1);
     }
     for (int i = 0; i < kTcRing; ++i) mbar_init(&sh.scale_full[i], 1);
     sh.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
+  if (warp == kTcIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "n"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = sh.tmem_base;              // scores of tile t, buffer k at column 128 t + 64 k; sums at 256 + 128 t
+  const uint32_t tmem = sh.tmem_base;              // scores of tile t at column 128 t; sums at 256 + 128 t
   grid_dependency_wait();
   TcStretch st = tc_locate(p, sh);
   if (threadIdx.x == 0) {
@@ -320,20 +309,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
   bool bad = false;
   TcPiece pc;
 
-  if (warp < 8) {
-    // ============================================================ a query row a thread
-    const int tile = warp >> 2, r = (warp & 3) * 32 + lane;
-    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem + lanes + tile * 128, o_addr = tmem + lanes + 256 + tile * 128;
+  if (warp < kTcConverter) {
+    // ============================================================ two threads a query row
+    const int tile = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t s_addr = tmem + lanes + tile * 128 + half * 64;                      // this thread's scores, and its weights
+    const uint32_t o_addr = tmem + lanes + 256 + tile * 128 + half * (DP / 2);          // its half of the sums
     unsigned char* q_row = q_sh + tile * kTileBytes + r * 128;
     int n_it = 0;            // steps of this tile so far
-    int stage = 0;           // stages of the CTA so far
+    int step = 0;            // steps of the CTA so far
+    int n_swap = 0;          // exchanges with the row's other thread so far
     bool ok = true;
+    // Gives x to the row's other thread and returns what that gives
+    auto swap = [&](float x) {
+      sh.swap[n_swap & 1][tile][half][r] = x;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.pair[tile][quarter]);
+      ok = mbar_wait_warp(&sh.pair[tile][quarter], n_swap & 1, abort_flag);
+      return sh.swap[n_swap++ & 1][tile][half ^ 1][r];
+    };
     while (ok && tc_next(p, st, pc)) {
-      const int stages = pc.u1 - pc.u0, steps = tc_steps(pc);
+      const int steps = pc.u1 - pc.u0;
       if (pc.u0 > 0 && threadIdx.x == 0)
         p.boundary[blockIdx.x] = {pc.seg0, pc.seg1, st.quota, pc.b, pc.head, pc.tile, 0};
-      if (tile * 128 >= pc.n_rows) { stage += stages; continue; }
+      if (tile * 128 >= pc.n_rows) { step += steps; continue; }
       if (p.kv_len[pc.b] > pc.q.s.len) bad = true;
       const int in_tile = tile * 128 + r;
       const bool on = in_tile < pc.n_rows;
@@ -341,7 +340,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       const RowAt at = {i_row, pc.head * p.group + flat - i_row * p.group};
       const int seen = on ? visible(p, pc.q.s, i_row) : 0;
 
-      // ---- the query row: largest element, power of two, f16 into the swizzled tile
+      // ---- the query row: largest element, power of two, this thread's half of it as f16 into the swizzled tile
       float cq;
       {
         const char* src = q_at(p, pc.b, pc.q.s.first, at);
@@ -362,7 +361,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         const float up = copysignf(exp2_int(min(14 - e, 127)), p.scale_log2e);   // the factor of a score is kept positive
         cq = exp2_int(max(e - 14, -126)) * fabsf(p.scale_log2e);
 #pragma unroll 4
-        for (int c = 0; c < DP / 8; ++c) {                                       // a second time, from the caches
+        for (int i = 0; i < DP / 16; ++i) {                                      // a second time, from the caches
+          const int c = half * (DP / 16) + i;
           float f[8];
           load8(c, f);
           const uint4 w = make_uint4(pack_f16(f[0] * up, f[1] * up), pack_f16(f[2] * up, f[3] * up), pack_f16(f[4] * up, f[5] * up),
@@ -374,51 +374,43 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         if (lane == 0) mbar_arrive(&sh.q_full[tile]);
       }
 
-      float m = -INFINITY, l = 0.f, ref = 0.f, v_top = 0.f;
-      uint32_t there = 0;
-      bool odd = false;      // a scale of the stage is 0 or NaN
-      for (int j = 0; j < steps && ok; ++j, ++n_it) {
-        const int slot = (stage + j / 2) & (kTcRing - 1), buf = n_it & 1;
-        // A tile that had nothing to do in the piece before may be stages ahead of the converters, and a wait tells a phase from
+      float m = -INFINITY, l = 0.f, ref = 0.f;
+      for (int j = 0; j < steps && ok; ++j, ++n_it, ++step) {
+        const int slot = step & (kTcRing - 1);
+        // A tile that had nothing to do in the piece before may be steps ahead of the converters, and a wait tells a phase from
         // the next only: the first scores of a piece are waited for before its first scales.
-        if (j == 0) ok = mbar_wait_warp(&sh.s_full[tile][buf], (n_it >> 1) & 1, abort_flag);
-        if (ok && (j & 1) == 0) {    // a new stage: its scales, and what follows from them for all rows alike
-          ok = mbar_wait_warp(&sh.scale_full[slot], ((stage + j / 2) / kTcRing) & 1, abort_flag);
-          if (!ok) break;
-          const float4 va = *reinterpret_cast<const float4*>(sh.vs[slot]), vb = *reinterpret_cast<const float4*>(sh.vs[slot] + 4);
-          v_top = fmaxf(fmaxf(fmaxf(va.x, va.y), fmaxf(va.z, va.w)), fmaxf(fmaxf(vb.x, vb.y), fmaxf(vb.z, vb.w)));
-          there = sh.there[slot];
-          const float k8 = sh.ks[slot][lane & 7], v8 = sh.vs[slot][lane & 7];
-          odd = __any_sync(0xffffffffu, !(k8 > 0.f) || v8 != v8);
-        }
-        // a new reference of the V scales; rare
+        if (j == 0) ok = mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
+        ok = ok && mbar_wait_warp(&sh.scale_full[slot], (step / kTcRing) & 1, abort_flag);
+        if (!ok) break;
+        // ---- the scales, and what follows from them for all rows alike; a new reference of the V scales is rare
+        const float k8 = sh.ks[slot][lane & 7], v8 = sh.vs[slot][lane & 7];
+        const uint32_t there = sh.there[slot];
+        const bool odd = __any_sync(0xffffffffu, !(k8 > 0.f) || v8 != v8);      // a scale that is 0 or NaN
+        float v_top = v8 == v8 ? v8 : 0.f;
+#pragma unroll
+        for (int off = 1; off < 8; off <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, off));
         float f = 1.f;
-        const bool moved = v_top > ref || (v_top < 0.125f * ref && v_top > 0.f);
-        if (moved) { f = ref / v_top; ref = v_top; }
-        if (moved || (j & 1) == 0) {
-          // the V scale of a group goes into the exponent, its inverse onto the group's share of the denominator; a group
-          // whose scale is far below the reference (or 0) gives weights that are 0 in f16 and still counts in the denominator
-          __syncwarp();
-          if (lane < 8) {
-            const float fv = ref > 0.f ? sh.vs[slot][lane] * (kWeightScale / ref) : 0.f * sh.vs[slot][lane];
-            const float shift = fv == fv ? fmaxf(__log2f(fv), -60.f) : fv;
-            sh.group[warp][lane] = make_float4(sh.ks[slot][lane], shift, ex2(-shift), 0.f);
-          }
-          __syncwarp();
+        if (v_top > ref || (v_top < 0.125f * ref && v_top > 0.f)) { f = ref / v_top; ref = v_top; }
+        // the V scale of a group goes into the exponent, its inverse onto the group's share of the denominator; a group whose
+        // scale is far below the reference (or 0) gives weights that are 0 in f16 and still counts in the denominator
+        if ((lane >> 2) == half) {
+          const float fv = ref > 0.f ? v8 * (kWeightScale / ref) : 0.f * v8;
+          const float shift = fv == fv ? fmaxf(__log2f(fv), -60.f) : fv;
+          sh.group[warp][lane & 3] = make_float4(k8, shift, ex2(-shift), 0.f);
         }
-        if (j > 0) ok = mbar_wait_warp(&sh.s_full[tile][buf], (n_it >> 1) & 1, abort_flag);
+        __syncwarp();
+        if (j > 0) ok = mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t sb_addr = s_addr + buf * kTcStep;
-        const float4* group = sh.group[warp] + (j & 1) * 4;
+        const float4* group = sh.group[warp];
         // the columns that this row sees, 32 to a word
-        const int vis = seen - pc.u0 * kTcKeys - j * kTcStep;
-        const uint32_t there4 = (there >> ((j & 1) * 4)) & 15u;
-        const bool masked = __any_sync(0xffffffffu, vis < kTcStep) || there4 != 15u;
-        auto hide = [&](uint32_t* v, int half, uint32_t with) {
-          const int n = vis - half * 32;
+        const int vis = seen - (pc.u0 + j) * kTcKeys - half * 64;
+        const uint32_t there4 = (there >> (half * 4)) & 15u;
+        const bool masked = __any_sync(0xffffffffu, vis < 64) || there4 != 15u;
+        auto hide = [&](uint32_t* v, int h, uint32_t with) {
+          const int n = vis - h * 32;
           const uint32_t mask = (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u) &
-                                (((there4 >> (2 * half)) & 1u ? 0xffffu : 0u) | ((there4 >> (2 * half + 1)) & 1u ? 0xffff0000u : 0u));
+                                (((there4 >> (2 * h)) & 1u ? 0xffffu : 0u) | ((there4 >> (2 * h + 1)) & 1u ? 0xffff0000u : 0u));
 #pragma unroll
           for (int k = 0; k < 32; ++k)
             if (!((mask >> k) & 1u)) v[k] = with;
@@ -426,48 +418,49 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 
         // ---- largest score
         float top = -INFINITY;
-        uint32_t v[64];
-        tmem_read64(sb_addr, v);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          if (masked) hide(v + h * 32, h, 0xff800000u);   // -inf
+          uint32_t v[32];
+          tmem_read32(s_addr + h * 32, v);
+          if (masked) hide(v, h, 0xff800000u);   // -inf
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            float x = __uint_as_float(v[h * 32 + g * 16]);
+            float x = __uint_as_float(v[g * 16]);
 #pragma unroll
-            for (int k = 1; k < 15; k += 2) x = fmaxf(fmaxf(x, __uint_as_float(v[h * 32 + g * 16 + k])), __uint_as_float(v[h * 32 + g * 16 + k + 1]));
-            x = fmaxf(x, __uint_as_float(v[h * 32 + g * 16 + 15]));
+            for (int k = 1; k < 15; k += 2) x = fmaxf(fmaxf(x, __uint_as_float(v[g * 16 + k])), __uint_as_float(v[g * 16 + k + 1]));
+            x = fmaxf(x, __uint_as_float(v[g * 16 + 15]));
             if (x > -INFINITY) top = fmaxf(top, x * group[h * 2 + g].x);
           }
         }
         top *= cq;
-        // ---- a new maximum rescales the sums; rare as well
-        const bool over = top > m + kLazy;
-        if (__any_sync(0xffffffffu, over)) {
+        top = fmaxf(top, swap(top));
+        if (!ok) break;
+        // ---- a new maximum rescales the sums; rare as well.  Both threads of a row decide alike.
+        if (__any_sync(0xffffffffu, top > m + kLazy)) {
           const float now = fmaxf(m, top), fm = now == -INFINITY ? 1.f : ex2(m - now);
           m = now;
           l *= fm;
           f *= fm;
         }
         if (j > 0 && __any_sync(0xffffffffu, f != 1.f)) {
-          ok = mbar_wait_warp(&sh.o_done[tile][buf ^ 1], ((n_it - 1) >> 1) & 1, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
+          // (the products with V of the step before are done: this step's scores were issued after them)
 #pragma unroll 1
-          for (int c = 0; c < DP; c += 16) {
-            uint32_t v[16];
-            tmem_read16(o_addr + c, v);
+          for (int c = 0; c < DP / 2; c += 16) {
+            uint32_t x[16];
+            tmem_read16(o_addr + c, x);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
-            tmem_st16(o_addr + c, v);
+            for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+            tmem_st16(o_addr + c, x);
           }
         }
-        // ---- weights over the scores, which are all in registers.  A masked score is -inf, its weight 0, as long as the scales
-        // are numbers above 0
+        // ---- weights over the scores, read a second time (the registers hold 32): the columns that a chunk is written to have
+        // been read before
         const float minus_m = m == -INFINITY ? 0.f : -m;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          uint32_t w[16];
+          uint32_t v[32], w[16];
+          tmem_read32(s_addr + h * 32, v);
+          if (masked) hide(v, h, 0xff800000u);   // a masked score is -inf, its weight 0, as long as the scales are numbers above 0
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             const float4 gr = group[h * 2 + g];
@@ -475,18 +468,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
             const uint64_t mul = pair(fk, fk), add = pair(shifted, shifted);
 #pragma unroll
             for (int k = g * 16; k < g * 16 + 16; k += 2) {
-              const float2 x = unpair(fma2(pair(__uint_as_float(v[h * 32 + k]), __uint_as_float(v[h * 32 + k + 1])), mul, add));
-              v[h * 32 + k] = __float_as_uint(ex2(x.x));
-              v[h * 32 + k + 1] = __float_as_uint(ex2(x.y));
+              const float2 x = unpair(fma2(pair(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), mul, add));
+              v[k] = __float_as_uint(ex2(x.x));
+              v[k + 1] = __float_as_uint(ex2(x.y));
             }
           }
-          if (masked && odd) hide(v + h * 32, h, 0u);
+          if (masked && odd) hide(v, h, 0u);
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             uint64_t sums = 0;
 #pragma unroll
             for (int k = 0; k < 16; k += 2) {
-              const float w0 = __uint_as_float(v[h * 32 + g * 16 + k]), w1 = __uint_as_float(v[h * 32 + g * 16 + k + 1]);
+              const float w0 = __uint_as_float(v[g * 16 + k]), w1 = __uint_as_float(v[g * 16 + k + 1]);
               sums = add2(sums, pair(w0, w1));
               w[g * 8 + k / 2] = pack_f16(w0, w1);
             }
@@ -494,17 +487,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
             const float sum = both.x + both.y;
             if (sum != 0.f) l = fmaf(sum, group[h * 2 + g].z, l);
           }
-          tmem_st16(sb_addr + h * 16, w);
+          tmem_st16(s_addr + h * 16, w);
         }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_full[tile][buf]);
+        if (lane == 0) mbar_arrive(&sh.p_full[tile]);
       }
       if (!ok) break;
-      stage += stages;
       // ---- results
-      ok = mbar_wait_warp(&sh.o_done[tile][(n_it - 1) & 1], ((n_it - 1) >> 1) & 1, abort_flag);
+      l += swap(l);
+      ok = ok && mbar_wait_warp(&sh.o_done[tile], (n_it - 1) & 1, abort_flag);
       if (!ok) break;
       tc_fence_after();
       const bool complete = pc.u0 == 0 && pc.u1 == pc.units;
@@ -512,9 +505,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       float* part = p.partial + (static_cast<size_t>(blockIdx.x) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(kTcRows, D);
       char* out = out_at(p, pc.b, pc.q.s.first, at);
 #pragma unroll 1
-      for (int c = 0; c < DP; c += 16) {
+      for (int i = 0; i < DP / 2; i += 16) {
         uint32_t v[16];
-        tmem_read16(o_addr + c, v);
+        tmem_read16(o_addr + i, v);
+        const int c = half * (DP / 2) + i;
         if (on && c < D) {
           float x[16];
 #pragma unroll
@@ -530,15 +524,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         }
       }
       tc_fence_before();
-      if (on) {
+      if (on && half == 0) {
         if (!complete) { part[kTcRows * D + in_tile] = m; part[kTcRows * D + kTcRows + in_tile] = l; }
         else if (p.lse) *lse_at(p, pc.b, pc.q.s.first, at) = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
       }
     }
-  } else if (warp < 12) {
+  } else if (warp < kTcIssuer) {
     // ============================================================ codes to f16
-    constexpr int kPer = DP / 16, kRowsPass = 128 / kPer, kLoads = 128 / kRowsPass;   // pieces of a token; tokens and loads of a pass
-    const int tid = threadIdx.x - 256, piece = tid % kPer, row0 = tid / kPer;
+    constexpr int kPer = DP / 16, kRowsPass = 128 / kPer, kLoads = 64 / kRowsPass;   // pieces of a token; tokens of a pass; loads of an item
+    const int tid = threadIdx.x - kTcConverter * 32, piece = tid % kPer, row0 = tid / kPer;
     const bool in_dim = piece * 16 < D;
     const size_t cell_bytes = static_cast<size_t>(p.block_size) * D;
     int step = 0;
@@ -555,17 +549,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         }
         return x;
       };
-      // codes of a step of K and of V, each on its way while the other is turned
-      uint4 raw_k[kLoads], raw_v[kLoads];
+      // An item is 64 keys of K or of V: four a step (K, K, V, V), two of them on their way while one is turned
+      uint4 raw[2][kLoads];
       const unsigned rows_mask = static_cast<unsigned>(p.block_size - 1);
-      auto load = [&](uint4* raw, const uint8_t* cache, int blk, int t0) {
+      auto load = [&](uint4* raw, const uint8_t* cache, int blk, int t0, int part) {    // part: 64 keys of the step
         const uint8_t* mine = cache + piece * 16;
         const unsigned cell = static_cast<unsigned>(blk) * static_cast<unsigned>(p.kv_heads) + static_cast<unsigned>(pc.head);
         const uint8_t* at[kLoads];
         uint32_t on[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {       // the 16-token group of a load is the same for all lanes
-          const int row = row0 + i * kRowsPass, group = (warp & 3) * (32 / kPer) / 16 + i * kRowsPass / 16;
+          const int row = part * 64 + row0 + i * kRowsPass, group = part * 4 + (warp & 3) * (32 / kPer) / 16 + i * kRowsPass / 16;
           const unsigned c = __shfl_sync(0xffffffffu, cell, group);
           const int block = __shfl_sync(0xffffffffu, blk, group);      // by all lanes, whatever they load
           on[i] = in_dim && t0 + row < pc.most && block >= 0;
@@ -574,10 +568,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) raw[i] = ld_nc_16_if(at[i], on[i]);
       };
-      auto store = [&](const uint4* raw, unsigned char* dst) {
+      auto store = [&](const uint4* raw, unsigned char* dst, int part) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-          const int row = row0 + i * kRowsPass;
+          const int row = part * 64 + row0 + i * kRowsPass;
           const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
           uint32_t h[8];
 #pragma unroll
@@ -587,26 +581,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
           *reinterpret_cast<uint4*>(at + ((c16 ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
           *reinterpret_cast<uint4*>(at + (((c16 + 1) ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
         }
-        fence_async();
-        __syncwarp();
       };
       int blk = blocks_at(pc.u0 * kTcKeys);
-      load(raw_k, p.k_cache, blk, pc.u0 * kTcKeys);
-      load(raw_v, p.v_cache, blk, pc.u0 * kTcKeys);
+      load(raw[0], p.k_cache, blk, pc.u0 * kTcKeys, 0);
+      load(raw[1], p.k_cache, blk, pc.u0 * kTcKeys, 1);
       int next = pc.u0 + 1 < pc.u1 ? blocks_at((pc.u0 + 1) * kTcKeys) : -1;
       for (int u = pc.u0; u < pc.u1 && ok; ++u, ++step) {
         const int s = step & 1, slot = step & (kTcRing - 1), t0 = u * kTcKeys;
+        const bool more = u + 1 < pc.u1;
         if (step >= 2) ok = mbar_wait_warp(&sh.k_empty[s], ((step >> 1) - 1) & 1, abort_flag);
         if (!ok) break;
-        float scale = 0.f;         // lanes 0-7 K, 8-15 V, of warp 8: on its way while the keys are turned
+        float scale = 0.f;         // lanes 0-7 K, 8-15 V, of the first warp: on its way while the keys are turned
         const int b8 = __shfl_sync(0xffffffffu, blk, lane & 7);
-        if (warp == 8) {
+        if (warp == kTcConverter) {
           const size_t cell = static_cast<size_t>(max(b8, 0)) * p.kv_heads + pc.head;
           if (lane < 16 && b8 >= 0) scale = __ldg((lane < 8 ? p.k_scale : p.v_scale) + cell);
         }
-        store(raw_k, k_sh + s * kTileBytes);
+        store(raw[0], k_sh + s * kTileBytes, 0);
+        load(raw[0], p.v_cache, blk, t0, 0);
+        store(raw[1], k_sh + s * kTileBytes, 1);
+        fence_async();
+        __syncwarp();
         if (lane == 0) mbar_arrive(&sh.k_full[s]);
-        if (warp == 8) {
+        load(raw[1], p.v_cache, blk, t0, 1);
+        if (warp == kTcConverter) {
           if (lane < 8) sh.ks[slot][lane] = b8 >= 0 ? scale : 1.f;      // (a group that is not there is masked)
           else if (lane < 16) sh.vs[slot][lane - 8] = scale;
           const unsigned there = __ballot_sync(0xffffffffu, blk >= 0);
@@ -614,12 +612,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.scale_full[slot]);
         }
-        if (u + 1 < pc.u1) load(raw_k, p.k_cache, next, t0 + kTcKeys);
         if (step >= 2) ok = mbar_wait_warp(&sh.v_empty[s], ((step >> 1) - 1) & 1, abort_flag);
         if (!ok) break;
-        store(raw_v, v_sh + s * kTileBytes);
+        store(raw[0], v_sh + s * kTileBytes, 0);
+        if (more) load(raw[0], p.k_cache, next, t0 + kTcKeys, 0);
+        store(raw[1], v_sh + s * kTileBytes, 1);
+        fence_async();
+        __syncwarp();
         if (lane == 0) mbar_arrive(&sh.v_full[s]);
-        if (u + 1 < pc.u1) load(raw_v, p.v_cache, next, t0 + kTcKeys);
+        if (more) load(raw[1], p.k_cache, next, t0 + kTcKeys, 1);
         blk = next;
         next = u + 2 < pc.u1 ? blocks_at(t0 + 2 * kTcKeys) : -1;
       }
@@ -627,51 +628,49 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
   } else {
     // ============================================================ products
     {
-      const uint32_t qk = idesc_f16(kTcStep, false), pv = idesc_f16(DP, true);
+      const uint32_t qk = idesc_f16(kTcKeys, false), pv = idesc_f16(DP, true);
       const uint32_t q_addr = smem_u32(q_sh), k_addr = smem_u32(k_sh), v_addr = smem_u32(v_sh);
-      int stage = 0, n0[2] = {0, 0}, n_piece[2] = {0, 0};     // n0: steps of a tile before this piece
+      int step = 0, n_it[2] = {0, 0}, n_piece[2] = {0, 0};
       bool ok = true;
-      // Scores of step j of the piece for tile t.  The weights that lie in the buffer have to be used up, not only issued.
-      auto scores = [&](int t, int j) {
-        const int n = n0[t] + j, s = (stage + j / 2) & 1;
-        if (n >= 2 && !mbar_wait_warp(&sh.o_done[t][n & 1], ((n - 2) >> 1) & 1, abort_flag)) return false;
-        tc_fence_after();
-        const uint32_t d = tmem + t * 128 + (n & 1) * kTcStep;
-        const uint64_t a = smem_desc_sw128(q_addr + t * kTileBytes), b = smem_desc_sw128(k_addr + s * kTileBytes + (j & 1) * kTcStep * 128);
+      auto scores = [&](int t, int s) {        // S of tile t from stage s of K
+        const uint64_t a = smem_desc_sw128(q_addr + t * kTileBytes), b = smem_desc_sw128(k_addr + s * kTileBytes);
 #pragma unroll
-        for (int c = 0; c < kDChunks; ++c) umma_f16_ss_x4(d, a + c * (kChunk >> 4), b + c * (kChunk >> 4), qk, c > 0);
-        umma_commit_warp(&sh.s_full[t][n & 1]);
-        return true;
+        for (int c = 0; c < kDChunks; ++c) umma_f16_ss_x4(tmem + t * 128, a + c * (kChunk >> 4), b + c * (kChunk >> 4), qk, c > 0);
+        umma_commit_warp(&sh.s_full[t]);
       };
       while (ok && tc_next(p, st, pc)) {
-        const int two = pc.n_rows > 128, steps = tc_steps(pc), total = steps << two, ahead = 2 + two;
+        const int two = pc.n_rows > 128;
         for (int t = 0; t <= two && ok; ++t) ok = mbar_wait_warp(&sh.q_full[t], n_piece[t]++ & 1, abort_flag);
-        // Tiles in turn: i-th products with V, then scores `ahead` of them: of the other tile's next step but one, into a buffer
-        // whose products with V were issued two places before and are done by now.  One loop, its code in one place: it is
-        // fetched anew each time, between the long loops of the other warps.
+        ok = ok && mbar_wait_warp(&sh.k_full[step & 1], (step >> 1) & 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        for (int t = 0; t <= two; ++t) scores(t, step & 1);
+        umma_commit_warp(&sh.k_empty[step & 1]);
+        for (int u = pc.u0; u < pc.u1 && ok; ++u, ++step) {
+          const int s = step & 1;
+          const bool more = u + 1 < pc.u1;
+          ok = mbar_wait_warp(&sh.v_full[s], (step >> 1) & 1, abort_flag);
+          if (more) ok = ok && mbar_wait_warp(&sh.k_full[s ^ 1], ((step + 1) >> 1) & 1, abort_flag);
 #pragma unroll 1
-        for (int i = -ahead; i < total && ok; ++i) {
-          if (i >= 0) {
-            const int t = i & two, j = i >> two, n = n0[t] + j, buf = n & 1, s = (stage + j / 2) & 1;
-            if (t == 0 && (j & 1) == 0 && !mbar_wait_warp(&sh.v_full[s], ((stage + j / 2) >> 1) & 1, abort_flag)) { ok = false; break; }
-            if (!mbar_wait_warp(&sh.p_full[t][buf], (n >> 1) & 1, abort_flag)) { ok = false; break; }
+          for (int t = 0; t <= two && ok; ++t) {
+            ok = mbar_wait_warp(&sh.p_full[t], n_it[t] & 1, abort_flag);
+            if (!ok) break;
             tc_fence_after();
-            const uint64_t b = desc_mn(v_addr + s * kTileBytes + (j & 1) * kTcStep * 128);
-            const uint32_t d = tmem + 256 + t * 128, a = tmem + t * 128 + buf * kTcStep;
-            static_assert(kTcStep == 64, "four products of 16 keys");
-            umma_f16_ts_x4(d, a, b, pv, j > 0);
-            umma_commit_warp(&sh.o_done[t][buf]);
-            if (t == two && ((j & 1) || j == steps - 1)) umma_commit_warp(&sh.v_empty[s]);
-          }
-          if (i + ahead < total) {
-            const int t = (i + ahead) & two, j = (i + ahead) >> two, s = (stage + j / 2) & 1;
-            if (t == 0 && (j & 1) == 0) ok = mbar_wait_warp(&sh.k_full[s], ((stage + j / 2) >> 1) & 1, abort_flag);
-            ok = ok && scores(t, j);
-            if (ok && t == two && ((j & 1) || j == steps - 1)) umma_commit_warp(&sh.k_empty[s]);
+            const uint64_t b = desc_mn(v_addr + s * kTileBytes);
+            umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128, b, pv, u > pc.u0);
+            umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128 + 64, b + (64 * 128 >> 4), pv, true);
+            umma_commit_warp(&sh.o_done[t]);
+            if (t == two) umma_commit_warp(&sh.v_empty[s]);
+            if (more) {        // the weights that lie where the next scores go have to be used up, not only issued
+              ok = mbar_wait_warp(&sh.o_done[t], n_it[t] & 1, abort_flag);
+              if (!ok) break;
+              tc_fence_after();
+              scores(t, s ^ 1);
+              if (t == two) umma_commit_warp(&sh.k_empty[s ^ 1]);
+            }
+            ++n_it[t];
           }
         }
-        for (int t = 0; t <= two; ++t) n0[t] += steps;
-        stage += pc.u1 - pc.u0;
       }
     }
     __syncwarp();
@@ -686,7 +685,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
     for (int i = 0; i < 64; ++i) __nanosleep(2000);   // products still in flight end before their memory is given back
     __syncthreads();
   }
-  if (warp == 12) {
+  if (warp == kTcIssuer) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
   }

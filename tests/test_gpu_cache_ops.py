@@ -373,6 +373,22 @@ def test_attention_of_cut_sequences(dtype, hq, hk, past, new):
     _attend_case("e4m3", dtype, hq, hk, 64, 16, past, new, True, padded=False, seed=3)
 
 
+def test_attention_of_many_pieces_gives_the_same_bits_every_time():
+    """Sequences of very different sizes on few CTAs: each runs through pieces with one and with two tiles of rows, whole and
+    cut, whose roles hand over to each other in every order that timing allows."""
+    past, new = [0, 500, 3, 700, 5, 3, 900], [130, 1, 66, 40, 1, 300, 1]
+    lens, off = [p + n for p, n in zip(past, new)], _offsets(new)
+    c, g = Cache("e4m3", 2, 16, 80, sum(-(-n // 16) for n in lens) + 2, 12), gen(13)
+    table = i32(_tables(lens, 16, 70, c.blocks, np.random.default_rng(0)))
+    q = torch.randn((off[-1], 4, 80), generator=g).to(torch.bfloat16).cuda()
+    args = (q, i32(lens), i32(off), table, *c.arrays, 0.05)
+    ws = vs.vscan_kv_attention_workspace(q, table, c.dev[0], 300)
+    first = vs.vscan_kv_attention(*args, max_q_len=300, workspace=ws).clone()
+    for _ in range(60):
+        assert torch.equal(vs.vscan_kv_attention(*args, max_q_len=300, workspace=ws), first)
+        assert vs.vscan_check(ws) == 0
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_rows_that_see_nothing(dtype):
     # no keys at all; more new rows than tokens: the first rows stand before every key
