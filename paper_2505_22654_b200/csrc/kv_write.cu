@@ -171,17 +171,21 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(WriteParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------- block form
-// A CTA owns a (block, head) of K or V: chunks of 16 elements, kHeld of them kept in registers between the maximum and the
-// codes, the rest (large blocks) read a second time from L2.
-constexpr int kBlockThreads = 128;
+// A CTA owns a block of tokens, a group of W warps at a time one (head, K or V) of it: chunks of 16 elements, kHeld of them a
+// lane in registers between the maximum and the codes, the rest (large blocks) read a second time from L2.  What the block's
+// place in sequence and table takes to find (a chain of four loads) is found once for all its heads, and where the lane's
+// chunks lie once for all units.  (32 x 259 rows x 32 heads of 128 in bf16: 123 us with a CTA
+// a unit, 43 us so, 4.7 TB/s.)
+// Small CTAs, so that the chain of one runs beside the copies of others.
+constexpr int kHeld = 4;
+__host__ __device__ constexpr int block_threads(int w) { return w == 8 ? 256 : 128; }
 
-template <typename T, int KV>
-__global__ void __launch_bounds__(kBlockThreads) block_kernel(WriteParams p) {
-  constexpr int kHeld = sizeof(T) == 2 ? 4 : 2;
-  __shared__ uint32_t warp_peak[kBlockThreads / 32];
+template <typename T, int KV, int W>
+__global__ void __launch_bounds__(block_threads(W), (sizeof(T) == 2 ? 768 : 512) / block_threads(W)) block_kernel(WriteParams p, int per_cta) {
+  constexpr int kThreads = block_threads(W), kGroups = kThreads / 32 / W;
+  __shared__ uint32_t warp_peak[kThreads / 32];
   grid_dependency_wait();
-  const int which = blockIdx.z, h = blockIdx.y, item = blockIdx.x;
-  const int per = p.rows / p.block_size + 2;               // padded: items of a sequence
+  const int item = blockIdx.x, per = p.rows / p.block_size + 2;   // padded: items of a sequence
   const int b = p.padded ? item / per : find_sequence(p.batch, item, [&](int i) {
     return static_cast<long long>(min(max(p.row_offset[i], 0), p.rows) >> p.shift) + 2 * i; });
   const Span sp = span_of(p, b);
@@ -196,55 +200,65 @@ __global__ void __launch_bounds__(kBlockThreads) block_kernel(WriteParams p) {
   const int off = j == 0 ? sp.start & (p.block_size - 1) : 0;
   const int n = static_cast<int>(min(end - col0, static_cast<long long>(p.block_size))) - off;
   const int i0 = static_cast<int>(col0 + off - sp.start);  // first new row of this block
-  const char* src = p.src[which] + (p.padded ? b * p.seq[which] : 0) + static_cast<long long>(sp.first + i0) * p.row[which] +
-                    static_cast<long long>(h) * p.head[which];
-  const size_t cell = static_cast<size_t>(block) * p.kv_heads + h;
-  const float old = off > 0 ? p.scale[which][cell] : 0.f;
   const int cpr = p.head_dim / 16, total = n * cpr;        // chunks
-  auto chunk_at = [&](int c) {
-    const int r = c / cpr;
-    return src + r * p.row[which] + (c - r * cpr) * 16 * static_cast<int>(sizeof(T));
-  };
-  Chunk<T> held[kHeld];
-  uint32_t peak = 0;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / W, in_group = threadIdx.x - group * W * 32;
+  const long long row0 = static_cast<long long>(sp.first) + i0;
+  int held_row[kHeld], held_col[kHeld];                    // of this lane's chunks; a row below 0: none
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) {
-    const int c = threadIdx.x + k * kBlockThreads;
-    held[k].zero();
-    if (c < total) held[k].load(chunk_at(c));
+    const int c = in_group + k * 32 * W;
+    held_row[k] = c < total ? c / cpr : -1;
+    held_col[k] = c < total ? (c - held_row[k] * cpr) * 16 * static_cast<int>(sizeof(T)) : 0;
   }
+  const int units = 2 * p.kv_heads, u0 = blockIdx.y * per_cta, u1 = min(u0 + per_cta, units);
+  for (int u = u0 + group; u < u1; u += kGroups) {
+    const int h = u >> 1, which = u & 1;
+    const char* src = p.src[which] + (p.padded ? b * p.seq[which] : 0) + row0 * p.row[which] + static_cast<long long>(h) * p.head[which];
+    const size_t cell = static_cast<size_t>(block) * p.kv_heads + h;
+    Chunk<T> held[kHeld];
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k) peak = max(peak, held[k].peak());
-  for (int c = threadIdx.x + kHeld * kBlockThreads; c < total; c += kBlockThreads) {
-    Chunk<T> x;
-    x.load(chunk_at(c));
-    peak = max(peak, x.peak());
-  }
-  peak = __reduce_max_sync(0xffffffffu, peak);
-  if ((threadIdx.x & 31) == 0) warp_peak[threadIdx.x >> 5] = peak;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kBlockThreads / 32; ++w) peak = max(peak, warp_peak[w]);
-  float inv, ratio;
-  const float s = new_scale<KV>(peak, off > 0, old, inv, ratio);
-  uint8_t* base = p.cache[which] + cell * p.block_size * p.head_dim;
-  uint8_t* dst = base + static_cast<size_t>(off) * p.head_dim;
-  if (ratio != 1.f)
-    for (int c = threadIdx.x; c < off * cpr; c += kBlockThreads) {
-      uint4* at = reinterpret_cast<uint4*>(base) + c;
-      *at = recode<KV>(*at, ratio);
+    for (int k = 0; k < kHeld; ++k) {
+      held[k].zero();
+      if (held_row[k] >= 0) held[k].load(src + held_row[k] * p.row[which] + held_col[k]);
     }
+    const float old = off > 0 ? p.scale[which][cell] : 0.f;
+    uint32_t peak = 0;
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k) {
-    const int c = threadIdx.x + k * kBlockThreads;
-    if (c < total) st_16(dst + static_cast<size_t>(c) * 16, held[k].template encode<KV>(inv));
+    for (int k = 0; k < kHeld; ++k) peak = max(peak, held[k].peak());
+    for (int c = in_group + kHeld * 32 * W; c < total; c += 32 * W) {
+      const int r = c / cpr;
+      Chunk<T> x;
+      x.load(src + r * p.row[which] + (c - r * cpr) * 16 * static_cast<int>(sizeof(T)));
+      peak = max(peak, x.peak());
+    }
+    peak = __reduce_max_sync(0xffffffffu, peak);
+    if constexpr (W > 1) {                                 // the groups of a CTA go their own ways: a barrier each
+      if (lane == 0) warp_peak[warp] = peak;
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(W * 32) : "memory");
+#pragma unroll
+      for (int w = 0; w < W; ++w) peak = max(peak, warp_peak[group * W + w]);
+    }
+    float inv, ratio;
+    const float s = new_scale<KV>(peak, off > 0, old, inv, ratio);
+    uint8_t* base = p.cache[which] + cell * p.block_size * p.head_dim;
+    uint8_t* dst = base + static_cast<size_t>(off) * p.head_dim;
+    if (ratio != 1.f)
+      for (int c = in_group; c < off * cpr; c += 32 * W) {
+        uint4* at = reinterpret_cast<uint4*>(base) + c;
+        *at = recode<KV>(*at, ratio);
+      }
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (held_row[k] >= 0) st_16(dst + static_cast<size_t>(in_group + k * 32 * W) * 16, held[k].template encode<KV>(inv));
+    for (int c = in_group + kHeld * 32 * W; c < total; c += 32 * W) {
+      const int r = c / cpr;
+      Chunk<T> x;
+      x.load(src + r * p.row[which] + (c - r * cpr) * 16 * static_cast<int>(sizeof(T)));
+      st_16(dst + static_cast<size_t>(c) * 16, x.template encode<KV>(inv));
+    }
+    if constexpr (W > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(W * 32) : "memory");   // old scale and maxima have been read
+    if (in_group == 0) p.scale[which][cell] = s;
   }
-  for (int c = threadIdx.x + kHeld * kBlockThreads; c < total; c += kBlockThreads) {
-    Chunk<T> x;
-    x.load(chunk_at(c));
-    st_16(dst + static_cast<size_t>(c) * 16, x.template encode<KV>(inv));
-  }
-  if (threadIdx.x == 0) p.scale[which][cell] = s;
 }
 
 static vscan_status validate_write(const vscan_kv_write_desc* d) {
@@ -291,8 +305,20 @@ static vscan_status launch_write(const WriteParams& p, cudaStream_t stream) {
                    : lanes <= 8 ? launch_dependent(append_kernel<T, KV, 8>, grid, dim3(kAppendThreads), 0, stream, p)
                                 : launch_dependent(append_kernel<T, KV, 16>, grid, dim3(kAppendThreads), 0, stream, p));
   } else {
+    // as many warps to a unit as keep its chunks in registers
+    const int chunks = p.block_size * p.head_dim / 16, w = chunks <= 128 ? 1 : chunks <= 256 ? 2 : chunks <= 512 ? 4 : 8;
+    // a CTA takes its warps' worth of units several times over while the grid still covers the SMs sixteen times
+    const long long units = 2ll * p.kv_heads, groups = block_threads(w) / 32 / w;
+    long long turns = items * units / (groups * 148 * 16);
+    turns = turns < 1 ? 1 : turns > 16 ? 16 : turns;
+    const long long split = (units + groups * turns - 1) / (groups * turns);
+    const int per_cta = static_cast<int>(((units + split - 1) / split + groups - 1) / groups * groups);
+    const dim3 grid(static_cast<unsigned>(items), static_cast<unsigned>((units + per_cta - 1) / per_cta));
     prof_before("kv_write", stream);
-    VSCAN_CUDA_TRY(launch_dependent(block_kernel<T, KV>, dim3(static_cast<unsigned>(items), p.kv_heads, 2), dim3(kBlockThreads), 0, stream, p));
+    VSCAN_CUDA_TRY(w == 1 ? launch_dependent(block_kernel<T, KV, 1>, grid, dim3(block_threads(w)), 0, stream, p, per_cta)
+                   : w == 2 ? launch_dependent(block_kernel<T, KV, 2>, grid, dim3(block_threads(w)), 0, stream, p, per_cta)
+                   : w == 4 ? launch_dependent(block_kernel<T, KV, 4>, grid, dim3(block_threads(w)), 0, stream, p, per_cta)
+                            : launch_dependent(block_kernel<T, KV, 8>, grid, dim3(block_threads(w)), 0, stream, p, per_cta));
   }
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
