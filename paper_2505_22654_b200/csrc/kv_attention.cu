@@ -335,15 +335,16 @@ static vscan_status launch_fma(const AttnParams& p, const Plan& pl, cudaStream_t
   return VSCAN_OK;
 }
 
-template <int KV, int DP>
+template <int KV, int DP, bool FULL>
 static vscan_status launch_mma(const AttnParams& p, const Plan& pl, cudaStream_t stream) {
   const size_t smem = (static_cast<size_t>(4) * pl.tile_rows * (DP + 2)) * sizeof(float);
   constexpr int MT = DP == 256 ? 1 : 2;
 #define VSCAN_MMA_CASE(NT)                                                                                          \
   if (pl.tile_rows == 8 * NT) {                                                                                     \
-    VSCAN_CUDA_TRY(allow_smem(mma_kernel<KV, DP, NT, MT>, smem));                                                   \
+    auto kernel = mma_kernel<KV, DP, NT, MT, FULL>;                                                                 \
+    VSCAN_CUDA_TRY(allow_smem(kernel, smem));                                                                       \
     prof_before("kv_attention_mma", stream);                                                                        \
-    VSCAN_CUDA_TRY(launch_dependent(mma_kernel<KV, DP, NT, MT>, dim3(pl.ctas), dim3(kMmaThreads), smem, stream, p)); \
+    VSCAN_CUDA_TRY(launch_dependent(kernel, dim3(pl.ctas), dim3(kMmaThreads), smem, stream, p));                    \
     prof_after(stream);                                                                                             \
     VSCAN_AFTER_LAUNCH();                                                                                           \
   }
@@ -366,9 +367,15 @@ static vscan_status launch_tc(const AttnParams& p, const Plan& pl, cudaStream_t 
 
 template <typename T, int KV>
 static vscan_status launch_scores(const AttnParams& p, const Plan& pl, cudaStream_t stream) {
-  if constexpr (sizeof(T) == 2)
-    return pl.tensor ? (p.head_dim <= 64 ? launch_tc<KV, 64>(p, pl, stream) : launch_tc<KV, 128>(p, pl, stream)) : p.head_dim <= 64 ? launch_mma<KV, 64>(p, pl, stream) : p.head_dim <= 128 ? launch_mma<KV, 128>(p, pl, stream)
-                                                                                    : launch_mma<KV, 256>(p, pl, stream);
+  if constexpr (sizeof(T) == 2) {
+    const int d = p.head_dim;
+    if (pl.tensor) return d <= 64 ? launch_tc<KV, 64>(p, pl, stream) : launch_tc<KV, 128>(p, pl, stream);
+    if (d == 64) return launch_mma<KV, 64, true>(p, pl, stream);
+    if (d == 128) return launch_mma<KV, 128, true>(p, pl, stream);
+    if (d == 256) return launch_mma<KV, 256, true>(p, pl, stream);
+    return d < 64 ? launch_mma<KV, 64, false>(p, pl, stream) : d < 128 ? launch_mma<KV, 128, false>(p, pl, stream)
+                                                                       : launch_mma<KV, 256, false>(p, pl, stream);
+  }
   else return launch_fma<T, KV>(p, pl, stream);
 }
 

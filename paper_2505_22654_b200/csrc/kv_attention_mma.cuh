@@ -60,8 +60,9 @@ __device__ __forceinline__ uint2 ld_nc_8(const void* p) {
   return r;
 }
 
-// DP: head_dim rounded up to 64, 128 or 256.  NT: tiles of 8 query rows.  MT: groups of 16 tokens of a step.
-template <int KV, int DP, int NT, int MT>
+// DP: head_dim rounded up to 64, 128 or 256.  NT: tiles of 8 query rows.  MT: groups of 16 tokens of a step.  FULL: head_dim is DP,
+// so that where a lane's pieces lie within a block is known at compile time.
+template <int KV, int DP, int NT, int MT, bool FULL>
 __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_kernel(AttnParams p) {
   constexpr int R = 8 * NT, KS = DP / 16, kPieces = DP / 64, kStep = 16 * MT;
   constexpr int kVWords = DP / 32;                   // 32-bit words of V codes of a lane and token
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
   float* l_sh = m_sh + 4 * R;
   __shared__ ScheduleShared sched;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const int D = p.head_dim;
+  const int D = FULL ? DP : p.head_dim;
   grid_dependency_wait();
   Stretch st = locate<kMmaThreads, true>(p, sched);
   if (threadIdx.x == 0) {
@@ -113,44 +114,62 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
         out[m] = x;
       }
     };
+    // A step that is there in full is loaded without conditions; the last one, and one with missing blocks, piece by piece,
+    // zeros for what is not there.
     auto load_k = [&](int t0) {
+      bool full = FULL && t0 + kStep <= stop;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) full = full && blk[m] >= 0;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         const int t = t0 + 16 * m;
         const size_t cell = static_cast<size_t>(max(blk[m], 0)) * p.kv_heads + head;
-        const uint8_t* base = p.k_cache + cell * cell_bytes + static_cast<size_t>((t & (p.block_size - 1)) + g) * D + c * 16;
-        ks[m] = 0.f;
-        if (blk[m] >= 0) ks[m] = __ldg(p.k_scale + cell);
+        const uint8_t* base = p.k_cache + cell * cell_bytes + ((t & (p.block_size - 1)) + g) * D + c * 16;
+        if (full) {
+          ks[m] = __ldg(p.k_scale + cell);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < kPieces; ++i) {
-            kraw[m][h][i] = make_uint4(0, 0, 0, 0);
-            if (blk[m] >= 0 && t + 8 * h + g < stop && i * 64 + c * 16 < D) kraw[m][h][i] = ld_nc_16(base + h * 8 * D + i * 64);
-          }
+            for (int i = 0; i < kPieces; ++i) kraw[m][h][i] = ld_nc_16(base + h * 8 * D + i * 64);
+        } else {
+          ks[m] = 0.f;
+          if (blk[m] >= 0) ks[m] = __ldg(p.k_scale + cell);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+              kraw[m][h][i] = make_uint4(0, 0, 0, 0);
+              if (blk[m] >= 0 && t + 8 * h + g < stop && i * 64 + c * 16 < D) kraw[m][h][i] = ld_nc_16(base + h * 8 * D + i * 64);
+            }
+        }
       }
     };
     auto load_v = [&](int t0) {
+      bool full = FULL && t0 + kStep <= stop;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) full = full && blk[m] >= 0;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         const int t = t0 + 16 * m;
         const size_t cell = static_cast<size_t>(max(blk[m], 0)) * p.kv_heads + head;
-        const uint8_t* base = p.v_cache + cell * cell_bytes + static_cast<size_t>(t & (p.block_size - 1)) * D;
+        const uint8_t* base = p.v_cache + cell * cell_bytes + ((t & (p.block_size - 1)) + 2 * c) * D + g * (DP == 64 ? 8 : 16);
         vsc[m] = 0.f;
-        if (blk[m] >= 0) vsc[m] = __ldg(p.v_scale + cell);
+        if (full || blk[m] >= 0) vsc[m] = __ldg(p.v_scale + cell);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int tok = 2 * c + (k & 1) + (k >> 1) * 8;
-          const bool on = blk[m] >= 0 && t + tok < stop;
+          const int tok = (k & 1) + (k >> 1) * 8;
+          const bool on = full || (blk[m] >= 0 && t + 2 * c + tok < stop);
           if constexpr (DP == 64) {
             uint2 v = make_uint2(0, 0);
-            if (on && g * 8 < D) v = ld_nc_8(base + tok * D + g * 8);
+            if (full) v = ld_nc_8(base + tok * D);
+            else if (on && g * 8 < D) v = ld_nc_8(base + tok * D);
             vraw[m][k][0] = v.x; vraw[m][k][1] = v.y;
           } else {
 #pragma unroll
             for (int i = 0; i < DP / 128; ++i) {
               uint4 v = make_uint4(0, 0, 0, 0);
-              if (on && i * 128 + g * 16 < D) v = ld_nc_16(base + tok * D + i * 128 + g * 16);
+              if (full) v = ld_nc_16(base + tok * D + i * 128);
+              else if (on && i * 128 + g * 16 < D) v = ld_nc_16(base + tok * D + i * 128);
               vraw[m][k][4 * i] = v.x; vraw[m][k][4 * i + 1] = v.y; vraw[m][k][4 * i + 2] = v.z; vraw[m][k][4 * i + 3] = v.w;
             }
           }
@@ -254,10 +273,12 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
         }
       }
       // masked: behind the row's last token, or in a block that is not there
-      const bool all = t0 + kStep <= fewest;
+      bool all = t0 + kStep <= fewest;
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-        if (!all || !there[mt]) {
+      for (int mt = 0; mt < MT; ++mt) all = all && there[mt];
+      if (!all) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
           const int t = t0 + 16 * mt + g;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -265,6 +286,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
             for (int k = 0; k < 4; ++k)
               if (!there[mt] || t + (k >> 1) * 8 >= seen[nt][k & 1]) x[mt][nt][k] = -INFINITY;
         }
+      }
       // the next step's keys replace this one's; its values follow once this step's are used up
       float vs_now[MT];
 #pragma unroll
@@ -322,12 +344,21 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float e[4];
+          if (all) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            // a masked score is -inf: so may be the maximum of a row that has seen nothing yet
-            e[k] = x[mt][nt][k] == -INFINITY ? 0.f : ex2(x[mt][nt][k] - m[nt][k & 1]);
-            l[nt][k & 1] += e[k];
-            e[k] = x[mt][nt][k] == -INFINITY ? 0.f : e[k] * fv;
+            for (int k = 0; k < 4; ++k) {
+              e[k] = ex2(x[mt][nt][k] - m[nt][k & 1]);
+              l[nt][k & 1] += e[k];
+              e[k] *= fv;
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              // a masked score is -inf: so may be the maximum of a row that has seen nothing yet
+              e[k] = x[mt][nt][k] == -INFINITY ? 0.f : ex2(x[mt][nt][k] - m[nt][k & 1]);
+              l[nt][k & 1] += e[k];
+              e[k] = x[mt][nt][k] == -INFINITY ? 0.f : e[k] * fv;
+            }
           }
           pb[nt][0] = transpose8x8(pack_f16(e[0], e[1]));
           pb[nt][1] = transpose8x8(pack_f16(e[2], e[3]));
