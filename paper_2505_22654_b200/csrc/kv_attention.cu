@@ -32,10 +32,10 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
   bool bad = false;
   Piece pc;
   while (next_piece(p, st, pc)) {
-    const Sequence& s = pc.s;
-    const int b = pc.b, head = pc.head, tile = pc.tile, u0 = pc.u0, u1 = pc.u1;
-    if (u0 > 0 && threadIdx.x == 0) p.boundary[blockIdx.x] = {pc.seg0, pc.seg0 + s.units, st.quota, b, head, tile, 0};
+    const Sequence& s = st.s;
+    const int b = st.b, head = st.head, tile = st.tile, u0 = pc.u0, u1 = pc.u1;
     const int n_rows = min(R, s.n * p.group - tile * R);
+    if (u0 > 0 && threadIdx.x == 0) p.boundary[blockIdx.x] = {st.seg0, st.seg0 + s.units, st.quota, b, head, tile, s.first, n_rows, 0};
     if (p.kv_len[b] > s.len) bad = true;
 
     __syncthreads();                              // the shared buffers of the segment before are done with
@@ -174,67 +174,115 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
     }
   }
   if (bad) p.flags[blockIdx.x] = VSCAN_ERR_INVALID_ARG;
+  grid_dependency_launch();
 }
 
 // ---------------------------------------------------------------------------------------------- joining cut segments
 // Where the stretch of worker k starts inside a segment that is cut there for the first time, the segment's rows from its
 // pieces: the last piece of worker k - 1, then the first ones of k, k + 1, ... up to the segment's end.  The pieces are
-// added in that order, so results do not depend on timing.  A warp takes a row; where workers are warps (few pieces a
-// segment), a warp takes a boundary.
-constexpr int kJoinThreads = 256;
+// added in a fixed order, so results do not depend on timing.  Three shapes of the work:
+//   few rows, workers are CTAs    a few segments in many pieces: CTA k joins segment k, its warps share a row's pieces
+//   few rows, workers are warps   many segments in two pieces or three: a warp takes a row
+//   256 rows a tile               a warp takes a row, again and again
+constexpr int kJoinThreads = 512;
+constexpr int kJoinWarps = kJoinThreads / 32;
+
+struct Pieces {          // of one segment
+  const float* first;
+  size_t stride;
+  int n;
+  __device__ __forceinline__ const float* at(int i) const { return first + (i == 0 ? 0 : 2 * i - 1) * stride; }
+};
+
+__device__ __forceinline__ bool cut_at(const AttnParams& p, int k, Boundary& bd, Pieces& pc) {
+  if (k == 0) return false;
+  bd = p.boundary[k];
+  const Boundary before = p.boundary[k - 1];
+  if (bd.seg1 == 0 || (before.seg1 != 0 && before.seg0 == bd.seg0)) return false;   // no cut, or not the segment's first
+  pc.stride = partial_floats(p.tile_rows, p.head_dim);
+  pc.n = static_cast<int>((bd.seg1 - 1) / bd.quota) - k + 2;                         // up to the worker of the segment's last unit
+  pc.first = p.partial + (static_cast<size_t>(k) * 2 - 1) * pc.stride;               // slot 1 of k - 1; then slot 0 of k, ...
+  return true;
+}
+
+// Row r's largest maximum over all pieces, then pieces i0, i0 + step, ... of its sums (lane: channels 4 lane .. + 3, and 128 on)
+__device__ __forceinline__ float join_row(const AttnParams& p, const Pieces& pc, int r, int i0, int step, float& den, float* acc) {
+  const int lane = threadIdx.x & 31, D = p.head_dim, R = p.tile_rows;
+  float top = -INFINITY;
+  for (int i = lane; i < pc.n; i += 32) top = fmaxf(top, pc.at(i)[R * D + r]);
+  top = warp_max(top);
+  const float base = top == -INFINITY ? 0.f : top;
+  den = 0.f;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) acc[c] = 0.f;
+#pragma unroll 6
+  for (int i = i0; i < pc.n; i += step) {
+    const float* part = pc.at(i);
+    const float f = ex2(part[R * D + r] - base);
+    den = fmaf(f, part[R * D + R + r], den);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int c = half * 128 + lane * 4;
+      if (c < D) {
+        const float4 o = *reinterpret_cast<const float4*>(part + r * D + c);
+        acc[half * 4] = fmaf(f, o.x, acc[half * 4]);
+        acc[half * 4 + 1] = fmaf(f, o.y, acc[half * 4 + 1]);
+        acc[half * 4 + 2] = fmaf(f, o.z, acc[half * 4 + 2]);
+        acc[half * 4 + 3] = fmaf(f, o.w, acc[half * 4 + 3]);
+      }
+    }
+  }
+  return top;
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
+  __shared__ float sums[kJoinWarps][256 + 1];
   grid_dependency_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = p.head_dim;
   const bool solo = p.status[1] != 0;
-  if (solo && warp >= kWorkersPerCta) return;
-  const int k0 = solo ? blockIdx.x * kWorkersPerCta + warp : blockIdx.x;
-  if (k0 == 0) return;
-  const Boundary bd = p.boundary[k0];
-  if (bd.seg1 == 0) return;
-  const Boundary before = p.boundary[k0 - 1];
-  if (before.seg1 != 0 && before.seg0 == bd.seg0) return;                   // the segment's first cut is an earlier one
-  const Sequence s = sequence_at(p, bd.b);
-  const int D = p.head_dim, R = p.tile_rows, rows = min(R, s.n * p.group - bd.tile * R);
-  const size_t stride = partial_floats(R, D);
-  const int pieces = static_cast<int>((bd.seg1 - 1) / bd.quota) - k0 + 2;   // up to the worker of the segment's last unit
-  const float* first = p.partial + (static_cast<size_t>(k0) * 2 - 1) * stride;   // slot 1 of k0 - 1; then slot 0 of k0, ...
-  auto piece = [&](int i) { return first + (i == 0 ? 0 : 2 * i - 1) * stride; };
-  for (int r = solo ? 0 : blockIdx.y * (kJoinThreads / 32) + warp; r < rows; r += solo ? 1 : gridDim.y * (kJoinThreads / 32)) {
-    float top = -INFINITY;
-    for (int i = lane; i < pieces; i += 32) top = fmaxf(top, piece(i)[R * D + r]);
-    top = warp_max(top);
-    const float base = top == -INFINITY ? 0.f : top;
-    float den = 0.f, acc[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) acc[c] = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < pieces; ++i) {
-      const float* part = piece(i);
-      const float f = ex2(part[R * D + r] - base);
-      den = fmaf(f, part[R * D + R + r], den);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int c = half * 128 + lane * 4;
-        if (c < D) {
-          const float4 o = *reinterpret_cast<const float4*>(part + r * D + c);
-          acc[half * 4] = fmaf(f, o.x, acc[half * 4]);
-          acc[half * 4 + 1] = fmaf(f, o.y, acc[half * 4 + 1]);
-          acc[half * 4 + 2] = fmaf(f, o.z, acc[half * 4 + 2]);
-          acc[half * 4 + 3] = fmaf(f, o.w, acc[half * 4 + 3]);
-        }
-      }
-    }
+  Boundary bd;
+  Pieces pc;
+  float den, acc[8];
+  auto finish = [&](int r, float top, float d, const float* x) {       // x: what this lane has of the row, as join_row gives it
     const RowAt at = row_at(p, bd.tile, bd.head, r);
-    char* out = out_at(p, bd.b, s.first, at);
+    char* out = out_at(p, bd.b, bd.first, at);
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-      const int d = (c / 4) * 128 + lane * 4 + c % 4;
-      if (d < D) store_out<T>(out, d, den == 0.f ? 0.f : acc[c] / den);
+      const int ch = (c / 4) * 128 + lane * 4 + c % 4;
+      if (ch < D) store_out<T>(out, ch, d == 0.f ? 0.f : x[c] / d);
     }
-    if (lane == 0 && p.lse) *lse_at(p, bd.b, s.first, at) = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.69314718055994531f;
+    if (lane == 0 && p.lse) *lse_at(p, bd.b, bd.first, at) = d == 0.f ? -INFINITY : (top + log2f(d)) * 0.69314718055994531f;
+  };
+  if (solo || p.tile_rows > 16) {
+    const int flat = blockIdx.y * kJoinWarps + warp;
+    const int k = solo ? blockIdx.x * kWorkersPerCta + flat % kWorkersPerCta : blockIdx.x;
+    const int r0 = solo ? flat / kWorkersPerCta : flat, turn = gridDim.y * kJoinWarps / (solo ? kWorkersPerCta : 1);
+    if (!cut_at(p, k, bd, pc)) return;
+    for (int r = r0; r < bd.rows; r += turn) {
+      const float top = join_row(p, pc, r, 0, 1, den, acc);
+      finish(r, top, den, acc);
+    }
+    return;
   }
+  if (!cut_at(p, blockIdx.x, bd, pc)) return;
+  // 8 rows: two warps a row; 16: one.  At most 16 rows a tile.
+  const int parts = kJoinWarps / (p.tile_rows <= 8 ? 8 : 16), r = warp / parts;
+  float top = 0.f;
+  if (r < bd.rows) {
+    top = join_row(p, pc, r, warp - r * parts, parts, den, acc);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) sums[warp][(c / 4) * 128 + lane * 4 + c % 4] = acc[c];
+    if (lane == 0) sums[warp][256] = den;
+  }
+  __syncthreads();
+  if (r >= bd.rows || warp != r * parts) return;
+  for (int w = 1; w < parts; ++w) {
+    den += sums[warp + w][256];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[c] += sums[warp + w][(c / 4) * 128 + lane * 4 + c % 4];
+  }
+  finish(r, top, den, acc);
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -293,7 +341,7 @@ static Plan plan_launch(const vscan_kv_attention_desc* d) {
     resident = 1;
   } else if (pl.mma) {
     pl.tile_rows = want <= 8 || d->head_dim > 128 ? 8 : 16;   // 16 rows of 256 channels do not fit the registers
-    resident = d->head_dim > 128 || pl.tile_rows > 8 ? 2 : 3;
+    resident = d->head_dim > 128 || pl.tile_rows > 8 ? 2 : 4;
   } else {
     pl.tile_rows = want <= 1 ? 1 : want <= 2 ? 2 : want <= 4 ? 4 : 8;
     resident = 4;
@@ -338,7 +386,7 @@ static vscan_status launch_fma(const AttnParams& p, const Plan& pl, cudaStream_t
 template <int KV, int DP, bool FULL>
 static vscan_status launch_mma(const AttnParams& p, const Plan& pl, cudaStream_t stream) {
   const size_t smem = (static_cast<size_t>(4) * pl.tile_rows * (DP + 2)) * sizeof(float);
-  constexpr int MT = DP == 256 ? 1 : 2;
+  constexpr int MT = 1;
 #define VSCAN_MMA_CASE(NT)                                                                                          \
   if (pl.tile_rows == 8 * NT) {                                                                                     \
     auto kernel = mma_kernel<KV, DP, NT, MT, FULL>;                                                                 \
@@ -386,7 +434,7 @@ static vscan_status launch_attention(const AttnParams& p, const Plan& pl, int kv
   // nothing can have been cut when the table has room for kWhole units only (few rows), or when one CTA did it all
   if ((!pl.tensor && static_cast<int64_t>(p.max_blocks) * p.block_size <= kWhole * kUnit) || pl.ctas == 1) return VSCAN_OK;
   prof_before("kv_attention_join", stream);
-  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, dim3(pl.ctas, pl.tensor ? kTcRows / 16 : 1), dim3(kJoinThreads), 0, stream, p));
+  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, dim3(pl.ctas, pl.tensor ? kTcRows / 32 : 1), dim3(kJoinThreads), 0, stream, p));
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
   return VSCAN_OK;

@@ -42,7 +42,7 @@ constexpr int kWorkersPerCta = 4;
 struct Boundary {       // what lies at the start of a worker's stretch
   long long seg0, seg1; // the segment that is cut there, as places on the line; seg1 = 0: none
   long long quota;
-  int b, head, tile, solo;   // solo: the workers are warps
+  int b, head, tile, first, rows, pad;   // first row of the sequence; query rows of the tile
 };
 
 struct Sequence {       // of one sequence: new rows, keys, tiles, units of a segment
@@ -67,10 +67,11 @@ struct ScheduleShared {
   int b[kWorkersPerCta];
 };
 
-struct Stretch {          // of a worker: [begin, end) of the line, where its first sequence is
-  long long begin, end, quota, seq0;
-  int b, worker, whole;
-  bool solo;
+struct Stretch {          // of a worker: [begin, end) of the line, and the segment that it is in
+  long long begin, end, quota, seq0, seg0;
+  Sequence s;
+  int b, head, tile, worker, whole;
+  bool solo, inside;
 };
 
 // The stretch of this thread's worker.  Called by all THREADS threads; SOLO: whether warps may be workers.
@@ -125,29 +126,37 @@ __device__ __forceinline__ Stretch locate(const AttnParams& p, ScheduleShared& s
   st.end = min(st.begin + st.quota, total);
   st.b = sh.b[k];                   // not set, and not used, where the stretch is empty
   st.seq0 = sh.seq0[k];
+  st.inside = false;
   return st;
 }
 
-// The next piece of a worker's stretch
-struct Piece {
-  Sequence s;
-  long long seg0;
-  int b, head, tile, u0, u1;
-};
+// The next piece of a worker's stretch: units u0 .. u1 - 1 of the segment that the stretch is in then.  Only the first takes
+// divisions; from there on segment follows segment, and a sequence's lengths are read once.
+struct Piece { int u0, u1; };
 __device__ __forceinline__ bool next_piece(const AttnParams& p, Stretch& st, Piece& pc) {
   while (st.begin < st.end) {
-    pc.s = sequence_at(p, st.b);
-    if (st.begin >= st.seq0 + pc.s.weight) { st.seq0 += pc.s.weight; ++st.b; continue; }
-    const long long seg = (st.begin - st.seq0) / pc.s.units;
-    pc.seg0 = st.seq0 + seg * pc.s.units;
-    pc.head = static_cast<int>(seg / pc.s.tiles);
-    pc.tile = static_cast<int>(seg - static_cast<long long>(pc.head) * pc.s.tiles);
-    pc.b = st.b;
-    const bool whole = pc.s.units <= st.whole;
-    pc.u0 = static_cast<int>(st.begin - pc.seg0);
-    st.begin = pc.seg0 + pc.s.units;
+    if (!st.inside) {
+      st.s = sequence_at(p, st.b);
+      if (st.begin >= st.seq0 + st.s.weight) { st.seq0 += st.s.weight; ++st.b; continue; }
+      const long long seg = (st.begin - st.seq0) / st.s.units;
+      st.seg0 = st.seq0 + seg * st.s.units;
+      st.head = static_cast<int>(seg / st.s.tiles);
+      st.tile = static_cast<int>(seg - static_cast<long long>(st.head) * st.s.tiles);
+      st.inside = true;
+    } else {                                             // the segment before is done with
+      st.seg0 = st.begin;
+      if (++st.tile == st.s.tiles) { st.tile = 0; ++st.head; }
+      if (st.head == p.kv_heads) {
+        st.seq0 += st.s.weight;
+        do st.s = sequence_at(p, ++st.b); while (st.s.tiles == 0);     // there is one: the stretch goes on
+        st.head = 0;
+      }
+    }
+    const bool whole = st.s.units <= st.whole;
+    pc.u0 = static_cast<int>(st.begin - st.seg0);
+    st.begin = st.seg0 + st.s.units;
     if (whole && pc.u0 > 0) continue;                    // the worker before this one has it
-    pc.u1 = whole ? pc.s.units : static_cast<int>(min(st.end - pc.seg0, static_cast<long long>(pc.s.units)));
+    pc.u1 = whole ? st.s.units : static_cast<int>(min(st.end - st.seg0, static_cast<long long>(st.s.units)));
     return true;
   }
   return false;

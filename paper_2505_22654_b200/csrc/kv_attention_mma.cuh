@@ -63,7 +63,7 @@ __device__ __forceinline__ uint2 ld_nc_8(const void* p) {
 // DP: head_dim rounded up to 64, 128 or 256.  NT: tiles of 8 query rows.  MT: groups of 16 tokens of a step.  FULL: head_dim is DP,
 // so that where a lane's pieces lie within a block is known at compile time.
 template <int KV, int DP, int NT, int MT, bool FULL>
-__global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_kernel(AttnParams p) {
+__global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_kernel(AttnParams p) {
   constexpr int R = 8 * NT, KS = DP / 16, kPieces = DP / 64, kStep = 16 * MT;
   constexpr int kVWords = DP / 32;                   // 32-bit words of V codes of a lane and token
   extern __shared__ __align__(16) float attn_smem[];
@@ -71,23 +71,36 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
   float* m_sh = o_sh + 4 * R * DP;
   float* l_sh = m_sh + 4 * R;
   __shared__ ScheduleShared sched;
+  __shared__ Stretch stretches[kMmaThreads / 32];     // of each warp: too much for its registers
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const int D = FULL ? DP : p.head_dim;
   grid_dependency_wait();
-  Stretch st = locate<kMmaThreads, true>(p, sched);
+  Stretch& st = stretches[threadIdx.x >> 5];
+  {
+    const Stretch found = locate<kMmaThreads, true>(p, sched);
+    if (lane == 0) st = found;
+    __syncwarp();
+  }
+  const int worker = st.worker;
+  const bool solo = st.solo;
   if (threadIdx.x == 0) {
-    if (blockIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = st.solo; }
+    if (blockIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = solo; }
     p.flags[blockIdx.x] = 0;
   }
-  const bool writes_boundary = lane == 0 && (st.solo || warp == 0);
-  if (writes_boundary) p.boundary[st.worker].seg1 = 0;
+  const bool writes_boundary = lane == 0 && (solo || warp == 0);
+  if (writes_boundary) p.boundary[worker].seg1 = 0;
   bool bad = false;
-  Piece pc;
-  while (next_piece(p, st, pc)) {
-    const Sequence& s = pc.s;
-    const int b = pc.b, head = pc.head, tile = pc.tile;
-    if (pc.u0 > 0 && writes_boundary) p.boundary[st.worker] = {pc.seg0, pc.seg0 + s.units, st.quota, b, head, tile, st.solo};
+  while (true) {
+    Piece pc = {0, 0};
+    __syncwarp();
+    if (lane == 0) next_piece(p, st, pc);
+    pc.u0 = __shfl_sync(0xffffffffu, pc.u0, 0);
+    pc.u1 = __shfl_sync(0xffffffffu, pc.u1, 0);
+    if (pc.u1 == 0) break;
+    const Sequence& s = st.s;
+    const int b = st.b, head = st.head, tile = st.tile;
     const int n_rows = min(R, s.n * p.group - tile * R);
+    if (pc.u0 > 0 && writes_boundary) p.boundary[worker] = {st.seg0, st.seg0 + s.units, st.quota, b, head, tile, s.first, n_rows, 0};
     if (p.kv_len[b] > s.len) bad = true;
 
     const int32_t* table = p.block_table + static_cast<size_t>(b) * p.max_blocks;
@@ -95,7 +108,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
     const int last_row = tile * R + n_rows - 1;
     const int most = visible(p, s, last_row / p.group);
     const int stop = min(most, pc.u1 * kUnit);
-    const int t_first = pc.u0 * kUnit + (st.solo ? 0 : warp * kStep), t_stride = st.solo ? kStep : 4 * kStep;
+    const int t_first = pc.u0 * kUnit + (solo ? 0 : warp * kStep), t_stride = solo ? kStep : 4 * kStep;
 
     // ---- loads of a step: block numbers, codes, scales
     int blk[MT], blk_next[MT];
@@ -180,7 +193,6 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
     load_k(t_first);
     load_v(t_first);
     load_table(t_first + t_stride, blk_next);
-
     // ---- queries: fragments of the rows g of each tile, scaled by a power of two; what a score is multiplied by
     uint32_t qf[KS][NT][2];
     float cq[NT][2], m[NT][2], l[NT][2];
@@ -384,14 +396,14 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
     // DP 64: 8 g + 4 w; else 128 (w / 4) + 16 g + 4 (w % 4); within a word o[2w][k], o[2w][k + 2], o[2w + 1][k], o[2w + 1][k + 2].
     const float unit = ref * (1.f / kWeightScale);
     const bool complete = pc.u0 == 0 && pc.u1 == s.units;
-    float* part = p.partial + (static_cast<size_t>(st.worker) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(R, D);
+    float* part = p.partial + (static_cast<size_t>(worker) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(R, D);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) l[nt][k] += __shfl_xor_sync(0xffffffffu, l[nt][k], off);
-    if (st.solo) {
+    if (solo) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -465,6 +477,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 3) mma_
     }
   }
   if (bad) p.flags[blockIdx.x] = VSCAN_ERR_INVALID_ARG;
+  grid_dependency_launch();
 }
 
 }  // namespace kv

@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
     while (ok && tc_next(p, st, pc)) {
       const int steps = pc.u1 - pc.u0;
       if (pc.u0 > 0 && threadIdx.x == 0)
-        p.boundary[blockIdx.x] = {pc.seg0, pc.seg1, st.quota, pc.b, pc.head, pc.tile, 0};
+        p.boundary[blockIdx.x] = {pc.seg0, pc.seg1, st.quota, pc.b, pc.head, pc.tile, pc.q.s.first, pc.n_rows, 0};
       if (tile * 128 >= pc.n_rows) { step += steps; continue; }
       if (p.kv_len[pc.b] > pc.q.s.len) bad = true;
       const int in_tile = tile * 128 + r;
