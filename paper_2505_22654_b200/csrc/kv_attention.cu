@@ -205,7 +205,8 @@ __device__ __forceinline__ bool cut_at(const AttnParams& p, int k, Boundary& bd,
   return true;
 }
 
-// Row r's largest maximum over all pieces, then pieces i0, i0 + step, ... of its sums (lane: channels 4 lane .. + 3, and 128 on)
+// Row r: its largest maximum over all pieces, its denominator, and pieces i0, i0 + step, ... of its sums (lane: channels
+// 4 lane .. + 3, and 128 on).  A lane has the maximum and denominator of a piece; 32 pieces at a time.
 __device__ __forceinline__ float join_row(const AttnParams& p, const Pieces& pc, int r, int i0, int step, float& den, float* acc) {
   const int lane = threadIdx.x & 31, D = p.head_dim, R = p.tile_rows;
   float top = -INFINITY;
@@ -215,29 +216,36 @@ __device__ __forceinline__ float join_row(const AttnParams& p, const Pieces& pc,
   den = 0.f;
 #pragma unroll
   for (int c = 0; c < 8; ++c) acc[c] = 0.f;
-#pragma unroll 6
-  for (int i = i0; i < pc.n; i += step) {
-    const float* part = pc.at(i);
-    const float f = ex2(part[R * D + r] - base);
-    den = fmaf(f, part[R * D + R + r], den);
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
+  for (int first = 0; first < pc.n; first += 32) {
+    float f = 0.f;
+    if (first + lane < pc.n) {
+      const float* part = pc.at(first + lane);
+      f = ex2(part[R * D + r] - base);
+      den = fmaf(f, part[R * D + R + r], den);
+    }
+    const int count = min(32, pc.n - first);
+    for (int half = 0; half < (D > 128 ? 2 : 1); ++half) {
       const int c = half * 128 + lane * 4;
-      if (c < D) {
-        const float4 o = *reinterpret_cast<const float4*>(part + r * D + c);
-        acc[half * 4] = fmaf(f, o.x, acc[half * 4]);
-        acc[half * 4 + 1] = fmaf(f, o.y, acc[half * 4 + 1]);
-        acc[half * 4 + 2] = fmaf(f, o.z, acc[half * 4 + 2]);
-        acc[half * 4 + 3] = fmaf(f, o.w, acc[half * 4 + 3]);
+      float4 a = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      if (half) a = make_float4(acc[4], acc[5], acc[6], acc[7]);
+#pragma unroll 8
+      for (int i = i0; i < count; i += step) {
+        const float g = __shfl_sync(0xffffffffu, f, i);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < D) o = *reinterpret_cast<const float4*>(pc.at(first + i) + r * D + c);
+        a.x = fmaf(g, o.x, a.x); a.y = fmaf(g, o.y, a.y); a.z = fmaf(g, o.z, a.z); a.w = fmaf(g, o.w, a.w);
       }
+      if (half) { acc[4] = a.x; acc[5] = a.y; acc[6] = a.z; acc[7] = a.w; }
+      else { acc[0] = a.x; acc[1] = a.y; acc[2] = a.z; acc[3] = a.w; }
     }
   }
+  den = warp_sum(den);
   return top;
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
-  __shared__ float sums[kJoinWarps][256 + 1];
+  __shared__ float sums[kJoinWarps][256];
   grid_dependency_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = p.head_dim;
   const bool solo = p.status[1] != 0;
@@ -273,12 +281,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
     top = join_row(p, pc, r, warp - r * parts, parts, den, acc);
 #pragma unroll
     for (int c = 0; c < 8; ++c) sums[warp][(c / 4) * 128 + lane * 4 + c % 4] = acc[c];
-    if (lane == 0) sums[warp][256] = den;
   }
   __syncthreads();
   if (r >= bd.rows || warp != r * parts) return;
   for (int w = 1; w < parts; ++w) {
-    den += sums[warp + w][256];
 #pragma unroll
     for (int c = 0; c < 8; ++c) acc[c] += sums[warp + w][(c / 4) * 128 + lane * 4 + c % 4];
   }

@@ -64,6 +64,7 @@ __device__ __forceinline__ Sequence sequence_at(const AttnParams& p, int b) {
 struct ScheduleShared {
   long long weight[32], segments[32];
   long long seq0[kWorkersPerCta];
+  Sequence s[kWorkersPerCta];
   int b[kWorkersPerCta];
 };
 
@@ -113,9 +114,9 @@ __device__ __forceinline__ Stretch locate(const AttnParams& p, ScheduleShared& s
     if (at <= begin && begin < at + sum) {
       long long first = at;
       for (int b = b0; b < b1; ++b) {
-        const long long w = sequence_at(p, b).weight;
-        if (begin < first + w) { sh.b[k] = b; sh.seq0[k] = first; break; }
-        first += w;
+        const Sequence s = sequence_at(p, b);
+        if (begin < first + s.weight) { sh.b[k] = b; sh.seq0[k] = first; sh.s[k] = s; break; }
+        first += s.weight;
       }
     }
   }
@@ -126,6 +127,7 @@ __device__ __forceinline__ Stretch locate(const AttnParams& p, ScheduleShared& s
   st.end = min(st.begin + st.quota, total);
   st.b = sh.b[k];                   // not set, and not used, where the stretch is empty
   st.seq0 = sh.seq0[k];
+  st.s = sh.s[k];
   st.inside = false;
   return st;
 }
@@ -136,12 +138,10 @@ struct Piece { int u0, u1; };
 __device__ __forceinline__ bool next_piece(const AttnParams& p, Stretch& st, Piece& pc) {
   while (st.begin < st.end) {
     if (!st.inside) {
-      st.s = sequence_at(p, st.b);
-      if (st.begin >= st.seq0 + st.s.weight) { st.seq0 += st.s.weight; ++st.b; continue; }
-      const long long seg = (st.begin - st.seq0) / st.s.units;
+      const unsigned long long at = st.begin - st.seq0, seg = (at >> 32) == 0 ? static_cast<unsigned>(at) / st.s.units : at / st.s.units;
       st.seg0 = st.seq0 + seg * st.s.units;
-      st.head = static_cast<int>(seg / st.s.tiles);
-      st.tile = static_cast<int>(seg - static_cast<long long>(st.head) * st.s.tiles);
+      st.head = (seg >> 32) == 0 ? static_cast<unsigned>(seg) / st.s.tiles : static_cast<int>(seg / st.s.tiles);
+      st.tile = static_cast<int>(seg - static_cast<unsigned long long>(st.head) * st.s.tiles);
       st.inside = true;
     } else {                                             // the segment before is done with
       st.seg0 = st.begin;

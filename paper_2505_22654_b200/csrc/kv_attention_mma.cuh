@@ -189,10 +189,38 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
         }
       }
     };
+    // the queries' loads first: they wait for nothing else
+    uint4 q_raw[NT][kPieces][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = nt * 8 + g;
+      const char* src = q_at(p, b, s.first, row_at(p, tile, head, r < n_rows ? r : 0));
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          q_raw[nt][i][k] = make_uint4(0, 0, 0, 0);
+          if (r < n_rows && i * 64 + c * 16 < D) q_raw[nt][i][k] = ld_nc_16(src + (i * 64 + c * 16) * 2 + k * 16);
+        }
+    }
     load_table(t_first, blk);
     load_k(t_first);
     load_v(t_first);
     load_table(t_first + t_stride, blk_next);
+    // Workers that are CTAs have little to do each and wait for DRAM most of the time: all their blocks (128 at most) are asked
+    // into L2 at once, a thread a block.  (Not so for warps: there is enough under way, and it made them slower.)
+    if (!solo) {
+      const int j = (pc.u0 * kUnit >> p.shift) + threadIdx.x;
+      if (static_cast<long long>(j) << p.shift < stop) {
+        const int x = table[j];
+        if (x >= 0 && x < p.num_blocks) {
+          const size_t at = (static_cast<size_t>(x) * p.kv_heads + head) * cell_bytes;
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.k_cache + at), "r"(static_cast<uint32_t>(cell_bytes)) : "memory");
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.v_cache + at), "r"(static_cast<uint32_t>(cell_bytes)) : "memory");
+        }
+      }
+    }
+
     // ---- queries: fragments of the rows g of each tile, scaled by a power of two; what a score is multiplied by
     uint32_t qf[KS][NT][2];
     float cq[NT][2], m[NT][2], l[NT][2];
@@ -200,20 +228,13 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
     int fewest = 0x7fffffff;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int r = nt * 8 + g;
-      uint4 raw[kPieces][2];
-      const bool on = r < n_rows;
-      const char* src = q_at(p, b, s.first, row_at(p, tile, head, on ? r : 0));
       float top = 0.f;
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
-        const int d0 = i * 64 + c * 16;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          raw[i][k] = make_uint4(0, 0, 0, 0);
-          if (on && d0 < D) raw[i][k] = ld_nc_16(src + d0 * 2 + k * 16);
           float f[8];
-          Vec16<__nv_bfloat16>::unpack(raw[i][k], f);
+          Vec16<__nv_bfloat16>::unpack(q_raw[nt][i][k], f);
 #pragma unroll
           for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
         }
@@ -227,7 +248,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           float f[8];
-          Vec16<__nv_bfloat16>::unpack(raw[i][k], f);
+          Vec16<__nv_bfloat16>::unpack(q_raw[nt][i][k], f);
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
             qf[i * 4 + k * 2 + w][nt][0] = pack_f16(f[4 * w] * up, f[4 * w + 1] * up);
