@@ -39,6 +39,7 @@ struct TcShared {
   uint32_t tmem_base;
   int abort_flag;
   float4 group[16][4];                    // per warp: of each of its 16-token groups {K scale, V shift, its inverse factor}
+  float q_scale[2][128];                  // [tile][row]: what a score is multiplied by
   float swap[2][2][2][128];               // [step parity][tile][half][row]: what the two threads of a row tell each other
   uint32_t there[kTcRing];                // of the 16-token groups of a step: a bit each, not there at all: 0
   alignas(16) float ks[kTcRing][8], vs[kTcRing][8];
@@ -49,19 +50,24 @@ struct TcShared {
 
 // ---------------------------------------------------------------------------------------------- division of the work
 // As for few rows, but a place on the line is a key seen by a query row, so that the triangle of a causal prompt is divided
-// evenly: tile k of a causal sequence weighs group * start + min(256 (k + 1), rows), which has a closed prefix sum.
+// evenly: tile k of a causal sequence weighs group * start + min(256 (k + 1), rows), at least one step, which has a closed
+// prefix sum.
 struct TcSequence {
   Sequence s;
-  long long base;       // what every tile weighs at least
+  long long base;       // what every tile sees at least
   long long rows;       // query rows; causal tiles weigh more one after another
   long long weight;     // of all tiles of a KV head
-  int tiles;
+  int tiles, light;     // light: tiles in front that weigh one step although they see less
 };
 
-__device__ __forceinline__ long long tiles_before(const TcSequence& q, bool causal, long long k) {
-  if (!causal) return k * q.base;
-  const long long grown = k < q.tiles ? k * (k + 1) * (kTcRows / 2) : static_cast<long long>(q.tiles - 1) * q.tiles * (kTcRows / 2) + q.rows;
-  return k * q.base + grown;
+__device__ __forceinline__ long long step_weight(const AttnParams& p) { return static_cast<long long>(kTcKeys) * p.group; }
+
+__device__ __forceinline__ long long tiles_before(const AttnParams& p, const TcSequence& q, long long k) {
+  const long long one = step_weight(p);
+  if (!p.causal) return k * max(q.base, one);
+  const long long n = min(k, static_cast<long long>(q.tiles - 1)), m = min(n, static_cast<long long>(q.light));
+  const long long sum = m * one + (n - m) * q.base + (n * (n + 1) - m * (m + 1)) * (kTcRows / 2);
+  return k < q.tiles ? sum : sum + max(q.base + q.rows, one);
 }
 
 __device__ __forceinline__ TcSequence tc_sequence_at(const AttnParams& p, int b) {
@@ -69,9 +75,15 @@ __device__ __forceinline__ TcSequence tc_sequence_at(const AttnParams& p, int b)
   q.s = sequence_at(p, b);
   q.rows = static_cast<long long>(q.s.n) * p.group;
   q.tiles = static_cast<int>((q.rows + kTcRows - 1) / kTcRows);
-  q.base = p.causal ? max(q.s.start, 0ll) * p.group : max(static_cast<long long>(q.s.len) * p.group, 1ll);
-  q.weight = q.tiles > 0 ? tiles_before(q, p.causal, q.tiles) : 0;
+  q.base = p.causal ? max(q.s.start, 0ll) * p.group : static_cast<long long>(q.s.len) * p.group;
+  q.light = static_cast<int>(max((max(step_weight(p) - q.base, 0ll) + kTcRows - 1) / kTcRows - 1, 0ll));
+  q.weight = q.tiles > 0 ? tiles_before(p, q, q.tiles) : 0;
   return q;
+}
+
+// Quotient of numbers that nearly always fit 32 bits
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? static_cast<unsigned>(a) / static_cast<unsigned>(b) : a / b;
 }
 
 struct TcStretch { long long begin, end, quota, seq0; int b; };
@@ -96,8 +108,8 @@ __device__ __forceinline__ TcStretch tc_locate(const AttnParams& p, TcShared& sh
     total += sh.weight[w];
   }
   TcStretch st;
-  // a stretch is at least four steps long, so that no two cuts fall into one step
-  st.quota = max((total + gridDim.x - 1) / gridDim.x, 4ll * kTcKeys * p.group);
+  // a stretch is at least a step long, so that no two cuts fall into one step
+  st.quota = max(quotient(total + gridDim.x - 1, gridDim.x), step_weight(p));
   st.begin = min(blockIdx.x * st.quota, total);
   st.end = min(st.begin + st.quota, total);
   long long at = before + incl - sum;
@@ -125,22 +137,22 @@ __device__ __forceinline__ bool tc_next(const AttnParams& p, TcStretch& st, TcPi
     pc.q = tc_sequence_at(p, st.b);
     const long long all = pc.q.weight * p.kv_heads;
     if (st.begin >= st.seq0 + all) { st.seq0 += all; ++st.b; continue; }
-    const long long head = (st.begin - st.seq0) / pc.q.weight, rel = st.begin - st.seq0 - head * pc.q.weight;
+    const long long head = quotient(st.begin - st.seq0, pc.q.weight), rel = st.begin - st.seq0 - head * pc.q.weight;
     int lo = 0, hi = pc.q.tiles;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (tiles_before(pc.q, p.causal, mid) <= rel) lo = mid; else hi = mid;
+      if (tiles_before(p, pc.q, mid) <= rel) lo = mid; else hi = mid;
     }
     pc.head = static_cast<int>(head); pc.tile = lo; pc.b = st.b;
-    pc.seg0 = st.begin - (rel - tiles_before(pc.q, p.causal, lo));
-    const long long seg_end = pc.seg0 + tiles_before(pc.q, p.causal, lo + 1) - tiles_before(pc.q, p.causal, lo);
+    pc.seg0 = st.begin - (rel - tiles_before(p, pc.q, lo));
+    const long long seg_end = pc.seg0 + tiles_before(p, pc.q, lo + 1) - tiles_before(p, pc.q, lo);
     pc.n_rows = static_cast<int>(min(static_cast<long long>(kTcRows), pc.q.rows - static_cast<long long>(lo) * kTcRows));
     pc.most = visible(p, pc.q.s, (lo * kTcRows + pc.n_rows - 1) / p.group);
     pc.units = max(1, (pc.most + kTcKeys - 1) / kTcKeys);
-    const long long per_unit = static_cast<long long>(kTcKeys) * p.group;
+    const long long per_unit = step_weight(p);
     pc.seg1 = min(seg_end, pc.seg0 + pc.units * per_unit);
-    pc.u0 = static_cast<int>(min((st.begin - pc.seg0) / per_unit, static_cast<long long>(pc.units)));
-    pc.u1 = st.end >= seg_end ? pc.units : static_cast<int>(min((st.end - pc.seg0) / per_unit, static_cast<long long>(pc.units)));
+    pc.u0 = static_cast<int>(min(quotient(st.begin - pc.seg0, per_unit), static_cast<long long>(pc.units)));
+    pc.u1 = st.end >= seg_end ? pc.units : static_cast<int>(min(quotient(st.end - pc.seg0, per_unit), static_cast<long long>(pc.units)));
     st.begin = seg_end;
     if (pc.u0 < pc.u1) return true;
   }
@@ -315,7 +327,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
     const uint32_t s_addr = tmem + lanes + tile * 128 + half * 64;                      // this thread's scores, and its weights
     const uint32_t o_addr = tmem + lanes + 256 + tile * 128 + half * (DP / 2);          // its half of the sums
-    unsigned char* q_row = q_sh + tile * kTileBytes + r * 128;
+    int n_piece = 0;         // pieces of this tile so far
     int n_it = 0;            // steps of this tile so far
     int step = 0;            // steps of the CTA so far
     int n_swap = 0;          // exchanges with the row's other thread so far
@@ -340,39 +352,41 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       const RowAt at = {i_row, pc.head * p.group + flat - i_row * p.group};
       const int seen = on ? visible(p, pc.q.s, i_row) : 0;
 
-      // ---- the query row: largest element, power of two, this thread's half of it as f16 into the swizzled tile
-      float cq;
+      // ---- the tile's queries: 16 bytes a thread and pass, each row's largest element among the lanes that have the row, a
+      // power of two, f16 into the swizzled tile
       {
-        const char* src = q_at(p, pc.b, pc.q.s.first, at);
-        auto load8 = [&](int c, float* f) {
-          uint4 raw = make_uint4(0, 0, 0, 0);
-          if (on && c * 8 < D) raw = *reinterpret_cast<const uint4*>(src + c * 16);
-          Vec16<__nv_bfloat16>::unpack(raw, f);
-        };
-        float top = 0.f;
-#pragma unroll 4
-        for (int c = 0; c < DP / 8; ++c) {
-          float f[8];
-          load8(c, f);
+        constexpr int kLanes = DP / 8, kPass = 256 / kLanes, kPasses = 128 / kPass;
+        const int t = threadIdx.x & 255, piece = t % kLanes, row0 = t / kLanes;
+        uint4 raw[kPasses];
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+          const int row = tile * 128 + row0 + i * kPass, f = pc.tile * kTcRows + row, new_row = f / p.group;
+          raw[i] = make_uint4(0, 0, 0, 0);
+          if (row < pc.n_rows && piece * 8 < D)
+            raw[i] = ld_nc_16(q_at(p, pc.b, pc.q.s.first, RowAt{new_row, pc.head * p.group + f - new_row * p.group}) + piece * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+          float f[8], top = 0.f;
+          Vec16<__nv_bfloat16>::unpack(raw[i], f);
 #pragma unroll
           for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
-        }
-        const int e = max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100);
-        const float up = copysignf(exp2_int(min(14 - e, 127)), p.scale_log2e);   // the factor of a score is kept positive
-        cq = exp2_int(max(e - 14, -126)) * fabsf(p.scale_log2e);
-#pragma unroll 4
-        for (int i = 0; i < DP / 16; ++i) {                                      // a second time, from the caches
-          const int c = half * (DP / 16) + i;
-          float f[8];
-          load8(c, f);
+#pragma unroll
+          for (int off = 1; off < kLanes; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+          const int e = max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), row = row0 + i * kPass;
+          const float up = copysignf(exp2_int(min(14 - e, 127)), p.scale_log2e);   // the factor of a score is kept positive
+          if (piece == 0) sh.q_scale[tile][row] = exp2_int(max(e - 14, -126)) * fabsf(p.scale_log2e);
           const uint4 w = make_uint4(pack_f16(f[0] * up, f[1] * up), pack_f16(f[2] * up, f[3] * up), pack_f16(f[4] * up, f[5] * up),
                                      pack_f16(f[6] * up, f[7] * up));
-          *reinterpret_cast<uint4*>(q_row + (c >> 3) * kChunk + (((c & 7) ^ (r & 7)) << 4)) = w;
+          *reinterpret_cast<uint4*>(q_sh + tile * kTileBytes + (piece >> 3) * kChunk + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = w;
         }
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_full[tile]);
+        ok = mbar_wait_warp(&sh.q_full[tile], n_piece++ & 1, abort_flag);
+        if (!ok) break;
       }
+      const float cq = sh.q_scale[tile][r];
 
       float m = -INFINITY, l = 0.f, ref = 0.f;
       for (int j = 0; j < steps && ok; ++j, ++n_it, ++step) {
