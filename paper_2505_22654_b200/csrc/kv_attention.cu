@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
 // added in a fixed order, so results do not depend on timing.  Three shapes of the work:
 //   few rows, workers are CTAs    a few segments in many pieces: CTA k joins segment k, its warps share a row's pieces
 //   few rows, workers are warps   many segments in two pieces or three: a warp takes a row
-//   256 rows a tile               a warp takes a row, again and again
+//   256 rows a tile               a CTA takes 32 rows: their factors first, then all their channels side by side
 constexpr int kJoinThreads = 512;
 constexpr int kJoinWarps = kJoinThreads / 32;
 
@@ -262,14 +262,86 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
     }
     if (lane == 0 && p.lse) *lse_at(p, bd.b, bd.first, at) = d == 0.f ? -INFINITY : (top + log2f(d)) * 0.69314718055994531f;
   };
-  if (solo || p.tile_rows > 16) {
-    const int flat = blockIdx.y * kJoinWarps + warp;
-    const int k = solo ? blockIdx.x * kWorkersPerCta + flat % kWorkersPerCta : blockIdx.x;
-    const int r0 = solo ? flat / kWorkersPerCta : flat, turn = gridDim.y * kJoinWarps / (solo ? kWorkersPerCta : 1);
+  if (solo) {
+    const int k = blockIdx.x * kWorkersPerCta + warp % kWorkersPerCta;
     if (!cut_at(p, k, bd, pc)) return;
-    for (int r = r0; r < bd.rows; r += turn) {
+    for (int r = warp / kWorkersPerCta; r < bd.rows; r += kJoinWarps / kWorkersPerCta) {
       const float top = join_row(p, pc, r, 0, 1, den, acc);
       finish(r, top, den, acc);
+    }
+    return;
+  }
+  if (p.tile_rows > 16) {
+    constexpr int kBatch = 96;                                    // pieces whose factors fit beside the rows' maxima and sums
+    float (*tops)[32] = reinterpret_cast<float (*)[32]>(&sums[0][0]);
+    float (*dens)[32] = tops + kJoinWarps;
+    float (*factor)[32] = dens + kJoinWarps;
+    static_assert((2 * kJoinWarps + kBatch) * 32 <= kJoinWarps * 256, "fits the sums");
+    if (!cut_at(p, blockIdx.x, bd, pc)) return;
+    const int R = p.tile_rows, r0 = blockIdx.y * 32, mine = r0 + lane, n_rows = min(32, bd.rows - r0);
+    if (n_rows <= 0) return;
+    float top = -INFINITY;
+    if (lane < n_rows)
+      for (int i = warp; i < pc.n; i += kJoinWarps) top = fmaxf(top, pc.at(i)[R * D + mine]);
+    tops[warp][lane] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, tops[w][lane]);
+    const float base = top == -INFINITY ? 0.f : top;
+    den = 0.f;
+    constexpr int kEach = 4;                                      // 32 rows x 256 channels at most, four at a time
+    const int per_row = D / 4, total = n_rows * per_row;
+    float4 o[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int first = 0; first < pc.n; first += kBatch) {
+      const int count = min(kBatch, pc.n - first);
+      for (int i = warp; i < count; i += kJoinWarps) {
+        float f = 0.f;
+        if (lane < n_rows) {
+          const float* part = pc.at(first + i);
+          f = ex2(part[R * D + mine] - base);
+          den = fmaf(f, part[R * D + R + mine], den);
+        }
+        factor[i][lane] = f;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int idx = threadIdx.x + e * kJoinThreads;
+        if (idx < total) {
+          const int row = idx / per_row, c = (idx - row * per_row) * 4;
+          for (int i = 0; i < count; ++i) {
+            const float f = factor[i][row];
+            const float4 x = *reinterpret_cast<const float4*>(pc.at(first + i) + static_cast<size_t>(r0 + row) * D + c);
+            o[e].x = fmaf(f, x.x, o[e].x); o[e].y = fmaf(f, x.y, o[e].y); o[e].z = fmaf(f, x.z, o[e].z); o[e].w = fmaf(f, x.w, o[e].w);
+          }
+        }
+      }
+      __syncthreads();
+    }
+    dens[warp][lane] = den;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int idx = threadIdx.x + e * kJoinThreads;
+      if (idx < total) {
+        const int row = idx / per_row, c = (idx - row * per_row) * 4;
+        float d = 0.f;
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) d += dens[w][row];
+        const RowAt at = row_at(p, bd.tile, bd.head, r0 + row);
+        char* out = out_at(p, bd.b, bd.first, at);
+        const float inv = d == 0.f ? 0.f : 1.f / d;
+        store_out<T>(out, c, o[e].x * inv); store_out<T>(out, c + 1, o[e].y * inv);
+        store_out<T>(out, c + 2, o[e].z * inv); store_out<T>(out, c + 3, o[e].w * inv);
+      }
+    }
+    if (warp == 0 && lane < n_rows && p.lse) {
+      float d = 0.f;
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) d += dens[w][lane];
+      *lse_at(p, bd.b, bd.first, row_at(p, bd.tile, bd.head, mine)) = d == 0.f ? -INFINITY : (top + log2f(d)) * 0.69314718055994531f;
     }
     return;
   }
@@ -437,8 +509,9 @@ template <typename T>
 static vscan_status launch_attention(const AttnParams& p, const Plan& pl, int kv_dtype, cudaStream_t stream) {
   const vscan_status st = kv_dtype == VSCAN_KV_E4M3 ? launch_scores<T, VSCAN_KV_E4M3>(p, pl, stream) : launch_scores<T, VSCAN_KV_I8>(p, pl, stream);
   if (st != VSCAN_OK) return st;
-  // nothing can have been cut when the table has room for kWhole units only (few rows), or when one CTA did it all
-  if ((!pl.tensor && static_cast<int64_t>(p.max_blocks) * p.block_size <= kWhole * kUnit) || pl.ctas == 1) return VSCAN_OK;
+  // nothing can have been cut when the table has room for kWhole units only (many rows: kTcWhole steps), or when one CTA did
+  // it all
+  if (static_cast<int64_t>(p.max_blocks) * p.block_size <= (pl.tensor ? kTcWhole * kTcKeys : kWhole * kUnit) || pl.ctas == 1) return VSCAN_OK;
   prof_before("kv_attention_join", stream);
   VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, dim3(pl.ctas, pl.tensor ? kTcRows / 32 : 1), dim3(kJoinThreads), 0, stream, p));
   prof_after(stream);

@@ -28,6 +28,7 @@ constexpr int kTcThreads = 672;
 constexpr int kTcConverter = 16, kTcIssuer = 20;   // first warp of each role
 constexpr int kTcRows = 256;          // query rows of a CTA
 constexpr int kTcKeys = 128;          // keys of a step
+constexpr int kTcWhole = 4;           // a tile of up to this many steps is not cut: joining 256 rows takes longer than they do
 constexpr int kTcRing = 4;            // steps whose scales are kept: the converters are at most three ahead of a reader
 constexpr int kChunk = 128 * 128;     // bytes of [128 rows x 64 f16]
 
@@ -153,8 +154,10 @@ __device__ __forceinline__ bool tc_next(const AttnParams& p, TcStretch& st, TcPi
     pc.seg1 = min(seg_end, pc.seg0 + pc.units * per_unit);
     pc.u0 = static_cast<int>(min(quotient(st.begin - pc.seg0, per_unit), static_cast<long long>(pc.units)));
     pc.u1 = st.end >= seg_end ? pc.units : static_cast<int>(min(quotient(st.end - pc.seg0, per_unit), static_cast<long long>(pc.units)));
+    const bool whole = pc.units <= kTcWhole, starts = st.begin == pc.seg0;
+    if (whole) { pc.u0 = 0; pc.u1 = pc.units; }
     st.begin = seg_end;
-    if (pc.u0 < pc.u1) return true;
+    if (whole ? starts : pc.u0 < pc.u1) return true;
   }
   return false;
 }
