@@ -4,9 +4,9 @@
 // the keys, 128 at a time:
 //   warps 0-7, 8-15  tile 0, 1: two threads a query row, 64 of the step's scores each.  Scores from tensor memory, running
 //                    maximum and sum, weights back to tensor memory, over the scores that they come from; the results at the end
-//   warps 16-19      K and V from codes to f16 in shared memory (128-byte swizzle), two stages each; a key that was turned
+//   warps 16-23      K and V from codes to f16 in shared memory (128-byte swizzle), two stages each; a key that was turned
 //                    once serves both tiles
-//   warp 20          issues the products: S[128 x 128] = Q K^T (operands in shared memory), O[128 x d] += P V with P read
+//   warp 24          issues the products: S[128 x 128] = Q K^T (operands in shared memory), O[128 x d] += P V with P read
 //                    from tensor memory and V, tokens down and channels across, as the MN-major operand
 // The two tiles take turns: while one's weights are made, the other's products run.  Tensor memory is full: two tiles of
 // scores and two of sums, 128 columns each.  (Scores of 64 keys in two buffers a tile would hide the products behind the
@@ -24,8 +24,10 @@
 namespace vscan {
 namespace kv {
 
-constexpr int kTcThreads = 672;
-constexpr int kTcConverter = 16, kTcIssuer = 20;   // first warp of each role
+constexpr int kTcThreads = 800;
+constexpr int kTcConverter = 16, kTcIssuer = 24;   // first warp of each role
+// 800 threads start with 72 registers each; the converters give 16 back, the 512 threads of the rows take 8 more:
+// 512 x 80 + 256 x 56 + 32 x 72 = 800 x 72.
 constexpr int kTcRows = 256;          // query rows of a CTA
 constexpr int kTcKeys = 128;          // keys of a step
 constexpr int kTcWhole = 4;           // a tile of up to this many steps is not cut: joining 256 rows takes longer than they do
@@ -299,7 +301,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.q_full[i], 8); mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 8); mbar_init(&sh.o_done[i], 1);
       for (int k = 0; k < 4; ++k) mbar_init(&sh.pair[i][k], 2);
-      mbar_init(&sh.k_full[i], 4); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.v_full[i], 4); mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.k_full[i], 8); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.v_full[i], 8); mbar_init(&sh.v_empty[i], 1);
     }
     for (int i = 0; i < kTcRing; ++i) mbar_init(&sh.scale_full[i], 1);
     sh.abort_flag = 0;
@@ -326,6 +328,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 
   if (warp < kTcConverter) {
     // ============================================================ two threads a query row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 80;");
     const int tile = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
     const uint32_t s_addr = tmem + lanes + tile * 128 + half * 64;                      // this thread's scores, and its weights
@@ -548,7 +551,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
     }
   } else if (warp < kTcIssuer) {
     // ============================================================ codes to f16
-    constexpr int kPer = DP / 16, kRowsPass = 128 / kPer, kLoads = 64 / kRowsPass;   // pieces of a token; tokens of a pass; loads of an item
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    constexpr int kPer = DP / 16, kRowsPass = 256 / kPer, kLoads = 64 / kRowsPass;   // pieces of a token; tokens of a pass; loads of an item
     const int tid = threadIdx.x - kTcConverter * 32, piece = tid % kPer, row0 = tid / kPer;
     const bool in_dim = piece * 16 < D;
     const size_t cell_bytes = static_cast<size_t>(p.block_size) * D;
@@ -576,7 +580,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         uint32_t on[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {       // the 16-token group of a load is the same for all lanes
-          const int row = part * 64 + row0 + i * kRowsPass, group = part * 4 + (warp & 3) * (32 / kPer) / 16 + i * kRowsPass / 16;
+          const int row = part * 64 + row0 + i * kRowsPass, group = part * 4 + (warp - kTcConverter) * (32 / kPer) / 16 + i * kRowsPass / 16;
           const unsigned c = __shfl_sync(0xffffffffu, cell, group);
           const int block = __shfl_sync(0xffffffffu, blk, group);      // by all lanes, whatever they load
           on[i] = in_dim && t0 + row < pc.most && block >= 0;
