@@ -671,7 +671,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
           const int s = step & 1;
           const bool more = u + 1 < pc.u1;
           ok = mbar_wait_warp(&sh.v_full[s], (step >> 1) & 1, abort_flag);
-          if (more) ok = ok && mbar_wait_warp(&sh.k_full[s ^ 1], ((step + 1) >> 1) & 1, abort_flag);
 #pragma unroll 1
           for (int t = 0; t <= two && ok; ++t) {
             ok = mbar_wait_warp(&sh.p_full[t], n_it[t] & 1, abort_flag);
@@ -683,7 +682,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
             umma_commit_warp(&sh.o_done[t]);
             if (t == two) umma_commit_warp(&sh.v_empty[s]);
             if (more) {        // the weights that lie where the next scores go have to be used up, not only issued
-              ok = mbar_wait_warp(&sh.o_done[t], n_it[t] & 1, abort_flag);
+              if (t == 0) ok = mbar_wait_warp(&sh.k_full[s ^ 1], ((step + 1) >> 1) & 1, abort_flag);
+              ok = ok && mbar_wait_warp(&sh.o_done[t], n_it[t] & 1, abort_flag);
               if (!ok) break;
               tc_fence_after();
               scores(t, s ^ 1);
