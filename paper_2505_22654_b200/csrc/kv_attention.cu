@@ -69,9 +69,9 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
         if (block < 0 || block >= p.num_blocks) { block = -1; bad = true; }
       }
       const size_t cell = static_cast<size_t>(max(block, 0)) * p.kv_heads + head;
-      float dot[R];
+      float dot[R], odd[R];                       // two chains of sums
 #pragma unroll
-      for (int r = 0; r < R; ++r) dot[r] = 0.f;
+      for (int r = 0; r < R; ++r) dot[r] = odd[r] = 0.f;
       float ks = 0.f, vsc = 0.f;
       if (block >= 0) {
         ks = p.k_scale[cell]; vsc = p.v_scale[cell];
@@ -86,7 +86,8 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
               const float4 qv = *reinterpret_cast<const float4*>(q_sh + r * D + c + 4 * k);
-              dot[r] = fmaf(qv.x, f[0], fmaf(qv.y, f[1], fmaf(qv.z, f[2], fmaf(qv.w, f[3], dot[r]))));
+              float& d = (k & 1) ? odd[r] : dot[r];
+              d = fmaf(qv.x, f[0], fmaf(qv.y, f[1], fmaf(qv.z, f[2], fmaf(qv.w, f[3], d))));
             }
           }
         }
@@ -95,9 +96,12 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const bool on = block >= 0 && t < seen[r];
-        const float x = on ? dot[r] * (ks * p.scale_log2e) : -INFINITY;
+        // the factor in two floats and the maximum taken off before the rounding: a weight near 1 is off by the exponential's
+        // error and the dot product's, not by the rounding of a large score
+        const float sum = dot[r] + odd[r], hi = ks * p.scale_log2e, lo = sum * (ks * p.scale_rest);
+        const float x = on ? fmaf(sum, hi, lo) : -INFINITY;
         const float top = fmaxf(m[r], warp_max(x)), base = top == -INFINITY ? 0.f : top;
-        const float e = on ? ex2(x - base) : 0.f;
+        const float e = on ? ex2(fmaf(sum, hi, lo - base)) : 0.f;
         if (top != m[r]) {
           const float f = ex2(m[r] - base);
           l[r] *= f;
@@ -558,7 +562,9 @@ extern "C" vscan_status vscan_kv_attention(const vscan_kv_attention_desc* d, voi
   p.rows = d->rows; p.padded = d->padded ? 1 : 0; p.max_q_len = d->max_q_len; p.causal = d->causal ? 1 : 0;
   while ((1 << p.shift) < p.block_size) ++p.shift;
   p.tile_rows = pl.tile_rows;
-  p.scale_log2e = d->scale * 1.4426950408889634f;
+  const double factor = static_cast<double>(d->scale) * 1.4426950408889634074;
+  p.scale_log2e = static_cast<float>(factor);
+  p.scale_rest = static_cast<float>(factor - p.scale_log2e);
   p.status = reinterpret_cast<uint32_t*>(ws);
   ws += kStatusBytes;
   p.flags = reinterpret_cast<uint32_t*>(ws);

@@ -22,7 +22,7 @@ struct AttnParams {
   const float* v_scale;
   int batch, q_heads, kv_heads, group, head_dim, block_size, shift, num_blocks, max_blocks, rows, padded, max_q_len, causal;
   int tile_rows;        // query rows (new row x head of the group) of a tile
-  float scale_log2e;
+  float scale_log2e, scale_rest;   // scale * log2(e), and what float32 leaves of it
   uint32_t* status;
   uint32_t* flags;             // [ctas] vscan_status: the CTA met a block or a length out of range, or gave up a wait
   struct Boundary* boundary;   // [ctas]
