@@ -185,11 +185,14 @@ __global__ void __launch_bounds__(kFmaThreads) fma_kernel(AttnParams p) {
 // Where the stretch of worker k starts inside a segment that is cut there for the first time, the segment's rows from its
 // pieces: the last piece of worker k - 1, then the first ones of k, k + 1, ... up to the segment's end.  The pieces are
 // added in a fixed order, so results do not depend on timing.  Three shapes of the work:
-//   few rows, workers are CTAs    a few segments in many pieces: CTA k joins segment k, its warps share a row's pieces
-//   few rows, workers are warps   many segments in two pieces or three: a warp takes a row
-//   256 rows a tile               a CTA takes 32 rows: their factors first, then all their channels side by side
+//   few rows, workers are CTAs    a few segments in many pieces: a CTA looks at kJoinLook boundaries, its warps share the rows and
+//                                 pieces of a segment that is cut there
+//   few rows, workers are warps   many segments in two pieces or three: a warp takes a boundary
+//   256 rows a tile               a CTA takes kJoinRows rows: their factors first, then all their channels side by side
 constexpr int kJoinThreads = 512;
 constexpr int kJoinWarps = kJoinThreads / 32;
+constexpr int kJoinRows = 128;    // of a tile of 256: two CTAs a cut, all resident at once (32 rows: 28 us for 147 cuts)
+constexpr int kJoinLook = 4;      // so that all CTAs of the launch are resident at once
 
 struct Pieces {          // of one segment
   const float* first;
@@ -248,7 +251,7 @@ __device__ __forceinline__ float join_row(const AttnParams& p, const Pieces& pc,
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
+__global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int n_ctas) {
   __shared__ float sums[kJoinWarps][256];
   grid_dependency_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = p.head_dim;
@@ -267,47 +270,51 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
     if (lane == 0 && p.lse) *lse_at(p, bd.b, bd.first, at) = d == 0.f ? -INFINITY : (top + log2f(d)) * 0.69314718055994531f;
   };
   if (solo) {
-    const int k = blockIdx.x * kWorkersPerCta + warp % kWorkersPerCta;
-    if (!cut_at(p, k, bd, pc)) return;
-    for (int r = warp / kWorkersPerCta; r < bd.rows; r += kJoinWarps / kWorkersPerCta) {
+    const int k = blockIdx.x * kJoinWarps + warp;
+    if (k >= n_ctas * kWorkersPerCta || !cut_at(p, k, bd, pc)) return;
+    for (int r = 0; r < bd.rows; ++r) {
       const float top = join_row(p, pc, r, 0, 1, den, acc);
       finish(r, top, den, acc);
     }
     return;
   }
   if (p.tile_rows > 16) {
-    constexpr int kBatch = 96;                                    // pieces whose factors fit beside the rows' maxima and sums
-    float (*tops)[32] = reinterpret_cast<float (*)[32]>(&sums[0][0]);
-    float (*dens)[32] = tops + kJoinWarps;
-    float (*factor)[32] = dens + kJoinWarps;
-    static_assert((2 * kJoinWarps + kBatch) * 32 <= kJoinWarps * 256, "fits the sums");
+    constexpr int kSlabs = kJoinRows / 32, kTurns = kJoinWarps / kSlabs;   // a warp has 32 of the rows, and every kTurns-th piece
+    constexpr int kBatch = 24;                                    // pieces whose factors fit beside the rows' maxima and sums
+    float (*tops)[kJoinRows] = reinterpret_cast<float (*)[kJoinRows]>(&sums[0][0]);
+    float (*dens)[kJoinRows] = tops + kTurns;
+    float (*factor)[kJoinRows] = dens + kTurns;
+    static_assert((2 * kTurns + kBatch) * kJoinRows <= kJoinWarps * 256, "fits the sums");
     if (!cut_at(p, blockIdx.x, bd, pc)) return;
-    const int R = p.tile_rows, r0 = blockIdx.y * 32, mine = r0 + lane, n_rows = min(32, bd.rows - r0);
+    const int R = p.tile_rows, r0 = blockIdx.y * kJoinRows, n_rows = min(kJoinRows, bd.rows - r0);
     if (n_rows <= 0) return;
+    const int in_slab = warp % kSlabs * 32 + lane, mine = r0 + in_slab, turn = warp / kSlabs;
+    const bool on = in_slab < n_rows;
     float top = -INFINITY;
-    if (lane < n_rows)
-      for (int i = warp; i < pc.n; i += kJoinWarps) top = fmaxf(top, pc.at(i)[R * D + mine]);
-    tops[warp][lane] = top;
+    if (on)
+      for (int i = turn; i < pc.n; i += kTurns) top = fmaxf(top, pc.at(i)[R * D + mine]);
+    tops[turn][in_slab] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, tops[w][lane]);
+    for (int w = 0; w < kTurns; ++w) top = fmaxf(top, tops[w][in_slab]);
     const float base = top == -INFINITY ? 0.f : top;
     den = 0.f;
-    constexpr int kEach = 4;                                      // 32 rows x 256 channels at most, four at a time
+    constexpr int kEach = 8;                                      // 128 rows x 128 channels at most, four at a time
+    static_assert(kEach * kJoinThreads * 4 >= kJoinRows * 128, "tiles of 256 rows have up to 128 channels");
     const int per_row = D / 4, total = n_rows * per_row;
     float4 o[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int first = 0; first < pc.n; first += kBatch) {
       const int count = min(kBatch, pc.n - first);
-      for (int i = warp; i < count; i += kJoinWarps) {
+      for (int i = turn; i < count; i += kTurns) {
         float f = 0.f;
-        if (lane < n_rows) {
+        if (on) {
           const float* part = pc.at(first + i);
           f = ex2(part[R * D + mine] - base);
           den = fmaf(f, part[R * D + R + mine], den);
         }
-        factor[i][lane] = f;
+        factor[i][in_slab] = f;
       }
       __syncthreads();
 #pragma unroll
@@ -324,7 +331,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
       }
       __syncthreads();
     }
-    dens[warp][lane] = den;
+    dens[turn][in_slab] = den;
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
@@ -333,7 +340,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
         const int row = idx / per_row, c = (idx - row * per_row) * 4;
         float d = 0.f;
 #pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) d += dens[w][row];
+        for (int w = 0; w < kTurns; ++w) d += dens[w][row];
         const RowAt at = row_at(p, bd.tile, bd.head, r0 + row);
         char* out = out_at(p, bd.b, bd.first, at);
         const float inv = d == 0.f ? 0.f : 1.f / d;
@@ -341,30 +348,36 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(AttnParams p) {
         store_out<T>(out, c + 2, o[e].z * inv); store_out<T>(out, c + 3, o[e].w * inv);
       }
     }
-    if (warp == 0 && lane < n_rows && p.lse) {
+    if (turn == 0 && on && p.lse) {
       float d = 0.f;
 #pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) d += dens[w][lane];
+      for (int w = 0; w < kTurns; ++w) d += dens[w][in_slab];
       *lse_at(p, bd.b, bd.first, row_at(p, bd.tile, bd.head, mine)) = d == 0.f ? -INFINITY : (top + log2f(d)) * 0.69314718055994531f;
     }
     return;
   }
-  if (!cut_at(p, blockIdx.x, bd, pc)) return;
+  const int look = blockIdx.x * kJoinLook + (lane & (kJoinLook - 1));
+  unsigned found = __ballot_sync(0xffffffffu, lane < kJoinLook && look < n_ctas && cut_at(p, look, bd, pc));
   // 8 rows: two warps a row; 16: one.  At most 16 rows a tile.
   const int parts = kJoinWarps / (p.tile_rows <= 8 ? 8 : 16), r = warp / parts;
-  float top = 0.f;
-  if (r < bd.rows) {
-    top = join_row(p, pc, r, warp - r * parts, parts, den, acc);
+  for (; found; found &= found - 1) {
+    cut_at(p, blockIdx.x * kJoinLook + __ffs(found) - 1, bd, pc);
+    float top = 0.f;
+    if (r < bd.rows) {
+      top = join_row(p, pc, r, warp - r * parts, parts, den, acc);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) sums[warp][(c / 4) * 128 + lane * 4 + c % 4] = acc[c];
-  }
-  __syncthreads();
-  if (r >= bd.rows || warp != r * parts) return;
-  for (int w = 1; w < parts; ++w) {
+      for (int c = 0; c < 8; ++c) sums[warp][(c / 4) * 128 + lane * 4 + c % 4] = acc[c];
+    }
+    __syncthreads();
+    if (r < bd.rows && warp == r * parts) {
+      for (int w = 1; w < parts; ++w) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) acc[c] += sums[warp + w][(c / 4) * 128 + lane * 4 + c % 4];
+        for (int c = 0; c < 8; ++c) acc[c] += sums[warp + w][(c / 4) * 128 + lane * 4 + c % 4];
+      }
+      finish(r, top, den, acc);
+    }
+    __syncthreads();
   }
-  finish(r, top, den, acc);
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -517,7 +530,9 @@ static vscan_status launch_attention(const AttnParams& p, const Plan& pl, int kv
   // it all
   if (static_cast<int64_t>(p.max_blocks) * p.block_size <= (pl.tensor ? kTcWhole * kTcKeys : kWhole * kUnit) || pl.ctas == 1) return VSCAN_OK;
   prof_before("kv_attention_join", stream);
-  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, dim3(pl.ctas, pl.tensor ? kTcRows / 32 : 1), dim3(kJoinThreads), 0, stream, p));
+  const dim3 grid = pl.tensor ? dim3(pl.ctas, kTcRows / kJoinRows) : dim3((pl.ctas + kJoinLook - 1) / kJoinLook);
+  static_assert(kJoinWarps == kJoinLook * kWorkersPerCta, "as many boundaries a CTA whichever the workers are");
+  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, grid, dim3(kJoinThreads), 0, stream, p, static_cast<int>(pl.ctas)));
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
   return VSCAN_OK;

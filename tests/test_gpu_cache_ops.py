@@ -339,7 +339,7 @@ def _attend_case(kv, dtype, hq, hk, d, bs, past, new, causal, padded, seed, max_
         assert (err <= tol).all(), (b, float((err / np.maximum(tol, 1e-30)).max()), np.argwhere(err > tol)[:4])
         fine = np.isfinite(ref_lse)
         np.testing.assert_array_equal(mine_lse[~fine], ref_lse[~fine])
-        err = np.abs(mine_lse - ref_lse)[fine]
+        err = np.abs(mine_lse[fine] - ref_lse[fine])
         assert (err <= (e + sums + np.abs(np.where(fine, ref_lse, 0)) * 2.0 ** -22)[fine]).all(), float(err.max())
     # rows that no sequence owns are as they were
     if padded:
@@ -567,6 +567,38 @@ def test_two_streams_and_two_graphs_with_workspaces_of_their_own():
             gr.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, outs))
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 1), ("bf16", 70), ("f32", 3)])
+def test_attention_captured_and_replayed_as_lengths_change(dtype, n):
+    """One graph, its lengths read from the GPU at each replay: short, long, none; the same bits as eager calls."""
+    H, bs, d, cols = 2, 32, 64, 40
+    c, g = Cache("i8", H, bs, d, 90, 7), gen(21)
+    table = i32([[int(v) for v in np.random.default_rng(1).permutation(80)[:cols]], list(range(40, 80))])
+    lens, off = i32([0, 0]), i32([0, 0, 0])
+    q = torch.randn((2 * n, 4, d), generator=g).to(DT[dtype]).cuda()
+    out, lse = torch.zeros_like(q), torch.zeros((2 * n, 4), device="cuda")
+    ws = vs.vscan_kv_attention_workspace(q, table, c.dev[0], n)
+    args = (q, lens, off, table, *c.arrays, 0.1)
+    vs.vscan_kv_attention(*args, max_q_len=n, out=out, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vs.vscan_kv_attention(*args, max_q_len=n, out=out, lse=lse, workspace=ws)
+    for a, b, ra, rb in [(1000, 77, n, n), (n, 1280, n, 1), (0, 5, 0, 1), (1279, 0, n, 0), (640, 641, 1, n)]:
+        lens.copy_(i32([a, b]))
+        off.copy_(i32([0, ra, ra + rb]))
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        graph.replay()
+        got = out.clone(), lse.clone()
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        vs.vscan_kv_attention(*args, max_q_len=n, out=out, lse=lse)
+        assert torch.equal(got[0], out) and torch.equal(got[1], lse) and vs.vscan_check(ws) == 0
+        out.fill_(-9.0)                      # every row that is owned is written, no other is
+        vs.vscan_kv_attention(*args, max_q_len=n, out=out)
+        assert torch.equal(out[:ra + rb], got[0][:ra + rb]) and (got[0][ra + rb:] == 7).all() and (out[ra + rb:] == -9).all()
 
 
 def test_python_face_refusals():
