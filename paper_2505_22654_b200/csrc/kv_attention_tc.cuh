@@ -283,6 +283,20 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// A warp's wait for the first scores of a piece.  A tile that has no rows in the piece before waits for all of that, which is
+// as long as the sequence: the limit of the other waits (tens of thousands of steps) is granted once more for every 2^17 tokens
+// that a table has room for.  If another role gives up, so does this wait.
+__device__ __noinline__ bool wait_scores(uint64_t* bar, uint32_t parity, int more, volatile int* abort_flag) {
+  bool got = false;
+  for (int turn = 0; turn <= more && !got && !*abort_flag; ++turn)
+    for (uint32_t i = 0; i < tc::kSpinLimit && !got; ++i) {
+      got = tc::mbar_try_wait(bar, parity);
+      if ((i & 1023u) == 1023u && *abort_flag) break;
+    }
+  if (!got) *abort_flag = 1;
+  return __all_sync(0xffffffffu, got);
+}
+
 template <int KV, int DP>
 __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
   using namespace tc;
@@ -390,6 +404,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_full[tile]);
         ok = mbar_wait_warp(&sh.q_full[tile], n_piece++ & 1, abort_flag);
+        // A tile that had nothing to do in the piece before may be steps ahead of the converters, and a wait tells a phase from
+        // the next only: the first scores of a piece are waited for before its first scales.
+        ok = ok && wait_scores(&sh.s_full[tile], n_it & 1, p.max_blocks >> (17 - p.shift), abort_flag);
         if (!ok) break;
       }
       const float cq = sh.q_scale[tile][r];
@@ -397,10 +414,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       float m = -INFINITY, l = 0.f, ref = 0.f;
       for (int j = 0; j < steps && ok; ++j, ++n_it, ++step) {
         const int slot = step & (kTcRing - 1);
-        // A tile that had nothing to do in the piece before may be steps ahead of the converters, and a wait tells a phase from
-        // the next only: the first scores of a piece are waited for before its first scales.
-        if (j == 0) ok = mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
-        ok = ok && mbar_wait_warp(&sh.scale_full[slot], (step / kTcRing) & 1, abort_flag);
+        ok = mbar_wait_warp(&sh.scale_full[slot], (step / kTcRing) & 1, abort_flag);
         if (!ok) break;
         // ---- the scales, and what follows from them for all rows alike; a new reference of the V scales is rare
         const float k8 = sh.ks[slot][lane & 7], v8 = sh.vs[slot][lane & 7];
