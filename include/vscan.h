@@ -494,11 +494,12 @@ vscan_status vscan_kv_write(const vscan_kv_write_desc* desc, void* stream);
  *             row (packed) or b, i (padded) by lse_stride = {sequence, head, row}
  *   max_q_len no sequence has more new rows than this (rows behind it are left as they were); 1 for decode steps.  The launch
  *             and the workspace are chosen from it.
- * Rows that no sequence owns are left as they were.  Tokens behind the table's last column, and tokens in blocks whose
+ * Rows that no sequence owns are left as they were.  Elements of out, and of lse, must not overlap each other.  Tokens behind the table's last column, and tokens in blocks whose
  * table entry is not in [0, num_blocks), count as not there; vscan_check then gives VSCAN_ERR_INVALID_ARG.
  * Scores, softmax statistics and sums are float32.
- * Workspace: vscan_kv_attention_workspace_bytes(desc), which reads the sizes only.
- * Limits of this build: q_heads / kv_heads <= 64; batch <= 8192.
+ * Workspace: vscan_kv_attention_workspace_bytes(desc), which reads the sizes only.  Calls that may run at the same time (on
+ * two streams, or in two graphs) need a workspace each.
+ * Limits of this build: q_heads / kv_heads <= 64; batch <= 8192; max_blocks * block_size and rows * q_heads <= 2^31 - 4096.
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t dtype;    /* vscan_dtype of q and out */

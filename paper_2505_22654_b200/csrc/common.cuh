@@ -74,6 +74,24 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline size_t dtype_bytes(int dtype) { return dtype == VSCAN_F32 ? 4 : 2; }
 
 // [a, a+na) and [b, b+nb) intersect?
+// Whether `dims` steps of n[i] elements each, st[i] apart, keep runs of `covered` elements off each other: ordered by step, each
+// has to step over what the smaller ones cover
+inline bool strides_apart(const int64_t* steps, const int64_t* sizes, int dims, int64_t covered) {
+  bool done[4] = {};
+  for (int a = 0; a < dims; ++a) {
+    int best = -1;
+    int64_t st = 0;
+    for (int c = 0; c < dims; ++c) {
+      const int64_t s = steps[c] < 0 ? -steps[c] : steps[c];
+      if (!done[c] && sizes[c] > 1 && (best < 0 || s < st)) { best = c; st = s; }
+    }
+    if (best < 0) return true;
+    if (st < covered) return false;
+    covered += st * (sizes[best] - 1);
+    done[best] = true;
+  }
+  return true;
+}
 inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   if (!a || !b || na == 0 || nb == 0) return false;
   uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);

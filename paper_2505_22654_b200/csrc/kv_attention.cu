@@ -381,6 +381,8 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int
 }
 
 // ---------------------------------------------------------------------------------------------- host side
+constexpr int64_t kMostTokens = 0x7ffff000;   // a step or a tile more still fits 32 bits
+
 static vscan_status validate_attention(const vscan_kv_attention_desc* d) {
   if (!d) return VSCAN_ERR_INVALID_ARG;
   if (d->dtype != VSCAN_F32 && d->dtype != VSCAN_BF16) return VSCAN_ERR_INVALID_ARG;
@@ -394,7 +396,7 @@ static vscan_status validate_attention(const vscan_kv_attention_desc* d) {
   if (!d->q || !d->out || !d->kv_len || !d->row_offset) return VSCAN_ERR_INVALID_ARG;
   if (cache && (!d->block_table || !d->k_cache || !d->v_cache || !d->k_scale || !d->v_scale)) return VSCAN_ERR_INVALID_ARG;
   if (d->head_dim > 256 || d->q_heads / d->kv_heads > 64 || d->batch > kMaxBatch || d->kv_heads > 65535 ||
-      static_cast<int64_t>(d->max_blocks) * d->block_size > 0x7fffffff || static_cast<int64_t>(d->rows) * d->q_heads > 0x7fffffff)
+      static_cast<int64_t>(d->max_blocks) * d->block_size > kMostTokens || static_cast<int64_t>(d->rows) * d->q_heads > kMostTokens)
     return VSCAN_ERR_UNSUPPORTED;
   const size_t e = dtype_bytes(d->dtype), B = d->batch, H = d->kv_heads;
   const bool padded = d->padded != 0;
@@ -402,6 +404,8 @@ static vscan_status validate_attention(const vscan_kv_attention_desc* d) {
   if (d->lse)
     for (int i = padded ? 0 : 1; i < 3; ++i)
       if (d->lse_stride[i] < 0 || d->lse_stride[i] > (int64_t{1} << 40)) return VSCAN_ERR_INVALID_ARG;
+  const int64_t sizes[3] = {padded ? d->batch : 1, d->q_heads, d->rows};
+  if (!strides_apart(d->out_stride, sizes, 3, d->head_dim) || (d->lse && !strides_apart(d->lse_stride, sizes, 3, 1))) return VSCAN_ERR_INVALID_ARG;
   struct Rng { const void* p; size_t n; };
   const size_t pool = static_cast<size_t>(d->num_blocks) * H;
   const Rng all[] = {{d->q, rows_extent(d->q_stride, B, d->q_heads, d->rows, d->head_dim, e, padded)},

@@ -203,18 +203,8 @@ static vscan_status validate(const vscan_rope_desc* d) {
   for (int i = 0; i < 2; ++i) {
     if (!io[i].in) continue;
     outs[i] = extent(io[i].out, io[i].so, d->batch, io[i].heads, d->seq_len, d->head_dim, e);
-    // ordered by stride, each dimension of the output has to step over what the smaller ones cover
-    int64_t n[3] = {d->batch, io[i].heads, d->seq_len}, st[3] = {io[i].so[0], io[i].so[1], io[i].so[2]}, covered = d->head_dim;
-    for (int a = 0; a < 3; ++a) st[a] = st[a] < 0 ? -st[a] : st[a];
-    for (int a = 0; a < 3; ++a) {
-      int best = -1;
-      for (int c = 0; c < 3; ++c)
-        if (n[c] > 1 && (best < 0 || st[c] < st[best])) best = c;
-      if (best < 0) break;
-      if (st[best] < covered) return VSCAN_ERR_INVALID_ARG;
-      covered += st[best] * (n[best] - 1);
-      n[best] = 1;
-    }
+    const int64_t n[3] = {d->batch, io[i].heads, d->seq_len};
+    if (!strides_apart(io[i].so, n, 3, d->head_dim)) return VSCAN_ERR_INVALID_ARG;
   }
   const size_t tokens = static_cast<size_t>(d->batch) * d->seq_len;
   for (int i = 0; i < 2; ++i) {

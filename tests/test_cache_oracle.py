@@ -210,6 +210,15 @@ def test_attention_refusals(L, change, status):
     assert L.vscan_kv_attention(C.byref(_attend_desc(**change)), BASE << 1, 1 << 30, None) == status
 
 
+@pytest.mark.parametrize("change,status", [
+    (dict(out_stride=vb._i64x3(0, 64, 0)), 1), (dict(out_stride=vb._i64x3(0, 0, 64)), 1), (dict(out_stride=vb._i64x3(0, 64, 448)), 1),
+    (dict(lse_stride=vb._i64x3(0, 1, 0)), 1), (dict(lse_stride=vb._i64x3(0, 1, 7)), 1),
+    (dict(padded=1), 1),                                                                 # sequences on top of each other
+    (dict(max_blocks=(1 << 27) - 128, num_blocks=1), 2), (dict(rows=(1 << 28) - 1, batch=1), 2)])
+def test_attention_outputs_do_not_overlap_themselves_and_fit_32_bits(L, change, status):
+    assert L.vscan_kv_attention(C.byref(_attend_desc(**change)), BASE << 1, 1 << 30, None) == status
+
+
 def test_attention_wants_its_workspace(L):
     d = _attend_desc()
     need = L.vscan_kv_attention_workspace_bytes(C.byref(d))
@@ -241,3 +250,9 @@ def test_python_face_refuses_what_is_not_on_a_gpu():
     with pytest.raises(ValueError):
         vb.vscan_kv_plan(*[torch.zeros(1, dtype=torch.int32)] * 2, torch.zeros((1, 1), dtype=torch.int32), torch.zeros(1, dtype=torch.int32),
                          torch.zeros(2, dtype=torch.int64), 16)
+
+
+def test_python_face_wants_a_truth_value():
+    t = torch.zeros(2)
+    with pytest.raises((TypeError, ValueError)):
+        vb.vscan_rope(torch.zeros(1, 1, 1, 8), None, torch.zeros(1, 1, 1, dtype=torch.int32), t, t.int(), inverse=torch.zeros(2))

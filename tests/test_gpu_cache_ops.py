@@ -601,6 +601,29 @@ def test_attention_captured_and_replayed_as_lengths_change(dtype, n):
         assert torch.equal(out[:ra + rb], got[0][:ra + rb]) and (got[0][ra + rb:] == 7).all() and (out[ra + rb:] == -9).all()
 
 
+@pytest.mark.parametrize("dtype,n", [("bf16", 1), ("bf16", 40), ("f32", 2)])
+def test_offsets_beyond_32_bits(dtype, n):
+    """A pool of more than 2^32 codes, its tokens in the last blocks: the same bits as from a small pool."""
+    B, hq, hk, bs, d = 2, 8, 4, 128, 128
+    lens, big = [300, 150 + n], (1 << 32) // (hk * bs * d) + 100
+    g = gen(5)
+    k, v = (torch.randn((sum(lens), hk, d), generator=g).to(DT[dtype]).cuda() for _ in range(2))
+    q = torch.randn((B * n, hq, d), generator=g).to(DT[dtype]).cuda()
+    outs = []
+    for blocks in (8, big):
+        pools = [torch.empty((blocks, hk, bs, d), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2)]
+        scales = [torch.empty((blocks, hk), device="cuda") for _ in range(2)]
+        table = i32([[blocks - 1, blocks - 4, blocks - 2], [blocks - 5, blocks - 3, -1]])
+        vs.vscan_kv_write(k, v, i32(lens), i32([0, lens[0], sum(lens)]), table, *pools, *scales)
+        out = vs.vscan_kv_attention(q, i32(lens), i32([0, n, 2 * n]), table, *pools, *scales, d ** -0.5, max_q_len=n)
+        outs.append((out, pools[0][blocks - 5:].view(torch.uint8).clone(), scales[1][blocks - 5:].clone()))
+        del pools
+    assert torch.equal(outs[0][0], outs[1][0]) and outs[0][0].abs().max() > 0
+    first, second = ({j: t[1][j] for j in range(5)} for t in outs)
+    assert all(torch.equal(first[j][:, :20], second[j][:, :20]) for j in range(5))
+    assert torch.equal(outs[0][2], outs[1][2])
+
+
 def test_python_face_refusals():
     c = Cache("e4m3", 2, 16, 32, 4, 0)
     q, lens, off, table = torch.zeros((1, 2, 32), device="cuda"), i32([1]), i32([0, 1]), i32([[0]])
