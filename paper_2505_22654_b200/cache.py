@@ -12,7 +12,8 @@ from . import binding as vb
 
 class VScanCache:
     """kv_dtype: "e4m3" or "i8".  `batch` sequences of at most max_blocks * block_size tokens each; `rows`: the most new
-    rows of a step over all sequences (their slots are kept in slot_map, their positions in row_pos)."""
+    rows of a step over all sequences (their slots are kept in slot_map, their positions in row_pos).
+    The calls of a cache follow each other: they go on one stream, or on streams that wait for one another."""
 
     def __init__(self, *, num_blocks, block_size, kv_heads, head_dim, batch, max_blocks, rows, kv_dtype="e4m3", device="cuda"):
         dt = {"e4m3": torch.float8_e4m3fn, "i8": torch.int8}[kv_dtype]
@@ -66,7 +67,8 @@ class VScanCache:
 
     def step(self, q, k, v, pos_ids, rope, new_len, scale, pairing=vb.ROPE_HALVES, out=None):
         """One step of a layer: rotary positions on q and k (rope = (inv_freq, axis)), plan, write, causal attention.  q, k, v
-        [batch, heads, rows, head_dim] padded, pos_ids [planes, batch, rows].  -> attention of the new rows, like q."""
+        [batch, heads, rows, head_dim] padded, pos_ids [planes, batch, rows], new_len at most `rows`.  -> attention of the new
+        rows, like q."""
         q, k = vb.vscan_rope(q, k, pos_ids, *rope, pairing=pairing)
         self.plan(new_len)
         self.write(k, v)

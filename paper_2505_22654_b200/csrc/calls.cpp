@@ -81,6 +81,12 @@ long integer(PyObject* o) {
   return v;
 }
 
+int32_t truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) { PyErr_Clear(); throw BadType("a truth value wanted"); }
+  return v;
+}
+
 // Runs `call(stream)` with the device current
 template <typename F>
 PyObject* on_stream(const Place& at_, F call) {
@@ -131,7 +137,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {   // q, k, pos_ids
     wants(x.dim() == 4, x, "q or k", "[batch, heads, seq_len, head_dim]");
     d.dtype = dtype_of(x);
     d.pairing = narrow(integer(a[5]), "pairing");
-    d.inverse = PyObject_IsTrue(a[6]) ? 1 : 0;
+    d.inverse = truth(a[6]);
     d.batch = narrow(x.size(0), "batch"); d.seq_len = narrow(x.size(2), "seq_len"); d.head_dim = narrow(x.size(3), "head_dim");
     wants(pos.dim() == 3 && pos.size(1) == x.size(0) && pos.size(2) == x.size(2), pos, "pos_ids", "[planes, batch, seq_len]");
     wants(freq.dim() == 1, freq, "inv_freq", "[rot_dim / 2]");
@@ -291,7 +297,7 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (scale == -1.0 && PyErr_Occurred()) { PyErr_Clear(); throw BadType("scale: a number wanted"); }
     d.scale = static_cast<float>(scale);
     d.max_q_len = narrow(integer(a[9]), "max_q_len");
-    d.causal = PyObject_IsTrue(a[10]) ? 1 : 0;
+    d.causal = truth(a[10]);
     wants(out.sizes() == q.sizes(), out, "out", "the shape of q");
     if (out.scalar_type() != q.scalar_type()) throw BadType("out: type differs from q");
     rows_of(out, d.batch, d.q_heads, d.head_dim, "out", d.rows, d.padded, d.out_stride);

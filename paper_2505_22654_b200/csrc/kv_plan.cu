@@ -222,7 +222,7 @@ extern "C" vscan_status vscan_kv_plan(const vscan_kv_plan_desc* d, void* stream_
   while ((1 << p.shift) < p.block_size) ++p.shift;
   // as many CTAs as the rows (four a thread) or the table rows (a warp each) can use, at most one per SM: each repeats
   // the prefix sums
-  const long long by_rows = (static_cast<long long>(d->rows) + kv::kPlanThreads * kv::kPlanRows - 1) / (kv::kPlanThreads * kv::kPlanRows);
+  const long long by_rows = !d->slot_map && !d->row_pos ? 0 : (static_cast<long long>(d->rows) + kv::kPlanThreads * kv::kPlanRows - 1) / (kv::kPlanThreads * kv::kPlanRows);
   const long long by_batch = (static_cast<long long>(d->batch) + 7) / 8;
   long long grid = by_rows > by_batch ? by_rows : by_batch;
   grid = grid < 1 ? 1 : grid > 148 ? 148 : grid;
