@@ -10,7 +10,8 @@ namespace kv {
 
 // ---------------------------------------------------------------------------------------------- float32 kernel
 // Products on the CUDA cores: no rounding of queries or weights to 16 bits.  A warp takes 32 neighbouring tokens at a time:
-// for the scores a lane owns a token, for the weighted sum a lane owns 4 or 8 channels.
+// for the scores a lane owns a token, for the weighted sum a lane owns 4 or 8 channels.  Bound by the CUDA cores' multiply-adds, two
+// a code and query row, and by the conversion of codes, two instructions a code.
 constexpr int kFmaThreads = 128;
 constexpr int kFmaWarps = kFmaThreads / 32;
 

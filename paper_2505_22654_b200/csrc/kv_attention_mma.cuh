@@ -13,6 +13,12 @@
 // its f16 form is exact down to 2^-28 of it; weights are rounded to f16 (2^-11 relative, above 2^-22 of the largest
 // weight) and scaled by 2^8 for that; scores, maxima, denominators and sums are float32.  The block's V scale goes onto the weights
 // relative to a running reference, which follows the scales so that the weights stay within three binades of their range.
+//
+// Measured: 256 sequences of 195 to 300 tokens, 32 heads of 128, 522 MB: 115 us, 4.6 TB/s, issue slots 43 % and ALU 42 % busy; 4
+// sequences of 9,000 to 16,500 tokens, 4 KV heads, 44 MB: 23 us and 5 for the join.  Four CTAs of four warps an SM, 4 KB a warp on
+// their way.  Codes through shared memory, three steps deep: 139 us where each lane copies its own, 108 us by bulk copies, which
+// took 10 % longer for few long sequences and 15 % for tiny ones.  Division in units of 16 tokens instead of 64: 112 us, but half
+// as long again for 114 sequences of up to 9 tokens.
 #pragma once
 
 #include "kv_attention.cuh"

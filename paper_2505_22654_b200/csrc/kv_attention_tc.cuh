@@ -15,6 +15,8 @@
 // Roundings as in the kernel for few rows: queries exact in f16 but for a power of two, weights in f16 relative to a
 // reference of the V scales, all else float32.  Per element of S: one fused multiply-add, one exponential, one add, one
 // multiply, half a conversion; 16 exponentials a cycle and SM take as long as the products at the tensor cores' rate.
+// Measured: 2 x 900 to 1,024 new rows x 28 heads behind 15,000 to 16,384 tokens, 448 GFLOP: 665 us, 673 TFLOP/s (tensor pipe 35 %,
+// issue slots 55 %, ALU 41 % busy), and 20 us for the join.
 // Every wait is bounded; on expiry the CTA says so in its flag word, frees its tensor memory and returns.
 #pragma once
 
