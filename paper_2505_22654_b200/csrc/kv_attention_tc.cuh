@@ -421,7 +421,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         // ---- the scales, and what follows from them for all rows alike; a new reference of the V scales is rare
         const float k8 = sh.ks[slot][lane & 7], v8 = sh.vs[slot][lane & 7];
         const uint32_t there = sh.there[slot];
-        const bool odd = __any_sync(0xffffffffu, !(k8 > 0.f) || v8 != v8);      // a scale that is 0 or NaN
         float v_top = v8 == v8 ? v8 : 0.f;
 #pragma unroll
         for (int off = 1; off < 8; off <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, off));
@@ -496,7 +495,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         for (int h = 0; h < 2; ++h) {
           uint32_t v[32], w[16];
           tmem_read32(s_addr + h * 32, v);
-          if (masked) hide(v, h, 0xff800000u);   // a masked score is -inf, its weight 0, as long as the scales are numbers above 0
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             const float4 gr = group[h * 2 + g];
@@ -509,7 +507,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
               v[k + 1] = __float_as_uint(ex2(x.y));
             }
           }
-          if (masked && odd) hide(v, h, 0u);
+          if (masked) hide(v, h, 0u);            // behind the products with the scales: those may be 0, or NaN
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             uint64_t sums = 0;
