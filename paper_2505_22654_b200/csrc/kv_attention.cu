@@ -253,6 +253,13 @@ __device__ __forceinline__ float join_row(const AttnParams& p, const Pieces& pc,
   return top;
 }
 
+// Pieces of bf16 queries have V scales in their references
+template <typename T>
+__device__ __forceinline__ float joined_log_sum(float m, float l) {
+  if constexpr (sizeof(T) == 2) return log_sum(m, l);
+  else return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int n_ctas) {
   __shared__ float sums[kJoinWarps][256];
@@ -270,7 +277,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int
       const int ch = (c / 4) * 128 + lane * 4 + c % 4;
       if (ch < D) store_out<T>(out, ch, d == 0.f ? 0.f : x[c] / d);
     }
-    if (lane == 0 && p.lse) *lse_at(p, bd.b, bd.first, at) = d == 0.f ? -INFINITY : (top + log2f(d)) * 0.69314718055994531f;
+    if (lane == 0 && p.lse) *lse_at(p, bd.b, bd.first, at) = joined_log_sum<T>(top, d);
   };
   if (solo) {
     const int k = blockIdx.x * kJoinWarps + warp;
@@ -355,7 +362,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int
       float d = 0.f;
 #pragma unroll
       for (int w = 0; w < kTurns; ++w) d += dens[w][in_slab];
-      *lse_at(p, bd.b, bd.first, row_at(p, bd.tile, bd.head, mine)) = d == 0.f ? -INFINITY : (top + log2f(d)) * 0.69314718055994531f;
+      *lse_at(p, bd.b, bd.first, row_at(p, bd.tile, bd.head, mine)) = joined_log_sum<T>(top, d);
     }
     return;
   }

@@ -171,6 +171,22 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// The V scale of a block, in the reference of a row and in the exponent of its weights, which are 2^8 where a token is the
+// reference.  vscan_kv_write makes scales of 2^-48 .. 2^48.  Tokens of a scale of 0 count in the denominator alone: 40 binades
+// lower in the weights than in the reference, they are below 2^-25 and 0 in f16, and far from 0 in the float32 sum.  NaN stays NaN.
+constexpr float kWeightShift = 8.f;
+constexpr float kWeightScale = 256.f;
+__device__ __forceinline__ float value_exponent(float s) { return s < 0x1p-126f ? -32.f : __log2f(s); }
+__device__ __forceinline__ float weight_exponent(float s) { return (s < 0x1p-126f ? -72.f : __log2f(s)) + kWeightShift; }
+
+// log of l 2^m.  Where V scales are part of m, l makes up for them: a whole number is moved from m to l, so that two large
+// numbers of opposite sign are not rounded before their sum is taken
+__device__ __forceinline__ float log_sum(float m, float l) {
+  if (l == 0.f) return -INFINITY;
+  const float whole = fminf(fmaxf(rintf(m), -32.f), 32.f);
+  return ((m - whole) + log2f(l * exp2_int(static_cast<int>(whole)))) * 0.69314718055994531f;
+}
+
 // Where row r (new row x head of the group) of a tile lies
 struct RowAt { int i, h; };
 __device__ __forceinline__ RowAt row_at(const AttnParams& p, int tile, int head, int r) {

@@ -27,8 +27,8 @@ namespace vscan {
 namespace kv {
 
 constexpr int kMmaThreads = 128;
-constexpr float kLazy = 6.f;          // a running maximum is raised when a score is over it by this many binades
-constexpr float kWeightScale = 256.f; // weights up to 2^6 become f16 values up to 2^14
+constexpr float kLazy = 6.f;          // a running maximum is raised when a score is over it by this many binades: weights up to 2^6 times
+                                      // kWeightScale, 2^14 in f16
 
 __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"

@@ -12,8 +12,10 @@
 // scores and two of sums, 128 columns each.  (Scores of 64 keys in two buffers a tile would hide the products behind the
 // weights, but a product 64 columns wide takes as long as one of 128: 70 and 65 cycles measured.)
 //
-// Roundings as in the kernel for few rows: queries exact in f16 but for a power of two, weights in f16 relative to a
-// reference of the V scales, all else float32.  Per element of S: one fused multiply-add, one exponential, one add, one
+// Roundings: queries exact in f16 but for a power of two; weights in f16, all else float32.  The V scale of a token's block is part of
+// its weight's exponent, and a row's reference is the largest sum of score and scale that the row has seen, so what a row loses
+// below the smallest step of f16 is small beside its own result, whatever the scales of blocks are that it does not see.  The
+// denominator takes the scale off again.  Per element of S: one fused multiply-add, one exponential, one add, one
 // multiply, half a conversion; 16 exponentials a cycle and SM take as long as the products at the tensor cores' rate.
 // Measured: 2 x 900 to 1,024 new rows x 28 heads behind 15,000 to 16,384 tokens, 448 GFLOP: 665 us, 673 TFLOP/s (tensor pipe 35 %,
 // issue slots 55 %, ALU 41 % busy), and 20 us for the join.
@@ -43,7 +45,8 @@ struct TcShared {
   uint64_t scale_full[kTcRing];
   uint32_t tmem_base;
   int abort_flag;
-  float4 group[16][4];                    // per warp: of each of its 16-token groups {K scale, V shift, its inverse factor}
+  float4 group[16][4];                    // per warp: of each of its 16-token groups {K scale, V scale's exponent in the reference,
+                                          // what takes it off a sum of weights, its exponent in the weights}
   float q_scale[2][128];                  // [tile][row]: what a score is multiplied by
   float swap[2][2][2][128];               // [step parity][tile][half][row]: what the two threads of a row tell each other
   uint32_t there[kTcRing];                // of the 16-token groups of a step: a bit each, not there at all: 0
@@ -413,25 +416,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       }
       const float cq = sh.q_scale[tile][r];
 
-      float m = -INFINITY, l = 0.f, ref = 0.f;
+      // m: the row's reference, a score plus its V scale's logarithm; weights are 2^8 at it, l in units of 2^m
+      float m = -INFINITY, l = 0.f;
       for (int j = 0; j < steps && ok; ++j, ++n_it, ++step) {
         const int slot = step & (kTcRing - 1);
         ok = mbar_wait_warp(&sh.scale_full[slot], (step / kTcRing) & 1, abort_flag);
         if (!ok) break;
-        // ---- the scales, and what follows from them for all rows alike; a new reference of the V scales is rare
+        // ---- the scales, and what follows from them for all rows alike
         const float k8 = sh.ks[slot][lane & 7], v8 = sh.vs[slot][lane & 7];
         const uint32_t there = sh.there[slot];
-        float v_top = v8 == v8 ? v8 : 0.f;
-#pragma unroll
-        for (int off = 1; off < 8; off <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, off));
-        float f = 1.f;
-        if (v_top > ref || (v_top < 0.125f * ref && v_top > 0.f)) { f = ref / v_top; ref = v_top; }
-        // the V scale of a group goes into the exponent, its inverse onto the group's share of the denominator; a group whose
-        // scale is far below the reference (or 0) gives weights that are 0 in f16 and still counts in the denominator
         if ((lane >> 2) == half) {
-          const float fv = ref > 0.f ? v8 * (kWeightScale / ref) : 0.f * v8;
-          const float shift = fv == fv ? fmaxf(__log2f(fv), -60.f) : fv;
-          sh.group[warp][lane & 3] = make_float4(k8, shift, ex2(-shift), 0.f);
+          const float up = weight_exponent(v8);
+          sh.group[warp][lane & 3] = make_float4(k8, value_exponent(v8), ex2(-up), up);
         }
         __syncwarp();
         if (j > 0) ok = mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
@@ -451,7 +447,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
             if (!((mask >> k) & 1u)) v[k] = with;
         };
 
-        // ---- largest score
+        // ---- largest sum of a score and its V scale
         float top = -INFINITY;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -464,18 +460,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 #pragma unroll
             for (int k = 1; k < 15; k += 2) x = fmaxf(fmaxf(x, __uint_as_float(v[g * 16 + k])), __uint_as_float(v[g * 16 + k + 1]));
             x = fmaxf(x, __uint_as_float(v[g * 16 + 15]));
-            if (x > -INFINITY) top = fmaxf(top, x * group[h * 2 + g].x);
+            if (x > -INFINITY) top = fmaxf(top, fmaf(x, cq * group[h * 2 + g].x, group[h * 2 + g].y));
           }
         }
-        top *= cq;
         top = fmaxf(top, swap(top));
         if (!ok) break;
-        // ---- a new maximum rescales the sums; rare as well.  Both threads of a row decide alike.
+        // ---- a new reference rescales the sums, which is rare.  Both threads of a row decide alike.
+        float f = 1.f;
         if (__any_sync(0xffffffffu, top > m + kLazy)) {
-          const float now = fmaxf(m, top), fm = now == -INFINITY ? 1.f : ex2(m - now);
+          const float now = fmaxf(m, top);
+          f = now == -INFINITY ? 1.f : ex2(m - now);
           m = now;
-          l *= fm;
-          f *= fm;
+          l *= f;
         }
         if (j > 0 && __any_sync(0xffffffffu, f != 1.f)) {
           // (the products with V of the step before are done: this step's scores were issued after them)
@@ -498,7 +494,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             const float4 gr = group[h * 2 + g];
-            const float fk = cq * gr.x, shifted = minus_m + gr.y;
+            const float fk = cq * gr.x, shifted = minus_m + gr.w;
             const uint64_t mul = pair(fk, fk), add = pair(shifted, shifted);
 #pragma unroll
             for (int k = g * 16; k < g * 16 + 16; k += 2) {
@@ -519,7 +515,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
             }
             const float2 both = unpair(sums);
             const float sum = both.x + both.y;
-            if (sum != 0.f) l = fmaf(sum, group[h * 2 + g].z, l);
+            if (sum != 0.f) l = fmaf(sum, group[h * 2 + g].z, l);   // (not where nothing is seen: the factor may be NaN)
           }
           tmem_st16(s_addr + h * 16, w);
         }
@@ -535,7 +531,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       if (!ok) break;
       tc_fence_after();
       const bool complete = pc.u0 == 0 && pc.u1 == pc.units;
-      const float unit = ref * (1.f / kWeightScale), mul = complete ? (l == 0.f ? 0.f : unit / l) : unit;
+      const float unit = 1.f / kWeightScale, mul = complete ? (l == 0.f ? 0.f : unit / l) : unit;
       float* part = p.partial + (static_cast<size_t>(blockIdx.x) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(kTcRows, D);
       char* out = out_at(p, pc.b, pc.q.s.first, at);
 #pragma unroll 1
@@ -560,7 +556,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       tc_fence_before();
       if (on && half == 0) {
         if (!complete) { part[kTcRows * D + in_tile] = m; part[kTcRows * D + kTcRows + in_tile] = l; }
-        else if (p.lse) *lse_at(p, pc.b, pc.q.s.first, at) = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+        else if (p.lse) *lse_at(p, pc.b, pc.q.s.first, at) = log_sum(m, l);
       }
     }
   } else if (warp < kTcIssuer) {
@@ -640,7 +636,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         if (lane == 0) mbar_arrive(&sh.k_full[s]);
         load(raw[1], p.v_cache, blk, t0, 1);
         if (warp == kTcConverter) {
-          if (lane < 8) sh.ks[slot][lane] = b8 >= 0 ? scale : 1.f;      // (a group that is not there is masked)
+          if (lane < 8) sh.ks[slot][lane] = b8 >= 0 ? scale : 1.f;      // (a group that is not there is masked; its V scale is 0)
           else if (lane < 16) sh.vs[slot][lane - 8] = scale;
           const unsigned there = __ballot_sync(0xffffffffu, blk >= 0);
           if (lane == 0) sh.there[slot] = there & 0xffu;

@@ -1,7 +1,8 @@
-"""vscan_kv_attention where a score's factor vanishes: scale 0, query rows of zeros, keys of zeros, negative scale; causal rows that
-see part of a 16-token group.  Against the float64 oracle, for every kernel the calls choose from.
+"""vscan_kv_attention at the edges of its numbers, against the float64 oracle and for every kernel the calls choose from: scores
+whose factor vanishes (scale 0, query rows and keys of zeros, negative scale) over partly masked 16-token groups; values of
+neighbouring blocks many binades apart.
 
-Tolerances as derived in test_gpu_cache_ops.py.
+Tolerances as derived in test_gpu_cache_ops.py, and beside the tests that have their own.
 """
 import numpy as np
 import pytest
@@ -56,3 +57,64 @@ def test_attention_where_a_scores_factor_vanishes(kv, scale, dtype, d, past, new
             assert (np.abs(got - ref) <= attend_tol(dtype, d, T, ref, weight, reach, v)).all()
             e, sums = (d + 8) * 2.0 ** -24 * reach, (T / 4 + 16) * 2.0 ** -24
             assert (np.abs(got_lse - ref_lse) <= e + sums + np.abs(ref_lse) * 2.0 ** -22).all()
+
+
+def _apart_check(kv, dtype, hq, H, d, past, new, v_exp, seed, q_gain=1.0):
+    """Values of neighbouring blocks v_exp[j] binades from 1, and each row measured by what it sees alone: the tolerance of
+    attend_tol, but the smallest step of a weight in 16 bits for a row of its own.  The row's largest product of weight and block
+    scale is 2^8 or more in that form, each is off by at most half of 2^-24, so in all tokens 2^-33 of what the largest code times that
+    largest product is.  Exponents that a block scale of up to 2^56 is part of are up to 256 in size with all that is added on the way:
+    2^-16 of a weight."""
+    bs, T, g = 16, past + new, gen(seed)
+    grow = torch.tensor([v_exp[t // bs % len(v_exp)] for t in range(T)]).double()[:, None, None]
+    k = torch.randn((T, H, d), generator=g).to(DT[dtype])
+    v = (torch.randn((T, H, d), generator=g).double() * torch.exp2(grow)).to(DT[dtype])
+    c, table = _written(kv, H, bs, d, [T], [k], [v])
+    q = (q_gain * torch.randn((new, hq, d), generator=g)).to(DT[dtype])
+    out, lse = torch.full_like(q, 7.0).cuda(), torch.full((new, hq), 7.0, device="cuda")
+    vs.vscan_kv_attention(q.cuda(), i32([T]), i32([0, new]), i32(table), *c.arrays, 0.125, max_q_len=new, out=out, lse=lse)
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    (kk, there), (vv, _) = (co.gather(c.codes[i], c.scale[i], table[0], T, bs, KV[kv][0]) for i in range(2))
+    ref, ref_lse, weight, reach = co.attention(q.double().numpy(), kk, vv, there, 0.125, True, past)
+    tol = attend_tol(dtype, d, T, ref, weight, reach, np.zeros(1))
+    wide = 2.0 ** -16 if dtype == "bf16" else 0.0
+    tol += wide * weight
+    if dtype == "bf16":
+        s = np.stack([c.scale[1][table[0][t // bs]] for t in range(T)])        # [T, H]
+        for i in range(new):
+            for j in range(hq):
+                x = 0.125 * (kk[:past + i + 1, j // (hq // H)] @ q[i, j].double().numpy())
+                p = np.exp(x - ref_lse[i, j])
+                tol[i, j] += T * 2.0 ** -33 * co.Q_MAX[KV[kv][0]] * (p * s[:past + i + 1, j // (hq // H)]).max()
+    err = np.abs(out - ref)
+    assert (err <= tol).all(), (float((err / tol).max()), np.argwhere(err > tol)[:4])
+    e, sums = (d + 8) * 2.0 ** -24 * reach, (T / 4 + 16) * 2.0 ** -24
+    assert (np.abs(lse - ref_lse) <= e + sums + wide + np.abs(ref_lse) * 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+@pytest.mark.parametrize("dtype,hq,H,d,past,new", [("bf16", 4, 2, 64, 0, 150), ("bf16", 2, 2, 128, 130, 300), ("bf16", 14, 2, 48, 40, 37),
+                                                     ("f32", 4, 2, 64, 20, 60)])
+@pytest.mark.parametrize("v_exp", [[0, 33], [-30, 10, -20, 40, 0, 30, -40, 5, 20], [40, 0, -40]])
+@pytest.mark.parametrize("q_gain", [1.0, 4.0])
+def test_attention_rows_do_not_depend_on_the_values_behind_them(kv, dtype, hq, H, d, past, new, v_exp, q_gain):
+    _apart_check(kv, dtype, hq, H, d, past, new, v_exp, seed=d + new, q_gain=q_gain)
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+@pytest.mark.parametrize("new", [2, 40])
+def test_attention_values_whose_scale_is_zero_weigh_but_give_nothing(kv, new):
+    """V scales of 0 (blocks filled by hand) over codes that are not 0: 0 times the code, and the tokens count in the denominator.
+    A sequence of such blocks alone gives exactly 0."""
+    H, d, bs, T, g = 1, 64, 16, 100, gen(new)
+    k, v = (torch.randn((T, H, d), generator=g).to(torch.bfloat16) for _ in range(2))
+    c, table = _written(kv, H, bs, d, [T, T], [k, k], [v, v])
+    zero = [table[0][1], table[0][4]] + table[1][:7]
+    c.scale[1][zero] = 0.0
+    c.dev_scale[1][zero] = 0.0
+    q = torch.randn((2 * new, 2, d), generator=g).to(torch.bfloat16)
+    out = vs.vscan_kv_attention(q.cuda(), i32([T, T]), i32([0, new, 2 * new]), i32(table), *c.arrays, 0.125, max_q_len=new)
+    (kk, there), (vv, _) = (co.gather(c.codes[i], c.scale[i], table[0], T, bs, KV[kv][0]) for i in range(2))
+    ref, _, weight, reach = co.attention(q[:new].double().numpy(), kk, vv, there, 0.125, True, T - new)
+    assert (np.abs(out[:new].double().cpu().numpy() - ref) <= attend_tol("bf16", d, T, ref, weight, reach, vv)).all()
+    assert (out[new:] == 0).all()
