@@ -237,6 +237,12 @@ __device__ __forceinline__ uint4 ld_nc_16_if(const void* p, uint32_t on) {
       : "l"(p), "r"(on));
   return r;
 }
+// The larger; NaN if one is
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 // Two float32 operations in one instruction
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   uint64_t r;
@@ -425,6 +431,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         // ---- the scales, and what follows from them for all rows alike
         const float k8 = sh.ks[slot][lane & 7], v8 = sh.vs[slot][lane & 7];
         const uint32_t there = sh.there[slot];
+        const bool odd = __any_sync(0xffffffffu, k8 != k8 || v8 != v8);
         if ((lane >> 2) == half) {
           const float up = weight_exponent(v8);
           sh.group[warp][lane & 3] = make_float4(k8, value_exponent(v8), ex2(-up), up);
@@ -491,10 +498,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         for (int h = 0; h < 2; ++h) {
           uint32_t v[32], w[16];
           tmem_read32(s_addr + h * 32, v);
+          if (masked) hide(v, h, 0xff800000u);   // -inf, and a weight of 0: the factor is held above 0
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             const float4 gr = group[h * 2 + g];
-            const float fk = cq * gr.x, shifted = minus_m + gr.w;
+            const float fk = max_nan(cq * gr.x, 0x1p-126f), shifted = minus_m + gr.w;
             const uint64_t mul = pair(fk, fk), add = pair(shifted, shifted);
 #pragma unroll
             for (int k = g * 16; k < g * 16 + 16; k += 2) {
@@ -503,7 +511,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
               v[k + 1] = __float_as_uint(ex2(x.y));
             }
           }
-          if (masked) hide(v, h, 0u);            // behind the products with the scales: those may be 0, or NaN
+          if (masked && odd) hide(v, h, 0u);     // scales that are NaN reach who sees them only
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             uint64_t sums = 0;
