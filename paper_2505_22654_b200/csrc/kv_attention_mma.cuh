@@ -10,9 +10,9 @@
 // the byte permutes that pair two tokens' codes.  P^T comes from S^T by an 8 x 8 transpose instruction.
 //
 // Roundings: codes are exact in f16; a query row is scaled by a power of two to 2^14 .. 2^15 at its largest element, so that
-// its f16 form is exact down to 2^-28 of it; weights are rounded to f16 (2^-11 relative, above 2^-22 of the largest
-// weight) and scaled by 2^8 for that; scores, maxima, denominators and sums are float32.  The block's V scale goes onto the weights
-// relative to a running reference, which follows the scales so that the weights stay within three binades of their range.
+// its f16 form is exact down to 2^-28 of it; weights are rounded to f16: 2^-11 relative, down to 2^-22 of the largest one.  The block's
+// V scale is part of a weight's exponent (and is taken off again for the denominator), so that this is the largest of what adds to
+// the result, not of the softmax alone, and no sum has to follow the scales.  Scores, references, denominators and sums are float32.
 //
 // Measured: 256 sequences of 195 to 300 tokens, 32 heads of 128, 522 MB: 115 us, 4.6 TB/s, issue slots 43 % and ALU 42 % busy; 4
 // sequences of 9,000 to 16,500 tokens, 4 KV heads, 44 MB: 23 us and 5 for the join.  Four CTAs of four warps an SM, 4 KB a warp on
@@ -279,7 +279,6 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[i][nt][k] = 0.f;
-    float ref = 0.f, inv_ref = 0.f;     // the sums are in units of ref / kWeightScale
 
     for (int t0 = t_first; t0 < stop; t0 += t_stride) {
       // ---- scores
@@ -334,17 +333,18 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
       load_k(t1);
       load_table(t1 + t_stride, blk_next);
 
-      // ---- running maxima: raised only when a score is well over them, so that the sums are seldom rescaled
+      // ---- references, largest sums of a score and its V scale's exponent: raised only when one is well over them, so that the
+      // sums are seldom rescaled
+      float lv[MT];
       bool over = false;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) lv[mt] = value_exponent(vs_now[mt]);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float top = -INFINITY;
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) top = fmaxf(top, fmaxf(x[mt][nt][k], x[mt][nt][k + 2]));
-          over = over || top > m[nt][k] + kLazy;
-        }
+          for (int mt = 0; mt < MT; ++mt) over = over || fmaxf(x[mt][nt][k], x[mt][nt][k + 2]) + lv[mt] > m[nt][k] + kLazy;
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
           for (int k = 0; k < 2; ++k) {
             float top = m[nt][k];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) top = fmaxf(top, fmaxf(x[mt][nt][k], x[mt][nt][k + 2]));
+            for (int mt = 0; mt < MT; ++mt) top = fmaxf(top, fmaxf(x[mt][nt][k], x[mt][nt][k + 2]) + lv[mt]);
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
             const float f = top == -INFINITY ? 1.f : ex2(m[nt][k] - top);
@@ -365,20 +365,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
       // ---- weights, and their sums with the values
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        if (vs_now[mt] > ref || vs_now[mt] < 0.125f * ref) {
-          if (vs_now[mt] > 0.f) {
-            const float f = ref / vs_now[mt];
-            ref = vs_now[mt];
-            inv_ref = kWeightScale / ref;
-#pragma unroll
-            for (int i = 0; i < KS; ++i)
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o[i][nt][k] *= f;
-          }
-        }
-        const float fv = vs_now[mt] * inv_ref;
+        const float up = weight_exponent(vs_now[mt]), down = ex2(-up);
         uint32_t pb[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -386,17 +373,16 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
           if (all) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              e[k] = ex2(x[mt][nt][k] - m[nt][k & 1]);
-              l[nt][k & 1] += e[k];
-              e[k] *= fv;
+              e[k] = ex2(x[mt][nt][k] + (up - m[nt][k & 1]));
+              l[nt][k & 1] = fmaf(e[k], down, l[nt][k & 1]);
             }
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              // a masked score is -inf: so may be the maximum of a row that has seen nothing yet
-              e[k] = x[mt][nt][k] == -INFINITY ? 0.f : ex2(x[mt][nt][k] - m[nt][k & 1]);
-              l[nt][k & 1] += e[k];
-              e[k] = x[mt][nt][k] == -INFINITY ? 0.f : e[k] * fv;
+              // a masked score is -inf: so may be the reference of a row that has seen nothing yet, and the scale may be NaN
+              const bool on = x[mt][nt][k] != -INFINITY;
+              e[k] = on ? ex2(x[mt][nt][k] + (up - m[nt][k & 1])) : 0.f;
+              if (on) l[nt][k & 1] = fmaf(e[k], down, l[nt][k & 1]);
             }
           }
           pb[nt][0] = transpose8x8(pack_f16(e[0], e[1]));
@@ -421,7 +407,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
 
     // ---- results.  Lane (g, c) has rows 2c, 2c + 1 of each tile; of the channels, word w of its values:
     // DP 64: 8 g + 4 w; else 128 (w / 4) + 16 g + 4 (w % 4); within a word o[2w][k], o[2w][k + 2], o[2w + 1][k], o[2w + 1][k + 2].
-    const float unit = ref * (1.f / kWeightScale);
+    constexpr float unit = 1.f / kWeightScale;
     const bool complete = pc.u0 == 0 && pc.u1 == s.units;
     float* part = p.partial + (static_cast<size_t>(worker) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(R, D);
 #pragma unroll
@@ -455,7 +441,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
           }
           if (g == 0) {
             if (!complete) { part[R * D + r] = m[nt][k]; part[R * D + R + r] = l[nt][k]; }
-            else if (p.lse) *lse_at(p, b, s.first, at) = l[nt][k] == 0.f ? -INFINITY : (m[nt][k] + log2f(l[nt][k])) * 0.69314718055994531f;
+            else if (p.lse) *lse_at(p, b, s.first, at) = log_sum(m[nt][k], l[nt][k]);
           }
         }
     } else {
@@ -495,7 +481,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
           const float inv = den == 0.f ? 0.f : 1.f / den;
           const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x * inv, v.y * inv), hi = __floats2bfloat162_rn(v.z * inv, v.w * inv);
           *reinterpret_cast<uint2*>(out_at(p, b, s.first, at) + d * 2) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-          if (d == 0 && p.lse) *lse_at(p, b, s.first, at) = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.69314718055994531f;
+          if (d == 0 && p.lse) *lse_at(p, b, s.first, at) = log_sum(top, den);
         } else {
           *reinterpret_cast<float4*>(part + r * D + d) = v;
           if (d == 0) { part[R * D + r] = top; part[R * D + R + r] = den; }

@@ -118,3 +118,32 @@ def test_attention_values_whose_scale_is_zero_weigh_but_give_nothing(kv, new):
     ref, _, weight, reach = co.attention(q[:new].double().numpy(), kk, vv, there, 0.125, True, T - new)
     assert (np.abs(out[:new].double().cpu().numpy() - ref) <= attend_tol("bf16", d, T, ref, weight, reach, vv)).all()
     assert (out[new:] == 0).all()
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+@pytest.mark.parametrize("hq,H,d,past,new", [(2, 2, 64, 149, 1), (4, 1, 128, 1000, 1), (14, 2, 48, 77, 2), (4, 2, 256, 60, 5)])
+@pytest.mark.parametrize("v_exp", [[0, 33], [-30, 10, -20, 40, 0, 30, -40, 5, 20], [40, 0, -40]])
+@pytest.mark.parametrize("q_gain", [1.0, 4.0, 8.0])
+def test_attention_of_few_rows_keeps_what_large_values_with_small_weights_add(kv, hq, H, d, past, new, v_exp, q_gain):
+    _apart_check(kv, "bf16", hq, H, d, past, new, v_exp, seed=d + new, q_gain=q_gain)
+
+
+@pytest.mark.parametrize("dtype,new,batch", [("bf16", 1, 2400), ("bf16", 17, 300), ("f32", 1, 2400)])
+def test_attention_of_the_largest_values_before_a_block_of_zeros(dtype, new, batch):
+    """100,000 tokens of values of 1.75 x 2^56, the largest that the cache holds, then a block of zeros, whose scale is the least: the
+    sums stay inside float32.  Keys are zero, so every visible token weighs the same.  Many sequences read the same blocks, so that
+    none is cut into short pieces."""
+    H, d, bs, big = 1, 16, 256, 400 * 256
+    T = big + new
+    k, v = torch.zeros((T, H, d)).to(DT[dtype]), torch.full((T, H, d), 1.75 * 2.0 ** 56).to(DT[dtype])
+    v[big:] = 0
+    blocks = -(-T // bs)
+    c = Cache("e4m3", H, bs, d, blocks, 0)
+    table = i32([list(range(blocks))] * batch)
+    vs.vscan_kv_write(k.cuda(), v.cuda(), i32([T]), i32([0, T]), table[:1], *c.arrays)
+    q = torch.ones((new * batch, H, d), dtype=DT[dtype], device="cuda")
+    out = vs.vscan_kv_attention(q, i32([T] * batch), i32(np.arange(batch + 1) * new), table, *c.arrays, 1.0, max_q_len=new).double().cpu()
+    want = 1.75 * 2.0 ** 56 * big / (big + torch.arange(1, new + 1).double())[None, :, None, None].expand(batch, new, H, d).reshape(out.shape)
+    # weights are equal (one rounding in common, which the denominator does not have); sums of T terms
+    tol = torch.finfo(DT[dtype]).eps / 2 + (T / 4 + 16) * 2.0 ** -24 + (2.0 ** -11 if dtype == "bf16" else 0) + 2.0 ** -16
+    assert ((out - want).abs() <= tol * want).all()
