@@ -81,6 +81,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const int D = FULL ? DP : p.head_dim;
   grid_dependency_wait();
+  if (threadIdx.x == 0) p.flags[blockIdx.x] = 0;     // before the barriers in locate(): any warp may set it behind them
   Stretch& st = stretches[threadIdx.x >> 5];
   {
     const Stretch found = locate<kMmaThreads, true>(p, sched);
@@ -89,10 +90,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
   }
   const int worker = st.worker;
   const bool solo = st.solo;
-  if (threadIdx.x == 0) {
-    if (blockIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = solo; }
-    p.flags[blockIdx.x] = 0;
-  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = solo; }
   const bool writes_boundary = lane == 0 && (solo || warp == 0);
   if (writes_boundary) p.boundary[worker].seg1 = 0;
   bool bad = false;

@@ -1,6 +1,6 @@
 """vscan_kv_attention at the edges of its numbers, against the float64 oracle and for every kernel the calls choose from: scores
 whose factor vanishes (scale 0, query rows and keys of zeros, negative scale) over partly masked 16-token groups; values of
-neighbouring blocks many binades apart.
+neighbouring blocks many binades apart; warps that run through many short sequences, and what they report.
 
 Tolerances as derived in test_gpu_cache_ops.py, and beside the tests that have their own.
 """
@@ -147,3 +147,17 @@ def test_attention_of_the_largest_values_before_a_block_of_zeros(dtype, new, bat
     # weights are equal (one rounding in common, which the denominator does not have); sums of T terms
     tol = torch.finfo(DT[dtype]).eps / 2 + (T / 4 + 16) * 2.0 ** -24 + (2.0 ** -11 if dtype == "bf16" else 0) + 2.0 ** -16
     assert ((out - want).abs() <= tol * want).all()
+
+
+def test_attention_reports_a_bad_block_whichever_warp_meets_it():
+    H, d, bs, B = 1, 64, 16, 2368                  # as many segments as warps
+    c, g = Cache("e4m3", H, bs, d, 8, 5), gen(6)
+    q = torch.randn((B, 1, d), generator=g).to(torch.bfloat16).cuda()
+    good = np.zeros((B, 1), dtype=np.int32)
+    ws = vs.vscan_kv_attention_workspace(q, i32(good), c.dev[0], 1)
+    for at in list(range(16)) + [2367, 1111, 593]:
+        bad = good.copy()
+        bad[at] = 8
+        for table, status in ((bad, 1), (good, 0)):
+            vs.vscan_kv_attention(q, i32([16] * B), i32(np.arange(B + 1)), i32(table), *c.arrays, 0.1, workspace=ws)
+            assert vs.vscan_check(ws) == status
