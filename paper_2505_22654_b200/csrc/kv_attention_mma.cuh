@@ -98,6 +98,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
     Piece pc = {0, 0};
     __syncwarp();
     if (lane == 0) next_piece(p, st, pc);
+    __syncwarp();                                     // a shuffle alone does not order what the lanes read of st
     pc.u0 = __shfl_sync(0xffffffffu, pc.u0, 0);
     pc.u1 = __shfl_sync(0xffffffffu, pc.u1, 0);
     if (pc.u1 == 0) break;

@@ -149,6 +149,25 @@ def test_attention_of_the_largest_values_before_a_block_of_zeros(dtype, new, bat
     assert ((out - want).abs() <= tol * want).all()
 
 
+def test_attention_of_many_short_sequences_a_warp_each_after_the_other():
+    """3,000 sequences of 0 to 40 tokens, a row each: a warp goes from sequence to sequence and head to head."""
+    H, hq, d, bs, B = 2, 6, 64, 16, 3000
+    rng, g = np.random.default_rng(3), gen(3)
+    lens = [int(n) for n in rng.integers(0, 41, size=B)]
+    ks, vals = ([torch.randn((n, H, d), generator=g).to(torch.bfloat16) for n in lens] for _ in range(2))
+    c, table = _written("e4m3", H, bs, d, lens, ks, vals)
+    q = torch.randn((B, hq, d), generator=g).to(torch.bfloat16)
+    args = (q.cuda(), i32(lens), i32(np.arange(B + 1)), i32(table), *c.arrays, 0.125)
+    out = vs.vscan_kv_attention(*args)
+    for _ in range(30):
+        assert torch.equal(vs.vscan_kv_attention(*args), out)
+    got = out.double().cpu().numpy()
+    for b, T in enumerate(lens):
+        (k, there), (v, _) = (co.gather(c.codes[i], c.scale[i], table[b], T, bs, co.E4M3) for i in range(2))
+        ref, _, weight, reach = co.attention(q[b:b + 1].double().numpy(), k, v, there, 0.125, True, T - 1)
+        assert (np.abs(got[b:b + 1] - ref) <= attend_tol("bf16", d, T, ref, weight, reach, v)).all(), b
+
+
 def test_attention_reports_a_bad_block_whichever_warp_meets_it():
     H, d, bs, B = 1, 64, 16, 2368                  # as many segments as warps
     c, g = Cache("e4m3", H, bs, d, 8, 5), gen(6)
