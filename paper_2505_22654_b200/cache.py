@@ -35,7 +35,7 @@ class VScanCache:
                       "report": torch.zeros(4, dtype=torch.int32, device=device)}
         self._plan["ring_state_out"], self._plan["kv_len"] = self._views(self._after)
         self._plan["ring_state_out"][1] = num_blocks
-        self._workspaces = {}
+        self._workspace, self._outgrown = None, []
 
     @staticmethod
     def _views(buf):
@@ -58,12 +58,32 @@ class VScanCache:
         """The new rows of the planned step, packed [rows, kv_heads, head_dim] or padded [batch, kv_heads, rows, head_dim]."""
         vb.vscan_kv_write(k, v, self.kv_len, self.row_offset, self.block_table, *self.arrays)
 
+    def _grow(self, q, max_q_len):
+        """One workspace serves all calls: the largest so far.  One that is too small stays where it is, since captured graphs may
+        write to it; each is at least twice as large as the one before, so these are less than the last one together."""
+        former, work = self._workspace, vb.vscan_kv_attention_workspace(q, self.block_table, self.k, max_q_len)
+        if former is not None:
+            work.reserve(2 * former.nbytes)
+            self._outgrown.append(former)
+            if not (q.is_cuda and torch.cuda.is_current_stream_capturing()):
+                former.buf[:4].zero_()           # from here on it says what such graphs leave there
+        work.buf[:4].zero_()
+        self._workspace = work
+
     def attend(self, q, scale, max_q_len=1, causal=True, out=None, lse=None):
-        key = (tuple(q.shape), q.dtype, max_q_len)
-        if key not in self._workspaces:
-            self._workspaces[key] = vb.vscan_kv_attention_workspace(q, self.block_table, self.k, max_q_len)
-        return vb.vscan_kv_attention(q, self.kv_len, self.row_offset, self.block_table, *self.arrays, scale, max_q_len=max_q_len,
-                                     causal=causal, out=out, lse=lse, workspace=self._workspaces[key])
+        """Attention of the planned step's new rows (vb.vscan_kv_attention).  -> out."""
+        if out is None:
+            out = torch.zeros_like(q)
+        if self._workspace is None:
+            self._grow(q, max_q_len)
+        args = (q, self.kv_len, self.row_offset, self.block_table, *self.arrays, scale, max_q_len, causal, out, lse)
+        try:
+            return vb.vscan_kv_attention(*args, workspace=self._workspace)
+        except vb.VScanError as e:
+            if e.status != vb.ERR_WORKSPACE:
+                raise
+        self._grow(q, max_q_len)
+        return vb.vscan_kv_attention(*args, workspace=self._workspace)
 
     def step(self, q, k, v, pos_ids, rope, new_len, scale, pairing=vb.ROPE_HALVES, out=None):
         """One step of a layer: rotary positions on q and k (rope = (inv_freq, axis)), plan, write, causal attention.  q, k, v
@@ -75,6 +95,7 @@ class VScanCache:
         return self.attend(q, scale, max_q_len=q.shape[2], out=out)
 
     def check(self):
-        """Synchronises and gives the status of the last attention call of each size (0, or that a block or a length was
-        out of range), and the code of the last plan."""
-        return max([vb.vscan_check(w) for w in self._workspaces.values()], default=0), int(self.report[0])
+        """Synchronises and gives the status of the last attention call (0, or that a block or a length was out of range; so of the
+        last replay of a graph that was captured before a larger call), and the code of the last plan."""
+        spaces = [w for w in (self._workspace, *self._outgrown) if w is not None]
+        return max([vb.vscan_check(w) for w in spaces], default=0), int(self.report[0])

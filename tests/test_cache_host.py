@@ -1,0 +1,60 @@
+"""What VScanCache does on the host, on CPU tensors, the library's calls replaced.  No GPU."""
+import pytest
+import torch
+
+from paper_2505_22654_b200 import binding as vb
+from paper_2505_22654_b200.cache import VScanCache
+
+
+def _cache(**kw):
+    return VScanCache(**{**dict(num_blocks=8, block_size=16, kv_heads=2, head_dim=32, batch=2, max_blocks=4, rows=64, device="cpu"), **kw})
+
+
+@pytest.fixture
+def attention(monkeypatch):
+    """vscan_kv_attention in which `rows` query rows need 1000 + rows * max_q_len bytes; -> the calls that went through."""
+    calls, need = [], lambda q, most: 1000 + q.shape[0] * most
+
+    def run(q, kv_len, row_offset, block_table, k, v, k_scale, v_scale, scale, max_q_len=1, causal=True, out=None, lse=None, workspace=None):
+        if workspace.nbytes < need(q, max_q_len):
+            raise vb.VScanError(vb.ERR_WORKSPACE, "vscan_kv_attention")
+        calls.append((q.shape[0], workspace))
+        return out
+
+    monkeypatch.setattr(vb, "vscan_kv_attention", run)
+    monkeypatch.setattr(vb, "vscan_kv_attention_workspace", lambda q, table, k, most: vb.Workspace(need(q, most), "cpu"))
+    monkeypatch.setattr(vb, "vscan_check", lambda w: int(w.buf[:4].view(torch.int32)))
+    return calls
+
+
+def test_one_workspace_whatever_the_row_counts_are(attention):
+    c = _cache()
+    for rows in [*range(1, 400), *range(400, 0, -1)]:
+        c.attend(torch.zeros((rows, 4, 32)), 1.0, max_q_len=1 + rows % 50)
+    held = {id(w): w for _, w in attention}.values()
+    assert len(attention) == 799 and len(held) <= 6
+    assert sum(w.nbytes for w in held) < 4 * (1000 + 400 * 50)
+
+
+def test_status_is_that_of_the_last_call_and_of_graphs_on_outgrown_workspaces(attention):
+    c = _cache()
+    assert c.check() == (0, 0)
+    c.attend(torch.zeros((1, 4, 32)), 1.0)
+    small = attention[-1][1]
+    small.buf[:4].view(torch.int32)[0] = vb.ERR_INVALID_ARG        # what a call with a bad table leaves
+    assert c.check() == (vb.ERR_INVALID_ARG, 0)
+    c.attend(torch.zeros((500, 4, 32)), 1.0, max_q_len=40)         # a good one, on a larger workspace
+    attention[-1][1].buf[:4].zero_()
+    assert attention[-1][1] is not small and c.check() == (0, 0)
+    small.buf[:4].view(torch.int32)[0] = vb.ERR_TIMEOUT            # a replay of a graph that holds the small one
+    assert c.check() == (vb.ERR_TIMEOUT, 0)
+
+
+def test_other_errors_of_the_attention_are_passed_on(attention, monkeypatch):
+    def refuse(*args, **kw):
+        raise vb.VScanError(vb.ERR_UNSUPPORTED, "vscan_kv_attention")
+    monkeypatch.setattr(vb, "vscan_kv_attention", refuse)
+    c = _cache()
+    with pytest.raises(vb.VScanError) as e:
+        c.attend(torch.zeros((1, 4, 32)), 1.0)
+    assert e.value.status == vb.ERR_UNSUPPORTED and c.check() == (0, 0)

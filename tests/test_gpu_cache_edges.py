@@ -1,6 +1,6 @@
 """vscan_kv_attention at the edges of its numbers, against the float64 oracle and for every kernel the calls choose from: scores
 whose factor vanishes (scale 0, query rows and keys of zeros, negative scale) over partly masked 16-token groups; values of
-neighbouring blocks many binades apart; warps that run through many short sequences, and what they report.
+neighbouring blocks many binades apart; warps that run through many short sequences, and what they report; the cache's workspace.
 
 Tolerances as derived in test_gpu_cache_ops.py, and beside the tests that have their own.
 """
@@ -180,3 +180,33 @@ def test_attention_reports_a_bad_block_whichever_warp_meets_it():
         for table, status in ((bad, 1), (good, 0)):
             vs.vscan_kv_attention(q, i32([16] * B), i32(np.arange(B + 1)), i32(table), *c.arrays, 0.1, workspace=ws)
             assert vs.vscan_check(ws) == status
+
+
+def test_cache_holds_one_workspace_whatever_the_row_counts_are():
+    """Packed prompts of 60 different row counts: memory grows by at most the two largest workspaces; a graph that was captured on a
+    small one gives the same bits afterwards."""
+    H, hq, d = 2, 4, 128
+    cache = vs.VScanCache(num_blocks=200, block_size=16, kv_heads=H, head_dim=d, batch=2, max_blocks=100, rows=2000)
+    g = gen(1)
+    k, v = (torch.randn((1500, H, d), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    q = torch.randn((1500, hq, d), generator=g).to(torch.bfloat16).cuda()
+    cache.plan(i32([300, 0]))
+    cache.write(k[:300], v[:300])
+    few, out = q[:1].contiguous(), torch.zeros((1, hq, d), dtype=torch.bfloat16, device="cuda")
+    cache.plan(i32([1, 0]))
+    cache.write(k[300:301], v[300:301])
+    want = cache.attend(few, 0.1).clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.attend(few, 0.1, out=out)
+    before = torch.cuda.memory_allocated()
+    for n in range(17, 77):
+        cache.attend(q[:n * 20], 0.1, max_q_len=n * 20)
+    assert cache.check() == (0, 0)
+    assert torch.cuda.memory_allocated() - before < 160 << 20
+    noise = [torch.full((8 << 20,), 255, dtype=torch.uint8, device="cuda") for _ in range(20)]      # over what has been let go
+    out.zero_()
+    graph.replay()
+    assert torch.equal(out, want) and cache.check() == (0, 0)
+    del noise
