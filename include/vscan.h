@@ -375,7 +375,9 @@ vscan_status vscan_llm_prune_ragged(const vscan_prune_ragged_desc* desc, void* w
  *   q, k      [batch][heads][seq_len][head_dim] by strides: element (b, h, s, c) lies at
  *             b * stride[0] + h * stride[1] + s * stride[2] + c.  Either of q and k may be NULL (with its output).
  *   q_out, k_out  likewise.  An output may be its own input (the same pointer and strides): then the call works in place.
- *             Otherwise outputs must not overlap inputs.  The elements of one output must not overlap each other.
+ *             Otherwise outputs must not overlap inputs, their own or the other's, nor each other, nor the elements of one output
+ *             each other.  Views of one buffer that cover each other's extents are taken where their elements can be told apart by
+ *             strides: heads side by side in a token, in a sequence, or in turn.
  * head_dim a multiple of 8, at most 512; rot_dim even, 2 .. head_dim; strides multiples of 16 bytes; pos_planes 1 .. 16.
  * No workspace.
  * ------------------------------------------------------------------------------------------- */

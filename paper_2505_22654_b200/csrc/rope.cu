@@ -165,12 +165,43 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(Params p) {
 
 struct Extent { const char* lo; size_t n; };
 
-// Bytes from the first to the last element of a tensor given by strides
-static Extent extent(const void* p, const int64_t* stride, int64_t batch, int64_t heads, int64_t tokens, int64_t dim, size_t e) {
-  int64_t lo = 0, hi = dim;
+// Elements from the first to the last of a tensor given by strides, as offsets from its start
+struct Span { int64_t lo, hi; };
+static Span span(const int64_t* stride, int64_t batch, int64_t heads, int64_t tokens, int64_t dim) {
+  Span r = {0, dim};
   const int64_t n[3] = {batch, heads, tokens};
-  for (int i = 0; i < 3; ++i) (stride[i] < 0 ? lo : hi) += stride[i] * (n[i] - 1);
-  return {static_cast<const char*>(p) + lo * static_cast<int64_t>(e), static_cast<size_t>(hi - lo) * e};
+  for (int i = 0; i < 3; ++i) (stride[i] < 0 ? r.lo : r.hi) += stride[i] * (n[i] - 1);
+  return r;
+}
+static Extent extent(const void* p, const int64_t* stride, int64_t batch, int64_t heads, int64_t tokens, int64_t dim, size_t e) {
+  const Span r = span(stride, batch, heads, tokens, dim);
+  return {static_cast<const char*>(p) + r.lo * static_cast<int64_t>(e), static_cast<size_t>(r.hi - r.lo) * e};
+}
+
+struct Rows { const void* p; const int64_t* stride; int64_t heads; };
+
+// Whether no element of a lies on one of b.  Extents that do not meet are apart; of those that do, the ways in which queries and
+// keys are usually views of one buffer are told apart, and anything else counts as not apart:
+//   with the same steps from sequence to sequence (token to token), each has its own stretch of every token (of every sequence);
+//   with the same steps in all three, the distance between the two is a fourth step of one tensor
+static bool apart(const Rows& a, const Rows& b, int64_t batch, int64_t tokens, int64_t dim, size_t e) {
+  const Extent ea = extent(a.p, a.stride, batch, a.heads, tokens, dim, e), eb = extent(b.p, b.stride, batch, b.heads, tokens, dim, e);
+  if (!overlaps(ea.lo, ea.n, eb.lo, eb.n)) return true;
+  const int64_t delta = (reinterpret_cast<intptr_t>(b.p) - reinterpret_cast<intptr_t>(a.p)) / static_cast<int64_t>(e);
+  if (batch > 1 && a.stride[0] != b.stride[0]) return false;
+  const int64_t counts[2] = {batch, tokens}, steps[2] = {a.stride[0], a.stride[2]};
+  for (int common = 1; common <= 2; ++common) {            // the sequences are common steps, then the tokens as well
+    if (common == 2 && tokens > 1 && a.stride[2] != b.stride[2]) return false;
+    Span own = span(a.stride, 1, a.heads, common == 2 ? 1 : tokens, dim), other = span(b.stride, 1, b.heads, common == 2 ? 1 : tokens, dim);
+    other.lo += delta;
+    other.hi += delta;
+    const int64_t both = (own.hi > other.hi ? own.hi : other.hi) - (own.lo < other.lo ? own.lo : other.lo);
+    if ((own.hi <= other.lo || other.hi <= own.lo) && strides_apart(steps, counts, common, both)) return true;
+  }
+  if (a.heads > 1 && b.heads > 1 && a.stride[1] != b.stride[1]) return false;
+  const int64_t all[4] = {a.stride[0], a.heads > 1 ? a.stride[1] : b.stride[1], a.stride[2], delta};
+  const int64_t sizes[4] = {batch, a.heads > b.heads ? a.heads : b.heads, tokens, 2};
+  return strides_apart(all, sizes, 4, dim);
 }
 
 static vscan_status validate(const vscan_rope_desc* d) {
@@ -197,7 +228,7 @@ static vscan_status validate(const vscan_rope_desc* d) {
     for (int j = 0; j < 3; ++j)
       if (strides[i][j] % per16 || strides[i][j] > (int64_t{1} << 40) || strides[i][j] < -(int64_t{1} << 40)) return VSCAN_ERR_INVALID_ARG;
   }
-  // outputs: apart from every input, but for the in-place form, and from each other; no two of their elements in one place
+  // outputs: apart from every input, but for the in-place form, and from each other; no two elements of one in one place
   struct Io { const void *in, *out; const int64_t *si, *so; int heads; };
   const Io io[2] = {{d->q, d->q_out, d->q_stride, d->q_out_stride, d->q_heads}, {d->k, d->k_out, d->k_stride, d->k_out_stride, d->k_heads}};
   Extent outs[2] = {};
@@ -212,13 +243,18 @@ static vscan_status validate(const vscan_rope_desc* d) {
     if (!io[i].in) continue;
     bool same = io[i].in == io[i].out;
     for (int j = 0; j < 3; ++j) same = same && io[i].si[j] == io[i].so[j];
-    // queries and keys may be views of one projection's output, turned in place: their extents then cover each other, so
-    // a tensor is compared with its own output only
     const Extent in = extent(io[i].in, io[i].si, d->batch, io[i].heads, d->seq_len, d->head_dim, e);
     if (!same && overlaps(in.lo, in.n, outs[i].lo, outs[i].n)) return VSCAN_ERR_INVALID_ARG;
     if (overlaps(outs[i].lo, outs[i].n, d->pos_ids, static_cast<size_t>(d->pos_planes) * tokens * 4) ||
         overlaps(outs[i].lo, outs[i].n, d->inv_freq, static_cast<size_t>(d->rot_dim) * 2) ||
         overlaps(outs[i].lo, outs[i].n, d->axis, static_cast<size_t>(d->rot_dim) * 2))
+      return VSCAN_ERR_INVALID_ARG;
+  }
+  if (d->q && d->k) {          // queries and keys may be views of one projection's output, turned in place
+    const Rows q = {d->q, d->q_stride, d->q_heads}, qo = {d->q_out, d->q_out_stride, d->q_heads};
+    const Rows k = {d->k, d->k_stride, d->k_heads}, ko = {d->k_out, d->k_out_stride, d->k_heads};
+    if (!apart(qo, k, d->batch, d->seq_len, d->head_dim, e) || !apart(ko, q, d->batch, d->seq_len, d->head_dim, e) ||
+        !apart(qo, ko, d->batch, d->seq_len, d->head_dim, e))
       return VSCAN_ERR_INVALID_ARG;
   }
   return VSCAN_OK;

@@ -1,7 +1,11 @@
-"""What VScanCache does on the host, on CPU tensors, the library's calls replaced.  No GPU."""
+"""What VScanCache does on the host, on CPU tensors, the library's calls replaced; outputs of vscan_rope on top of each other or of the
+other side's input.  No GPU."""
+import ctypes as C
+
 import pytest
 import torch
 
+from paper_2505_22654_b200 import _build
 from paper_2505_22654_b200 import binding as vb
 from paper_2505_22654_b200.cache import VScanCache
 
@@ -58,3 +62,37 @@ def test_other_errors_of_the_attention_are_passed_on(attention, monkeypatch):
     with pytest.raises(vb.VScanError) as e:
         c.attend(torch.zeros((1, 4, 32)), 1.0)
     assert e.value.status == vb.ERR_UNSUPPORTED and c.check() == (0, 0)
+
+
+# --------------------------------------------------------------------------- vscan_rope
+BASE, B, S, D = 1 << 40, 2, 5, 64       # host-side checks never read these addresses
+FAR = 1 << 34
+
+
+def _rope(hq, hk, **sides):
+    """Status of a bf16 call whose sides are (address in elements of 2 bytes, strides); any that is not given is far from the rest."""
+    _build.build()
+    d = vb.RopeDesc(vb.BF16, 0, 0, B, S, hq, hk, D, 32, 3)
+    for i, name in enumerate(("pos_ids", "inv_freq", "axis")):
+        setattr(d, name, BASE + (20 + i) * FAR)
+    for i, (name, heads) in enumerate((("q", hq), ("q_out", hq), ("k", hk), ("k_out", hk))):
+        at, strides = sides.get(name, ((4 + i) * FAR, (heads * S * D, S * D, D)))
+        setattr(d, name, BASE + 2 * at)
+        setattr(d, name + "_stride", vb._i64x3(*strides))
+    return vb.lib().vscan_rope(C.byref(d), None)
+
+
+PLAIN = (4 * S * D, S * D, D)             # [B, 4, S, D]
+FUSED = (S * 8 * D, D, 8 * D)             # four heads of [B, S, 8, D]
+
+
+@pytest.mark.parametrize("sides", [
+    dict(q_out=(0, PLAIN), k_out=(0, PLAIN)), dict(q_out=(0, PLAIN), k_out=(8, PLAIN)), dict(q_out=(0, PLAIN), k_out=(S * D, PLAIN)),
+    dict(q=(0, PLAIN), q_out=(FAR, PLAIN), k=(FAR, PLAIN), k_out=(0, PLAIN)),                      # each into the other
+    dict(k=(0, PLAIN), q_out=(0, PLAIN)), dict(q=(0, PLAIN), k_out=(0, PLAIN)),
+    dict(q=(0, PLAIN), q_out=(0, PLAIN), k=(0, PLAIN)),                                            # in place, but the keys read it too
+    dict(q_out=(0, FUSED), k_out=(3 * D, FUSED)), dict(q_out=(0, FUSED), k_out=(4 * D + 8, FUSED)), dict(q_out=(0, FUSED), k_out=(5 * D, FUSED)),
+    dict(q_out=(0, FUSED), k_out=(8 * D, FUSED)),                                                  # one token on
+    dict(q_out=(0, FUSED), k_out=(4 * D, PLAIN)), dict(q_out=(0, FUSED), k_out=(4 * D, (S * 8 * D, D, 4 * D)))])
+def test_rope_outputs_on_each_other_or_on_the_other_input_are_refused(sides):
+    assert _rope(4, 4, **sides) == vb.ERR_INVALID_ARG

@@ -1,6 +1,7 @@
 """vscan_kv_attention at the edges of its numbers, against the float64 oracle and for every kernel the calls choose from: scores
 whose factor vanishes (scale 0, query rows and keys of zeros, negative scale) over partly masked 16-token groups; values of
-neighbouring blocks many binades apart; warps that run through many short sequences, and what they report; the cache's workspace.
+neighbouring blocks many binades apart; warps that run through many short sequences, and what they report; the cache's workspace; queries and keys that
+are views of one buffer.
 
 Tolerances as derived in test_gpu_cache_ops.py, and beside the tests that have their own.
 """
@@ -210,3 +211,26 @@ def test_cache_holds_one_workspace_whatever_the_row_counts_are():
     graph.replay()
     assert torch.equal(out, want) and cache.check() == (0, 0)
     del noise
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["tokens", "heads", "turns", "sides", "rows", "groups"])
+@pytest.mark.parametrize("hq,hk", [(4, 4), (6, 2), (1, 1)])
+def test_rope_in_place_on_views_of_one_buffer(dtype, layout, hq, hk):
+    """Queries and keys side by side in a token, in a sequence, head by head in turn, as two halves, one behind the other in the rows
+    of a head, and the tokens in front of the sequences: the same bits as out of place, and nothing else changed."""
+    B, S, d, g = 2, 5, 64, gen(hq)
+    if layout in ("turns", "rows") and hq != hk:
+        pytest.skip("needs as many query as key heads")
+    shape = {"tokens": (B, S, hq + 2 * hk, d), "heads": (B, hq + 2 * hk, S, d), "turns": (B, S, hq, 3, d), "sides": (hq + 2 * hk, B, S, d),
+             "rows": (B, hq, 3 * S, d), "groups": (S, B, hq + 2 * hk, d)}[layout]
+    buf = torch.randn(shape, generator=g).to(DT[dtype]).cuda()
+    q, k, rest = {"tokens": lambda: [t.transpose(1, 2) for t in buf.split([hq, hk, hk], 2)], "heads": lambda: buf.split([hq, hk, hk], 1),
+                  "turns": lambda: [buf[:, :, :, i].transpose(1, 2) for i in range(3)],
+                  "sides": lambda: [t.transpose(0, 1) for t in buf.split([hq, hk, hk], 0)], "rows": lambda: buf.split(S, 2),
+                  "groups": lambda: [t.permute(1, 2, 0, 3) for t in buf.split([hq, hk, hk], 2)]}[layout]()
+    pos = torch.randint(0, 900, (2, B, S), generator=g, dtype=torch.int32).cuda()
+    table, before = vs.rope_table(d, [20, 12]), rest.clone()
+    want = vs.vscan_rope(q, k, pos, *table, q_out=torch.empty(q.shape, dtype=q.dtype, device="cuda"), k_out=torch.empty(k.shape, dtype=q.dtype, device="cuda"))
+    vs.vscan_rope(q, k, pos, *table, q_out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(rest, before)
