@@ -453,7 +453,7 @@ static Plan plan_launch(const vscan_kv_attention_desc* d) {
     resident = d->head_dim > 128 || pl.tile_rows > 8 ? 2 : 4;
   } else {
     pl.tile_rows = want <= 1 ? 1 : want <= 2 ? 2 : want <= 4 ? 4 : 8;
-    resident = 4;
+    resident = pl.tile_rows > 4 ? 2 : 4;   // 8 rows take 243 to 254 registers of 128 threads
   }
   // as many CTAs as fit the SMs at once, no more than there can be units
   const int64_t rows = d->padded ? static_cast<int64_t>(d->batch) * (d->rows < d->max_q_len ? d->rows : d->max_q_len) : d->rows;

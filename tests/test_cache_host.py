@@ -1,5 +1,5 @@
 """What VScanCache does on the host, on CPU tensors, the library's calls replaced; outputs of vscan_rope on top of each other or of the
-other side's input.  No GPU."""
+other side's input; how many CTAs an attention call plans for.  No GPU."""
 import ctypes as C
 
 import pytest
@@ -96,3 +96,16 @@ FUSED = (S * 8 * D, D, 8 * D)             # four heads of [B, S, 8, D]
     dict(q_out=(0, FUSED), k_out=(4 * D, PLAIN)), dict(q_out=(0, FUSED), k_out=(4 * D, (S * 8 * D, D, 4 * D)))])
 def test_rope_outputs_on_each_other_or_on_the_other_input_are_refused(sides):
     assert _rope(4, 4, **sides) == vb.ERR_INVALID_ARG
+
+
+# --------------------------------------------------------------------------- vscan_kv_attention
+@pytest.mark.parametrize("max_q_len,rows,per_sm", [(1, 4, 4), (50, 8, 2)])
+def test_float32_attention_plans_for_the_ctas_that_fit_at_once(max_q_len, rows, per_sm):
+    """The workspace has room for two partial results a CTA, and no launch has more CTAs than the registers of 148 SMs hold: 128
+    registers a thread for tiles of 4 rows, up to 254 for tiles of 8."""
+    _build.build()
+    d = vb.KvAttentionDesc(vb.F32, vb.KV_E4M3, 40, 8, 2, 64, 16, 10000, 200, 2000, 0, max_q_len, 1, 0.125)
+    up = lambda n: -(-n // 256) * 256  # noqa: E731
+    ctas = 148 * per_sm
+    want = 256 + up(4 * ctas) + up(48 * ctas) + up(2 * ctas * rows * (64 + 2) * 4)
+    assert vb.lib().vscan_kv_attention_workspace_bytes(C.byref(d)) == want
