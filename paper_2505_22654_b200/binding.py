@@ -456,11 +456,12 @@ def vscan_kv_plan(past_len, new_len, block_table, free_ring, ring_state, block_s
     """Block tables, slot maps and offsets from request lengths (see include/vscan.h).  past_len, new_len [B] int32,
     block_table [B, max_blocks] int32 and free_ring [num_blocks] int32 (both updated in place), ring_state [2] int64.
     `out`: a dict of the tensors to write (kv_len, row_offset, ring_state_out, report and, if wanted, slot_map and row_pos);
-    what is missing is made here, slot_map and row_pos with `rows` entries (None: they are not wanted).  -> that dict."""
+    what is missing is made here, slot_map and row_pos with `rows` entries (None: they are not wanted).  A step of more new rows than
+    `rows`, or than a given slot_map or row_pos has entries, is not planned (code 4).  -> that dict."""
     o = {} if out is None else out
     sized = [o[name].shape[0] for name in ("slot_map", "row_pos") if o.get(name) is not None]
     if sized:
-        rows = min(sized)
+        rows = min(sized if rows is None else [*sized, rows])
     elif rows is None:
         rows = 0x7fffffff
         o.setdefault("slot_map", None)

@@ -1,5 +1,6 @@
 """What VScanCache does on the host, on CPU tensors, the library's calls replaced; outputs of vscan_rope on top of each other or of the
-other side's input; how many CTAs an attention call plans for.  No GPU."""
+other side's input; how many CTAs an attention call plans for; the row limit of a plan.
+No GPU."""
 import ctypes as C
 
 import pytest
@@ -109,3 +110,24 @@ def test_float32_attention_plans_for_the_ctas_that_fit_at_once(max_q_len, rows, 
     ctas = 148 * per_sm
     want = 256 + up(4 * ctas) + up(48 * ctas) + up(2 * ctas * rows * (64 + 2) * 4)
     assert vb.lib().vscan_kv_attention_workspace_bytes(C.byref(d)) == want
+
+
+# --------------------------------------------------------------------------- vscan_kv_plan
+@pytest.mark.parametrize("rows,slots,places,limit", [(None, 40, None, 40), (None, 40, 30, 30), (25, 40, 30, 25), (50, 40, 50, 40), (25, None, None, 25),
+                                                     (None, None, None, 2 ** 31 - 1)])
+def test_plan_keeps_to_the_least_of_its_row_limits(monkeypatch, rows, slots, places, limit):
+    given = []
+
+    class Calls:
+        @staticmethod
+        def kv_plan(*args):
+            given.append(args)
+            return vb.OK
+
+    monkeypatch.setattr(vb, "_CALLS", Calls)
+    i32 = lambda *n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    out = {name: t for name, t in (("slot_map", slots and torch.zeros(slots, dtype=torch.int64)), ("row_pos", places and i32(places))) if t is not None}
+    o = vb.vscan_kv_plan(i32(2), i32(2), i32(2, 4), i32(9), torch.zeros(2, dtype=torch.int64), 16, rows=rows, out=out)
+    assert given[0][6] == limit
+    for name, size in (("slot_map", slots), ("row_pos", places)):
+        assert (o[name] is None) if (rows, slots, places) == (None, None, None) else o[name].shape[0] == (size or limit)
