@@ -54,6 +54,12 @@ class VScanCache:
         self._before.copy_(self._after)
         vb.vscan_kv_plan(self._past_len, new_len, self.block_table, self.free_ring, self._past_state, self.block_size, out=self._plan)
 
+    def _take_back(self):
+        """The last plan undone, for a step whose rows are refused afterwards: lengths and ring as before it, no new rows.  The blocks
+        that it took lie in front of the ring's head again, those that it put back behind its tail."""
+        self._after.copy_(self._before)
+        self.row_offset.zero_()
+
     def write(self, k, v):
         """The new rows of the planned step, packed [rows, kv_heads, head_dim] or padded [batch, kv_heads, rows, head_dim]."""
         vb.vscan_kv_write(k, v, self.kv_len, self.row_offset, self.block_table, *self.arrays)
@@ -88,11 +94,15 @@ class VScanCache:
     def step(self, q, k, v, pos_ids, rope, new_len, scale, pairing=vb.ROPE_HALVES, out=None):
         """One step of a layer: rotary positions on q and k (rope = (inv_freq, axis)), plan, write, causal attention.  q, k, v
         [batch, heads, rows, head_dim] padded, pos_ids [planes, batch, rows], new_len at most `rows`.  -> attention of the new
-        rows, like q."""
+        rows, like q.  If a tensor is refused, lengths and tables are as they were."""
         q, k = vb.vscan_rope(q, k, pos_ids, *rope, pairing=pairing)
         self.plan(new_len)
-        self.write(k, v)
-        return self.attend(q, scale, max_q_len=q.shape[2], out=out)
+        try:
+            self.write(k, v)
+            return self.attend(q, scale, max_q_len=q.shape[2], out=out)
+        except Exception:
+            self._take_back()
+            raise
 
     def check(self):
         """Synchronises and gives the status of the last attention call (0, or that a block or a length was out of range; so of the

@@ -96,11 +96,16 @@ class VScanReducer:
     def cache_survivors(self, cache, new_len=None):
         """The K / V rows that the last pass kept become the sequences' tokens in a VScanCache of the layer (Sec. 4.2: from
         layer k on the cache holds survivors only).  new_len [B] int32 on the GPU, made here if not given: S_out for every
-        sequence.  The cache's sequences must be empty or end with the tokens that these follow."""
+        sequence.  The cache's sequences must be empty or end with the tokens that these follow.  If the cache does not take rows
+        of these heads, lengths and tables are as they were."""
         if new_len is None:
             new_len = torch.full((self.B,), self.S_out, dtype=torch.int32, device=self.merged.device)
         cache.plan(new_len)
-        cache.write(self.out2["k"], self.out2["v"])
+        try:
+            cache.write(self.out2["k"], self.out2["v"])
+        except Exception:
+            cache._take_back()
+            raise
 
     def check(self) -> int:
         """Synchronises the current stream and reads the device status words of both workspaces: 0, or

@@ -1,7 +1,7 @@
 """vscan_kv_attention at the edges of its numbers, against the float64 oracle and for every kernel the calls choose from: scores
 whose factor vanishes (scale 0, query rows and keys of zeros, negative scale) over partly masked 16-token groups; values of
-neighbouring blocks many binades apart; warps that run through many short sequences, and what they report; the cache's workspace; queries and keys that
-are views of one buffer.
+neighbouring blocks many binades apart; warps that run through many short sequences, and what they report; the cache's workspace and what it does where a
+tensor is refused; queries and keys that are views of one buffer.
 
 Tolerances as derived in test_gpu_cache_ops.py, and beside the tests that have their own.
 """
@@ -234,3 +234,42 @@ def test_rope_in_place_on_views_of_one_buffer(dtype, layout, hq, hk):
     want = vs.vscan_rope(q, k, pos, *table, q_out=torch.empty(q.shape, dtype=q.dtype, device="cuda"), k_out=torch.empty(k.shape, dtype=q.dtype, device="cuda"))
     vs.vscan_rope(q, k, pos, *table, q_out=q, k_out=k)
     assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(rest, before)
+
+
+def test_a_refused_step_leaves_the_cache_as_it_was():
+    B, H, hq, d, g = 2, 2, 4, 64, gen(2)
+    caches = [vs.VScanCache(num_blocks=20, block_size=16, kv_heads=H, head_dim=d, batch=B, max_blocks=6, rows=64) for _ in range(2)]
+    t = lambda heads, n: torch.randn((B, heads, n, d), generator=g).to(torch.bfloat16).cuda()  # noqa: E731
+    rope, pos = vs.rope_table(d, [32]), torch.zeros((1, B, 20), dtype=torch.int32, device="cuda")
+    first, second = (t(hq, 20), t(H, 20), t(H, 20)), (t(hq, 3), t(H, 3), t(H, 3))
+    for c in caches:
+        c.step(*first, pos, rope, i32([20, 15]), 0.125)
+    c, other = caches
+    before = [c.kv_len.tolist(), c._plan["ring_state_out"].tolist()]
+    p3, n3 = pos[:, :, :3].contiguous(), i32([3, -15])
+    q, k, v = second
+    for bad in ((q, k, v[:, :1]), (q, k, v.float()), (q, k, v[..., :48]), (q[..., :48], k[..., :48], v[..., :48]), (q[:, :3], k, v)):
+        with pytest.raises((ValueError, TypeError, vs.VScanError)):
+            c.step(*bad, p3, rope if bad[0].shape[-1] == d else vs.rope_table(48, [24]), n3, 0.125)
+        assert [c.kv_len.tolist(), c._plan["ring_state_out"].tolist()] == before and c.row_offset.tolist() == [0] * (B + 1)
+        assert (c.attend(q, 0.125, max_q_len=3) == 0).all()
+    with pytest.raises((ValueError, vs.VScanError)):
+        c.step(q, k, v, p3, rope, n3, 0.125, out=torch.zeros_like(q[:, :1]))
+    outs = [x.step(q, k, v, p3, rope, n3, 0.125) for x in caches]
+    assert torch.equal(*outs) and c.kv_len.tolist() == other.kv_len.tolist() == [23, 0]
+    assert c._plan["ring_state_out"].tolist() == other._plan["ring_state_out"].tolist()
+    n = [row[:2] for row in c.block_table.tolist()]
+    assert n[0] == other.block_table.tolist()[0][:2]
+
+
+def test_survivors_that_a_cache_does_not_take_leave_it_as_it_was():
+    from synth import CONFIGS, stage2_inputs
+    cfg = CONFIGS[2].with_(name="cache_run", B=2, C=1, k2=32, Hq=8, Hkv=4, d=64, Dh=256, pos_planes=3)
+    d2 = stage2_inputs(cfg, 0, cfg.B)
+    red = vs.VScanReducer.from_config(cfg)
+    bf = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda().to(torch.bfloat16)  # noqa: E731
+    red.stage2(bf(d2["q_last"]), bf(d2["k"]), bf(d2["v"]), bf(d2["hidden"]), torch.from_numpy(np.ascontiguousarray(d2["pos_ids"])).cuda())
+    cache = vs.VScanCache(num_blocks=40, block_size=16, kv_heads=2, head_dim=64, batch=2, max_blocks=20, rows=2 * red.S_out)
+    with pytest.raises(ValueError):
+        red.cache_survivors(cache)
+    assert cache.kv_len.tolist() == [0, 0] and cache.row_offset.tolist() == [0, 0, 0]
