@@ -648,7 +648,8 @@ def fma_rate_tflops(blocks: int = 148 * 16, iters: int = 1 << 15, repeats: int =
 
 
 def vscan_check(workspace: Workspace) -> int:
-    return int(lib().vscan_check(workspace.ptr, _stream()))
+    """Status that the last call left in this workspace; waits for the current stream of the workspace's device."""
+    return int(lib().vscan_check(workspace.ptr, torch.cuda.current_stream(workspace.buf.device).cuda_stream))
 
 
 def vscan_selftest_bounded_wait(workspace: Workspace, polls: int = 2000) -> None:

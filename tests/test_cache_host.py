@@ -1,6 +1,6 @@
 """What VScanCache does on the host, on CPU tensors, the library's calls replaced; outputs of vscan_rope on top of each other or of the
-other side's input; how many CTAs an attention call plans for; the row limit of a plan.
-No GPU."""
+other side's input; how many CTAs an attention call plans for; the row limit of a plan; which
+stream a status is waited for on.  No GPU."""
 import ctypes as C
 
 import pytest
@@ -131,3 +131,16 @@ def test_plan_keeps_to_the_least_of_its_row_limits(monkeypatch, rows, slots, pla
     assert given[0][6] == limit
     for name, size in (("slot_map", slots), ("row_pos", places)):
         assert (o[name] is None) if (rows, slots, places) == (None, None, None) else o[name].shape[0] == (size or limit)
+
+
+# --------------------------------------------------------------------------- vscan_check
+def test_check_waits_for_the_stream_of_the_workspaces_device(monkeypatch):
+    """Calls on tensors of another device than the current one run on that device's stream."""
+    from types import SimpleNamespace
+    asked = []
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: SimpleNamespace(cuda_stream={None: 11, torch.device("cuda", 1): 22}[device]))
+    monkeypatch.setattr(vb, "lib", lambda: SimpleNamespace(vscan_check=lambda ptr, stream: asked.append((ptr, stream)) or vb.OK))
+    buf = SimpleNamespace(device=torch.device("cuda", 1), data_ptr=lambda: 4096)
+    work = vb.Workspace.__new__(vb.Workspace)
+    work.buf = buf
+    assert vb.vscan_check(work) == vb.OK and asked == [(4096, 22)]
