@@ -405,7 +405,7 @@ vscan_status vscan_rope(const vscan_rope_desc* desc, void* stream);
  *
  * A cache is a pool of num_blocks blocks; a block holds block_size consecutive tokens of one sequence:
  *   k_cache, v_cache  [num_blocks][kv_heads][block_size][head_dim] of `kv_dtype` (one byte an element)
- *   k_scale, v_scale  [num_blocks][kv_heads] float32; an element stands for code * scale
+ *   k_scale, v_scale  [num_blocks][kv_heads] float32, not negative; an element stands for code * scale
  *   block_table       [batch][max_blocks] int32: block of tokens [j * block_size, (j + 1) * block_size) of a sequence
  *   kv_len            [batch] int32: tokens of each sequence, the new ones of this step included
  *   row_offset        [batch + 1] int32, from 0, not falling: sequence b has n_b = row_offset[b + 1] - row_offset[b] new
@@ -498,7 +498,8 @@ vscan_status vscan_kv_write(const vscan_kv_write_desc* desc, void* stream);
  *             and the workspace are chosen from it.
  * Rows that no sequence owns are left as they were.  Elements of out, and of lse, must not overlap each other.  Tokens behind the table's last column, and tokens in blocks whose
  * table entry is not in [0, num_blocks), count as not there; vscan_check then gives VSCAN_ERR_INVALID_ARG.
- * Scores, softmax statistics and sums are float32.
+ * Scores, softmax statistics and sums are float32.  For float32 queries so are the weights; for bf16 queries they are rounded to
+ * float16 (2^-11 relative, down to 2^-22 of the row's largest product of weight and V scale) before they meet V.
  * Workspace: vscan_kv_attention_workspace_bytes(desc), which reads the sizes only.  Calls that may run at the same time (on
  * two streams, or in two graphs) need a workspace each.
  * Limits of this build: q_heads / kv_heads <= 64; batch <= 8192; max_blocks * block_size and rows * q_heads <= 2^31 - 4096.

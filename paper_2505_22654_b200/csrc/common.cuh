@@ -73,7 +73,6 @@ inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline size_t dtype_bytes(int dtype) { return dtype == VSCAN_F32 ? 4 : 2; }
 
-// [a, a+na) and [b, b+nb) intersect?
 // Whether `dims` steps of n[i] elements each, st[i] apart, keep runs of `covered` elements off each other: ordered by step, each
 // has to step over what the smaller ones cover
 inline bool strides_apart(const int64_t* steps, const int64_t* sizes, int dims, int64_t covered) {
@@ -92,6 +91,7 @@ inline bool strides_apart(const int64_t* steps, const int64_t* sizes, int dims, 
   }
   return true;
 }
+// [a, a+na) and [b, b+nb) intersect?
 inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   if (!a || !b || na == 0 || nb == 0) return false;
   uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);

@@ -294,9 +294,9 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// A warp's wait for the first scores of a piece.  A tile that has no rows in the piece before waits for all of that, which is
-// as long as the sequence: the limit of the other waits (tens of thousands of steps) is granted once more for every 2^17 tokens
-// that a table has room for.  If another role gives up, so does this wait.
+// A warp's wait for the first scores of a piece.  A tile that has no rows in the pieces before waits for all of those: the limit of
+// the other waits, 4 s or some two million steps, is granted once more for every 2^17 tokens that a table has room for.  If another
+// role gives up, so does this wait.
 __device__ __noinline__ bool wait_scores(uint64_t* bar, uint32_t parity, int more, volatile int* abort_flag) {
   bool got = false;
   for (int turn = 0; turn <= more && !got && !*abort_flag; ++turn)

@@ -20,7 +20,8 @@ struct Side {
   int heads;
 };
 
-// Division of n < 2^31 by a number that the host knows: a high product, an add and a shift
+// Division of n < 2^31 by a number that the host knows: a high product, an add and a shift (Granlund and Montgomery, "Division by
+// invariant integers using multiplication", 1994)
 struct Divisor {
   unsigned d, m, l;
   void set(unsigned by) {
