@@ -13,7 +13,7 @@ namespace kv {
 // for the scores a lane owns a token, for the weighted sum a lane owns 4 or 8 channels.  Bound by its loads (a lane's key
 // comes 16 bytes at a time, a row of the cache apart from its neighbour's) and by instructions, about four a code for one row.
 // Measured: 256 sequences of 195 to 300 tokens, 32 heads of 128, 522 MB: 302 us, 1.7 TB/s; 4 of 9,000 to 16,500 tokens, 28 / 4
-// heads, 44 MB: 78 us.  Keys kept in L1 for their second half: 290 and 89 us.
+// heads, 44 MB: 78 us.  Keys kept in L1 for their second half: 290 and 89 us.  2 x 200 new rows behind 4,000 tokens, 28 / 4 heads: 1.27 ms.
 constexpr int kFmaThreads = 128;
 constexpr int kFmaWarps = kFmaThreads / 32;
 
