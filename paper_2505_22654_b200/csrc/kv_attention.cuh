@@ -171,13 +171,14 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// The V scale of a block, in the reference of a row and in the exponent of its weights, which are 2^8 where a token is the
-// reference.  vscan_kv_write makes scales of 2^-48 .. 2^48.  Tokens of a scale of 0 count in the denominator alone: 40 binades
-// lower in the weights than in the reference, they are below 2^-25 and 0 in f16, and far from 0 in the float32 sum.  NaN stays NaN.
+// bf16 queries: the V scale of a block is part of the exponent of its weights, which are 2^8 where a token is the reference of its row.
+// vscan_kv_write makes scales of 2^-48 .. 2^48.  A block may hold a scale far above what is left in it (its large tokens were taken
+// back), so the reference comes down again behind it: once the scales that a row sees are more than kFollow binades lower, to the
+// largest that it has been less the scale then, plus the scale now.  With scales held between 2^-30 and 2^30 for that, it is never
+// more than 60 binades below what it has been, and the sums keep inside float32.
 constexpr float kWeightShift = 8.f;
 constexpr float kWeightScale = 256.f;
-__device__ __forceinline__ float value_exponent(float s) { return s < 0x1p-126f ? -32.f : __log2f(s); }
-__device__ __forceinline__ float weight_exponent(float s) { return (s < 0x1p-126f ? -72.f : __log2f(s)) + kWeightShift; }
+constexpr int kFollow = 3;
 
 // log of l 2^m.  Where V scales are part of m, l makes up for them: a whole number is moved from m to l, so that two large
 // numbers of opposite sign are not rounded before their sum is taken

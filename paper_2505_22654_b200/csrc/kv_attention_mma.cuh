@@ -12,9 +12,9 @@
 // Roundings: codes are exact in f16; a query row is scaled by a power of two to 2^14 .. 2^15 at its largest element, so that
 // its f16 form is exact down to 2^-28 of it; weights are rounded to f16: 2^-11 relative, down to 2^-22 of the largest one.  The block's
 // V scale is part of a weight's exponent (and is taken off again for the denominator), so that this is the largest of what adds to
-// the result, not of the softmax alone, and no sum has to follow the scales.  Scores, references, denominators and sums are float32.
+// the result, not of the softmax alone.  A scale of 0 makes its codes 0.  Scores, references, denominators and sums are float32.
 //
-// Measured: 256 sequences of 195 to 300 tokens, 32 heads of 128, 522 MB: 113 us, 4.6 TB/s, issue slots 44 % and ALU 42 % busy; 4
+// Measured: 256 sequences of 195 to 300 tokens, 32 heads of 128, 522 MB: 115 us, 4.5 TB/s, issue slots 44 % and ALU 42 % busy; 4
 // sequences of 9,000 to 16,500 tokens, 4 KV heads, 44 MB: 23 us and 5 for the join.  Four CTAs of four warps an SM, 4 KB a warp on
 // their way.  Codes through shared memory, three steps deep: 139 us where each lane copies its own, 108 us by bulk copies, which
 // took 10 % longer for few long sequences and 15 % for tiny ones.  Division in units of 16 tokens instead of 64: 112 us, but half
@@ -29,6 +29,8 @@ namespace kv {
 constexpr int kMmaThreads = 128;
 constexpr float kLazy = 6.f;          // a running maximum is raised when a score is over it by this many binades: weights up to 2^6 times
                                       // kWeightScale, 2^14 in f16
+
+__device__ __forceinline__ float follow_bounds(float binade) { return fminf(fmaxf(binade, -30.f), 30.f); }
 
 __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -77,6 +79,8 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
   float* m_sh = o_sh + 4 * R * DP;
   float* l_sh = m_sh + 4 * R;
   __shared__ ScheduleShared sched;
+  __shared__ float peaks[NT][2][kMmaThreads];         // of each lane's rows: the largest that the reference has been, less the scales that it
+                                                      // stood for
   __shared__ Stretch stretches[kMmaThreads / 32];     // of each warp: too much for its registers
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const int D = FULL ? DP : p.head_dim;
@@ -279,6 +283,10 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[i][nt][k] = 0.f;
 
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) peaks[nt][0][threadIdx.x] = peaks[nt][1][threadIdx.x] = -INFINITY;
+    float low = -1000.f;                // kFollow below the V scales that the references stand for; a scale of 0 is below that always
+
     for (int t0 = t_first; t0 < stop; t0 += t_stride) {
       // ---- scores
       float x[MT][NT][4];
@@ -332,12 +340,16 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
       load_k(t1);
       load_table(t1 + t_stride, blk_next);
 
-      // ---- references, largest sums of a score and its V scale's exponent: raised only when one is well over them, so that the
-      // sums are seldom rescaled
+      // ---- references, largest sums of a score and its V scale's exponent: raised only when one is well over them, lowered only when
+      // the scales come down, so that the sums are seldom rescaled
       float lv[MT];
       bool over = false;
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) lv[mt] = value_exponent(vs_now[mt]);
+      for (int mt = 0; mt < MT; ++mt) {
+        lv[mt] = __log2f(vs_now[mt]);
+        low = fmaxf(low, lv[mt] - kFollow);
+        over = over || lv[mt] < low;                    // (so is the scale 0)
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -345,17 +357,35 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) over = over || fmaxf(x[mt][nt][k], x[mt][nt][k + 2]) + lv[mt] > m[nt][k] + kLazy;
       if (__any_sync(0xffffffffu, over)) {
+        bool down = false;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          if (lv[mt] == -INFINITY) {      // a scale of 0: no value, whatever the codes are; the tokens count in the denominator
+            lv[mt] = -48.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int w = 0; w < kVWords; ++w) vraw[mt][k][w] = 0;
+          }
+          if (there[mt] && lv[mt] < low) {
+            low = lv[mt] - kFollow;
+            down = true;
+          }
+        }
+        const float binade = follow_bounds(low + kFollow);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            float top = m[nt][k];
+            float& peak = peaks[nt][k][threadIdx.x];
+            float top = down ? fminf(m[nt][k], peak + binade) : m[nt][k];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) top = fmaxf(top, fmaxf(x[mt][nt][k], x[mt][nt][k + 2]) + lv[mt]);
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
             const float f = top == -INFINITY ? 1.f : ex2(m[nt][k] - top);
             m[nt][k] = top;
+            peak = fmaxf(peak, top - binade);
             l[nt][k] *= f;
 #pragma unroll
             for (int i = 0; i < KS; ++i) { o[i][nt][k] *= f; o[i][nt][k + 2] *= f; }
@@ -364,7 +394,7 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 || NT > 1 ? 2 : 4) mma_
       // ---- weights, and their sums with the values
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        const float up = weight_exponent(vs_now[mt]), down = ex2(-up);
+        const float up = lv[mt] + kWeightShift, down = ex2(-up);
         uint32_t pb[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {

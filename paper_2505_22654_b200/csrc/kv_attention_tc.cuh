@@ -14,9 +14,10 @@
 //
 // Roundings: queries exact in f16 but for a power of two; weights in f16, all else float32.  The V scale of a token's block is part of
 // its weight's exponent, and a row's reference is the largest sum of score and scale that the row has seen, so what a row loses
-// below the smallest step of f16 is small beside its own result, whatever the scales of blocks are that it does not see.  The
-// denominator takes the scale off again.  Per element of S: one fused multiply-add, one exponential, one add, one
-// multiply, half a conversion; 16 exponentials a cycle and SM take as long as the products at the tensor cores' rate.
+// below the smallest step of f16 is small beside its own result, whatever the scales of blocks are that it does not see.  Behind
+// a step of larger scales the reference comes down by what the scales do.  The denominator takes the scale off again.
+// Per element of S: one fused multiply-add, one exponential, one add, one multiply, half a conversion; 16 exponentials a cycle and SM
+// take as long as the products at the tensor cores' rate.
 // Measured: 2 x 900 to 1,024 new rows x 28 heads behind 15,000 to 16,384 tokens, 448 GFLOP: 677 us, 662 TFLOP/s (tensor pipe 36 %,
 // issue slots 54 %, ALU 41 % busy), and 20 us for the join.  At 72 registers a thread, what 800 threads can have, the compiler keeps
 // about 40 words of a thread in local memory.
@@ -295,6 +296,17 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// The V scale of a block, in the reference of a row and in the exponent of its weights.  Tokens of a scale of 0 count in the
+// denominator alone: 40 binades lower in the weights than in the reference, they are below 2^-25 and 0 in f16, and far from 0 in the
+// float32 sum.  NaN stays NaN.
+__device__ __forceinline__ float value_exponent(float s) { return s < 0x1p-126f ? -32.f : __log2f(s); }
+__device__ __forceinline__ float weight_exponent(float s) { return (s < 0x1p-126f ? -72.f : __log2f(s)) + kWeightShift; }
+// Its binade, held within what a reference follows; kNoScale where it is 0 or NaN
+constexpr int kNoScale = -1000;
+__device__ __forceinline__ int scale_binade(float s) {
+  return s > 0.f ? min(max(static_cast<int>(__float_as_uint(s) >> 23) - 127, -30), 30) : kNoScale;
+}
+
 // A warp's wait for the first scores of a piece.  A tile that has no rows in the pieces before waits for all of those: the limit of
 // the other waits, 4 s or some two million steps, is granted once more for every 2^17 tokens that a table has room for.  If another
 // role gives up, so does this wait.
@@ -425,6 +437,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
 
       // m: the row's reference, a score plus its V scale's logarithm; weights are 2^8 at it, l in units of 2^m
       float m = -INFINITY, l = 0.f;
+      float peak = -INFINITY;  // the largest that m has been, less the scales that it stood for
+      int binade = -30;        // of the V scales that m stands for
       for (int j = 0; j < steps && ok; ++j, ++n_it, ++step) {
         const int slot = step & (kTcRing - 1);
         ok = mbar_wait_warp(&sh.scale_full[slot], (step / kTcRing) & 1, abort_flag);
@@ -473,11 +487,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         }
         top = fmaxf(top, swap(top));
         if (!ok) break;
+        // ---- the largest V scale that this row sees in the step: its groups are the first ones.  (Taken here rather than beside the other
+        // scales: one register less over the scores, 682 us against 688.)
+        int up_to = scale_binade(sh.vs[slot][lane & 7]);
+        const int groups = min(max(seen - (pc.u0 + j) * kTcKeys + 15, 0) >> 4, 8);
+        if (__all_sync(0xffffffffu, groups == 8)) {
+          up_to = __reduce_max_sync(0xffffffffu, up_to);
+        } else {
+#pragma unroll
+          for (int off = 1; off < 8; off <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, up_to, off, 8);
+            if ((lane & 7) >= off) up_to = max(up_to, x);
+          }
+          up_to = __shfl_sync(0xffffffffu, up_to, max(groups - 1, 0));
+          if (groups == 0) up_to = kNoScale;
+        }
         // ---- a new reference rescales the sums, which is rare.  Both threads of a row decide alike.
         float f = 1.f;
-        if (__any_sync(0xffffffffu, top > m + kLazy)) {
-          const float now = fmaxf(m, top);
+        binade = max(binade, up_to);
+        const bool down = static_cast<unsigned>(binade - up_to - kFollow - 1) < 128u;       // and there is such a scale
+        if (__any_sync(0xffffffffu, top > m + kLazy || down)) {
+          if (down) binade = up_to;
+          const float now = fmaxf(down ? fminf(m, peak + static_cast<float>(binade)) : m, top);
           f = now == -INFINITY ? 1.f : ex2(m - now);
+          peak = fmaxf(peak, now - static_cast<float>(binade));
           m = now;
           l *= f;
         }

@@ -1,6 +1,6 @@
 """vscan_kv_attention at the edges of its numbers, against the float64 oracle and for every kernel the calls choose from: scores
 whose factor vanishes (scale 0, query rows and keys of zeros, negative scale) over partly masked 16-token groups; values of
-neighbouring blocks many binades apart; warps that run through many short sequences, and what they report; the cache's workspace and what it does where a
+neighbouring blocks many binades apart, and scales far above what a block holds; warps that run through many short sequences, and what they report; the cache's workspace and what it does where a
 tensor is refused; queries and keys that are views of one buffer.
 
 Tolerances as derived in test_gpu_cache_ops.py, and beside the tests that have their own.
@@ -273,3 +273,59 @@ def test_survivors_that_a_cache_does_not_take_leave_it_as_it_was():
     with pytest.raises(ValueError):
         red.cache_survivors(cache)
     assert cache.kv_len.tolist() == [0, 0] and cache.row_offset.tolist() == [0, 0, 0]
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+@pytest.mark.parametrize("dtype,hq,H,d,new", [("bf16", 2, 2, 64, 1), ("bf16", 4, 1, 128, 2), ("bf16", 4, 1, 256, 1), ("bf16", 4, 2, 64, 60), ("bf16", 2, 1, 128, 300),
+                                                ("f32", 2, 2, 64, 3)])
+@pytest.mark.parametrize("over", [12, 25, 50])
+@pytest.mark.parametrize("q_gain", [0.1, 3.0])
+def test_attention_beside_blocks_whose_scale_is_far_above_what_they_hold(kv, dtype, hq, H, d, new, over, q_gain):
+    """A block keeps the scale of large tokens that were taken back. Every third block (many rows: every third step of 128 keys) has
+    codes of 0 under a scale 2^over times the others'; what the other blocks add keeps the precision that it has without them."""
+    T, bs, g = 700, 16, gen(over + new)
+    few = new * (hq // H) <= 16
+    k, v = torch.randn((T, H, d), generator=g).to(DT[dtype]), torch.randn((T, H, d), generator=g).to(DT[dtype])
+    v *= 2.0 ** -20 if over == 50 else 1.0
+    stale = [j for j in range(T // bs) if (j % 3 == 1 if few or dtype == "f32" else j // 8 % 3 == 1)]
+    for j in stale:
+        v[j * bs:(j + 1) * bs] = 0
+    c, table = _written(kv, H, bs, d, [T], [k], [v])
+    high = float(c.scale[1][table[0][0]].max()) * 2.0 ** over
+    at = [table[0][j] for j in stale]
+    c.scale[1][at], c.dev_scale[1][at] = high, high
+    q = (q_gain * torch.randn((new, hq, d), generator=g)).to(DT[dtype])
+    out = vs.vscan_kv_attention(q.cuda(), i32([T]), i32([0, new]), i32(table), *c.arrays, d ** -0.5, max_q_len=new).double().cpu().numpy()
+    (kk, there), (vv, _) = (co.gather(c.codes[i], c.scale[i], table[0], T, bs, KV[kv][0]) for i in range(2))
+    ref, _, weight, reach = co.attention(q.double().numpy(), kk, vv, there, d ** -0.5, True, T - new)
+    err, tol = np.abs(out - ref), attend_tol(dtype, d, T, ref, weight, reach, vv)
+    assert (err <= tol).all(), (float((err / tol).max()), np.argwhere(err > tol)[:4])
+
+
+@pytest.mark.parametrize("dtype,new,batch", [("bf16", 1, 2400), ("bf16", 20, 160), ("f32", 1, 600)])
+@pytest.mark.parametrize("over", [25, 50])
+def test_attention_of_scales_that_come_and_go_while_scores_fall(dtype, new, batch, over):
+    """Stretches of 128 keys, values of 1 and stale blocks (codes of 0 under a scale 2^over times the others') in turn, each 20 below the one
+    before in score: the first stretch has all the weight, and what follows must not move its sums out of float32.  Many sequences read the same blocks,
+    so that none is cut into short pieces."""
+    H, d, bs, run, turns, g = 1, 16, 16, 128, 12, gen(over)
+    T = 2 * run * turns
+    k, v = torch.zeros((T, H, d)), torch.ones((T, H, d)) + torch.rand((T, H, d), generator=g)
+    k[:, 0, 0] = -20.0 * (torch.arange(T) // run)
+    v *= 2.0 ** -20 if over == 50 else 1.0
+    stale = [j for j in range(T // bs) if j // 8 % 2 == 1]
+    for j in stale:
+        v[j * bs:(j + 1) * bs] = 0
+    c, table = _written("e4m3", H, bs, d, [T], [k.to(DT[dtype])], [v.to(DT[dtype])])
+    at = [table[0][j] for j in stale]
+    high = float(c.scale[1][table[0][0]].max()) * 2.0 ** over
+    c.scale[1][at], c.dev_scale[1][at] = high, high
+    q = torch.zeros((batch * new, H, d), dtype=DT[dtype])
+    q[..., 0] = 1.0
+    out, lse = torch.zeros_like(q).cuda(), torch.zeros((batch * new, H), device="cuda")
+    vs.vscan_kv_attention(q.cuda(), i32([T] * batch), i32(np.arange(batch + 1) * new), i32(table * batch), *c.arrays, 1.0, max_q_len=new, causal=False,
+                          out=out, lse=lse)
+    (kk, there), (vv, _) = (co.gather(c.codes[i], c.scale[i], table[0], T, bs, co.E4M3) for i in range(2))
+    ref, ref_lse, weight, reach = co.attention(q[:1].double().numpy(), kk, vv, there, 1.0, False, 0)
+    tol = attend_tol(dtype, d, T, ref, weight, np.full_like(reach, 20.0), vv)
+    assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all() and (np.abs(lse.double().cpu().numpy() - ref_lse) <= 1e-4).all()
