@@ -14,7 +14,7 @@
 // V scale is part of a weight's exponent (and is taken off again for the denominator), so that this is the largest of what adds to
 // the result, not of the softmax alone.  A scale of 0 makes its codes 0.  Scores, references, denominators and sums are float32.
 //
-// Measured: 256 sequences of 195 to 300 tokens, 32 heads of 128, 522 MB: 115 us, 4.5 TB/s, issue slots 44 % and ALU 42 % busy; 4
+// Measured: 256 sequences of 195 to 300 tokens, 32 heads of 128, 522 MB: 115 us, 4.5 TB/s, issue slots 43 % and ALU 42 % busy; 4
 // sequences of 9,000 to 16,500 tokens, 4 KV heads, 44 MB: 23 us and 5 for the join.  Four CTAs of four warps an SM, 4 KB a warp on
 // their way.  Codes through shared memory, three steps deep: 139 us where each lane copies its own, 108 us by bulk copies, which
 // took 10 % longer for few long sequences and 15 % for tiny ones.  Division in units of 16 tokens instead of 64: 112 us, but half

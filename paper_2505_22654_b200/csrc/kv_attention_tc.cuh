@@ -18,7 +18,7 @@
 // a step of larger scales the reference comes down by what the scales do.  The denominator takes the scale off again.
 // Per element of S: one fused multiply-add, one exponential, one add, one multiply, half a conversion; 16 exponentials a cycle and SM
 // take as long as the products at the tensor cores' rate.
-// Measured: 2 x 900 to 1,024 new rows x 28 heads behind 15,000 to 16,384 tokens, 448 GFLOP: 677 us, 662 TFLOP/s (tensor pipe 36 %,
+// Measured: 2 x 900 to 1,024 new rows x 28 heads behind 15,000 to 16,384 tokens, 448 GFLOP: 672 us, 667 TFLOP/s (tensor pipe 35 %,
 // issue slots 54 %, ALU 41 % busy), and 20 us for the join.  At 72 registers a thread, what 800 threads can have, the compiler keeps
 // about 40 words of a thread in local memory.
 // Every wait is bounded; on expiry the CTA says so in its flag word, frees its tensor memory and returns.
