@@ -15,6 +15,9 @@
  *     vscan_kv_plan                 block tables, slot maps and offsets of a paged KV cache from request lengths
  *     vscan_kv_write                K / V rows into a cache held in 8 bits with a scale per block of tokens and head
  *     vscan_kv_attention            attention over that cache
+ *     vscan_attention               attention over whole prompts, K and V in the model's own type
+ *     vscan_kv_weigh                attention weights gathered for each cached token
+ *     vscan_kv_evict                the tokens that gathered least leave the cache
  *
  * Conventions shared by every entry point
  *   - Returns a vscan_status.  Nothing throws, aborts or traps.  Arguments are validated on the
@@ -527,10 +530,122 @@ size_t vscan_kv_attention_workspace_bytes(const vscan_kv_attention_desc* desc);
 vscan_status vscan_kv_attention(const vscan_kv_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * vscan_attention: out = softmax(scale * q K^T) V with K and V in the type of the queries: whole prompts of a decoder, layers of a vision
+ * encoder, new rows behind keys that the caller still holds.  Query head h reads KV head floor(h * kv_heads / q_heads).
+ *   row_offset [batch + 1] int32, from 0, not falling: sequence b has n_b = row_offset[b + 1] - row_offset[b] query rows
+ *   kv_offset  optional [batch + 1] int32, likewise for keys: m_b.  NULL: row_offset serves both
+ *   causal != 0: row i of the n_b stands at m_b - n_b + i and sees the keys up to itself; else every row sees all m_b.  A row
+ *   that sees nothing gives 0 (and lse -inf).  What lies in keys and values that a row does not see never reaches it, infinities and
+ *   NaN included.
+ *   q, out    rows of q_heads x head_dim, k, v rows of kv_heads x head_dim, all of `dtype`, packed or padded as described at the
+ *             paged cache: element (row, h, c) at (offset[b] + i) * stride[2] + h * stride[1] + c, or b * stride[0] + i * stride[2] +
+ *             h * stride[1] + c; `rows` and `kv_rows` are those of the whole buffer, or per sequence
+ *   lse       optional float32 output: log of the sum of exp(scale * q k) over the keys seen, by lse_stride
+ *   max_q_len no sequence has more query rows than this (rows behind it are left as they were)
+ * Rows and keys that lie outside the buffers are not there.  Rows that no sequence owns are left as they were.  Elements of out, and
+ * of lse, must not overlap each other.
+ * Scores, softmax statistics and sums are float32; for bf16 the weights are rounded to bf16 before they meet V.
+ * Workspace: vscan_attention_workspace_bytes(desc), which reads the sizes only.  Calls that may run at the same time (on two streams,
+ * or in two graphs) need a workspace each.
+ * head_dim: a multiple of 8, at most 256; strides multiples of 16 bytes.  Limits of this build: q_heads / kv_heads <= 64; batch <= 8192;
+ * rows * q_heads and kv_rows <= 2^31 - 4096.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype; /* vscan_dtype */
+  int32_t batch, q_heads, kv_heads, head_dim, rows, kv_rows, padded, max_q_len, causal;
+  float scale;
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  float* lse;
+  int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3], lse_stride[3]; /* sequence (padded only), head, row */
+  const int32_t* row_offset;
+  const int32_t* kv_offset;
+} vscan_attention_desc;
+
+size_t vscan_attention_workspace_bytes(const vscan_attention_desc* desc);
+vscan_status vscan_attention(const vscan_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * vscan_kv_weigh: how much attention each cached token has been given, gathered step by step.
+ *   weight    [num_blocks][kv_heads][block_size] float32, in and out.  For token t of a sequence with new rows, KV head g:
+ *               weight = (t < kv_len - n_b ? decay * weight : 0) + sum of exp(scale * q[i][h] . k[t][g] - lse[i][h])
+ *             over the last `window` of the n_b new rows i and the heads h of g, as far as they see t (`causal` as in
+ *             vscan_kv_attention).  A token that is new in this step starts from 0 whatever its place held; from then on every step that
+ *             writes tokens is followed by this call.  A sequence without new rows keeps its weights.
+ *   q, lse    of the new rows, in the layouts of vscan_kv_attention: what that call took and gave, or vscan_attention.  A row whose
+ *             lse is -inf sees nothing and gives nothing.
+ *   max_q_len no sequence has more new rows than this (rows behind it are not there; the launch is chosen from it)
+ * Tokens in blocks whose table entry is not in [0, num_blocks), and behind the table's last column, are passed over.  Sums are float32,
+ * in a fixed order.  No two sequences may hold the same block.  No workspace.  Limits as for vscan_kv_attention.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype;    /* vscan_dtype of q */
+  int32_t kv_dtype; /* vscan_kv_dtype */
+  int32_t batch, q_heads, kv_heads, head_dim, block_size, num_blocks, max_blocks, rows, padded;
+  int32_t max_q_len, window, causal;
+  float scale, decay;
+  const void* q;
+  const float* lse;
+  int64_t q_stride[3], lse_stride[3]; /* sequence (padded only), head, row */
+  const int32_t* kv_len;
+  const int32_t* row_offset;
+  const int32_t* block_table;
+  const void* k_cache;
+  const float* k_scale;
+  float* weight;
+} vscan_kv_weigh_desc;
+
+vscan_status vscan_kv_weigh(const vscan_kv_weigh_desc* desc, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * vscan_kv_evict: of each sequence the min(budget, kv_len) tokens that rank highest stay, the others leave the cache.
+ *   rank      of token t: above all others if t < keep_first or t >= kv_len - keep_last; else its weight (see vscan_kv_weigh) for the
+ *             KV head (per_head != 0), or the sum of its weights over the heads, taken in 64 bits and rounded to float32, for all heads
+ *             alike.  NaN ranks as -inf.  Equal ranks: the lowest t stays.
+ *   budget    [batch] int32, less than 0 counts as 0; no budget is larger than max_keep (larger ones count as max_keep)
+ * The tokens that stay keep their order and move to the front of the sequence's blocks; a head's own tokens with per_head.  A (block, head)
+ * all of whose tokens stay in their places is left alone; the others are written as vscan_kv_write would write the values into an
+ * empty block: the least scale 2^e, codes rounded once (without loss unless a scale grows).  Places behind the last token that stays hold
+ * what they held or what was moved.
+ *   weight    [num_blocks][kv_heads][block_size] float32
+ *   weight_out optional, like weight: receives the weights of the tokens that stay, in their new places (of every sequence); it may be
+ *             `weight` itself, else it must not overlap it
+ *   kept      optional [batch][heads][max_keep] int32 output (heads = kv_heads with per_head, else 1): the tokens that stay, by their old
+ *             places, ascending; entries behind the last one are left as they were
+ *   delta     [batch] int32 output: minus the number of tokens that left.  This is the new_len that vscan_kv_plan takes next: it
+ *             shortens the sequences and puts their blocks back.  kv_len itself stays as it is.
+ * A sequence whose kv_len is less than 0 or beyond its table, or that has a block whose table entry is not in [0, num_blocks), is left
+ * alone (delta 0, kept and weight_out untouched); vscan_check then gives VSCAN_ERR_INVALID_ARG.  No two sequences may hold the same block.
+ * Workspace: vscan_kv_evict_workspace_bytes(desc), which reads the sizes only; calls that may run at the same time need one each.
+ * Limits of this build: batch <= 8192; kv_heads <= 65535; max_blocks * block_size <= 2^31 - 4096;
+ * batch * kv_heads * (max_keep / block_size + 1) <= 2^28.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t kv_dtype; /* vscan_kv_dtype */
+  int32_t batch, kv_heads, head_dim, block_size, num_blocks, max_blocks, max_keep, keep_first, keep_last, per_head;
+  const int32_t* kv_len;
+  const int32_t* budget;
+  const int32_t* block_table;
+  const float* weight;
+  float* weight_out;
+  void* k_cache;
+  void* v_cache;
+  float* k_scale;
+  float* v_scale;
+  int32_t* kept;
+  int32_t* delta;
+} vscan_kv_evict_desc;
+
+size_t vscan_kv_evict_workspace_bytes(const vscan_kv_evict_desc* desc);
+vscan_status vscan_kv_evict(const vscan_kv_evict_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Housekeeping.
  * vscan_check: synchronises `stream` and reads the device status word at the start of a workspace
  * that the preceding call used; VSCAN_OK, VSCAN_ERR_TIMEOUT (a bounded wait expired),
- * VSCAN_ERR_INVALID_ARG (vscan_kv_attention met a block or a length that is out of range) or VSCAN_ERR_CUDA.  Only calls that take a non-empty workspace write that word.
+ * VSCAN_ERR_INVALID_ARG (vscan_kv_attention or vscan_kv_evict met a block or a length that is out of range) or VSCAN_ERR_CUDA.  Only calls that take a non-empty workspace write that word.
  * vscan_last_cuda_error: cudaError_t value of the last failing runtime call on this thread (0 if none).
  * vscan_kernel_launches: number of kernels this library has launched in this process so far.
  * ------------------------------------------------------------------------------------------- */

@@ -112,6 +112,28 @@ class KvAttentionDesc(C.Structure):
                 ("k_scale", _vp), ("v_scale", _vp)]
 
 
+class AttentionDesc(C.Structure):
+    _fields_ = [("dtype", _i32), ("batch", _i32), ("q_heads", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("rows", _i32), ("kv_rows", _i32),
+                ("padded", _i32), ("max_q_len", _i32), ("causal", _i32), ("scale", _f32), ("q", _vp), ("k", _vp), ("v", _vp), ("out", _vp),
+                ("lse", _vp), ("q_stride", _i64x3), ("k_stride", _i64x3), ("v_stride", _i64x3), ("out_stride", _i64x3), ("lse_stride", _i64x3),
+                ("row_offset", _vp), ("kv_offset", _vp)]
+
+
+class KvWeighDesc(C.Structure):
+    _fields_ = [("dtype", _i32), ("kv_dtype", _i32), ("batch", _i32), ("q_heads", _i32), ("kv_heads", _i32), ("head_dim", _i32),
+                ("block_size", _i32), ("num_blocks", _i32), ("max_blocks", _i32), ("rows", _i32), ("padded", _i32), ("max_q_len", _i32),
+                ("window", _i32), ("causal", _i32), ("scale", _f32), ("decay", _f32), ("q", _vp), ("lse", _vp), ("q_stride", _i64x3),
+                ("lse_stride", _i64x3), ("kv_len", _vp), ("row_offset", _vp), ("block_table", _vp), ("k_cache", _vp), ("k_scale", _vp),
+                ("weight", _vp)]
+
+
+class KvEvictDesc(C.Structure):
+    _fields_ = [("kv_dtype", _i32), ("batch", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("block_size", _i32), ("num_blocks", _i32),
+                ("max_blocks", _i32), ("max_keep", _i32), ("keep_first", _i32), ("keep_last", _i32), ("per_head", _i32), ("kv_len", _vp),
+                ("budget", _vp), ("block_table", _vp), ("weight", _vp), ("weight_out", _vp), ("k_cache", _vp), ("v_cache", _vp), ("k_scale", _vp),
+                ("v_scale", _vp), ("kept", _vp), ("delta", _vp)]
+
+
 class VScanError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -154,6 +176,12 @@ def lib() -> C.CDLL:
         L.vscan_kv_attention_workspace_bytes.restype = C.c_size_t
         L.vscan_kv_attention_workspace_bytes.argtypes = [C.POINTER(KvAttentionDesc)]
         L.vscan_kv_attention.restype, L.vscan_kv_attention.argtypes = _i32, [C.POINTER(KvAttentionDesc), _vp, C.c_size_t, _vp]
+        for name, desc in (("attention", AttentionDesc), ("kv_evict", KvEvictDesc)):
+            ws = getattr(L, f"vscan_{name}_workspace_bytes")
+            ws.restype, ws.argtypes = C.c_size_t, [C.POINTER(desc)]
+            f = getattr(L, f"vscan_{name}")
+            f.restype, f.argtypes = _i32, [C.POINTER(desc), _vp, C.c_size_t, _vp]
+        L.vscan_kv_weigh.restype, L.vscan_kv_weigh.argtypes = _i32, [C.POINTER(KvWeighDesc), _vp]
         L.vscan_score_select.restype = _i32
         L.vscan_score_select.argtypes = [C.POINTER(ScoreSelectDesc), _vp]
         L.vscan_version.restype = _i32
@@ -405,7 +433,8 @@ def _calls():
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
         loader.exec_module(module)
         module.init(*[C.cast(getattr(L, "vscan_" + name), C.c_void_p).value
-                      for name in ("rope", "kv_plan", "kv_write", "kv_attention", "kv_attention_workspace_bytes")])
+                      for name in ("rope", "kv_plan", "kv_write", "kv_attention", "kv_attention_workspace_bytes", "attention",
+                                   "attention_workspace_bytes", "kv_weigh", "kv_evict", "kv_evict_workspace_bytes")])
         _CALLS = module
     return _CALLS
 
@@ -506,6 +535,59 @@ def vscan_kv_attention(q, kv_len, row_offset, block_table, k_cache, v_cache, k_s
     if st != OK:
         raise VScanError(st, "vscan_kv_attention")
     return out
+
+
+def vscan_attention_workspace(q, k, row_offset, max_q_len):
+    """A workspace for vscan_attention calls of these sizes."""
+    return Workspace((_CALLS or _calls()).attention_bytes(q, k, row_offset, max_q_len), q.device)
+
+
+def vscan_attention(q, k, v, row_offset, scale, max_q_len, kv_offset=None, causal=True, out=None, lse=None, workspace=None):
+    """Attention over whole prompts, K and V in the type of the queries (float32 or bfloat16).  Packed: q [rows, Hq, d], k and v [kv_rows,
+    Hkv, d], sequences cut by row_offset and kv_offset [B + 1] int32 (kv_offset None: the same as row_offset).  Padded: q [B, Hq, rows, d], k
+    and v [B, Hkv, kv_rows, d], lengths from the same offsets.  Any strides with a contiguous last dimension.  causal: row i of n stands at
+    keys - n + i and sees the keys up to itself; else it sees all of its sequence.  out (made here, zeroed, if not given) like q; lse, if
+    given, [rows, Hq] or [B, Hq, rows] float32 receives the log of the sum of exponentials.  max_q_len: no sequence has more query
+    rows.  -> out."""
+    if out is None:
+        out = torch.zeros_like(q)
+    if workspace is None:
+        workspace = vscan_attention_workspace(q, k, row_offset, max_q_len)
+    st = (_CALLS or _calls()).attention(q, k, v, row_offset, kv_offset, scale, max_q_len, causal, out, lse, workspace.buf)
+    if st != OK:
+        raise VScanError(st, "vscan_attention")
+    return out
+
+
+def vscan_kv_weigh(q, lse, kv_len, row_offset, block_table, k_cache, k_scale, weight, scale, max_q_len=1, decay=1.0, window=None, causal=True):
+    """Attention weights gathered for each cached token (see include/vscan.h): weight [num_blocks, Hkv, block_size] float32, in place.  q and
+    lse of the step's new rows, as vscan_kv_attention or vscan_attention took and gave them; the last `window` rows of a sequence count
+    (None: all).  Tokens of the step start from 0, older ones from decay * weight."""
+    st = (_CALLS or _calls()).kv_weigh(q, lse, kv_len, row_offset, block_table, k_cache, k_scale, weight, scale, max_q_len, decay, window, causal)
+    if st != OK:
+        raise VScanError(st, "vscan_kv_weigh")
+
+
+def vscan_kv_evict_workspace(block_table, k_cache, max_keep, per_head=True):
+    """A workspace for vscan_kv_evict calls of these sizes."""
+    return Workspace((_CALLS or _calls()).kv_evict_bytes(block_table, k_cache, max_keep, per_head), k_cache.device)
+
+
+def vscan_kv_evict(kv_len, budget, block_table, weight, k_cache, v_cache, k_scale, v_scale, max_keep, keep_first=0, keep_last=0, per_head=True,
+                   weight_out=None, kept=None, delta=None, workspace=None):
+    """Of each sequence the min(budget, kv_len) tokens that rank highest stay (see include/vscan.h): the first keep_first and last keep_last,
+    then those of the largest weight, per KV head or for all heads alike.  The cache is changed in place; no budget counts for more than
+    max_keep.  weight_out (may be weight itself) receives the weights in their new places, kept [B, Hkv or 1, max_keep] int32 the old
+    places.  -> delta [B] int32, the new_len that vscan_kv_plan takes next."""
+    if delta is None:
+        delta = torch.empty_like(kv_len)
+    if workspace is None:
+        workspace = vscan_kv_evict_workspace(block_table, k_cache, max_keep, per_head)
+    st = (_CALLS or _calls()).kv_evict(kv_len, budget, block_table, weight, k_cache, v_cache, k_scale, v_scale, max_keep, keep_first, keep_last,
+                                       per_head, weight_out, kept, delta, workspace.buf)
+    if st != OK:
+        raise VScanError(st, "vscan_kv_evict")
+    return delta
 
 
 # ------------------------------------------------------------------------------------------ ragged batches

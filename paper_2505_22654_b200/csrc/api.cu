@@ -83,9 +83,9 @@ extern "C" vscan_status vscan_check(const void* workspace, void* stream) {
                                  static_cast<cudaStream_t>(stream)));
   VSCAN_CUDA_TRY(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
   if (word & kStatusFlags) {
-    uint32_t flags[1024];
+    uint32_t flags[kMostStatusFlags];
     const uint32_t n = word & ~kStatusFlags;
-    if (n > 1024) return VSCAN_ERR_INVALID_ARG;   // not a status that any call leaves
+    if (n > kMostStatusFlags) return VSCAN_ERR_INVALID_ARG;   // not a status that any call leaves
     VSCAN_CUDA_TRY(cudaMemcpyAsync(flags, static_cast<const char*>(workspace) + kStatusBytes, n * sizeof(uint32_t),
                                    cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream)));
     VSCAN_CUDA_TRY(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));

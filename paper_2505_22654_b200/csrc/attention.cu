@@ -1,0 +1,359 @@
+// vscan_attention: softmax(scale * q K^T) V of packed or padded sequences, K and V in the queries' own type.
+//
+// The division of the work, and the join of what it cuts, are those of the attention over the paged cache: a line of tiles of query
+// rows (new rows x heads of a group, so that a key that was read serves all of them) against steps of keys, in equal stretches.
+#include "attention_division.cuh"
+#include "attention_join.cuh"
+
+#include <type_traits>
+
+namespace vscan {
+namespace kv {
+
+struct PromptParams : AttnParams {
+  const char* k;
+  const char* v;
+  long long k_seq, k_head, k_row, v_seq, v_head, v_row;   // bytes
+  const int32_t* kv_offset;
+  int kv_rows;
+};
+
+// First key row of sequence b in the buffer (padded: 0), and its keys, held inside the buffer
+__device__ __forceinline__ void key_span(const PromptParams& p, int b, int& first, int& n) {
+  const long long lo = p.kv_offset[b], given = max(p.kv_offset[b + 1] - lo, 0ll);
+  first = p.padded ? 0 : static_cast<int>(lo);
+  const long long room = p.padded ? p.kv_rows : lo < 0 ? 0 : max(p.kv_rows - lo, 0ll);
+  n = static_cast<int>(min(given, room));
+}
+
+__device__ __forceinline__ Sequence sequence_at(const PromptParams& p, int b) {
+  Sequence s;
+  const long long lo = p.row_offset[b], given = max(p.row_offset[b + 1] - lo, 0ll);
+  s.first = p.padded ? 0 : static_cast<int>(lo);
+  const long long room = p.padded ? p.rows : lo < 0 ? 0 : max(p.rows - lo, 0ll);
+  s.n = static_cast<int>(min(min(given, room), static_cast<long long>(p.max_q_len)));
+  int first;
+  key_span(p, b, first, s.len);
+  s.start = max(static_cast<long long>(p.kv_offset[b + 1]) - p.kv_offset[b], 0ll) - given;
+  s.tiles = s.units = 0;
+  s.weight = 0;
+  return s;
+}
+
+// ---------------------------------------------------------------------------------------------- products on the CUDA cores
+// float32 queries (no rounding of queries or weights to 16 bits), and bf16 heads of more than 128 channels.  A CTA takes 64 query rows and
+// 64 keys a step; a thread 4 x 4 scores, then 4 rows x DP / 16 channels of the sums.  Keys and weights take turns in one buffer.
+constexpr int kFlatThreads = 256, kFlatRows = 64, kFlatKeys = 64, kFlatWhole = 4;
+using FlatShape = TileShape<kFlatThreads, kFlatRows, kFlatKeys, kFlatWhole>;
+template <int DP>
+constexpr size_t flat_smem() { return (static_cast<size_t>(kFlatRows) * (DP + 4) + static_cast<size_t>(kFlatKeys) * (DP + 4) + static_cast<size_t>(kFlatKeys) * DP) * 4; }
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(PromptParams p) {
+  constexpr int kQ = DP + 4, kP = kFlatKeys + 4, kChunks = DP / 64;
+  static_assert(kP <= kQ, "weights lie over the keys");
+  extern __shared__ __align__(16) float flat_sh[];
+  float* q_sh = flat_sh;                        // [rows][DP + 4]
+  float* k_sh = q_sh + kFlatRows * kQ;          // [keys][DP + 4]; weights [rows][keys + 4]
+  float* v_sh = k_sh + kFlatKeys * kQ;          // [keys][DP]
+  __shared__ DivisionShared division;
+  const int tid = threadIdx.x, x = tid & 15, y = tid >> 4, D = p.head_dim;
+  grid_dependency_wait();
+  TcStretch st = tc_locate<FlatShape>(p, division);
+  if (tid == 0) {
+    if (blockIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = 0; }
+    p.boundary[blockIdx.x].seg1 = 0;
+    p.flags[blockIdx.x] = 0;
+  }
+  TcPiece pc;
+  // Rows of a buffer as floats into shared memory, zeros beyond `there` rows and D channels
+  auto fill = [&](float* dst, int pitch, int there, auto at) {
+    constexpr int kElems = Vec16<T>::kElems, kVecs = DP / kElems;
+    for (int i = tid; i < 64 * kVecs; i += kFlatThreads) {
+      const int r = i / kVecs, c = (i - r * kVecs) * kElems;
+      float f[kElems];
+#pragma unroll
+      for (int j = 0; j < kElems; ++j) f[j] = 0.f;
+      if (r < there && c < D) Vec16<T>::unpack(ld_nc_16(at(r) + c * static_cast<int>(sizeof(T))), f);
+#pragma unroll
+      for (int j = 0; j < kElems; j += 4) *reinterpret_cast<float4*>(dst + r * pitch + c + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+    }
+  };
+  while (tc_next<FlatShape>(p, st, pc)) {
+    const Sequence& s = pc.q.s;
+    if (pc.u0 > 0 && tid == 0) p.boundary[blockIdx.x] = {pc.seg0, pc.seg1, st.quota, pc.b, pc.head, pc.tile, s.first, pc.n_rows, 0};
+    int key0, keys;
+    key_span(p, pc.b, key0, keys);
+    const char* k = p.k + (p.padded ? pc.b * p.k_seq : key0 * p.k_row) + pc.head * p.k_head;
+    const char* v = p.v + (p.padded ? pc.b * p.v_seq : key0 * p.v_row) + pc.head * p.v_head;
+    auto row_of = [&](int r) {
+      const int flat = pc.tile * kFlatRows + r, i = flat / p.group;
+      return RowAt{i, pc.head * p.group + flat - i * p.group};
+    };
+    __syncthreads();                            // the buffers of the piece before are done with
+    fill(q_sh, kQ, pc.n_rows, [&](int r) { return q_at(p, pc.b, s.first, row_of(r)); });
+    int seen[4];
+    float m[4], l[4], o[4][4 * kChunks];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = y * 4 + i;
+      seen[i] = r < pc.n_rows ? visible(p, s, row_of(r).i) : 0;
+      m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4 * kChunks; ++c) o[i][c] = 0.f;
+    }
+    for (int u = pc.u0; u < pc.u1; ++u) {
+      const int t0 = u * kFlatKeys, there = min(pc.most - t0, kFlatKeys);
+      __syncthreads();                          // weights and values of the step before are done with
+      fill(k_sh, kQ, there, [&](int r) { return k + (t0 + r) * p.k_row; });
+      fill(v_sh, DP, there, [&](int r) { return v + (t0 + r) * p.v_row; });
+      __syncthreads();
+      float dot[4][4];                          // rows 4 y + i, keys x + 16 j
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dot[i][j] = 0.f;
+#pragma unroll 4
+      for (int c = 0; c < DP; c += 4) {
+        float4 a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          a[i] = *reinterpret_cast<const float4*>(q_sh + (y * 4 + i) * kQ + c);
+          b[i] = *reinterpret_cast<const float4*>(k_sh + (x + 16 * i) * kQ + c);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            dot[i][j] = fmaf(a[i].x, b[j].x, fmaf(a[i].y, b[j].y, fmaf(a[i].z, b[j].z, fmaf(a[i].w, b[j].w, dot[i][j]))));
+      }
+      __syncthreads();                          // keys are done with: weights take their place
+      float e[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // the factor in two floats and the maximum taken off before the rounding: a weight near 1 is off by the exponential's error and
+        // the dot product's, not by the rounding of a large score
+        float top = m[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool on = t0 + x + 16 * j < seen[i];
+          if (on) top = fmaxf(top, fmaf(dot[i][j], p.scale_log2e, dot[i][j] * p.scale_rest));
+        }
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        const float base = top == -INFINITY ? 0.f : top, f = ex2(m[i] - base);
+        if (top != m[i]) {
+          l[i] *= f;
+#pragma unroll
+          for (int c = 0; c < 4 * kChunks; ++c) o[i][c] *= f;
+          m[i] = top;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool on = t0 + x + 16 * j < seen[i];
+          e[i][j] = on ? ex2(fmaf(dot[i][j], p.scale_log2e, fmaf(dot[i][j], p.scale_rest, -base))) : 0.f;
+          l[i] += e[i][j];
+          k_sh[(y * 4 + i) * kP + x + 16 * j] = e[i][j];
+        }
+      }
+      __syncthreads();
+      // a row's own keys only: what lies in the others may be infinite
+      const int fewest = min(min(seen[0], seen[1]), min(seen[2], seen[3])) - t0;
+      auto add = [&](auto masked) {
+#pragma unroll 2
+        for (int t = 0; t < there; t += 4) {
+          float w[4][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 f = *reinterpret_cast<const float4*>(k_sh + (y * 4 + i) * kP + t);
+            w[i][0] = f.x; w[i][1] = f.y; w[i][2] = f.z; w[i][3] = f.w;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+              const float4 f = *reinterpret_cast<const float4*>(v_sh + (t + j) * DP + c * 64 + x * 4);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                if (decltype(masked)::value && t0 + t + j >= seen[i]) continue;
+                o[i][4 * c] = fmaf(w[i][j], f.x, o[i][4 * c]);
+                o[i][4 * c + 1] = fmaf(w[i][j], f.y, o[i][4 * c + 1]);
+                o[i][4 * c + 2] = fmaf(w[i][j], f.z, o[i][4 * c + 2]);
+                o[i][4 * c + 3] = fmaf(w[i][j], f.w, o[i][4 * c + 3]);
+              }
+            }
+        }
+      };
+      if (fewest >= there) add(std::false_type{});
+      else add(std::true_type{});
+    }
+    const bool complete = pc.u0 == 0 && pc.u1 == pc.units;
+    float* part = p.partial + (static_cast<size_t>(blockIdx.x) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(kFlatRows, D);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float sum = l[i];
+#pragma unroll
+      for (int off = 1; off < 16; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      const int r = y * 4 + i;
+      if (r >= pc.n_rows) continue;
+      const RowAt at = row_of(r);
+      char* out = out_at(p, pc.b, s.first, at);
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        const int ch = c * 64 + x * 4;
+        if (ch >= D) continue;
+        if (complete) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) store_out<T>(out, ch + j, sum == 0.f ? 0.f : o[i][4 * c + j] / sum);
+        } else {
+          *reinterpret_cast<float4*>(part + static_cast<size_t>(r) * D + ch) = make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
+        }
+      }
+      if (x == 0) {
+        if (!complete) { part[kFlatRows * D + r] = m[i]; part[kFlatRows * D + kFlatRows + r] = sum; }
+        else if (p.lse) *lse_at(p, pc.b, s.first, at) = sum == 0.f ? -INFINITY : (m[i] + log2f(sum)) * 0.69314718055994531f;
+      }
+    }
+  }
+  grid_dependency_launch();
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+constexpr int64_t kMostRows = 0x7ffff000;   // a step or a tile more still fits 32 bits
+
+static vscan_status validate_prompt(const vscan_attention_desc* d) {
+  if (!d) return VSCAN_ERR_INVALID_ARG;
+  if (d->dtype != VSCAN_F32 && d->dtype != VSCAN_BF16) return VSCAN_ERR_INVALID_ARG;
+  if (d->batch < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || d->q_heads % d->kv_heads || d->head_dim <= 0 || d->head_dim % 8 || d->rows < 0 ||
+      d->kv_rows < 0 || d->max_q_len < 0)
+    return VSCAN_ERR_INVALID_ARG;
+  if (d->scale - d->scale != 0.f) return VSCAN_ERR_INVALID_ARG;
+  if (d->batch == 0 || d->rows == 0 || d->max_q_len == 0) return VSCAN_OK;
+  if (!d->q || !d->out || !d->row_offset || (d->kv_rows > 0 && (!d->k || !d->v))) return VSCAN_ERR_INVALID_ARG;
+  if (d->head_dim > 256 || d->q_heads / d->kv_heads > 64 || d->batch > kMaxBatch || d->kv_heads > 65535 ||
+      static_cast<int64_t>(d->rows) * d->q_heads > kMostRows || d->kv_rows > kMostRows)
+    return VSCAN_ERR_UNSUPPORTED;
+  const size_t e = dtype_bytes(d->dtype), B = d->batch;
+  const bool padded = d->padded != 0;
+  if (!strides_ok(d->q_stride, e, padded) || !strides_ok(d->out_stride, e, padded) || !strides_ok(d->k_stride, e, padded) ||
+      !strides_ok(d->v_stride, e, padded))
+    return VSCAN_ERR_INVALID_ARG;
+  if (d->lse)
+    for (int i = padded ? 0 : 1; i < 3; ++i)
+      if (d->lse_stride[i] < 0 || d->lse_stride[i] > (int64_t{1} << 40)) return VSCAN_ERR_INVALID_ARG;
+  const int64_t sizes[3] = {padded ? d->batch : 1, d->q_heads, d->rows};
+  if (!strides_apart(d->out_stride, sizes, 3, d->head_dim) || (d->lse && !strides_apart(d->lse_stride, sizes, 3, 1))) return VSCAN_ERR_INVALID_ARG;
+  struct Rng { const void* p; size_t n; };
+  const Rng all[] = {{d->q, rows_extent(d->q_stride, B, d->q_heads, d->rows, d->head_dim, e, padded)},
+                     {d->k, rows_extent(d->k_stride, B, d->kv_heads, d->kv_rows, d->head_dim, e, padded)},
+                     {d->v, rows_extent(d->v_stride, B, d->kv_heads, d->kv_rows, d->head_dim, e, padded)},
+                     {d->row_offset, (B + 1) * 4}, {d->kv_offset, (B + 1) * 4},
+                     {d->out, rows_extent(d->out_stride, B, d->q_heads, d->rows, d->head_dim, e, padded)},
+                     {d->lse, d->lse ? rows_extent(d->lse_stride, B, d->q_heads, d->rows, 1, 4, padded) : 0}};
+  constexpr int kInputs = 5, kAll = 7;
+  for (const Rng& r : all)
+    if (r.p && !aligned16(r.p)) return VSCAN_ERR_INVALID_ARG;
+  for (int o = kInputs; o < kAll; ++o)
+    for (int i = 0; i < o; ++i)
+      if (overlaps(all[o].p, all[o].n, all[i].p, all[i].n)) return VSCAN_ERR_INVALID_ARG;
+  return VSCAN_OK;
+}
+
+// Rows of a tile, keys of a step, CTAs of the launch
+struct PromptPlan { int tile_rows, keys; unsigned ctas; };
+
+static PromptPlan plan_prompt(const vscan_attention_desc* d) {
+  PromptPlan pl;
+  const int group = d->q_heads / d->kv_heads;
+  pl.tile_rows = kFlatRows;
+  pl.keys = kFlatKeys;
+  const int64_t resident = d->head_dim > 128 ? 1 : 2;
+  // as many CTAs as fit the SMs at once, no more than there can be steps
+  const int64_t rows = d->padded ? static_cast<int64_t>(d->batch) * (d->rows < d->max_q_len ? d->rows : d->max_q_len) : d->rows;
+  const int64_t tiles = rows * group / pl.tile_rows + d->batch, steps = (static_cast<int64_t>(d->kv_rows) + pl.keys - 1) / pl.keys;
+  int64_t most = 148 * resident;
+  if (steps < 1) { if (tiles * d->kv_heads < most) most = tiles * d->kv_heads; }
+  else if (tiles * d->kv_heads <= most / steps) most = tiles * d->kv_heads * steps;
+  pl.ctas = static_cast<unsigned>(most < 1 ? 1 : most);
+  return pl;
+}
+
+// workspace: status word | a flag per CTA | boundaries | partial results
+static size_t prompt_flag_bytes(const PromptPlan& pl) { return round_up(pl.ctas * sizeof(uint32_t), 256); }
+static size_t prompt_boundary_bytes(const PromptPlan& pl) { return round_up(pl.ctas * sizeof(Boundary), 256); }
+
+template <typename T, int DP>
+static vscan_status launch_flat(const PromptParams& p, const PromptPlan& pl, cudaStream_t stream) {
+  constexpr size_t smem = flat_smem<DP>();
+  VSCAN_CUDA_TRY(allow_smem(flat_kernel<T, DP>, smem));
+  prof_before("attention_flat", stream);
+  VSCAN_CUDA_TRY(launch_dependent(flat_kernel<T, DP>, dim3(pl.ctas), dim3(kFlatThreads), smem, stream, p));
+  prof_after(stream);
+  VSCAN_AFTER_LAUNCH();
+  return VSCAN_OK;
+}
+
+template <typename T>
+static vscan_status launch_prompt(const PromptParams& p, const PromptPlan& pl, cudaStream_t stream) {
+  const vscan_status st = p.head_dim <= 64 ? launch_flat<T, 64>(p, pl, stream) : p.head_dim <= 128 ? launch_flat<T, 128>(p, pl, stream)
+                                                                                                     : launch_flat<T, 256>(p, pl, stream);
+  if (st != VSCAN_OK) return st;
+  // nothing can have been cut when no sequence has more keys than a whole tile's, or when one CTA did it all
+  if (p.kv_rows <= kFlatWhole * pl.keys || pl.ctas == 1) return VSCAN_OK;
+  prof_before("attention_join", stream);
+  const dim3 grid(pl.ctas, (pl.tile_rows + kJoinRows - 1) / kJoinRows);
+  VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, grid, dim3(kJoinThreads), 0, stream, static_cast<const AttnParams&>(p), static_cast<int>(pl.ctas)));
+  prof_after(stream);
+  VSCAN_AFTER_LAUNCH();
+  return VSCAN_OK;
+}
+
+}  // namespace kv
+}  // namespace vscan
+
+using namespace vscan;
+
+extern "C" size_t vscan_attention_workspace_bytes(const vscan_attention_desc* d) {
+  if (!d || d->batch <= 0 || d->rows <= 0 || d->max_q_len <= 0 || d->q_heads <= 0 || d->kv_heads <= 0 || d->head_dim <= 0 || d->head_dim > 256 ||
+      d->q_heads / d->kv_heads > 64 || d->kv_rows < 0)
+    return kStatusBytes;
+  const kv::PromptPlan pl = kv::plan_prompt(d);
+  return kStatusBytes + kv::prompt_flag_bytes(pl) + kv::prompt_boundary_bytes(pl) +
+         round_up(2 * static_cast<size_t>(pl.ctas) * kv::partial_floats(pl.tile_rows, d->head_dim) * 4, 256);
+}
+
+extern "C" vscan_status vscan_attention(const vscan_attention_desc* d, void* workspace, size_t workspace_bytes, void* stream_) {
+  const vscan_status st = kv::validate_prompt(d);
+  if (st != VSCAN_OK) return st;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  if (!workspace || !aligned256(workspace) || workspace_bytes < vscan_attention_workspace_bytes(d)) return VSCAN_ERR_WORKSPACE;
+  if (d->batch == 0 || d->rows == 0 || d->max_q_len == 0) {
+    VSCAN_CUDA_TRY(cudaMemsetAsync(workspace, 0, sizeof(uint32_t), stream));
+    return VSCAN_OK;
+  }
+  const kv::PromptPlan pl = kv::plan_prompt(d);
+  const long long e = static_cast<long long>(dtype_bytes(d->dtype));
+  char* ws = static_cast<char*>(workspace);
+  kv::PromptParams p = {};
+  p.q = static_cast<const char*>(d->q); p.k = static_cast<const char*>(d->k); p.v = static_cast<const char*>(d->v);
+  p.out = static_cast<char*>(d->out); p.lse = d->lse;
+  p.q_seq = d->q_stride[0] * e; p.q_head = d->q_stride[1] * e; p.q_row = d->q_stride[2] * e;
+  p.k_seq = d->k_stride[0] * e; p.k_head = d->k_stride[1] * e; p.k_row = d->k_stride[2] * e;
+  p.v_seq = d->v_stride[0] * e; p.v_head = d->v_stride[1] * e; p.v_row = d->v_stride[2] * e;
+  p.o_seq = d->out_stride[0] * e; p.o_head = d->out_stride[1] * e; p.o_row = d->out_stride[2] * e;
+  p.l_seq = d->lse_stride[0]; p.l_head = d->lse_stride[1]; p.l_row = d->lse_stride[2];
+  p.row_offset = d->row_offset; p.kv_offset = d->kv_offset ? d->kv_offset : d->row_offset;
+  p.batch = d->batch; p.q_heads = d->q_heads; p.kv_heads = d->kv_heads; p.group = d->q_heads / d->kv_heads; p.head_dim = d->head_dim;
+  p.rows = d->rows; p.kv_rows = d->kv_rows; p.padded = d->padded ? 1 : 0; p.max_q_len = d->max_q_len; p.causal = d->causal ? 1 : 0;
+  p.tile_rows = pl.tile_rows;
+  const double factor = static_cast<double>(d->scale) * 1.4426950408889634074;
+  p.scale_log2e = static_cast<float>(factor);
+  p.scale_rest = static_cast<float>(factor - p.scale_log2e);
+  p.status = reinterpret_cast<uint32_t*>(ws);
+  ws += kStatusBytes;
+  p.flags = reinterpret_cast<uint32_t*>(ws);
+  ws += kv::prompt_flag_bytes(pl);
+  p.boundary = reinterpret_cast<kv::Boundary*>(ws);
+  p.partial = reinterpret_cast<float*>(ws + kv::prompt_boundary_bytes(pl));
+  return d->dtype == VSCAN_F32 ? kv::launch_prompt<float>(p, pl, stream) : kv::launch_prompt<__nv_bfloat16>(p, pl, stream);
+}

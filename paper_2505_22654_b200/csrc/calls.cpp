@@ -1,4 +1,4 @@
-// Argument marshalling of the Python face for vscan_rope and the vscan_kv_* calls: takes tensors, checks them, fills the
+// Argument marshalling of the Python face for vscan_rope, vscan_attention and the vscan_kv_* calls: takes tensors, checks them, fills the
 // descriptors and calls the library on the current stream of the tensors' device.  A decode step makes these calls for every
 // layer and token; the same marshalling in Python costs 15 to 20 us a call, several times what the kernels take.
 // The library itself stays free of torch: its entry points are given to this module as addresses.
@@ -23,6 +23,11 @@ struct Entries {
   decltype(&vscan_kv_write) kv_write;
   decltype(&vscan_kv_attention) kv_attention;
   decltype(&vscan_kv_attention_workspace_bytes) kv_attention_workspace_bytes;
+  decltype(&vscan_attention) attention;
+  decltype(&vscan_attention_workspace_bytes) attention_workspace_bytes;
+  decltype(&vscan_kv_weigh) kv_weigh;
+  decltype(&vscan_kv_evict) kv_evict;
+  decltype(&vscan_kv_evict_workspace_bytes) kv_evict_workspace_bytes;
 } g_entries;
 
 struct BadType : std::runtime_error { using std::runtime_error::runtime_error; };
@@ -79,6 +84,12 @@ long integer(PyObject* o) {
   const long v = PyLong_AsLong(o);
   if (v == -1 && PyErr_Occurred()) { PyErr_Clear(); throw BadType("an integer wanted"); }
   return v;
+}
+
+float number(PyObject* o, const char* name) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); throw BadType(std::string(name) + ": a number wanted"); }
+  return static_cast<float>(v);
 }
 
 int32_t truth(PyObject* o) {
@@ -198,7 +209,17 @@ PyObject* kv_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // ------------------------------------------------------------------------------------------ write, attention
-// The cache arrays, and the lengths, of a write or attention descriptor
+// Type and sizes of a cache
+template <typename D>
+void codes_of(const at::Tensor& k, D& d) {
+  const auto type = k.scalar_type();
+  if (type != at::kFloat8_e4m3fn && type != at::kChar) throw BadType(std::string("k_cache: float8_e4m3fn or int8 wanted, ") + c10::toString(type) + " given");
+  d.kv_dtype = type == at::kChar ? VSCAN_KV_I8 : VSCAN_KV_E4M3;
+  d.num_blocks = narrow(k.size(0), "k_cache"); d.kv_heads = narrow(k.size(1), "k_cache");
+  d.block_size = narrow(k.size(2), "k_cache"); d.head_dim = narrow(k.size(3), "k_cache");
+}
+
+// The cache arrays, and the lengths, of a write, attention or eviction descriptor
 template <typename D>
 void cache_of(const Place& at_, PyObject* const* a, D& d) {   // k_cache, v_cache, k_scale, v_scale
   const at::Tensor &k = tensor(a[0], "k_cache"), &v = tensor(a[1], "v_cache"), &ks = tensor(a[2], "k_scale"), &vs = tensor(a[3], "v_scale");
@@ -206,11 +227,8 @@ void cache_of(const Place& at_, PyObject* const* a, D& d) {   // k_cache, v_cach
   wants(v.sizes() == k.sizes(), v, "v_cache", "the shape of k_cache");
   wants(ks.dim() == 2 && ks.size(0) == k.size(0) && ks.size(1) == k.size(1), ks, "k_scale", "[num_blocks, kv_heads]");
   wants(vs.dim() == 2 && vs.size(0) == k.size(0) && vs.size(1) == k.size(1), vs, "v_scale", "[num_blocks, kv_heads]");
+  codes_of(k, d);
   const auto type = k.scalar_type();
-  if (type != at::kFloat8_e4m3fn && type != at::kChar) throw BadType(std::string("k_cache: float8_e4m3fn or int8 wanted, ") + c10::toString(type) + " given");
-  d.kv_dtype = type == at::kChar ? VSCAN_KV_I8 : VSCAN_KV_E4M3;
-  d.num_blocks = narrow(k.size(0), "k_cache"); d.kv_heads = narrow(k.size(1), "k_cache");
-  d.block_size = narrow(k.size(2), "k_cache"); d.head_dim = narrow(k.size(3), "k_cache");
   d.k_cache = static_cast<uint8_t*>(whole(at_, k, type, "k_cache"));
   d.v_cache = static_cast<uint8_t*>(whole(at_, v, type, "v_cache"));
   d.k_scale = static_cast<float*>(whole(at_, ks, at::kFloat, "k_scale"));
@@ -261,11 +279,23 @@ PyObject* kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {   // k, v, kv_
   });
 }
 
-void queries_of(const at::Tensor& q, vscan_kv_attention_desc& d) {
+template <typename D>
+void queries_of(const at::Tensor& q, D& d) {
   wants(q.dim() == 3 || q.dim() == 4, q, "q", "[rows, heads, head_dim] or [batch, heads, rows, head_dim]");
   d.dtype = dtype_of(q);
   d.q_heads = narrow(q.size(1), "q");
   rows_of(q, d.batch, d.q_heads, d.head_dim, "q", d.rows, d.padded, d.q_stride);
+}
+
+float* logarithms_of(const Place& at_, const at::Tensor& lse, const at::Tensor& q, int32_t padded, int64_t* st) {
+  if (lse.scalar_type() != at::kFloat) throw BadType("lse: float32 wanted");
+  bool same = lse.dim() == q.dim() - 1;
+  for (int64_t i = 0; same && i < lse.dim(); ++i) same = lse.size(i) == q.size(i);
+  wants(same, lse, "lse", "the shape of q without its last dimension");
+  st[0] = padded ? step(lse, 0) : 0;
+  st[1] = step(lse, 1);
+  st[2] = step(lse, padded ? 2 : 0);
+  return static_cast<float*>(at_.ptr(lse));
 }
 
 PyObject* kv_attention_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {   // q, block_table, k_cache, max_q_len
@@ -293,9 +323,7 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     cache_of(at_, a + 4, d);
     lengths_of(at_, a + 1, d);
     queries_of(q, d);
-    const double scale = PyFloat_AsDouble(a[8]);
-    if (scale == -1.0 && PyErr_Occurred()) { PyErr_Clear(); throw BadType("scale: a number wanted"); }
-    d.scale = static_cast<float>(scale);
+    d.scale = number(a[8], "scale");
     d.max_q_len = narrow(integer(a[9]), "max_q_len");
     d.causal = truth(a[10]);
     wants(out.sizes() == q.sizes(), out, "out", "the shape of q");
@@ -303,38 +331,166 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     rows_of(out, d.batch, d.q_heads, d.head_dim, "out", d.rows, d.padded, d.out_stride);
     d.q = at_.ptr(q);
     d.out = at_.ptr(out);
-    if (a[12] != Py_None) {
-      const at::Tensor& lse = tensor(a[12], "lse");
-      if (lse.scalar_type() != at::kFloat) throw BadType("lse: float32 wanted");
-      bool same = lse.dim() == q.dim() - 1;
-      for (int64_t i = 0; same && i < lse.dim(); ++i) same = lse.size(i) == q.size(i);
-      wants(same, lse, "lse", "the shape of q without its last dimension");
-      d.lse_stride[0] = d.padded ? step(lse, 0) : 0;
-      d.lse_stride[1] = step(lse, 1);
-      d.lse_stride[2] = step(lse, d.padded ? 2 : 0);
-      d.lse = static_cast<float*>(at_.ptr(lse));
-    }
+    if (a[12] != Py_None) d.lse = logarithms_of(at_, tensor(a[12], "lse"), q, d.padded, d.lse_stride);
     void* p = whole(at_, ws, at::kByte, "workspace");
     const size_t bytes = static_cast<size_t>(ws.numel());
     return on_stream(at_, [&](void* s) { return g_entries.kv_attention(&d, p, bytes, s); });
   });
 }
 
+// ------------------------------------------------------------------------------------------ attention over whole prompts
+// q and k: sizes, types, layouts
+void prompt_sizes(const at::Tensor& q, const at::Tensor& k, const at::Tensor& off, vscan_attention_desc& d) {
+  wants(off.dim() == 1 && off.size(0) >= 1, off, "row_offset", "[batch + 1]");
+  d.batch = narrow(off.size(0) - 1, "batch");
+  wants(q.dim() == 3 || q.dim() == 4, q, "q", "[rows, heads, head_dim] or [batch, heads, rows, head_dim]");
+  wants(k.dim() == q.dim(), k, "k", "the layout of q");
+  d.dtype = dtype_of(q);
+  d.q_heads = narrow(q.size(1), "q"); d.kv_heads = narrow(k.size(1), "k"); d.head_dim = narrow(q.size(-1), "q");
+  rows_of(q, d.batch, d.q_heads, d.head_dim, "q", d.rows, d.padded, d.q_stride);
+  int32_t padded;
+  rows_of(k, d.batch, d.kv_heads, d.head_dim, "k", d.kv_rows, padded, d.k_stride);
+  if (padded != d.padded) throw BadValue("q and k: one packed, the other padded");
+}
+
+PyObject* attention_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {   // q, k, row_offset, max_q_len
+  return guarded(n, 4, [&]() -> PyObject* {
+    vscan_attention_desc d = {};
+    prompt_sizes(tensor(a[0], "q"), tensor(a[1], "k"), tensor(a[2], "row_offset"), d);
+    d.max_q_len = narrow(integer(a[3]), "max_q_len");
+    return PyLong_FromSize_t(g_entries.attention_workspace_bytes(&d));
+  });
+}
+
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // q, k, v, row_offset, kv_offset, scale, max_q_len, causal, out, lse, workspace
+  return guarded(n, 11, [&]() -> PyObject* {
+    const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &off = tensor(a[3], "row_offset");
+    const at::Tensor &out = tensor(a[8], "out"), &ws = tensor(a[10], "workspace");
+    const Place at_(q);
+    vscan_attention_desc d = {};
+    prompt_sizes(q, k, off, d);
+    if (k.scalar_type() != q.scalar_type() || v.scalar_type() != q.scalar_type() || out.scalar_type() != q.scalar_type())
+      throw BadType("k, v, out: types differ from q");
+    wants(v.sizes() == k.sizes(), v, "v", "the shape of k");
+    wants(out.sizes() == q.sizes(), out, "out", "the shape of q");
+    int32_t rows, padded;
+    rows_of(v, d.batch, d.kv_heads, d.head_dim, "v", rows, padded, d.v_stride);
+    rows_of(out, d.batch, d.q_heads, d.head_dim, "out", rows, padded, d.out_stride);
+    d.row_offset = static_cast<const int32_t*>(whole(at_, off, at::kInt, "row_offset"));
+    if (a[4] != Py_None) {
+      const at::Tensor& t = tensor(a[4], "kv_offset");
+      wants(t.dim() == 1 && t.size(0) == off.size(0), t, "kv_offset", "[batch + 1]");
+      d.kv_offset = static_cast<const int32_t*>(whole(at_, t, at::kInt, "kv_offset"));
+    }
+    d.scale = number(a[5], "scale");
+    d.max_q_len = narrow(integer(a[6]), "max_q_len");
+    d.causal = truth(a[7]);
+    d.q = at_.ptr(q); d.k = at_.ptr(k); d.v = at_.ptr(v); d.out = at_.ptr(out);
+    if (a[9] != Py_None) d.lse = logarithms_of(at_, tensor(a[9], "lse"), q, d.padded, d.lse_stride);
+    void* p = whole(at_, ws, at::kByte, "workspace");
+    const size_t bytes = static_cast<size_t>(ws.numel());
+    return on_stream(at_, [&](void* s) { return g_entries.attention(&d, p, bytes, s); });
+  });
+}
+
+// ------------------------------------------------------------------------------------------ weights of cached tokens, eviction
+float* weights_of(const Place& at_, const at::Tensor& w, const at::Tensor& k, const char* name) {
+  wants(w.dim() == 3 && w.size(0) == k.size(0) && w.size(1) == k.size(1) && w.size(2) == k.size(2), w, name, "[num_blocks, kv_heads, block_size]");
+  return static_cast<float*>(whole(at_, w, at::kFloat, name));
+}
+
+PyObject* kv_weigh(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // q, lse, kv_len, row_offset, block_table, k_cache, k_scale, weight, scale, max_q_len, decay, window, causal
+  return guarded(n, 13, [&]() -> PyObject* {
+    const at::Tensor &q = tensor(a[0], "q"), &lse = tensor(a[1], "lse"), &k = tensor(a[5], "k_cache"), &ks = tensor(a[6], "k_scale");
+    const Place at_(q);
+    vscan_kv_weigh_desc d = {};
+    lengths_of(at_, a + 2, d);
+    wants(k.dim() == 4, k, "k_cache", "[num_blocks, kv_heads, block_size, head_dim]");
+    wants(ks.dim() == 2 && ks.size(0) == k.size(0) && ks.size(1) == k.size(1), ks, "k_scale", "[num_blocks, kv_heads]");
+    codes_of(k, d);
+    d.k_cache = whole(at_, k, k.scalar_type(), "k_cache");
+    d.k_scale = static_cast<const float*>(whole(at_, ks, at::kFloat, "k_scale"));
+    d.weight = weights_of(at_, tensor(a[7], "weight"), k, "weight");
+    queries_of(q, d);
+    d.q = at_.ptr(q);
+    d.lse = logarithms_of(at_, lse, q, d.padded, d.lse_stride);
+    d.scale = number(a[8], "scale");
+    d.max_q_len = narrow(integer(a[9]), "max_q_len");
+    d.decay = number(a[10], "decay");
+    d.window = a[11] == Py_None ? INT32_MAX : narrow(integer(a[11]), "window");
+    d.causal = truth(a[12]);
+    return on_stream(at_, [&](void* s) { return g_entries.kv_weigh(&d, s); });
+  });
+}
+
+PyObject* kv_evict_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {   // block_table, k_cache, max_keep, per_head
+  return guarded(n, 4, [&]() -> PyObject* {
+    const at::Tensor &table = tensor(a[0], "block_table"), &k = tensor(a[1], "k_cache");
+    wants(table.dim() == 2, table, "block_table", "[batch, max_blocks]");
+    wants(k.dim() == 4, k, "k_cache", "[num_blocks, kv_heads, block_size, head_dim]");
+    vscan_kv_evict_desc d = {};
+    codes_of(k, d);
+    d.batch = narrow(table.size(0), "batch"); d.max_blocks = narrow(table.size(1), "block_table");
+    d.max_keep = narrow(integer(a[2]), "max_keep");
+    d.per_head = truth(a[3]);
+    return PyLong_FromSize_t(g_entries.kv_evict_workspace_bytes(&d));
+  });
+}
+
+PyObject* kv_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // kv_len, budget, block_table, weight, k_cache, v_cache, k_scale, v_scale, max_keep, keep_first, keep_last, per_head, weight_out, kept, delta,
+  // workspace
+  return guarded(n, 16, [&]() -> PyObject* {
+    const at::Tensor &len = tensor(a[0], "kv_len"), &budget = tensor(a[1], "budget"), &table = tensor(a[2], "block_table"), &k = tensor(a[4], "k_cache");
+    const at::Tensor &delta = tensor(a[14], "delta"), &ws = tensor(a[15], "workspace");
+    const Place at_(len);
+    vscan_kv_evict_desc d = {};
+    cache_of(at_, a + 4, d);
+    wants(len.dim() == 1, len, "kv_len", "[batch]");
+    wants(budget.sizes() == len.sizes(), budget, "budget", "[batch]");
+    wants(delta.sizes() == len.sizes(), delta, "delta", "[batch]");
+    wants(table.dim() == 2 && table.size(0) == len.size(0), table, "block_table", "[batch, max_blocks]");
+    d.batch = narrow(len.size(0), "batch"); d.max_blocks = narrow(table.size(1), "block_table");
+    d.max_keep = narrow(integer(a[8]), "max_keep"); d.keep_first = narrow(integer(a[9]), "keep_first"); d.keep_last = narrow(integer(a[10]), "keep_last");
+    d.per_head = truth(a[11]);
+    d.kv_len = static_cast<const int32_t*>(whole(at_, len, at::kInt, "kv_len"));
+    d.budget = static_cast<const int32_t*>(whole(at_, budget, at::kInt, "budget"));
+    d.delta = static_cast<int32_t*>(whole(at_, delta, at::kInt, "delta"));
+    d.block_table = static_cast<const int32_t*>(whole(at_, table, at::kInt, "block_table"));
+    d.weight = weights_of(at_, tensor(a[3], "weight"), k, "weight");
+    if (a[12] != Py_None) d.weight_out = weights_of(at_, tensor(a[12], "weight_out"), k, "weight_out");
+    if (a[13] != Py_None) {
+      const at::Tensor& kept = tensor(a[13], "kept");
+      wants(kept.dim() == 3 && kept.size(0) == len.size(0) && kept.size(1) == (d.per_head ? k.size(1) : 1) && kept.size(2) == d.max_keep, kept, "kept",
+            "[batch, heads, max_keep]");
+      d.kept = static_cast<int32_t*>(whole(at_, kept, at::kInt, "kept"));
+    }
+    void* p = whole(at_, ws, at::kByte, "workspace");
+    const size_t bytes = static_cast<size_t>(ws.numel());
+    return on_stream(at_, [&](void* s) { return g_entries.kv_evict(&d, p, bytes, s); });
+  });
+}
+
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {   // addresses of the library's entry points
-  return guarded(n, 5, [&]() -> PyObject* {
-    void* p[5];
-    for (int i = 0; i < 5; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+  return guarded(n, 10, [&]() -> PyObject* {
+    void* p[10];
+    for (int i = 0; i < 10; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
     if (PyErr_Occurred()) { PyErr_Clear(); throw BadType("addresses wanted"); }
     g_entries = {reinterpret_cast<decltype(g_entries.rope)>(p[0]), reinterpret_cast<decltype(g_entries.kv_plan)>(p[1]),
                  reinterpret_cast<decltype(g_entries.kv_write)>(p[2]), reinterpret_cast<decltype(g_entries.kv_attention)>(p[3]),
-                 reinterpret_cast<decltype(g_entries.kv_attention_workspace_bytes)>(p[4])};
+                 reinterpret_cast<decltype(g_entries.kv_attention_workspace_bytes)>(p[4]), reinterpret_cast<decltype(g_entries.attention)>(p[5]),
+                 reinterpret_cast<decltype(g_entries.attention_workspace_bytes)>(p[6]), reinterpret_cast<decltype(g_entries.kv_weigh)>(p[7]),
+                 reinterpret_cast<decltype(g_entries.kv_evict)>(p[8]), reinterpret_cast<decltype(g_entries.kv_evict_workspace_bytes)>(p[9])};
     Py_RETURN_NONE;
   });
 }
 
 #define VSCAN_CALL(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {VSCAN_CALL(init), VSCAN_CALL(rope), VSCAN_CALL(kv_plan), VSCAN_CALL(kv_write), VSCAN_CALL(kv_attention_bytes),
-                           VSCAN_CALL(kv_attention), {nullptr, nullptr, 0, nullptr}};
+                           VSCAN_CALL(kv_attention), VSCAN_CALL(attention_bytes), VSCAN_CALL(attention), VSCAN_CALL(kv_weigh),
+                           VSCAN_CALL(kv_evict_bytes), VSCAN_CALL(kv_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

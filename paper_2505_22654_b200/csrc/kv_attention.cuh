@@ -75,9 +75,10 @@ struct Stretch {          // of a worker: [begin, end) of the line, and the segm
   bool solo, inside;
 };
 
-// The stretch of this thread's worker.  Called by all THREADS threads; SOLO: whether warps may be workers.
-template <int THREADS, bool SOLO>
-__device__ __forceinline__ Stretch locate(const AttnParams& p, ScheduleShared& sh) {
+// The stretch of this thread's worker.  Called by all THREADS threads; SOLO: whether warps may be workers.  P: AttnParams, or what a
+// call with another sequence_at() derives from it.
+template <int THREADS, bool SOLO, typename P>
+__device__ __forceinline__ Stretch locate(const P& p, ScheduleShared& sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = (p.batch + THREADS - 1) / THREADS, b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
   long long sum = 0, segments = 0;
@@ -135,7 +136,8 @@ __device__ __forceinline__ Stretch locate(const AttnParams& p, ScheduleShared& s
 // The next piece of a worker's stretch: units u0 .. u1 - 1 of the segment that the stretch is in then.  Only the first takes
 // divisions; from there on segment follows segment, and a sequence's lengths are read once.
 struct Piece { int u0, u1; };
-__device__ __forceinline__ bool next_piece(const AttnParams& p, Stretch& st, Piece& pc) {
+template <typename P>
+__device__ __forceinline__ bool next_piece(const P& p, Stretch& st, Piece& pc) {
   while (st.begin < st.end) {
     if (!st.inside) {
       const unsigned long long at = st.begin - st.seq0, seg = (at >> 32) == 0 ? static_cast<unsigned>(at) / st.s.units : at / st.s.units;

@@ -24,6 +24,7 @@
 // Every wait is bounded; on expiry the CTA says so in its flag word, frees its tensor memory and returns.
 #pragma once
 
+#include "attention_division.cuh"
 #include "kv_attention_mma.cuh"
 #include "tc_common.cuh"
 
@@ -37,6 +38,7 @@ constexpr int kTcConverter = 16, kTcIssuer = 24;   // first warp of each role
 constexpr int kTcRows = 256;          // query rows of a CTA
 constexpr int kTcKeys = 128;          // keys of a step
 constexpr int kTcWhole = 4;           // a tile of up to this many steps is not cut: joining 256 rows takes longer than they do
+using TcShape = TileShape<kTcThreads, kTcRows, kTcKeys, kTcWhole>;
 constexpr int kTcRing = 4;            // steps whose scales are kept: the converters are at most three ahead of a reader
 constexpr int kChunk = 128 * 128;     // bytes of [128 rows x 64 f16]
 
@@ -53,123 +55,8 @@ struct TcShared {
   float swap[2][2][2][128];               // [step parity][tile][half][row]: what the two threads of a row tell each other
   uint32_t there[kTcRing];                // of the 16-token groups of a step: a bit each, not there at all: 0
   alignas(16) float ks[kTcRing][8], vs[kTcRing][8];
-  long long weight[kTcThreads / 32];
-  long long seq0;
-  int b;
+  DivisionShared division;
 };
-
-// ---------------------------------------------------------------------------------------------- division of the work
-// As for few rows, but a place on the line is a key seen by a query row, so that the triangle of a causal prompt is divided
-// evenly: tile k of a causal sequence weighs group * start + min(256 (k + 1), rows), at least one step, which has a closed
-// prefix sum.
-struct TcSequence {
-  Sequence s;
-  long long base;       // what every tile sees at least
-  long long rows;       // query rows; causal tiles weigh more one after another
-  long long weight;     // of all tiles of a KV head
-  int tiles, light;     // light: tiles in front that weigh one step although they see less
-};
-
-__device__ __forceinline__ long long step_weight(const AttnParams& p) { return static_cast<long long>(kTcKeys) * p.group; }
-
-__device__ __forceinline__ long long tiles_before(const AttnParams& p, const TcSequence& q, long long k) {
-  const long long one = step_weight(p);
-  if (!p.causal) return k * max(q.base, one);
-  const long long n = min(k, static_cast<long long>(q.tiles - 1)), m = min(n, static_cast<long long>(q.light));
-  const long long sum = m * one + (n - m) * q.base + (n * (n + 1) - m * (m + 1)) * (kTcRows / 2);
-  return k < q.tiles ? sum : sum + max(q.base + q.rows, one);
-}
-
-__device__ __forceinline__ TcSequence tc_sequence_at(const AttnParams& p, int b) {
-  TcSequence q;
-  q.s = sequence_at(p, b);
-  q.rows = static_cast<long long>(q.s.n) * p.group;
-  q.tiles = static_cast<int>((q.rows + kTcRows - 1) / kTcRows);
-  q.base = p.causal ? max(q.s.start, 0ll) * p.group : static_cast<long long>(q.s.len) * p.group;
-  q.light = static_cast<int>(max((max(step_weight(p) - q.base, 0ll) + kTcRows - 1) / kTcRows - 1, 0ll));
-  q.weight = q.tiles > 0 ? tiles_before(p, q, q.tiles) : 0;
-  return q;
-}
-
-// Quotient of numbers that nearly always fit 32 bits
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? static_cast<unsigned>(a) / static_cast<unsigned>(b) : a / b;
-}
-
-struct TcStretch { long long begin, end, quota, seq0; int b; };
-
-__device__ __forceinline__ TcStretch tc_locate(const AttnParams& p, TcShared& sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int per = (p.batch + kTcThreads - 1) / kTcThreads, b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
-  long long sum = 0;
-  for (int b = b0; b < b1; ++b) sum += tc_sequence_at(p, b).weight * p.kv_heads;
-  long long incl = sum;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long t = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += t;
-  }
-  if (lane == 31) sh.weight[warp] = incl;
-  __syncthreads();
-  long long before = 0, total = 0;
-#pragma unroll
-  for (int w = 0; w < kTcThreads / 32; ++w) {
-    if (w < warp) before += sh.weight[w];
-    total += sh.weight[w];
-  }
-  TcStretch st;
-  // a stretch is at least a step long, so that no two cuts fall into one step
-  st.quota = max(quotient(total + gridDim.x - 1, gridDim.x), step_weight(p));
-  st.begin = min(blockIdx.x * st.quota, total);
-  st.end = min(st.begin + st.quota, total);
-  long long at = before + incl - sum;
-  if (at <= st.begin && st.begin < at + sum) {
-    for (int b = b0; b < b1; ++b) {
-      const long long w = tc_sequence_at(p, b).weight * p.kv_heads;
-      if (st.begin < at + w) { sh.b = b; sh.seq0 = at; break; }
-      at += w;
-    }
-  }
-  __syncthreads();
-  st.b = sh.b;
-  st.seq0 = sh.seq0;
-  return st;
-}
-
-struct TcPiece {
-  TcSequence q;
-  long long seg0, seg1;   // seg1: the end of what there is to do, as a place on the line
-  int b, head, tile, n_rows, most, u0, u1, units;
-};
-
-__device__ __forceinline__ bool tc_next(const AttnParams& p, TcStretch& st, TcPiece& pc) {
-  while (st.begin < st.end) {
-    pc.q = tc_sequence_at(p, st.b);
-    const long long all = pc.q.weight * p.kv_heads;
-    if (st.begin >= st.seq0 + all) { st.seq0 += all; ++st.b; continue; }
-    const long long head = quotient(st.begin - st.seq0, pc.q.weight), rel = st.begin - st.seq0 - head * pc.q.weight;
-    int lo = 0, hi = pc.q.tiles;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (tiles_before(p, pc.q, mid) <= rel) lo = mid; else hi = mid;
-    }
-    pc.head = static_cast<int>(head); pc.tile = lo; pc.b = st.b;
-    pc.seg0 = st.begin - (rel - tiles_before(p, pc.q, lo));
-    const long long seg_end = pc.seg0 + tiles_before(p, pc.q, lo + 1) - tiles_before(p, pc.q, lo);
-    pc.n_rows = static_cast<int>(min(static_cast<long long>(kTcRows), pc.q.rows - static_cast<long long>(lo) * kTcRows));
-    pc.most = visible(p, pc.q.s, (lo * kTcRows + pc.n_rows - 1) / p.group);
-    pc.units = max(1, (pc.most + kTcKeys - 1) / kTcKeys);
-    const long long per_unit = step_weight(p);
-    pc.seg1 = min(seg_end, pc.seg0 + pc.units * per_unit);
-    pc.u0 = static_cast<int>(min(quotient(st.begin - pc.seg0, per_unit), static_cast<long long>(pc.units)));
-    pc.u1 = st.end >= seg_end ? pc.units : static_cast<int>(min(quotient(st.end - pc.seg0, per_unit), static_cast<long long>(pc.units)));
-    const bool whole = pc.units <= kTcWhole, starts = st.begin == pc.seg0;
-    if (whole) { pc.u0 = 0; pc.u1 = pc.units; }
-    st.begin = seg_end;
-    if (whole ? starts : pc.u0 < pc.u1) return true;
-  }
-  return false;
-}
 
 // ---------------------------------------------------------------------------------------------- instructions
 // The issuing warp stays converged: all lanes run its control flow and compute the descriptors, which are warp-uniform, and one
@@ -354,7 +241,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;              // scores of tile t at column 128 t; sums at 256 + 128 t
   grid_dependency_wait();
-  TcStretch st = tc_locate(p, sh);
+  TcStretch st = tc_locate<TcShape>(p, sh.division);
   if (threadIdx.x == 0) {
     if (blockIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = 0; }
     p.boundary[blockIdx.x].seg1 = 0;
@@ -384,7 +271,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
       ok = mbar_wait_warp(&sh.pair[tile][quarter], n_swap & 1, abort_flag);
       return sh.swap[n_swap++ & 1][tile][half ^ 1][r];
     };
-    while (ok && tc_next(p, st, pc)) {
+    while (ok && tc_next<TcShape>(p, st, pc)) {
       const int steps = pc.u1 - pc.u0;
       if (pc.u0 > 0 && threadIdx.x == 0)
         p.boundary[blockIdx.x] = {pc.seg0, pc.seg1, st.quota, pc.b, pc.head, pc.tile, pc.q.s.first, pc.n_rows, 0};
@@ -610,7 +497,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
     const size_t cell_bytes = static_cast<size_t>(p.block_size) * D;
     int step = 0;
     bool ok = true;
-    while (ok && tc_next(p, st, pc)) {
+    while (ok && tc_next<TcShape>(p, st, pc)) {
       const int32_t* table = p.block_table + static_cast<size_t>(pc.b) * p.max_blocks;
       // lanes 0-7 know the blocks of the 16-token groups of a step
       auto blocks_at = [&](int t0) {
@@ -711,7 +598,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) tc_kernel(AttnParams p) {
         for (int c = 0; c < kDChunks; ++c) umma_f16_ss_x4(tmem + t * 128, a + c * (kChunk >> 4), b + c * (kChunk >> 4), qk, c > 0);
         umma_commit_warp(&sh.s_full[t]);
       };
-      while (ok && tc_next(p, st, pc)) {
+      while (ok && tc_next<TcShape>(p, st, pc)) {
         const int two = pc.n_rows > 128;
         for (int t = 0; t <= two && ok; ++t) ok = mbar_wait_warp(&sh.q_full[t], n_piece[t]++ & 1, abort_flag);
         ok = ok && mbar_wait_warp(&sh.k_full[step & 1], (step >> 1) & 1, abort_flag);

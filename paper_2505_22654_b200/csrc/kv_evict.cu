@@ -1,0 +1,386 @@
+// vscan_kv_evict: the tokens that gathered least weight leave the paged 8-bit cache.
+//
+// Two launches.  rank_kernel: a CTA a (sequence, head), or a sequence where all heads keep the same tokens, finds the threshold of
+// the weights by an exact radix select and writes the places of the tokens that stay, ascending.  move_kernel: a group of warps a
+// (block of the result, head, K or V) gathers the block's codes from where they lie and writes them in place.
+//
+// In place: token j of the result comes from place src(j) >= j.  A unit holds all codes of its block in registers, says so in a
+// flag, and writes once every unit in front of it that reads from the block it will write has said so too.  Those units have begun
+// before it (units are handed out by a counter) and wait for nobody before they have read, so the waits end.
+#include "kv_common.cuh"
+#include "topk.cuh"
+
+namespace vscan {
+namespace kv {
+
+constexpr int64_t kMostTokens = 0x7ffff000;
+constexpr unsigned kEvictPolls = 1u << 22;   // of about 100 ns
+
+struct EvictParams {
+  const int32_t* kv_len;
+  const int32_t* budget;
+  const int32_t* block_table;
+  const float* weight;
+  float* weight_out;
+  uint8_t* cache[2];
+  float* scale[2];
+  int32_t* kept;          // the caller's, or in the workspace
+  int32_t* delta;
+  uint32_t* status;
+  uint32_t* bad;          // [batch] vscan_status of a sequence
+  int2* stay;             // [batch] tokens that stay, -1: left alone; 1 where some leave
+  uint32_t* next;         // units handed out so far
+  uint32_t* read;         // [batch][kv_heads][2][columns] a unit has read its codes
+  uint32_t* keys;         // [batch][heads][max_blocks * block_size] where shared memory does not hold them
+  int batch, kv_heads, heads, head_dim, block_size, shift, num_blocks, max_blocks, max_keep, keep_first, keep_last, columns, held;
+};
+
+// ---------------------------------------------------------------------------------------------- which tokens stay
+// Reads 4 bytes a token and head, once; everything after that is the latency of five passes over keys in shared memory.
+__device__ __forceinline__ uint32_t rank_key(float w) { return float_to_key(w == w ? w : -INFINITY); }
+
+__global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
+  extern __shared__ uint32_t rank_smem[];
+  __shared__ SelectScratch sc;
+  const int b = blockIdx.y, head = blockIdx.x;
+  grid_dependency_wait();
+  const int room = p.max_blocks << p.shift, len = p.kv_len[b];
+  const int most = min(max(p.budget[b], 0), p.max_keep);
+  const int32_t* table = p.block_table + static_cast<size_t>(b) * p.max_blocks;
+  const int used = len > 0 && len <= room ? ((len - 1) >> p.shift) + 1 : 0;
+  bool wrong = len < 0 || len > room;
+  for (int j = threadIdx.x; j < used; j += blockDim.x) wrong = wrong || table[j] < 0 || table[j] >= p.num_blocks;
+  wrong = __syncthreads_or(wrong);
+  const int n = wrong ? -1 : min(most, len);
+  if (head == 0 && threadIdx.x == 0) {
+    if (b == 0) { p.status[0] = kStatusFlags | static_cast<uint32_t>(p.batch); *p.next = 0; }
+    p.bad[b] = wrong ? VSCAN_ERR_INVALID_ARG : 0;
+    p.stay[b] = make_int2(n, n >= 0 && n < len);
+    p.delta[b] = wrong ? 0 : n - len;
+  }
+  // the flags of the heads that this CTA speaks for
+  const int each = p.heads == 1 ? p.kv_heads : 1, flags = each * 2 * p.columns;
+  uint32_t* read = p.read + (static_cast<size_t>(b) * p.kv_heads + (p.heads == 1 ? 0 : head)) * 2 * p.columns;
+  for (int i = threadIdx.x; i < flags; i += blockDim.x) read[i] = 0;
+  int32_t* out = p.kept + (static_cast<size_t>(b) * p.heads + head) * p.max_keep;
+  if (n <= 0) return;
+  if (n == len) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) out[i] = i;
+    return;
+  }
+  uint32_t* keys = p.held >= len ? rank_smem : p.keys + (static_cast<size_t>(b) * p.heads + head) * room;
+  for (int t = threadIdx.x; t < len; t += blockDim.x) {
+    const float* w = p.weight + (static_cast<size_t>(table[t >> p.shift]) * p.kv_heads << p.shift) + (t & (p.block_size - 1));
+    float rank;
+    if (t < p.keep_first || t >= static_cast<long long>(len) - p.keep_last) {
+      rank = INFINITY;
+    } else if (p.heads > 1 || p.kv_heads == 1) {
+      rank = __ldg(w + (static_cast<size_t>(head) << p.shift));
+    } else {
+      double sum = 0.;
+      for (int h = 0; h < p.kv_heads; ++h) sum += __ldg(w + (static_cast<size_t>(h) << p.shift));
+      rank = static_cast<float>(sum);
+    }
+    keys[t] = rank_key(rank);
+  }
+  __syncthreads();
+  uint32_t threshold;
+  int need;
+  block_radix_select(keys, nullptr, len, n, sc, threshold, need);
+  int above = 0, equal = 0;                          // of the tokens in front: over the threshold, and on it
+  for (int t0 = 0; t0 < len; t0 += blockDim.x) {
+    const int t = t0 + threadIdx.x;
+    const uint32_t key = t < len ? keys[t] : 0u;
+    const bool over = t < len && key > threshold, on = t < len && key == threshold;
+    int total;
+    const int before = block_exclusive_scan((over ? 1 << 16 : 0) + (on ? 1 : 0), sc.warp_sums, total);
+    const int e = equal + (before & 0xffff);
+    if (over || (on && e < need)) out[above + (before >> 16) + min(e, need)] = t;
+    above += total >> 16;
+    equal += total & 0xffff;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- moving them
+// Largest magnitude among 16 codes, as a code (a byte whose order is that of the magnitudes)
+template <int KV>
+__device__ __forceinline__ uint32_t peak_code(const uint4& v) {
+  uint32_t m;
+  if constexpr (KV == VSCAN_KV_E4M3)
+    m = __vmaxu4(__vmaxu4(v.x & 0x7f7f7f7fu, v.y & 0x7f7f7f7fu), __vmaxu4(v.z & 0x7f7f7f7fu, v.w & 0x7f7f7f7fu));
+  else
+    m = __vmaxu4(__vmaxu4(__vabs4(v.x), __vabs4(v.y)), __vmaxu4(__vabs4(v.z), __vabs4(v.w)));
+  m = __vmaxu4(m, m >> 16);
+  return max(m & 0xffu, (m >> 8) & 0xffu);
+}
+template <int KV>
+__device__ __forceinline__ float code_magnitude(uint32_t code) {
+  if constexpr (KV == VSCAN_KV_E4M3) {
+    float f[4];
+    decode4<KV>(code, f);
+    return f[0];                                     // the code of NaN gives NaN
+  } else {
+    return static_cast<float>(code);                 // 128 where the code is -128
+  }
+}
+// 16 codes of one scale as codes of another: the value, then its code
+template <int KV>
+__device__ __forceinline__ uint4 recode(const uint4& old, float scale, float inv) {
+  const uint32_t w[4] = {old.x, old.y, old.z, old.w};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float f[4];
+    decode4<KV>(w[i], f);
+    r[i] = encode4<KV>(f[0] * scale * inv, f[1] * scale * inv, f[2] * scale * inv, f[3] * scale * inv);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+__host__ __device__ constexpr int move_threads(int w) { return w == 8 ? 256 : 128; }
+
+template <int KV, int W, int HELD>
+__global__ void __launch_bounds__(move_threads(W)) move_kernel(EvictParams p) {
+  constexpr int kThreads = move_threads(W), kGroups = kThreads / 32 / W, kWeights = 8 / W;   // weights of a lane: 256 a block at most
+  __shared__ uint32_t peaks[kThreads / 32];
+  __shared__ uint32_t ticket;
+  __shared__ int quit;
+  grid_dependency_wait();
+  if (threadIdx.x == 0) { ticket = atomicAdd(p.next, 1u); quit = 0; }
+  __syncthreads();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / W, in_group = threadIdx.x - group * W * 32;
+  const long long unit = static_cast<long long>(ticket) * kGroups + group;
+  const int which = static_cast<int>(unit & 1);
+  long long rest = unit >> 1;
+  const int h = static_cast<int>(rest % p.kv_heads);
+  rest /= p.kv_heads;
+  const int b = static_cast<int>(rest % p.batch), j = static_cast<int>(rest / p.batch);
+  if (j >= p.columns) return;                        // (a group of eight warps is its whole CTA)
+  const int2 stay = p.stay[b];
+  const int first = j << p.shift, n = min(stay.x - first, p.block_size);
+  if (n <= 0) return;
+  const bool moves_weights = which == 0 && p.weight_out && (stay.y || p.weight_out != p.weight);
+  if (!stay.y && !moves_weights) return;
+  const int32_t* table = p.block_table + static_cast<size_t>(b) * p.max_blocks;
+  const int32_t* src = p.kept + (static_cast<size_t>(b) * p.heads + (p.heads > 1 ? h : 0)) * p.max_keep;
+  const size_t to = static_cast<size_t>(table[j]) * p.kv_heads + h;
+  const int last = src[first + n - 1];
+  const bool stays = last == first + n - 1;          // places ascend and none is below its number: then all of the block's tokens stay
+  const int mask = p.block_size - 1;
+
+  float w[kWeights];
+  if (moves_weights) {
+#pragma unroll
+    for (int k = 0; k < kWeights; ++k) {
+      const int r = in_group + k * 32 * W;
+      if (r < n) {
+        const int t = src[first + r];
+        w[k] = p.weight[((static_cast<size_t>(table[t >> p.shift]) * p.kv_heads + h) << p.shift) + (t & mask)];
+      }
+    }
+  }
+  auto store_weights = [&]() {
+    if (moves_weights) {
+#pragma unroll
+      for (int k = 0; k < kWeights; ++k) {
+        const int r = in_group + k * 32 * W;
+        if (r < n) p.weight_out[(to << p.shift) + r] = w[k];
+      }
+    }
+  };
+  if (stays) {                                       // nothing moves, and nobody waits for this unit
+    if (p.weight_out != p.weight) store_weights();
+    return;
+  }
+
+  const int cpr = p.head_dim / 16, total = n * cpr;
+  const uint8_t* codes = p.cache[which];
+  uint4 held[HELD];
+  float scale[HELD];
+  float top = 0.f;
+#pragma unroll
+  for (int k = 0; k < HELD; ++k) {
+    const int c = in_group + k * 32 * W;
+    held[k] = make_uint4(0, 0, 0, 0);
+    scale[k] = 0.f;
+    if (c < total) {
+      const int r = c / cpr, t = src[first + r];
+      const size_t from = static_cast<size_t>(table[t >> p.shift]) * p.kv_heads + h;
+      scale[k] = p.scale[which][from];
+      held[k] = *reinterpret_cast<const uint4*>(codes + ((from << p.shift) + (t & mask)) * p.head_dim + (c - r * cpr) * 16);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < HELD; ++k) {
+    const float m = code_magnitude<KV>(peak_code<KV>(held[k])) * scale[k];
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(m)));
+  }
+  uint32_t peak = __reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu);
+  if constexpr (W > 1) {
+    if (lane == 0) peaks[warp] = peak;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) peak = max(peak, peaks[i]);
+  } else {
+    __syncwarp();
+  }
+  // ---- all of the group's reads are done: say so, then wait for the units in front that read from the block to be written
+  uint32_t* read = p.read + ((static_cast<size_t>(b) * p.kv_heads + h) * 2 + which) * p.columns;
+  bool ok = true;
+  if (W == 1 || warp == 0) {
+    if (lane == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(read + j) : "memory");
+    for (int c0 = j - 1; c0 >= 0; c0 -= 32) {
+      const int c = c0 - lane;
+      const bool reads = c >= 0 && src[(c << p.shift) + mask] >= first;     // its last token comes from this block or from behind it
+      unsigned polls = 0;
+      uint32_t done = !reads;
+      while (!done && polls < kEvictPolls) {
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(read + c) : "memory");
+        if (!done) { __nanosleep(100); ++polls; }
+      }
+      ok = __all_sync(0xffffffffu, done != 0) && ok;
+      if (!ok || !__all_sync(0xffffffffu, reads)) break;                    // units further in front read from further in front
+    }
+    if constexpr (W > 1) { if (!ok && lane == 0) quit = 1; }
+  }
+  if constexpr (W > 1) {
+    __syncthreads();
+    ok = quit == 0;
+  }
+  if (!ok) {
+    if (in_group == 0) p.bad[b] = VSCAN_ERR_TIMEOUT;
+    return;
+  }
+  const float s = peak < 0x7f800000u ? exp2_int(scale_exponent<KV>(__uint_as_float(peak))) : __uint_as_float(0x7fc00000u);
+  const bool nan = s != s;
+  const float inv = nan ? 0.f : exp2_int(-scale_exponent<KV>(__uint_as_float(peak)));
+  uint8_t* dst = p.cache[which] + (to << p.shift) * p.head_dim;
+#pragma unroll
+  for (int k = 0; k < HELD; ++k) {
+    const int c = in_group + k * 32 * W;
+    if (c < total) {
+      uint4 v = held[k];
+      if (nan) v = make_uint4(0, 0, 0, 0);
+      else if (scale[k] != s) v = recode<KV>(v, scale[k], inv);
+      st_16(dst + static_cast<size_t>(c) * 16, v);
+    }
+  }
+  if (in_group == 0) p.scale[which][to] = s;
+  store_weights();
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+static vscan_status validate_evict(const vscan_kv_evict_desc* d) {
+  if (!d) return VSCAN_ERR_INVALID_ARG;
+  if (d->kv_dtype != VSCAN_KV_E4M3 && d->kv_dtype != VSCAN_KV_I8) return VSCAN_ERR_INVALID_ARG;
+  if (d->batch < 0 || d->kv_heads <= 0 || d->head_dim <= 0 || d->head_dim % 16 || d->num_blocks < 0 || d->max_blocks < 0 || d->max_keep < 0 ||
+      d->keep_first < 0 || d->keep_last < 0 || !block_size_ok(d->block_size))
+    return VSCAN_ERR_INVALID_ARG;
+  if (d->batch == 0) return VSCAN_OK;
+  if (!d->kv_len || !d->budget || !d->delta) return VSCAN_ERR_INVALID_ARG;
+  if ((d->max_blocks > 0 && !d->block_table) ||
+      (d->num_blocks > 0 && d->max_blocks > 0 && (!d->weight || !d->k_cache || !d->v_cache || !d->k_scale || !d->v_scale)))
+    return VSCAN_ERR_INVALID_ARG;
+  if (d->head_dim > 256 || d->batch > kMaxBatch || d->kv_heads > 65535 || static_cast<int64_t>(d->max_blocks) * d->block_size > kMostTokens ||
+      static_cast<int64_t>(d->batch) * d->kv_heads * (d->max_keep / d->block_size + 1) > (int64_t{1} << 28))
+    return VSCAN_ERR_UNSUPPORTED;
+  struct Rng { const void* p; size_t n; };
+  const size_t B = d->batch, H = d->kv_heads, pool = static_cast<size_t>(d->num_blocks) * H, bs = d->block_size;
+  const Rng all[] = {{d->kv_len, B * 4}, {d->budget, B * 4}, {d->block_table, B * d->max_blocks * 4}, {d->weight, pool * bs * 4},
+                     {d->weight_out == d->weight ? nullptr : d->weight_out, pool * bs * 4},
+                     {d->k_cache, pool * bs * d->head_dim}, {d->v_cache, pool * bs * d->head_dim}, {d->k_scale, pool * 4}, {d->v_scale, pool * 4},
+                     {d->kept, B * (d->per_head ? H : 1) * d->max_keep * 4}, {d->delta, B * 4}};
+  constexpr int kInputs = 4, kAll = 11;
+  for (const Rng& r : all)
+    if (r.p && !aligned16(r.p)) return VSCAN_ERR_INVALID_ARG;
+  for (int o = kInputs; o < kAll; ++o)
+    for (int i = 0; i < o; ++i)
+      if (overlaps(all[o].p, all[o].n, all[i].p, all[i].n)) return VSCAN_ERR_INVALID_ARG;
+  return VSCAN_OK;
+}
+
+// workspace: status word | a word per sequence | tokens that stay | counter | flags of the units | kept, if the caller wants none | keys
+constexpr size_t kHeldKeys = 16384;      // in shared memory, 64 KB: beyond that they pass through L2
+struct EvictLayout {
+  size_t bad, stay, next, read, kept, keys, bytes;
+  int columns, heads;
+};
+static EvictLayout layout_of(const vscan_kv_evict_desc* d) {
+  EvictLayout l;
+  const size_t B = d->batch, H = d->kv_heads, room = static_cast<size_t>(d->max_blocks) * d->block_size;
+  l.columns = static_cast<int>((static_cast<int64_t>(d->max_keep) + d->block_size - 1) / d->block_size);
+  l.heads = d->per_head ? d->kv_heads : 1;
+  l.bad = kStatusBytes;
+  l.stay = l.bad + round_up(B * 4, 256);
+  l.next = l.stay + round_up(B * 8, 256);
+  l.read = l.next + 256;
+  l.kept = l.read + round_up(B * H * 2 * l.columns * 4, 256);
+  // (counted whether or not the caller has a buffer for them, so that the size depends on sizes only)
+  l.keys = l.kept + round_up(B * l.heads * static_cast<size_t>(d->max_keep) * 4, 256);
+  l.bytes = l.keys + (room > kHeldKeys ? round_up(B * l.heads * room * 4, 256) : 0);
+  return l;
+}
+
+template <int KV>
+static vscan_status launch_evict(const EvictParams& p, cudaStream_t stream) {
+  const int64_t room = static_cast<int64_t>(p.max_blocks) * p.block_size;
+  const int threads = room <= 1024 ? 128 : room <= 4096 ? 256 : 1024;
+  const size_t smem = static_cast<size_t>(p.held) * 4;
+  VSCAN_CUDA_TRY(allow_smem(rank_kernel, smem));
+  prof_before("kv_evict_rank", stream);
+  VSCAN_CUDA_TRY(launch_dependent(rank_kernel, dim3(p.heads, p.batch), dim3(threads), smem, stream, p));
+  prof_after(stream);
+  VSCAN_AFTER_LAUNCH();
+  if (p.columns == 0) return VSCAN_OK;
+  // as many warps to a unit as keep its codes in registers
+  const int chunks = p.block_size * p.head_dim / 16, w = chunks <= 256 ? 1 : 8, groups = move_threads(w) / 32 / w;
+  const int64_t units = static_cast<int64_t>(p.batch) * p.kv_heads * 2 * p.columns;
+  const dim3 grid(static_cast<unsigned>((units + groups - 1) / groups));
+  prof_before("kv_evict_move", stream);
+  VSCAN_CUDA_TRY(chunks <= 128 ? launch_dependent(move_kernel<KV, 1, 4>, grid, dim3(move_threads(1)), 0, stream, p)
+                 : chunks <= 256 ? launch_dependent(move_kernel<KV, 1, 8>, grid, dim3(move_threads(1)), 0, stream, p)
+                 : chunks <= 1024 ? launch_dependent(move_kernel<KV, 8, 4>, grid, dim3(move_threads(8)), 0, stream, p)
+                 : chunks <= 2048 ? launch_dependent(move_kernel<KV, 8, 8>, grid, dim3(move_threads(8)), 0, stream, p)
+                                  : launch_dependent(move_kernel<KV, 8, 16>, grid, dim3(move_threads(8)), 0, stream, p));
+  prof_after(stream);
+  VSCAN_AFTER_LAUNCH();
+  return VSCAN_OK;
+}
+
+}  // namespace kv
+}  // namespace vscan
+
+using namespace vscan;
+
+extern "C" size_t vscan_kv_evict_workspace_bytes(const vscan_kv_evict_desc* d) {
+  if (!d || d->batch <= 0 || d->kv_heads <= 0 || d->max_blocks < 0 || d->max_keep < 0 || !kv::block_size_ok(d->block_size)) return kStatusBytes;
+  return kv::layout_of(d).bytes;
+}
+
+extern "C" vscan_status vscan_kv_evict(const vscan_kv_evict_desc* d, void* workspace, size_t workspace_bytes, void* stream_) {
+  const vscan_status st = kv::validate_evict(d);
+  if (st != VSCAN_OK) return st;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  if (!workspace || !aligned256(workspace) || workspace_bytes < vscan_kv_evict_workspace_bytes(d)) return VSCAN_ERR_WORKSPACE;
+  if (d->batch == 0) {
+    VSCAN_CUDA_TRY(cudaMemsetAsync(workspace, 0, sizeof(uint32_t), stream));
+    return VSCAN_OK;
+  }
+  const kv::EvictLayout l = kv::layout_of(d);
+  char* ws = static_cast<char*>(workspace);
+  kv::EvictParams p = {};
+  p.kv_len = d->kv_len; p.budget = d->budget; p.block_table = d->block_table; p.weight = d->weight; p.weight_out = d->weight_out;
+  p.cache[0] = static_cast<uint8_t*>(d->k_cache); p.cache[1] = static_cast<uint8_t*>(d->v_cache);
+  p.scale[0] = d->k_scale; p.scale[1] = d->v_scale;
+  p.kept = d->kept ? d->kept : reinterpret_cast<int32_t*>(ws + l.kept);
+  p.delta = d->delta;
+  p.status = reinterpret_cast<uint32_t*>(ws); p.bad = reinterpret_cast<uint32_t*>(ws + l.bad); p.stay = reinterpret_cast<int2*>(ws + l.stay);
+  p.next = reinterpret_cast<uint32_t*>(ws + l.next); p.read = reinterpret_cast<uint32_t*>(ws + l.read); p.keys = reinterpret_cast<uint32_t*>(ws + l.keys);
+  p.batch = d->batch; p.kv_heads = d->kv_heads; p.heads = l.heads; p.head_dim = d->head_dim; p.block_size = d->block_size;
+  p.num_blocks = d->num_blocks; p.max_blocks = d->max_blocks; p.max_keep = d->max_keep; p.keep_first = d->keep_first; p.keep_last = d->keep_last;
+  p.columns = l.columns;
+  const int64_t room = static_cast<int64_t>(d->max_blocks) * d->block_size;
+  p.held = static_cast<int>(room < static_cast<int64_t>(kv::kHeldKeys) ? room : kv::kHeldKeys);
+  while ((1 << p.shift) < p.block_size) ++p.shift;
+  return d->kv_dtype == VSCAN_KV_E4M3 ? kv::launch_evict<VSCAN_KV_E4M3>(p, stream) : kv::launch_evict<VSCAN_KV_I8>(p, stream);
+}
