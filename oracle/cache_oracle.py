@@ -169,3 +169,77 @@ def attention(q, k, v, there, scale, causal, start):
             lse[i, h] = top + np.log(e.sum())
             reach[i, h] = abs(scale) * (np.abs(kk) @ np.abs(q[i, h])).max()
     return out, lse, weight, reach
+
+
+# --------------------------------------------------------------------------- weights of cached tokens, and eviction by them
+def weigh(weight, rows, lse, codes, scale, kv_len, table, block_size, kind, factor, decay=1.0, window=None, causal=True):
+    """weight [blocks, H, bs] float64, changed in place; rows and lse: per sequence [n, Hq, d] and [n, Hq].  -> like weight, what was
+    added times the largest |factor| sum |q| |k| of what it is made of (what the tolerances of the tests are made of)."""
+    nb, H = scale.shape
+    slack = np.zeros_like(weight)
+    for b, (q, z) in enumerate(zip(rows, lse)):
+        n, T = len(q), int(kv_len[b])
+        if n == 0:
+            continue
+        start, group = T - n, q.shape[1] // H
+        k, there = gather(codes, scale, table[b], T, block_size, kind)
+        for t in range(len(k)):
+            if not there[t]:
+                continue
+            blk, at = int(table[b][t // block_size]), t % block_size
+            for h in range(H):
+                total = decay * weight[blk, h, at] if t < start else 0.0
+                for i in range(max(0, n - (n if window is None else window)), n):
+                    if causal and t > start + i:
+                        continue
+                    for hq in range(h * group, (h + 1) * group):
+                        if z[i, hq] == -np.inf:
+                            continue
+                        e = np.exp(factor * (q[i, hq] @ k[t, h]) - z[i, hq])
+                        total += e
+                        slack[blk, h, at] += e * (abs(factor) * (np.abs(q[i, hq]) @ np.abs(k[t, h])) + abs(z[i, hq]))
+                weight[blk, h, at] = total
+    return slack
+
+
+def evict(codes, scale, weight, kv_len, budget, table, block_size, kind, max_keep, first=0, last=0, per_head=True):
+    """codes [2][blocks, H, bs, d] uint8 and scale [2][blocks, H] (K and V), changed in place.  -> kept, per sequence and head (one for all
+    with per_head False) a list of places; delta; weight_out: a dict (block, head, place) -> weight; and which sequences are not in order."""
+    values = code_values(kind)
+    nb, H = scale[0].shape
+    kept, delta, out, wrong = [], [], {}, []
+    for b, T in enumerate(int(n) for n in kv_len):
+        row = [int(v) for v in table[b]]
+        if T < 0 or T > len(row) * block_size or any(not 0 <= row[j] < nb for j in range(-(-T // block_size))):
+            wrong.append(b)
+            delta.append(0)
+            kept.append(None)
+            continue
+        n = min(max(int(budget[b]), 0), max_keep, T)
+        delta.append(n - T)
+        where = [(row[t // block_size], t % block_size) for t in range(T)]
+        w = np.array([[weight[blk, h, at] for blk, at in where] for h in range(H)], dtype=np.float64).reshape(H, T)
+        rank = w if per_head else w.sum(0, keepdims=True).astype(np.float32).astype(np.float64)
+        rank = np.where(np.isnan(rank), -np.inf, rank)
+        mine = []
+        for r in rank:
+            key = [(-np.inf if t < first or t >= T - last else -r[t], t) for t in range(T)]
+            mine.append(sorted(t for _, t in sorted(key)[:n]))
+        kept.append(mine)
+        full = [[where[t] for t in range(T)]] * H
+        for h in range(H):
+            places = mine[h if per_head else 0]
+            for j, t in enumerate(places):
+                out[(*where[j][:1], h, where[j][1])] = w[h, t]
+            for i in range(2):
+                src = [(codes[i][full[h][t][0], h, full[h][t][1]].copy(), scale[i][full[h][t][0], h]) for t in places]
+                for j0 in range(0, n, block_size):
+                    part = range(j0, min(j0 + block_size, n))
+                    if all(places[j] == j for j in part):
+                        continue
+                    x = np.array([values[src[j][0]] * src[j][1] for j in part])
+                    s = least_scale(np.abs(x).max(), kind) if np.isfinite(x).all() else np.nan
+                    blk = row[j0 // block_size]
+                    codes[i][blk, h, :len(part)] = encode(x / s, kind) if s == s else 0
+                    scale[i][blk, h] = s
+    return kept, delta, out, wrong

@@ -2,43 +2,13 @@
 //
 // The division of the work, and the join of what it cuts, are those of the attention over the paged cache: a line of tiles of query
 // rows (new rows x heads of a group, so that a key that was read serves all of them) against steps of keys, in equal stretches.
-#include "attention_division.cuh"
 #include "attention_join.cuh"
+#include "attention_tc.cuh"
 
 #include <type_traits>
 
 namespace vscan {
 namespace kv {
-
-struct PromptParams : AttnParams {
-  const char* k;
-  const char* v;
-  long long k_seq, k_head, k_row, v_seq, v_head, v_row;   // bytes
-  const int32_t* kv_offset;
-  int kv_rows;
-};
-
-// First key row of sequence b in the buffer (padded: 0), and its keys, held inside the buffer
-__device__ __forceinline__ void key_span(const PromptParams& p, int b, int& first, int& n) {
-  const long long lo = p.kv_offset[b], given = max(p.kv_offset[b + 1] - lo, 0ll);
-  first = p.padded ? 0 : static_cast<int>(lo);
-  const long long room = p.padded ? p.kv_rows : lo < 0 ? 0 : max(p.kv_rows - lo, 0ll);
-  n = static_cast<int>(min(given, room));
-}
-
-__device__ __forceinline__ Sequence sequence_at(const PromptParams& p, int b) {
-  Sequence s;
-  const long long lo = p.row_offset[b], given = max(p.row_offset[b + 1] - lo, 0ll);
-  s.first = p.padded ? 0 : static_cast<int>(lo);
-  const long long room = p.padded ? p.rows : lo < 0 ? 0 : max(p.rows - lo, 0ll);
-  s.n = static_cast<int>(min(min(given, room), static_cast<long long>(p.max_q_len)));
-  int first;
-  key_span(p, b, first, s.len);
-  s.start = max(static_cast<long long>(p.kv_offset[b + 1]) - p.kv_offset[b], 0ll) - given;
-  s.tiles = s.units = 0;
-  s.weight = 0;
-  return s;
-}
 
 // ---------------------------------------------------------------------------------------------- products on the CUDA cores
 // float32 queries (no rounding of queries or weights to 16 bits), and bf16 heads of more than 128 channels.  A CTA takes 64 query rows and
@@ -260,14 +230,17 @@ static vscan_status validate_prompt(const vscan_attention_desc* d) {
 }
 
 // Rows of a tile, keys of a step, CTAs of the launch
-struct PromptPlan { int tile_rows, keys; unsigned ctas; };
+struct PromptPlan { int tile_rows, keys, whole; unsigned ctas; };
 
-static PromptPlan plan_prompt(const vscan_attention_desc* d) {
+static bool prompt_tensor(const vscan_attention_desc* d) { return d->dtype == VSCAN_BF16 && d->head_dim <= 128 && d->kv_rows > 0; }
+
+static PromptPlan plan_prompt(const vscan_attention_desc* d, bool tensor) {
   PromptPlan pl;
   const int group = d->q_heads / d->kv_heads;
-  pl.tile_rows = kFlatRows;
-  pl.keys = kFlatKeys;
-  const int64_t resident = d->head_dim > 128 ? 1 : 2;
+  pl.tile_rows = tensor ? kPtRows : kFlatRows;
+  pl.keys = tensor ? kPtKeys : kFlatKeys;
+  pl.whole = tensor ? kPtWhole : kFlatWhole;
+  const int64_t resident = tensor || d->head_dim > 128 ? 1 : 2;
   // as many CTAs as fit the SMs at once, no more than there can be steps
   const int64_t rows = d->padded ? static_cast<int64_t>(d->batch) * (d->rows < d->max_q_len ? d->rows : d->max_q_len) : d->rows;
   const int64_t tiles = rows * group / pl.tile_rows + d->batch, steps = (static_cast<int64_t>(d->kv_rows) + pl.keys - 1) / pl.keys;
@@ -281,6 +254,37 @@ static PromptPlan plan_prompt(const vscan_attention_desc* d) {
 // workspace: status word | a flag per CTA | boundaries | partial results
 static size_t prompt_flag_bytes(const PromptPlan& pl) { return round_up(pl.ctas * sizeof(uint32_t), 256); }
 static size_t prompt_boundary_bytes(const PromptPlan& pl) { return round_up(pl.ctas * sizeof(Boundary), 256); }
+static size_t prompt_bytes(const PromptPlan& pl, int head_dim) {
+  return kStatusBytes + prompt_flag_bytes(pl) + prompt_boundary_bytes(pl) + round_up(2 * static_cast<size_t>(pl.ctas) * partial_floats(pl.tile_rows, head_dim) * 4, 256);
+}
+
+// Tiles of 128 rows x 64 channels of k or v.  False where TMA does not take the strides: heads or rows on top of each other, for one
+static bool rows_map(const vscan_attention_desc* d, const void* rows, const int64_t* st, CUtensorMap* map) {
+  const auto encode = tc::encode_fn();
+  if (!encode) return false;
+  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(d->head_dim), static_cast<cuuint64_t>(d->kv_rows), static_cast<cuuint64_t>(d->kv_heads),
+                              static_cast<cuuint64_t>(d->padded ? d->batch : 1)};
+  const int64_t step[3] = {st[2], st[1], d->padded ? st[0] : 0};
+  cuuint64_t strides[3];
+  for (int i = 0; i < 3; ++i) {
+    if (dims[i + 1] > 1 && step[i] == 0) return false;
+    strides[i] = dims[i + 1] > 1 ? static_cast<cuuint64_t>(step[i]) * 2 : 16;
+  }
+  const cuuint32_t box[4] = {64, kPtKeys, 1, 1}, each[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(rows), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DP>
+static vscan_status launch_prompt_tc(const PromptParams& p, const PromptPlan& pl, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
+  constexpr size_t smem = 1024 + (2 + kPtStages) * static_cast<size_t>(DP / 64) * kChunk;
+  VSCAN_CUDA_TRY(allow_smem(prompt_tc_kernel<DP>, smem));
+  prof_before("attention_tc", stream);
+  VSCAN_CUDA_TRY(launch_dependent(prompt_tc_kernel<DP>, dim3(pl.ctas), dim3(kPtThreads), smem, stream, p, k, v));
+  prof_after(stream);
+  VSCAN_AFTER_LAUNCH();
+  return VSCAN_OK;
+}
 
 template <typename T, int DP>
 static vscan_status launch_flat(const PromptParams& p, const PromptPlan& pl, cudaStream_t stream) {
@@ -294,12 +298,14 @@ static vscan_status launch_flat(const PromptParams& p, const PromptPlan& pl, cud
 }
 
 template <typename T>
-static vscan_status launch_prompt(const PromptParams& p, const PromptPlan& pl, cudaStream_t stream) {
-  const vscan_status st = p.head_dim <= 64 ? launch_flat<T, 64>(p, pl, stream) : p.head_dim <= 128 ? launch_flat<T, 128>(p, pl, stream)
-                                                                                                     : launch_flat<T, 256>(p, pl, stream);
-  if (st != VSCAN_OK) return st;
-  // nothing can have been cut when no sequence has more keys than a whole tile's, or when one CTA did it all
-  if (p.kv_rows <= kFlatWhole * pl.keys || pl.ctas == 1) return VSCAN_OK;
+static vscan_status launch_flats(const PromptParams& p, const PromptPlan& pl, cudaStream_t stream) {
+  return p.head_dim <= 64 ? launch_flat<T, 64>(p, pl, stream) : p.head_dim <= 128 ? launch_flat<T, 128>(p, pl, stream) : launch_flat<T, 256>(p, pl, stream);
+}
+
+template <typename T>
+static vscan_status launch_prompt_join(const PromptParams& p, const PromptPlan& pl, cudaStream_t stream) {
+  // nothing can have been cut when no sequence has more keys than a tile that stays whole, or when one CTA did it all
+  if (p.kv_rows <= pl.whole * pl.keys || pl.ctas == 1) return VSCAN_OK;
   prof_before("attention_join", stream);
   const dim3 grid(pl.ctas, (pl.tile_rows + kJoinRows - 1) / kJoinRows);
   VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, grid, dim3(kJoinThreads), 0, stream, static_cast<const AttnParams&>(p), static_cast<int>(pl.ctas)));
@@ -317,9 +323,9 @@ extern "C" size_t vscan_attention_workspace_bytes(const vscan_attention_desc* d)
   if (!d || d->batch <= 0 || d->rows <= 0 || d->max_q_len <= 0 || d->q_heads <= 0 || d->kv_heads <= 0 || d->head_dim <= 0 || d->head_dim > 256 ||
       d->q_heads / d->kv_heads > 64 || d->kv_rows < 0)
     return kStatusBytes;
-  const kv::PromptPlan pl = kv::plan_prompt(d);
-  return kStatusBytes + kv::prompt_flag_bytes(pl) + kv::prompt_boundary_bytes(pl) +
-         round_up(2 * static_cast<size_t>(pl.ctas) * kv::partial_floats(pl.tile_rows, d->head_dim) * 4, 256);
+  const size_t flat = kv::prompt_bytes(kv::plan_prompt(d, false), d->head_dim);      // strides decide between the two
+  const size_t tensor = kv::prompt_tensor(d) ? kv::prompt_bytes(kv::plan_prompt(d, true), d->head_dim) : 0;
+  return flat > tensor ? flat : tensor;
 }
 
 extern "C" vscan_status vscan_attention(const vscan_attention_desc* d, void* workspace, size_t workspace_bytes, void* stream_) {
@@ -331,7 +337,9 @@ extern "C" vscan_status vscan_attention(const vscan_attention_desc* d, void* wor
     VSCAN_CUDA_TRY(cudaMemsetAsync(workspace, 0, sizeof(uint32_t), stream));
     return VSCAN_OK;
   }
-  const kv::PromptPlan pl = kv::plan_prompt(d);
+  CUtensorMap k_map, v_map;
+  const bool tensor = kv::prompt_tensor(d) && kv::rows_map(d, d->k, d->k_stride, &k_map) && kv::rows_map(d, d->v, d->v_stride, &v_map);
+  const kv::PromptPlan pl = kv::plan_prompt(d, tensor);
   const long long e = static_cast<long long>(dtype_bytes(d->dtype));
   char* ws = static_cast<char*>(workspace);
   kv::PromptParams p = {};
@@ -355,5 +363,8 @@ extern "C" vscan_status vscan_attention(const vscan_attention_desc* d, void* wor
   ws += kv::prompt_flag_bytes(pl);
   p.boundary = reinterpret_cast<kv::Boundary*>(ws);
   p.partial = reinterpret_cast<float*>(ws + kv::prompt_boundary_bytes(pl));
-  return d->dtype == VSCAN_F32 ? kv::launch_prompt<float>(p, pl, stream) : kv::launch_prompt<__nv_bfloat16>(p, pl, stream);
+  const vscan_status done = tensor ? (d->head_dim <= 64 ? kv::launch_prompt_tc<64>(p, pl, k_map, v_map, stream) : kv::launch_prompt_tc<128>(p, pl, k_map, v_map, stream))
+                            : d->dtype == VSCAN_F32 ? kv::launch_flats<float>(p, pl, stream) : kv::launch_flats<__nv_bfloat16>(p, pl, stream);
+  if (done != VSCAN_OK) return done;
+  return d->dtype == VSCAN_F32 ? kv::launch_prompt_join<float>(p, pl, stream) : kv::launch_prompt_join<__nv_bfloat16>(p, pl, stream);
 }

@@ -1,0 +1,493 @@
+// Attention over whole prompts for bf16 on the 5th-generation tensor cores, head_dim up to 128.
+//
+// A CTA takes 256 query rows (new rows x heads of a group) of one KV head as two tiles of 128 and runs over its stretch of the keys,
+// 128 at a time:
+//   warps 0-3, 4-7   tile 0, 1: a thread a query row.  Scores from tensor memory into registers, running maximum and sum, weights back to
+//                    tensor memory as bf16, over the scores that they come from
+//   warps 8-11       the results of both tiles: tensor memory to memory, while the others begin the next piece; and the values of a step
+//                    that some row does not see in full (below)
+//   warp 12          issues the products: S[128 x 128] = Q K^T (operands in shared memory), O[128 x d] += P V with P read from tensor
+//                    memory and V, tokens down and channels across, as the MN-major operand
+//   warp 13          K and V by TMA, a ring of four tiles of 128 rows
+//   warps 14, 15     the queries of tile 0, 1: rows of a packed group are gathered, 16 bytes a lane and copy
+// The two tiles take turns: while one's weights are made, the other's products run.  A step takes the tensor cores 2,048 cycles (32
+// products of 64) and the exponentials, 32,768 at 16 a cycle, as many.
+//
+// The reference that is taken off a row's scores is raised only when a score is over it by 2^kLazy, so the sums are seldom rescaled; weights
+// are then up to 2^kLazy, which bf16 does not mind.  Weights are rounded to bf16, whose error (2^-9 of each weight, of either sign) is
+// averaged over the keys and stays below the rounding of the result; their sum is taken before the rounding.
+//
+// Masked weights are 0, but 0 times an infinity is not: in a step that some row does not see in full, values that are not finite are
+// made 0 in shared memory before the product, and what they give to the rows that do see them is put together beside it.
+// Every wait is bounded; on expiry the CTA says so in its flag word, frees its tensor memory and returns.
+#pragma once
+
+#include "attention_prompt.cuh"
+#include "kv_attention_tc.cuh"
+
+namespace vscan {
+namespace kv {
+
+constexpr int kPtThreads = 512, kPtRows = 256, kPtKeys = 128, kPtWhole = 4;
+constexpr int kPtHelper = 8, kPtIssuer = 12, kPtKeysLoader = 13, kPtQueries = 14;   // first warp of each role
+constexpr int kPtStages = 4;
+// 512 threads start with 128 registers each: 256 x 192 + 128 x 72 + 128 x 56 = 512 x 128.
+using PtShape = TileShape<kPtThreads, kPtRows, kPtKeys, kPtWhole>;
+
+struct PtShared {
+  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2], o_free[2], stat_full[2];   // of the tiles
+  uint64_t kv_full[kPtStages], kv_empty[kPtStages];
+  uint64_t dirty[2], clean[2];                // of steps that are seen in part, in turn: their values are under way, and cleaned
+  uint32_t tmem_base;
+  int abort_flag;
+  float2 stat[2][128];                        // [tile][row]: reference and sum
+  uint32_t odd[2][128][8];                    // [tile][row]: channels that get +inf (4 words) and -inf
+  uint32_t found[2][4];                       // of a step that is seen in part: keys whose values are not all finite, a word of each warp
+  DivisionShared division;
+};
+
+// ---------------------------------------------------------------------------------------------- instructions
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+// 16 bytes, or zeros, to shared memory
+__device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+// bf16 x bf16 -> float32, M = 128; b_mn: the second operand MN-major
+__device__ __forceinline__ uint32_t idesc_bf16(int n, bool b_mn) { return idesc_f16(n, b_mn) | (1u << 7) | (1u << 10); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 "
+      "[%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+        "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+        "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+        "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      : "memory");
+}
+
+
+// A wait that may last for all of a piece: the limit of the other waits, 4 s or some two million steps, is granted once more for every
+// 2^17 keys that there may be.  If another role gives up, so does this wait.
+__device__ __forceinline__ bool wait_piece(const PromptParams& p, uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  bool got = false;
+  for (int turn = p.kv_rows >> 17; turn >= 0 && !got && !*abort_flag; --turn)
+    for (uint32_t i = 0; i < tc::kSpinLimit && !got; ++i) {
+      got = tc::mbar_try_wait(bar, parity);
+      if ((i & 1023u) == 1023u && *abort_flag) break;
+    }
+  if (!got) *abort_flag = 1;
+  return __all_sync(0xffffffffu, got);
+}
+
+// Steps of a piece that some row does not see in full: from this one on
+__device__ __forceinline__ int first_partial(const PromptParams& p, const TcPiece& pc) {
+  return max(pc.u0, visible(p, pc.q.s, pc.tile * kPtRows / p.group) / kPtKeys);
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p, const __grid_constant__ CUtensorMap k_map,
+                                                                  const __grid_constant__ CUtensorMap v_map) {
+  using namespace tc;
+  constexpr int kDChunks = DP / 64, kTileBytes = kDChunks * kChunk;
+  extern __shared__ unsigned char smem_dyn[];
+  __shared__ PtShared sh;
+  unsigned char* base = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
+  unsigned char* q_sh = base;                      // [2 tiles]
+  unsigned char* kv_sh = q_sh + 2 * kTileBytes;    // [stages]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int D = p.head_dim;
+  volatile int* abort_flag = &sh.abort_flag;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 4);
+      mbar_init(&sh.o_done[i], 1); mbar_init(&sh.o_free[i], 4); mbar_init(&sh.stat_full[i], 4);
+      mbar_init(&sh.dirty[i], 1); mbar_init(&sh.clean[i], 4);
+    }
+    for (int i = 0; i < kPtStages; ++i) { mbar_init(&sh.kv_full[i], 1); mbar_init(&sh.kv_empty[i], 1); }
+    sh.abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kPtIssuer) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem_base;              // scores of tile t at column 128 t; sums at 256 + 128 t
+  grid_dependency_wait();
+  TcStretch st = tc_locate<PtShape>(p, sh.division);
+  if (threadIdx.x == 0) {
+    if (blockIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = 0; }
+    p.boundary[blockIdx.x].seg1 = 0;
+    p.flags[blockIdx.x] = 0;
+  }
+  __syncthreads();
+  TcPiece pc;
+
+  if (warp < kPtHelper) {
+    // ============================================================ a thread a query row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    const int tile = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t s_addr = tmem + lanes + tile * 128;            // this row's scores, and its weights
+    const uint32_t o_addr = tmem + lanes + 256 + tile * 128;
+    const float factor = fmaxf(fabsf(p.scale_log2e), 0x1p-126f);  // held above 0: a masked score stays -inf
+    const bool negative = p.scale_log2e < 0.f;
+    int n_it = 0, n_piece = 0;                                    // steps and pieces of this tile so far
+    bool ok = true;
+    while (ok && tc_next<PtShape>(p, st, pc)) {
+      if (pc.u0 > 0 && threadIdx.x == 0)
+        p.boundary[blockIdx.x] = {pc.seg0, pc.seg1, st.quota, pc.b, pc.head, pc.tile, pc.q.s.first, pc.n_rows, 0};
+      if (tile * 128 >= pc.n_rows) continue;
+      const int in_tile = tile * 128 + r;
+      const int seen = in_tile < pc.n_rows ? visible(p, pc.q.s, (pc.tile * kPtRows + in_tile) / p.group) : 0;
+      float m = -INFINITY, l = 0.f;      // reference and sum of the weights, in units of 2^m
+      for (int u = pc.u0; u < pc.u1; ++u, ++n_it) {
+        ok = u == pc.u0 ? wait_piece(p, &sh.s_full[tile], n_it & 1, abort_flag) : mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t v[128];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) tmem_read32(s_addr + h * 32, v + h * 32);
+        if (negative) {
+#pragma unroll
+          for (int k = 0; k < 128; ++k) v[k] ^= 0x80000000u;
+        }
+        const int vis = seen - u * kPtKeys;
+        if (__any_sync(0xffffffffu, vis < kPtKeys)) {
+#pragma unroll
+          for (int k = 0; k < 128; ++k)
+            if (k >= vis) v[k] = 0xff800000u;      // -inf
+        }
+        float top[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top[k] = __uint_as_float(v[k]);
+#pragma unroll
+        for (int k = 4; k < 124; k += 8)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top[i] = fmaxf(fmaxf(top[i], __uint_as_float(v[k + i])), __uint_as_float(v[k + 4 + i]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], __uint_as_float(v[124 + i]));
+        const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * factor;
+        if (__any_sync(0xffffffffu, most > m + kLazy)) {
+          const float now = fmaxf(m, most), f = now == m ? 1.f : ex2(m - now);
+          m = now;
+          l *= f;
+          // (the products with V of the step before are done: this step's scores were issued after them)
+          if (u > pc.u0 && __any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 16) {
+              uint32_t x[16];
+              tmem_read16(o_addr + c, x);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+              tmem_st16(o_addr + c, x);
+            }
+          }
+        }
+        const float minus_m = m == -INFINITY ? 0.f : -m;
+        const uint64_t mul = pair(factor, factor), add = pair(minus_m, minus_m);
+        uint64_t sums[2] = {0, 0};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            const int at = h * 64 + 2 * k;
+            const float2 x = unpair(fma2(pair(__uint_as_float(v[at]), __uint_as_float(v[at + 1])), mul, add));
+            const float e0 = ex2(x.x), e1 = ex2(x.y);
+            sums[k & 1] = add2(sums[k & 1], pair(e0, e1));
+            w[k] = pack_bf16(e0, e1);
+          }
+          tmem_st32(s_addr + h * 32, w);
+        }
+        const float2 both = unpair(add2(sums[0], sums[1]));
+        l += both.x + both.y;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_full[tile]);
+      }
+      if (!ok) break;
+      // ---- reference and sum to the warps that write the results, which are done with those of the piece before
+      if (n_piece > 0) ok = wait_piece(p, &sh.o_free[tile], (n_piece - 1) & 1, abort_flag);
+      if (!ok) break;
+      sh.stat[tile][r] = make_float2(m, l);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.stat_full[tile]);
+      ++n_piece;
+    }
+  } else if (warp < kPtIssuer) {
+    // ============================================================ results; values of steps that are seen in part
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    const int quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    int pos = 0;                 // tiles of K and V that the pieces before have taken
+    int n_partial = 0, n_piece[2] = {0, 0};
+    bool ok = true;
+    while (ok && tc_next<PtShape>(p, st, pc)) {
+      const int two = pc.n_rows > 128;
+      bool odd = false;          // some value is not finite; the same in all of these warps
+      int seen[2];
+      for (int t = 0; t < 2; ++t) seen[t] = t * 128 + r < pc.n_rows ? visible(p, pc.q.s, (pc.tile * kPtRows + t * 128 + r) / p.group) : 0;
+      for (int u = first_partial(p, pc); u < pc.u1 && ok; ++u, ++n_partial) {
+        const int at = pos + 1 + 2 * (u - pc.u0), s = at % kPtStages;
+        ok = wait_piece(p, &sh.dirty[n_partial & 1], (n_partial >> 1) & 1, abort_flag) &&
+             mbar_wait_warp(&sh.kv_full[s], (at / kPtStages) & 1, abort_flag);
+        if (!ok) break;
+        // a row of 64 channels is 128 bytes; 16-byte pieces of a row may be in any order
+        unsigned char* tile = kv_sh + s * kTileBytes;
+        unsigned found = 0;                        // rows of this thread's pieces, 16 a chunk
+#pragma unroll 1
+        for (int c = 0; c < kDChunks; ++c)
+#pragma unroll 4
+          for (int i = 0; i < 8; ++i) {
+            uint4* x = reinterpret_cast<uint4*>(tile + c * kChunk) + i * 128 + r;
+            uint4 w = *x;
+            auto bad = [](uint32_t y) { return ((y & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };     // exponent all ones
+            const uint32_t b0 = bad(w.x), b1 = bad(w.y), b2 = bad(w.z), b3 = bad(w.w);
+            if (b0 | b1 | b2 | b3) {
+              auto clear = [](uint32_t y, uint32_t b) { return y & ~((b & 0x8000u ? 0xffffu : 0u) | (b & 0x80000000u ? 0xffff0000u : 0u)); };
+              *x = make_uint4(clear(w.x, b0), clear(w.y, b1), clear(w.z, b2), clear(w.w, b3));
+              found |= 1u << i;
+            }
+          }
+        // key 16 i + 4 quarter + g is bit 4 i + g of the warp's word: eight lanes have a key's pieces
+        uint32_t mine = 0;
+        if (__any_sync(0xffffffffu, found != 0)) {
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t hits = __ballot_sync(0xffffffffu, (found >> i) & 1u);
+            for (int g = 0; g < 4; ++g)
+              if ((hits >> (8 * g)) & 0xffu) mine |= 1u << (4 * i + g);
+          }
+        }
+        uint32_t (&words)[4] = sh.found[n_partial & 1];
+        fence_async();
+        if (lane == 0) words[quarter] = mine;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.clean[n_partial & 1]);
+        ok = mbar_wait_warp(&sh.clean[n_partial & 1], (n_partial >> 1) & 1, abort_flag);    // the words of all four
+        if (ok && (words[0] | words[1] | words[2] | words[3])) {   // rare: what those values give to the rows that see them, from memory
+          if (!odd)
+            for (int t = 0; t < 2; ++t)
+              for (int i = 0; i < 8; ++i) sh.odd[t][r][i] = 0;
+          odd = true;
+          int key0, keys;
+          key_span(p, pc.b, key0, keys);
+          const char* v = p.v + (p.padded ? pc.b * p.v_seq : key0 * p.v_row) + pc.head * p.v_head;
+          const int t1 = min(max(seen[0], seen[1]), (u + 1) * kPtKeys);
+          for (int t = u * kPtKeys; t < t1; ++t) {
+            if (!((words[(t >> 2) & 3] >> (((t >> 4) & 7) * 4 + (t & 3))) & 1u)) continue;
+            for (int c = 0; c < D; ++c) {
+              const float x = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(v + t * p.v_row)[c]);
+              if (x - x == 0.f) continue;
+              for (int i = 0; i < 2; ++i) {
+                if (t >= seen[i]) continue;
+                if (!(x < 0.f)) sh.odd[i][r][c >> 5] |= 1u << (c & 31);
+                if (!(x > 0.f)) sh.odd[i][r][4 + (c >> 5)] |= 1u << (c & 31);
+              }
+            }
+          }
+        }
+      }
+      pos += 2 * (pc.u1 - pc.u0);
+      const bool complete = pc.u0 == 0 && pc.u1 == pc.units;
+      for (int t = 0; t <= two && ok; ++t) {
+        ok = wait_piece(p, &sh.stat_full[t], n_piece[t] & 1, abort_flag) && wait_piece(p, &sh.o_done[t], n_piece[t] & 1, abort_flag);
+        if (!ok) break;
+        ++n_piece[t];
+        tc_fence_after();
+        const int in_tile = t * 128 + r;
+        const bool on = in_tile < pc.n_rows;
+        const float2 stat = sh.stat[t][r];
+        const int flat = pc.tile * kPtRows + (on ? in_tile : 0), i_row = flat / p.group;
+        const RowAt at = {i_row, pc.head * p.group + flat - i_row * p.group};
+        const float mul = complete ? (stat.y == 0.f ? 0.f : 1.f / stat.y) : 1.f;
+        float* part = p.partial + (static_cast<size_t>(blockIdx.x) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(kPtRows, D);
+        char* out = out_at(p, pc.b, pc.q.s.first, at);
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 32) {
+          uint32_t v[32];
+          tmem_read32(tmem + lanes + 256 + t * 128 + c, v);
+          if (on && c < D) {
+          float x[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) x[k] = __uint_as_float(v[k]);
+          if (odd) {
+            const uint32_t up = sh.odd[t][r][c >> 5], down = sh.odd[t][r][4 + (c >> 5)];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              if ((up >> k) & 1u) x[k] += INFINITY;
+              if ((down >> k) & 1u) x[k] -= INFINITY;
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 32; k += 8) {
+            if (c + k >= D) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[k + i] *= mul;
+            if (complete) {
+              st_16(out + (c + k) * 2, Vec16<__nv_bfloat16>::pack(x + k));
+            } else {
+              *reinterpret_cast<float4*>(part + static_cast<size_t>(in_tile) * D + c + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+              *reinterpret_cast<float4*>(part + static_cast<size_t>(in_tile) * D + c + k + 4) = make_float4(x[k + 4], x[k + 5], x[k + 6], x[k + 7]);
+            }
+          }
+          }
+          __syncwarp();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.o_free[t]);
+        if (on) {
+          if (!complete) { part[kPtRows * D + in_tile] = stat.x; part[kPtRows * D + kPtRows + in_tile] = stat.y; }
+          else if (p.lse) *lse_at(p, pc.b, pc.q.s.first, at) = log_sum(stat.x, stat.y);
+        }
+      }
+    }
+  } else if (warp == kPtIssuer) {
+    // ============================================================ products
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    const uint32_t qk = idesc_bf16(kPtKeys, false), pv = idesc_bf16(DP, true);
+    const uint32_t q_addr = smem_u32(q_sh), kv_addr = smem_u32(kv_sh);
+    int pos = 0, n_partial = 0, n_it[2] = {0, 0}, n_piece[2] = {0, 0};
+    bool ok = true;
+    auto scores = [&](int t, int s) {        // S of tile t from stage s
+      const uint64_t a = smem_desc_sw128(q_addr + t * kTileBytes), b = smem_desc_sw128(kv_addr + s * kTileBytes);
+#pragma unroll
+      for (int c = 0; c < kDChunks; ++c) umma_f16_ss_x4(tmem + t * 128, a + c * (kChunk >> 4), b + c * (kChunk >> 4), qk, c > 0);
+    };
+    auto wait_kv = [&](int at) { return mbar_wait_warp(&sh.kv_full[at % kPtStages], (at / kPtStages) & 1, abort_flag); };
+    while (ok && tc_next<PtShape>(p, st, pc)) {
+      const int two = pc.n_rows > 128, partial = first_partial(p, pc);
+      for (int t = 0; t <= two && ok; ++t) ok = mbar_wait_warp(&sh.q_full[t], n_piece[t] & 1, abort_flag);
+      ok = ok && wait_kv(pos);
+      if (!ok) break;
+      tc_fence_after();
+      for (int t = 0; t <= two; ++t) {
+        scores(t, pos % kPtStages);
+        umma_commit_warp(&sh.s_full[t]);
+        if (pc.u0 + 1 == pc.u1) umma_commit_warp(&sh.q_empty[t]);
+      }
+      umma_commit_warp(&sh.kv_empty[pos % kPtStages]);
+      ++pos;
+      for (int u = pc.u0; u < pc.u1 && ok; ++u) {
+        const int vs = pos % kPtStages, ks = (pos + 1) % kPtStages;
+        const bool more = u + 1 < pc.u1;
+        ok = wait_kv(pos);
+        if (u >= partial) {
+          ok = ok && mbar_wait_warp(&sh.clean[n_partial & 1], (n_partial >> 1) & 1, abort_flag);
+          ++n_partial;
+        }
+#pragma unroll 1
+        for (int t = 0; t <= two && ok; ++t) {
+          if (u == pc.u0 && n_piece[t] > 0) ok = wait_piece(p, &sh.o_free[t], (n_piece[t] - 1) & 1, abort_flag);
+          ok = ok && mbar_wait_warp(&sh.p_full[t], n_it[t] & 1, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t b = desc_mn(kv_addr + vs * kTileBytes);
+          umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128, b, pv, u > pc.u0);
+          umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128 + 32, b + (64 * 128 >> 4), pv, true);
+          if (more) {            // over the weights that the products before this one read: products run in the order of their issue
+            if (t == 0) ok = wait_kv(pos + 1);
+            if (!ok) break;
+            tc_fence_after();
+            scores(t, ks);
+            umma_commit_warp(&sh.s_full[t]);
+            if (u + 2 == pc.u1) umma_commit_warp(&sh.q_empty[t]);
+          } else {
+            umma_commit_warp(&sh.o_done[t]);
+          }
+          ++n_it[t];
+        }
+        if (!ok) break;
+        umma_commit_warp(&sh.kv_empty[vs]);
+        if (more) umma_commit_warp(&sh.kv_empty[ks]);
+        pos += more ? 2 : 1;
+      }
+      for (int t = 0; t <= two; ++t) ++n_piece[t];
+    }
+    __syncwarp();
+  } else if (warp == kPtKeysLoader) {
+    // ============================================================ keys and values
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (lane == 0) {
+      int pos = 0, n_partial = 0;
+      bool ok = true;
+      while (ok && tc_next<PtShape>(p, st, pc)) {
+        int key0, keys;
+        key_span(p, pc.b, key0, keys);
+        const int partial = first_partial(p, pc), seq = p.padded ? pc.b : 0;
+        for (int i = 2 * pc.u0; i < 2 * pc.u1 && ok; ++i, ++pos) {
+          const int s = pos % kPtStages, u = i >> 1;
+          if (pos >= kPtStages) ok = mbar_wait(&sh.kv_empty[s], (pos / kPtStages - 1) & 1, abort_flag);
+          if (!ok) break;
+          mbar_arrive_expect_tx(&sh.kv_full[s], kTileBytes);
+#pragma unroll
+          for (int c = 0; c < kDChunks; ++c)
+            tma_load_4d(kv_sh + s * kTileBytes + c * kChunk, (i & 1) ? &v_map : &k_map, &sh.kv_full[s], c * 64, key0 + u * kPtKeys, pc.head, seq);
+          if ((i & 1) && u >= partial) { mbar_arrive(&sh.dirty[n_partial & 1]); ++n_partial; }
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ============================================================ queries of a tile
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    constexpr int kLanes = DP / 8, kPass = 32 / kLanes;      // 16-byte pieces of a row; rows of a pass
+    const int tile = warp - kPtQueries, piece = lane % kLanes, row0 = lane / kLanes;
+    const uint32_t dst0 = smem_u32(q_sh + tile * kTileBytes + (piece >> 3) * kChunk);
+    const bool in_dim = piece * 8 < D;
+    int n_piece = 0;
+    bool ok = true;
+    while (ok && tc_next<PtShape>(p, st, pc)) {
+      const int n = min(pc.n_rows - tile * 128, 128);        // (rows behind them stay what they were: nobody takes their results)
+      if (n <= 0) continue;
+      if (n_piece > 0) ok = wait_piece(p, &sh.q_empty[tile], (n_piece - 1) & 1, abort_flag);
+      if (!ok) break;
+      const int flat = pc.tile * kPtRows + tile * 128 + row0;
+      int i = flat / p.group, h = flat - i * p.group;
+      const char* src = q_at(p, pc.b, pc.q.s.first, RowAt{0, pc.head * p.group}) + piece * 16;
+#pragma unroll 4
+      for (int row = row0; row < n; row += kPass) {
+        copy_async_16(dst0 + row * 128 + (((piece & 7) ^ (row & 7)) << 4), in_dim ? src + i * p.q_row + h * p.q_head : src, in_dim);
+        for (h += kPass; h >= p.group; h -= p.group) ++i;
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.q_full[tile]);
+      ++n_piece;
+    }
+  }
+
+  // ------------------------------------------------------------ teardown
+  tc_fence_before();
+  __syncthreads();
+  if (sh.abort_flag) {
+    if (threadIdx.x == 0) p.flags[blockIdx.x] = VSCAN_ERR_TIMEOUT;
+    for (int i = 0; i < 64; ++i) __nanosleep(2000);   // products and copies still in flight end before their memory is given back
+    __syncthreads();
+  }
+  if (warp == kPtIssuer) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+  }
+}
+
+}  // namespace kv
+}  // namespace vscan

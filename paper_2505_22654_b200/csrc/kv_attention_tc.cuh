@@ -197,7 +197,7 @@ __device__ __forceinline__ int scale_binade(float s) {
 // A warp's wait for the first scores of a piece.  A tile that has no rows in the pieces before waits for all of those: the limit of
 // the other waits, 4 s or some two million steps, is granted once more for every 2^17 tokens that a table has room for.  If another
 // role gives up, so does this wait.
-__device__ __noinline__ bool wait_scores(uint64_t* bar, uint32_t parity, int more, volatile int* abort_flag) {
+static __device__ __noinline__ bool wait_scores(uint64_t* bar, uint32_t parity, int more, volatile int* abort_flag) {
   bool got = false;
   for (int turn = 0; turn <= more && !got && !*abort_flag; ++turn)
     for (uint32_t i = 0; i < tc::kSpinLimit && !got; ++i) {
