@@ -237,7 +237,7 @@ static bool prompt_tensor(const vscan_attention_desc* d) { return d->dtype == VS
 static PromptPlan plan_prompt(const vscan_attention_desc* d, bool tensor) {
   PromptPlan pl;
   const int group = d->q_heads / d->kv_heads;
-  pl.tile_rows = tensor ? kPtRows : kFlatRows;
+  pl.tile_rows = tensor ? 2 * (128 / group) * group : kFlatRows;      // whole tokens of the group's heads
   pl.keys = tensor ? kPtKeys : kFlatKeys;
   pl.whole = tensor ? kPtWhole : kFlatWhole;
   const int64_t resident = tensor || d->head_dim > 128 ? 1 : 2;
@@ -258,29 +258,38 @@ static size_t prompt_bytes(const PromptPlan& pl, int head_dim) {
   return kStatusBytes + prompt_flag_bytes(pl) + prompt_boundary_bytes(pl) + round_up(2 * static_cast<size_t>(pl.ctas) * partial_floats(pl.tile_rows, head_dim) * 4, 256);
 }
 
-// Tiles of 128 rows x 64 channels of k or v.  False where TMA does not take the strides: heads or rows on top of each other, for one
-static bool rows_map(const vscan_attention_desc* d, const void* rows, const int64_t* st, CUtensorMap* map) {
+// Boxes of 64 channels x `inner` x `outer` of q (heads of a group, tokens), k or v (rows, a head).  False where TMA does not take the strides: heads
+// or rows on top of each other, for one
+static bool rows_map(const vscan_attention_desc* d, const void* at, const int64_t (&sizes)[2], const int64_t (&steps)[2], int64_t seq_step, int inner,
+                     int outer, CUtensorMap* map) {
   const auto encode = tc::encode_fn();
   if (!encode) return false;
-  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(d->head_dim), static_cast<cuuint64_t>(d->kv_rows), static_cast<cuuint64_t>(d->kv_heads),
-                              static_cast<cuuint64_t>(d->padded ? d->batch : 1)};
-  const int64_t step[3] = {st[2], st[1], d->padded ? st[0] : 0};
-  cuuint64_t strides[3];
+  const int64_t all[3] = {sizes[0], sizes[1], d->padded ? d->batch : 1}, step[3] = {steps[0], steps[1], seq_step};
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(d->head_dim)}, strides[3];
   for (int i = 0; i < 3; ++i) {
-    if (dims[i + 1] > 1 && step[i] == 0) return false;
-    strides[i] = dims[i + 1] > 1 ? static_cast<cuuint64_t>(step[i]) * 2 : 16;
+    if (all[i] > 1 && step[i] == 0) return false;
+    dims[i + 1] = static_cast<cuuint64_t>(all[i]);
+    strides[i] = all[i] > 1 ? static_cast<cuuint64_t>(step[i]) * 2 : 16;
   }
-  const cuuint32_t box[4] = {64, kPtKeys, 1, 1}, each[4] = {1, 1, 1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(rows), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(inner), static_cast<cuuint32_t>(outer), 1}, each[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(at), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+struct PromptMaps { CUtensorMap q, k, v; };
+static bool prompt_maps(const vscan_attention_desc* d, PromptMaps& m) {
+  const int group = d->q_heads / d->kv_heads;
+  const int64_t q_sizes[2] = {d->q_heads, d->rows}, kv_sizes[2] = {d->kv_rows, d->kv_heads};
+  const int64_t q_steps[2] = {d->q_stride[1], d->q_stride[2]}, k_steps[2] = {d->k_stride[2], d->k_stride[1]}, v_steps[2] = {d->v_stride[2], d->v_stride[1]};
+  return rows_map(d, d->q, q_sizes, q_steps, d->q_stride[0], group, 128 / group, &m.q) &&
+         rows_map(d, d->k, kv_sizes, k_steps, d->k_stride[0], kPtKeys, 1, &m.k) && rows_map(d, d->v, kv_sizes, v_steps, d->v_stride[0], kPtKeys, 1, &m.v);
 }
 
 template <int DP>
-static vscan_status launch_prompt_tc(const PromptParams& p, const PromptPlan& pl, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
+static vscan_status launch_prompt_tc(const PromptParams& p, const PromptPlan& pl, const PromptMaps& m, cudaStream_t stream) {
   constexpr size_t smem = 1024 + (2 + kPtStages) * static_cast<size_t>(DP / 64) * kChunk;
   VSCAN_CUDA_TRY(allow_smem(prompt_tc_kernel<DP>, smem));
   prof_before("attention_tc", stream);
-  VSCAN_CUDA_TRY(launch_dependent(prompt_tc_kernel<DP>, dim3(pl.ctas), dim3(kPtThreads), smem, stream, p, k, v));
+  VSCAN_CUDA_TRY(launch_dependent(prompt_tc_kernel<DP>, dim3(pl.ctas), dim3(kPtThreads), smem, stream, p, m.q, m.k, m.v));
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
   return VSCAN_OK;
@@ -337,8 +346,8 @@ extern "C" vscan_status vscan_attention(const vscan_attention_desc* d, void* wor
     VSCAN_CUDA_TRY(cudaMemsetAsync(workspace, 0, sizeof(uint32_t), stream));
     return VSCAN_OK;
   }
-  CUtensorMap k_map, v_map;
-  const bool tensor = kv::prompt_tensor(d) && kv::rows_map(d, d->k, d->k_stride, &k_map) && kv::rows_map(d, d->v, d->v_stride, &v_map);
+  kv::PromptMaps maps;
+  const bool tensor = kv::prompt_tensor(d) && kv::prompt_maps(d, maps);
   const kv::PromptPlan pl = kv::plan_prompt(d, tensor);
   const long long e = static_cast<long long>(dtype_bytes(d->dtype));
   char* ws = static_cast<char*>(workspace);
@@ -363,7 +372,7 @@ extern "C" vscan_status vscan_attention(const vscan_attention_desc* d, void* wor
   ws += kv::prompt_flag_bytes(pl);
   p.boundary = reinterpret_cast<kv::Boundary*>(ws);
   p.partial = reinterpret_cast<float*>(ws + kv::prompt_boundary_bytes(pl));
-  const vscan_status done = tensor ? (d->head_dim <= 64 ? kv::launch_prompt_tc<64>(p, pl, k_map, v_map, stream) : kv::launch_prompt_tc<128>(p, pl, k_map, v_map, stream))
+  const vscan_status done = tensor ? (d->head_dim <= 64 ? kv::launch_prompt_tc<64>(p, pl, maps, stream) : kv::launch_prompt_tc<128>(p, pl, maps, stream))
                             : d->dtype == VSCAN_F32 ? kv::launch_flats<float>(p, pl, stream) : kv::launch_flats<__nv_bfloat16>(p, pl, stream);
   if (done != VSCAN_OK) return done;
   return d->dtype == VSCAN_F32 ? kv::launch_prompt_join<float>(p, pl, stream) : kv::launch_prompt_join<__nv_bfloat16>(p, pl, stream);

@@ -6,10 +6,12 @@
 namespace vscan {
 namespace kv {
 
-// Threads of a CTA, query rows of a tile, keys of a step, and the steps up to which a tile is not cut
-template <int THREADS, int ROWS, int KEYS, int WHOLE>
+// Threads of a CTA, query rows of a tile, keys of a step, and the steps up to which a tile is not cut.  ROWS 0: rows of a tile are known at
+// run time only.  EXTRA: what a tile weighs, in steps, beside its own: its start and end.
+template <int THREADS, int ROWS, int KEYS, int WHOLE, int EXTRA = 0>
 struct TileShape {
-  static constexpr int kThreads = THREADS, kRows = ROWS, kKeys = KEYS, kWhole = WHOLE;
+  static constexpr int kThreads = THREADS, kKeys = KEYS, kWhole = WHOLE, kExtra = EXTRA;
+  __device__ __forceinline__ static int rows(const AttnParams& p) { return ROWS > 0 ? ROWS : p.tile_rows; }
 };
 
 struct DivisionShared {
@@ -34,11 +36,16 @@ __device__ __forceinline__ long long step_weight(const AttnParams& p) { return s
 
 template <typename S>
 __device__ __forceinline__ long long tiles_before(const AttnParams& p, const TcSequence& q, long long k) {
-  const long long one = step_weight<S>(p);
-  if (!p.causal) return k * max(q.base, one);
+  const long long one = step_weight<S>(p), extra = k * one * S::kExtra;
+  if (!p.causal) return k * max(q.base, one) + extra;
   const long long n = min(k, static_cast<long long>(q.tiles - 1)), m = min(n, static_cast<long long>(q.light));
-  const long long sum = m * one + (n - m) * q.base + (n * (n + 1) - m * (m + 1)) * (S::kRows / 2);
+  const long long sum = m * one + (n - m) * q.base + (n * (n + 1) - m * (m + 1)) * (S::rows(p) / 2) + extra;
   return k < q.tiles ? sum : sum + max(q.base + q.rows, one);
+}
+
+// Quotient of numbers that nearly always fit 32 bits
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? static_cast<unsigned>(a) / static_cast<unsigned>(b) : a / b;
 }
 
 template <typename S, typename P>
@@ -46,16 +53,11 @@ __device__ __forceinline__ TcSequence tc_sequence_at(const P& p, int b) {
   TcSequence q;
   q.s = sequence_at(p, b);
   q.rows = static_cast<long long>(q.s.n) * p.group;
-  q.tiles = static_cast<int>((q.rows + S::kRows - 1) / S::kRows);
+  q.tiles = static_cast<int>(quotient(q.rows + S::rows(p) - 1, S::rows(p)));
   q.base = p.causal ? max(q.s.start, 0ll) * p.group : static_cast<long long>(q.s.len) * p.group;
-  q.light = static_cast<int>(max((max(step_weight<S>(p) - q.base, 0ll) + S::kRows - 1) / S::kRows - 1, 0ll));
+  q.light = static_cast<int>(max(quotient(max(step_weight<S>(p) - q.base, 0ll) + S::rows(p) - 1, S::rows(p)) - 1, 0ll));
   q.weight = q.tiles > 0 ? tiles_before<S>(p, q, q.tiles) : 0;
   return q;
-}
-
-// Quotient of numbers that nearly always fit 32 bits
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? static_cast<unsigned>(a) / static_cast<unsigned>(b) : a / b;
 }
 
 struct TcStretch { long long begin, end, quota, seq0; int b; };
@@ -82,7 +84,7 @@ __device__ __forceinline__ TcStretch tc_locate(const P& p, DivisionShared& sh) {
   }
   TcStretch st;
   // a stretch is at least a step long, so that no two cuts fall into one step
-  st.quota = max(quotient(total + gridDim.x - 1, gridDim.x), step_weight<S>(p));
+  st.quota = max(quotient(total + gridDim.x - 1, gridDim.x), step_weight<S>(p) * (1 + S::kExtra));
   st.begin = min(blockIdx.x * st.quota, total);
   st.end = min(st.begin + st.quota, total);
   long long at = before + incl - sum;
@@ -97,6 +99,13 @@ __device__ __forceinline__ TcStretch tc_locate(const P& p, DivisionShared& sh) {
   st.b = sh.b;
   st.seq0 = sh.seq0;
   return st;
+}
+
+// The step of a tile that place x of its weight falls into; what a tile weighs beside its steps lies in front of them
+template <typename S>
+__device__ __forceinline__ int step_at(long long x, long long per_unit, int units) {
+  if (S::kExtra > 0) x = max(x - S::kExtra * per_unit, 0ll);
+  return static_cast<int>(min(quotient(x, per_unit), static_cast<long long>(units)));
 }
 
 struct TcPiece {
@@ -120,13 +129,13 @@ __device__ __forceinline__ bool tc_next(const P& p, TcStretch& st, TcPiece& pc) 
     pc.head = static_cast<int>(head); pc.tile = lo; pc.b = st.b;
     pc.seg0 = st.begin - (rel - tiles_before<S>(p, pc.q, lo));
     const long long seg_end = pc.seg0 + tiles_before<S>(p, pc.q, lo + 1) - tiles_before<S>(p, pc.q, lo);
-    pc.n_rows = static_cast<int>(min(static_cast<long long>(S::kRows), pc.q.rows - static_cast<long long>(lo) * S::kRows));
-    pc.most = visible(p, pc.q.s, (lo * S::kRows + pc.n_rows - 1) / p.group);
+    pc.n_rows = static_cast<int>(min(static_cast<long long>(S::rows(p)), pc.q.rows - static_cast<long long>(lo) * S::rows(p)));
+    pc.most = visible(p, pc.q.s, (lo * S::rows(p) + pc.n_rows - 1) / p.group);
     pc.units = max(1, (pc.most + S::kKeys - 1) / S::kKeys);
     const long long per_unit = step_weight<S>(p);
-    pc.seg1 = min(seg_end, pc.seg0 + pc.units * per_unit);
-    pc.u0 = static_cast<int>(min(quotient(st.begin - pc.seg0, per_unit), static_cast<long long>(pc.units)));
-    pc.u1 = st.end >= seg_end ? pc.units : static_cast<int>(min(quotient(st.end - pc.seg0, per_unit), static_cast<long long>(pc.units)));
+    pc.seg1 = min(seg_end, pc.seg0 + (pc.units + S::kExtra) * per_unit);
+    pc.u0 = step_at<S>(st.begin - pc.seg0, per_unit, pc.units);
+    pc.u1 = st.end >= seg_end ? pc.units : step_at<S>(st.end - pc.seg0, per_unit, pc.units);
     const bool whole = pc.units <= S::kWhole, starts = st.begin == pc.seg0;
     if (whole) { pc.u0 = 0; pc.u1 = pc.units; }
     st.begin = seg_end;

@@ -1,6 +1,6 @@
 // Attention over whole prompts for bf16 on the 5th-generation tensor cores, head_dim up to 128.
 //
-// A CTA takes 256 query rows (new rows x heads of a group) of one KV head as two tiles of 128 and runs over its stretch of the keys,
+// A CTA takes up to 256 query rows (new rows x heads of a group) of one KV head as two tiles of up to 128 and runs over its stretch of the keys,
 // 128 at a time:
 //   warps 0-3, 4-7   tile 0, 1: a thread a query row.  Scores from tensor memory into registers, running maximum and sum, weights back to
 //                    tensor memory as bf16, over the scores that they come from
@@ -8,8 +8,9 @@
 //                    that some row does not see in full (below)
 //   warp 12          issues the products: S[128 x 128] = Q K^T (operands in shared memory), O[128 x d] += P V with P read from tensor
 //                    memory and V, tokens down and channels across, as the MN-major operand
-//   warp 13          K and V by TMA, a ring of four tiles of 128 rows
-//   warps 14, 15     the queries of tile 0, 1: rows of a packed group are gathered, 16 bytes a lane and copy
+//   warp 13          queries, K and V by TMA; K and V in a ring of four tiles of 128 rows
+//   warp 14          plans: what the next pieces of the stretch are, a few ahead of all others
+// A tile of 128 rows has whole tokens of the group's heads (126 rows for groups of seven), so that TMA can bring them.
 // The two tiles take turns: while one's weights are made, the other's products run.  A step takes the tensor cores 2,048 cycles (32
 // products of 64) and the exponentials, 32,768 at 16 a cycle, as many.
 //
@@ -28,11 +29,19 @@
 namespace vscan {
 namespace kv {
 
-constexpr int kPtThreads = 512, kPtRows = 256, kPtKeys = 128, kPtWhole = 4;
-constexpr int kPtHelper = 8, kPtIssuer = 12, kPtKeysLoader = 13, kPtQueries = 14;   // first warp of each role
-constexpr int kPtStages = 4;
+constexpr int kPtThreads = 512, kPtKeys = 128, kPtWhole = 4, kPtExtra = 1;
+constexpr int kPtHelper = 8, kPtIssuer = 12, kPtLoader = 13, kPtPlanner = 14;   // first warp of each role
+constexpr int kPtStages = 4, kPtPlan = 4;
+constexpr int kPtReaders = 14;       // warps that read the plan
 // 512 threads start with 128 registers each: 256 x 192 + 128 x 72 + 128 x 56 = 512 x 128.
-using PtShape = TileShape<kPtThreads, kPtRows, kPtKeys, kPtWhole>;
+using PtShape = TileShape<kPtThreads, 0, kPtKeys, kPtWhole, kPtExtra>;
+
+struct PtPiece {         // steps u0 .. u1 - 1 of a tile; u1 = 0: there is no more
+  int b, head, tile, n_rows, first, key0, len, u0, u1, units;
+  int partial;           // steps from this one on are not seen in full by some row
+  int token;             // of the sequence's rows, the tile's first
+  long long start;       // position of the sequence's first row
+};
 
 struct PtShared {
   uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2], o_free[2], stat_full[2];   // of the tiles
@@ -43,6 +52,8 @@ struct PtShared {
   float2 stat[2][128];                        // [tile][row]: reference and sum
   uint32_t odd[2][128][8];                    // [tile][row]: channels that get +inf (4 words) and -inf
   uint32_t found[2][4];                       // of a step that is seen in part: keys whose values are not all finite, a word of each warp
+  uint64_t plan_full[kPtPlan], plan_empty[kPtPlan];
+  PtPiece plan[kPtPlan];
   DivisionShared division;
 };
 
@@ -52,10 +63,6 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, u
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
       ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
       : "memory");
-}
-// 16 bytes, or zeros, to shared memory
-__device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src, bool on) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
 // bf16 x bf16 -> float32, M = 128; b_mn: the second operand MN-major
 __device__ __forceinline__ uint32_t idesc_bf16(int n, bool b_mn) { return idesc_f16(n, b_mn) | (1u << 7) | (1u << 10); }
@@ -90,14 +97,72 @@ __device__ __forceinline__ bool wait_piece(const PromptParams& p, uint64_t* bar,
   return __all_sync(0xffffffffu, got);
 }
 
-// Steps of a piece that some row does not see in full: from this one on
-__device__ __forceinline__ int first_partial(const PromptParams& p, const TcPiece& pc) {
-  return max(pc.u0, visible(p, pc.q.s, pc.tile * kPtRows / p.group) / kPtKeys);
+// Keys that row `token` of a sequence sees
+__device__ __forceinline__ int keys_seen(const PromptParams& p, const PtPiece& pc, int token) {
+  if (!p.causal) return pc.len;
+  return static_cast<int>(min(max(pc.start + token + 1, 0ll), static_cast<long long>(pc.len)));
 }
 
+// The pieces of a CTA's stretch one after another, by a warp whose lanes all do the same
+struct PtPlanner {
+  TcStretch st;
+  TcSequence q;
+  long long seg0;        // of the tile that the stretch is in
+  int key0, head, tile;
+  bool inside;
+
+  __device__ __forceinline__ void enter(const PromptParams& p, int b) {
+    st.b = b;
+    q = tc_sequence_at<PtShape>(p, b);
+    int keys;
+    key_span(p, b, key0, keys);
+  }
+  __device__ __forceinline__ bool next(const PromptParams& p, PtPiece& pc, Boundary& cut) {
+    const long long one = step_weight<PtShape>(p);
+    while (st.begin < st.end) {
+      if (!inside) {                                     // the stretch's first tile takes a search
+        enter(p, st.b);
+        head = static_cast<int>(quotient(st.begin - st.seq0, q.weight));
+        const long long rel = st.begin - st.seq0 - head * q.weight;
+        int lo = 0, hi = q.tiles;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (tiles_before<PtShape>(p, q, mid) <= rel) lo = mid; else hi = mid;
+        }
+        tile = lo;
+        seg0 = st.begin - (rel - tiles_before<PtShape>(p, q, lo));
+        inside = true;
+      } else if (tile == q.tiles) {
+        tile = 0;
+        if (++head == p.kv_heads) {
+          head = 0;
+          do enter(p, st.b + 1); while (q.tiles == 0);   // there is one: the stretch goes on
+        }
+      }
+      const long long mine = !p.causal ? q.base : q.base + (tile + 1 < q.tiles ? static_cast<long long>(p.tile_rows) * (tile + 1) : q.rows);
+      const long long seg_end = seg0 + max(mine, one) + kPtExtra * one;
+      pc.b = st.b; pc.head = head; pc.tile = tile; pc.first = q.s.first; pc.key0 = key0; pc.len = q.s.len; pc.start = q.s.start;
+      const int tokens = p.tile_rows / p.group;
+      pc.token = tile * tokens;
+      const int n = min(q.s.n - pc.token, tokens);
+      pc.n_rows = n * p.group;
+      pc.units = max(1, (keys_seen(p, pc, pc.token + n - 1) + kPtKeys - 1) / kPtKeys);
+      const bool starts = st.begin == seg0, ends = st.end >= seg_end, whole = pc.units <= kPtWhole;
+      pc.u0 = whole || starts ? 0 : step_at<PtShape>(st.begin - seg0, one, pc.units);
+      pc.u1 = whole || ends ? pc.units : step_at<PtShape>(st.end - seg0, one, pc.units);
+      pc.partial = max(pc.u0, keys_seen(p, pc, pc.token) / kPtKeys);
+      cut = {seg0, min(seg_end, seg0 + (pc.units + kPtExtra) * one), st.quota, st.b, head, tile, q.s.first, pc.n_rows, 0};
+      ++tile;
+      st.begin = seg0 = seg_end;
+      if (whole ? starts : pc.u0 < pc.u1) return true;
+    }
+    return false;
+  }
+};
+
 template <int DP>
-__global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p, const __grid_constant__ CUtensorMap k_map,
-                                                                  const __grid_constant__ CUtensorMap v_map) {
+__global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p, const __grid_constant__ CUtensorMap q_map,
+                                                                  const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using namespace tc;
   constexpr int kDChunks = DP / 64, kTileBytes = kDChunks * kChunk;
   extern __shared__ unsigned char smem_dyn[];
@@ -116,6 +181,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       mbar_init(&sh.dirty[i], 1); mbar_init(&sh.clean[i], 4);
     }
     for (int i = 0; i < kPtStages; ++i) { mbar_init(&sh.kv_full[i], 1); mbar_init(&sh.kv_empty[i], 1); }
+    for (int i = 0; i < kPtPlan; ++i) { mbar_init(&sh.plan_full[i], 1); mbar_init(&sh.plan_empty[i], kPtReaders); }
     sh.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -128,14 +194,26 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;              // scores of tile t at column 128 t; sums at 256 + 128 t
   grid_dependency_wait();
-  TcStretch st = tc_locate<PtShape>(p, sh.division);
+  const TcStretch st = tc_locate<PtShape>(p, sh.division);
   if (threadIdx.x == 0) {
     if (blockIdx.x == 0) { p.status[0] = kStatusFlags | gridDim.x; p.status[1] = 0; }
     p.boundary[blockIdx.x].seg1 = 0;
     p.flags[blockIdx.x] = 0;
   }
   __syncthreads();
-  TcPiece pc;
+  PtPiece pc;
+  int n_plan = 0;                                  // pieces read so far
+  // The next piece of the plan; false where there is none, or another role gave up
+  auto next = [&]() {
+    const int slot = n_plan % kPtPlan;
+    if (!wait_piece(p, &sh.plan_full[slot], (n_plan / kPtPlan) & 1, abort_flag)) return false;
+    pc = sh.plan[slot];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.plan_empty[slot]);
+    ++n_plan;
+    return pc.u1 > 0;
+  };
+  const int tokens = p.tile_rows / (2 * p.group), half = tokens * p.group;      // tokens and rows of a tile of 128
 
   if (warp < kPtHelper) {
     // ============================================================ a thread a query row
@@ -148,12 +226,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
     const bool negative = p.scale_log2e < 0.f;
     int n_it = 0, n_piece = 0;                                    // steps and pieces of this tile so far
     bool ok = true;
-    while (ok && tc_next<PtShape>(p, st, pc)) {
-      if (pc.u0 > 0 && threadIdx.x == 0)
-        p.boundary[blockIdx.x] = {pc.seg0, pc.seg1, st.quota, pc.b, pc.head, pc.tile, pc.q.s.first, pc.n_rows, 0};
-      if (tile * 128 >= pc.n_rows) continue;
-      const int in_tile = tile * 128 + r;
-      const int seen = in_tile < pc.n_rows ? visible(p, pc.q.s, (pc.tile * kPtRows + in_tile) / p.group) : 0;
+    while (ok && next()) {
+      if (tile * half >= pc.n_rows) continue;
+      const int seen = r < half && tile * half + r < pc.n_rows ? keys_seen(p, pc, pc.token + tile * tokens + r / p.group) : 0;
       float m = -INFINITY, l = 0.f;      // reference and sum of the weights, in units of 2^m
       for (int u = pc.u0; u < pc.u1; ++u, ++n_it) {
         ok = u == pc.u0 ? wait_piece(p, &sh.s_full[tile], n_it & 1, abort_flag) : mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
@@ -235,15 +310,17 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const int quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    const int r_token = r / p.group, r_head = r - r_token * p.group;
     int pos = 0;                 // tiles of K and V that the pieces before have taken
     int n_partial = 0, n_piece[2] = {0, 0};
     bool ok = true;
-    while (ok && tc_next<PtShape>(p, st, pc)) {
-      const int two = pc.n_rows > 128;
+    while (ok && next()) {
+      const int two = pc.n_rows > half;
       bool odd = false;          // some value is not finite; the same in all of these warps
       int seen[2];
-      for (int t = 0; t < 2; ++t) seen[t] = t * 128 + r < pc.n_rows ? visible(p, pc.q.s, (pc.tile * kPtRows + t * 128 + r) / p.group) : 0;
-      for (int u = first_partial(p, pc); u < pc.u1 && ok; ++u, ++n_partial) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) seen[t] = r < half && t * half + r < pc.n_rows ? keys_seen(p, pc, pc.token + t * tokens + r_token) : 0;
+      for (int u = pc.partial; u < pc.u1 && ok; ++u, ++n_partial) {
         const int at = pos + 1 + 2 * (u - pc.u0), s = at % kPtStages;
         ok = wait_piece(p, &sh.dirty[n_partial & 1], (n_partial >> 1) & 1, abort_flag) &&
              mbar_wait_warp(&sh.kv_full[s], (at / kPtStages) & 1, abort_flag);
@@ -286,9 +363,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
             for (int t = 0; t < 2; ++t)
               for (int i = 0; i < 8; ++i) sh.odd[t][r][i] = 0;
           odd = true;
-          int key0, keys;
-          key_span(p, pc.b, key0, keys);
-          const char* v = p.v + (p.padded ? pc.b * p.v_seq : key0 * p.v_row) + pc.head * p.v_head;
+          const char* v = p.v + (p.padded ? pc.b * p.v_seq : pc.key0 * p.v_row) + pc.head * p.v_head;
           const int t1 = min(max(seen[0], seen[1]), (u + 1) * kPtKeys);
           for (int t = u * kPtKeys; t < t1; ++t) {
             if (!((words[(t >> 2) & 3] >> (((t >> 4) & 7) * 4 + (t & 3))) & 1u)) continue;
@@ -311,14 +386,13 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
         if (!ok) break;
         ++n_piece[t];
         tc_fence_after();
-        const int in_tile = t * 128 + r;
-        const bool on = in_tile < pc.n_rows;
+        const int in_tile = t * half + r;
+        const bool on = r < half && in_tile < pc.n_rows;
         const float2 stat = sh.stat[t][r];
-        const int flat = pc.tile * kPtRows + (on ? in_tile : 0), i_row = flat / p.group;
-        const RowAt at = {i_row, pc.head * p.group + flat - i_row * p.group};
+        const RowAt at = {pc.token + t * tokens + r_token, pc.head * p.group + r_head};
         const float mul = complete ? (stat.y == 0.f ? 0.f : 1.f / stat.y) : 1.f;
-        float* part = p.partial + (static_cast<size_t>(blockIdx.x) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(kPtRows, D);
-        char* out = out_at(p, pc.b, pc.q.s.first, at);
+        float* part = p.partial + (static_cast<size_t>(blockIdx.x) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(p.tile_rows, D);
+        char* out = out_at(p, pc.b, pc.first, at);
 #pragma unroll 1
         for (int c = 0; c < DP; c += 32) {
           uint32_t v[32];
@@ -354,8 +428,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.o_free[t]);
         if (on) {
-          if (!complete) { part[kPtRows * D + in_tile] = stat.x; part[kPtRows * D + kPtRows + in_tile] = stat.y; }
-          else if (p.lse) *lse_at(p, pc.b, pc.q.s.first, at) = log_sum(stat.x, stat.y);
+          if (!complete) { part[p.tile_rows * D + in_tile] = stat.x; part[p.tile_rows * D + p.tile_rows + in_tile] = stat.y; }
+          else if (p.lse) *lse_at(p, pc.b, pc.first, at) = log_sum(stat.x, stat.y);
         }
       }
     }
@@ -372,8 +446,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       for (int c = 0; c < kDChunks; ++c) umma_f16_ss_x4(tmem + t * 128, a + c * (kChunk >> 4), b + c * (kChunk >> 4), qk, c > 0);
     };
     auto wait_kv = [&](int at) { return mbar_wait_warp(&sh.kv_full[at % kPtStages], (at / kPtStages) & 1, abort_flag); };
-    while (ok && tc_next<PtShape>(p, st, pc)) {
-      const int two = pc.n_rows > 128, partial = first_partial(p, pc);
+    while (ok && next()) {
+      const int two = pc.n_rows > half;
       for (int t = 0; t <= two && ok; ++t) ok = mbar_wait_warp(&sh.q_full[t], n_piece[t] & 1, abort_flag);
       ok = ok && wait_kv(pos);
       if (!ok) break;
@@ -389,7 +463,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
         const int vs = pos % kPtStages, ks = (pos + 1) % kPtStages;
         const bool more = u + 1 < pc.u1;
         ok = wait_kv(pos);
-        if (u >= partial) {
+        if (u >= pc.partial) {
           ok = ok && mbar_wait_warp(&sh.clean[n_partial & 1], (n_partial >> 1) & 1, abort_flag);
           ++n_partial;
         }
@@ -422,57 +496,65 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       for (int t = 0; t <= two; ++t) ++n_piece[t];
     }
     __syncwarp();
-  } else if (warp == kPtKeysLoader) {
-    // ============================================================ keys and values
+  } else if (warp == kPtLoader) {
+    // ============================================================ queries, keys and values
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (lane == 0) {
-      int pos = 0, n_partial = 0;
-      bool ok = true;
-      while (ok && tc_next<PtShape>(p, st, pc)) {
-        int key0, keys;
-        key_span(p, pc.b, key0, keys);
-        const int partial = first_partial(p, pc), seq = p.padded ? pc.b : 0;
-        for (int i = 2 * pc.u0; i < 2 * pc.u1 && ok; ++i, ++pos) {
-          const int s = pos % kPtStages, u = i >> 1;
-          if (pos >= kPtStages) ok = mbar_wait(&sh.kv_empty[s], (pos / kPtStages - 1) & 1, abort_flag);
-          if (!ok) break;
+    int pos = 0, n_partial = 0, n_piece[2] = {0, 0};
+    bool ok = true;
+    while (ok && next()) {
+      const int seq = p.padded ? pc.b : 0, two = pc.n_rows > half;
+      for (int i = 2 * pc.u0; i < 2 * pc.u1 && ok; ++i, ++pos) {
+        const int s = pos % kPtStages, u = i >> 1;
+        if (pos >= kPtStages) ok = mbar_wait_warp(&sh.kv_empty[s], (pos / kPtStages - 1) & 1, abort_flag);
+        if (!ok) break;
+        if (lane == 0) {
           mbar_arrive_expect_tx(&sh.kv_full[s], kTileBytes);
 #pragma unroll
           for (int c = 0; c < kDChunks; ++c)
-            tma_load_4d(kv_sh + s * kTileBytes + c * kChunk, (i & 1) ? &v_map : &k_map, &sh.kv_full[s], c * 64, key0 + u * kPtKeys, pc.head, seq);
-          if ((i & 1) && u >= partial) { mbar_arrive(&sh.dirty[n_partial & 1]); ++n_partial; }
+            tma_load_4d(kv_sh + s * kTileBytes + c * kChunk, (i & 1) ? &v_map : &k_map, &sh.kv_full[s], c * 64, pc.key0 + u * kPtKeys, pc.head, seq);
+          if ((i & 1) && u >= pc.partial) mbar_arrive(&sh.dirty[n_partial & 1]);
+        }
+        if ((i & 1) && u >= pc.partial) ++n_partial;
+        if (i == 2 * pc.u0) {                                // the first keys do not wait for the queries of the piece before
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (t > two || !ok) continue;
+            if (n_piece[t] > 0) ok = wait_piece(p, &sh.q_empty[t], (n_piece[t] - 1) & 1, abort_flag);
+            if (!ok) continue;
+            ++n_piece[t];
+            if (lane == 0) {
+              mbar_arrive_expect_tx(&sh.q_full[t], kDChunks * half * 128);
+#pragma unroll
+              for (int c = 0; c < kDChunks; ++c)
+                tma_load_4d(q_sh + t * kTileBytes + c * kChunk, &q_map, &sh.q_full[t], c * 64, pc.head * p.group, pc.first + pc.token + t * tokens, seq);
+            }
+          }
         }
       }
     }
     __syncwarp();
-  } else {
-    // ============================================================ queries of a tile
+  } else if (warp == kPtPlanner) {
+    // ============================================================ what there is to do
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    constexpr int kLanes = DP / 8, kPass = 32 / kLanes;      // 16-byte pieces of a row; rows of a pass
-    const int tile = warp - kPtQueries, piece = lane % kLanes, row0 = lane / kLanes;
-    const uint32_t dst0 = smem_u32(q_sh + tile * kTileBytes + (piece >> 3) * kChunk);
-    const bool in_dim = piece * 8 < D;
-    int n_piece = 0;
-    bool ok = true;
-    while (ok && tc_next<PtShape>(p, st, pc)) {
-      const int n = min(pc.n_rows - tile * 128, 128);        // (rows behind them stay what they were: nobody takes their results)
-      if (n <= 0) continue;
-      if (n_piece > 0) ok = wait_piece(p, &sh.q_empty[tile], (n_piece - 1) & 1, abort_flag);
+    PtPlanner plan = {st};
+    bool ok = true, more = true;
+    while (ok && more) {
+      const int slot = n_plan % kPtPlan;
+      Boundary cut;
+      more = plan.next(p, pc, cut);
+      if (!more) pc.u1 = 0;
+      if (n_plan >= kPtPlan) ok = wait_piece(p, &sh.plan_empty[slot], (n_plan / kPtPlan - 1) & 1, abort_flag);
       if (!ok) break;
-      const int flat = pc.tile * kPtRows + tile * 128 + row0;
-      int i = flat / p.group, h = flat - i * p.group;
-      const char* src = q_at(p, pc.b, pc.q.s.first, RowAt{0, pc.head * p.group}) + piece * 16;
-#pragma unroll 4
-      for (int row = row0; row < n; row += kPass) {
-        copy_async_16(dst0 + row * 128 + (((piece & 7) ^ (row & 7)) << 4), in_dim ? src + i * p.q_row + h * p.q_head : src, in_dim);
-        for (h += kPass; h >= p.group; h -= p.group) ++i;
+      if (lane == 0) {
+        if (more && pc.u0 > 0) p.boundary[blockIdx.x] = cut;
+        sh.plan[slot] = pc;
+        mbar_arrive(&sh.plan_full[slot]);
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      fence_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.q_full[tile]);
-      ++n_piece;
+      ++n_plan;
     }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   }
 
   // ------------------------------------------------------------ teardown
