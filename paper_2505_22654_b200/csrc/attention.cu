@@ -232,7 +232,8 @@ static vscan_status validate_prompt(const vscan_attention_desc* d) {
 // Rows of a tile, keys of a step, CTAs of the launch
 struct PromptPlan { int tile_rows, keys, whole; unsigned ctas; };
 
-static bool prompt_tensor(const vscan_attention_desc* d) { return d->dtype == VSCAN_BF16 && d->head_dim <= 128 && d->kv_rows > 0; }
+// (a negative factor would turn the masks around: no model has one)
+static bool prompt_tensor(const vscan_attention_desc* d) { return d->dtype == VSCAN_BF16 && d->head_dim <= 128 && d->kv_rows > 0 && d->scale >= 0.f; }
 
 static PromptPlan plan_prompt(const vscan_attention_desc* d, bool tensor) {
   PromptPlan pl;
@@ -333,7 +334,7 @@ extern "C" size_t vscan_attention_workspace_bytes(const vscan_attention_desc* d)
       d->q_heads / d->kv_heads > 64 || d->kv_rows < 0)
     return kStatusBytes;
   const size_t flat = kv::prompt_bytes(kv::plan_prompt(d, false), d->head_dim);      // strides decide between the two
-  const size_t tensor = kv::prompt_tensor(d) ? kv::prompt_bytes(kv::plan_prompt(d, true), d->head_dim) : 0;
+  const size_t tensor = d->dtype == VSCAN_BF16 && d->head_dim <= 128 ? kv::prompt_bytes(kv::plan_prompt(d, true), d->head_dim) : 0;
   return flat > tensor ? flat : tensor;
 }
 

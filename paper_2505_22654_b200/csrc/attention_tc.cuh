@@ -44,7 +44,7 @@ struct PtPiece {         // steps u0 .. u1 - 1 of a tile; u1 = 0: there is no mo
 };
 
 struct PtShared {
-  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_done[2], o_free[2], stat_full[2];   // of the tiles
+  uint64_t q_full[2], q_empty[2], s_full[2], p_half[2], p_full[2], o_done[2], o_free[2], stat_full[2];   // of the tiles
   uint64_t kv_full[kPtStages], kv_empty[kPtStages];
   uint64_t dirty[2], clean[2];                // of steps that are seen in part, in turn: their values are under way, and cleaned
   uint32_t tmem_base;
@@ -84,6 +84,12 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
 }
 
 
+// The largest of three; NaN if one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 // A wait that may last for all of a piece: the limit of the other waits, 4 s or some two million steps, is granted once more for every
 // 2^17 keys that there may be.  If another role gives up, so does this wait.
 __device__ __forceinline__ bool wait_piece(const PromptParams& p, uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
@@ -176,7 +182,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 4);
+      mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.p_half[i], 4); mbar_init(&sh.p_full[i], 4);
       mbar_init(&sh.o_done[i], 1); mbar_init(&sh.o_free[i], 4); mbar_init(&sh.stat_full[i], 4);
       mbar_init(&sh.dirty[i], 1); mbar_init(&sh.clean[i], 4);
     }
@@ -222,44 +229,51 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
     const uint32_t s_addr = tmem + lanes + tile * 128;            // this row's scores, and its weights
     const uint32_t o_addr = tmem + lanes + 256 + tile * 128;
-    const float factor = fmaxf(fabsf(p.scale_log2e), 0x1p-126f);  // held above 0: a masked score stays -inf
-    const bool negative = p.scale_log2e < 0.f;
+    const float factor = fmaxf(p.scale_log2e, 0x1p-126f);         // held above 0: a masked score stays -inf
     int n_it = 0, n_piece = 0;                                    // steps and pieces of this tile so far
     bool ok = true;
     while (ok && next()) {
       if (tile * half >= pc.n_rows) continue;
       const int seen = r < half && tile * half + r < pc.n_rows ? keys_seen(p, pc, pc.token + tile * tokens + r / p.group) : 0;
       float m = -INFINITY, l = 0.f;      // reference and sum of the weights, in units of 2^m
+      float minus_m = 0.f;               // what is added to a score; NaN where the reference is infinite
       for (int u = pc.u0; u < pc.u1; ++u, ++n_it) {
         ok = u == pc.u0 ? wait_piece(p, &sh.s_full[tile], n_it & 1, abort_flag) : mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
+        // a row that does not see all of the step: scores of -inf into tensor memory first, in a loop of its own (a body of 128 scores in two
+        // forms is more than the instruction cache holds)
+        const int vis = seen - u * kPtKeys;
+        const bool masked = __any_sync(0xffffffffu, vis < kPtKeys);
+        if (masked) {
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t x[32];
+            tmem_read32(s_addr + q * 32, x);
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              if (q * 32 + k >= vis) x[k] = 0xff800000u;
+            tmem_st32(s_addr + q * 32, x);
+          }
+          tmem_wait_st();
+        }
         uint32_t v[128];
 #pragma unroll
         for (int h = 0; h < 4; ++h) tmem_read32(s_addr + h * 32, v + h * 32);
-        if (negative) {
-#pragma unroll
-          for (int k = 0; k < 128; ++k) v[k] ^= 0x80000000u;
-        }
-        const int vis = seen - u * kPtKeys;
-        if (__any_sync(0xffffffffu, vis < kPtKeys)) {
-#pragma unroll
-          for (int k = 0; k < 128; ++k)
-            if (k >= vis) v[k] = 0xff800000u;      // -inf
-        }
         float top[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) top[k] = __uint_as_float(v[k]);
 #pragma unroll
         for (int k = 4; k < 124; k += 8)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top[i] = fmaxf(fmaxf(top[i], __uint_as_float(v[k + i])), __uint_as_float(v[k + 4 + i]));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], __uint_as_float(v[124 + i]));
-        const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * factor;
-        if (__any_sync(0xffffffffu, most > m + kLazy)) {
-          const float now = fmaxf(m, most), f = now == m ? 1.f : ex2(m - now);
+          for (int i = 0; i < 4; ++i) top[i] = max3_nan(top[i], __uint_as_float(v[k + i]), __uint_as_float(v[k + 4 + i]));
+        top[0] = max3_nan(top[0], __uint_as_float(v[124]), __uint_as_float(v[125]));
+        top[1] = max3_nan(top[1], __uint_as_float(v[126]), __uint_as_float(v[127]));
+        const float most = max_nan(max3_nan(top[0], top[1], top[2]), top[3]) * factor;     // NaN where a score is
+        if (__any_sync(0xffffffffu, !(most <= m + kLazy))) {
+          const float now = max_nan(m, most), f = now == m ? 1.f : ex2(m - now);
           m = now;
+          minus_m = m == -INFINITY ? 0.f : m == INFINITY ? __uint_as_float(0x7fc00000u) : -m;
           l *= f;
           // (the products with V of the step before are done: this step's scores were issued after them)
           if (u > pc.u0 && __any_sync(0xffffffffu, f != 1.f)) {
@@ -273,22 +287,26 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
             }
           }
         }
-        const float minus_m = m == -INFINITY ? 0.f : -m;
         const uint64_t mul = pair(factor, factor), add = pair(minus_m, minus_m);
         uint64_t sums[2] = {0, 0};
+        auto weigh = [&](int q) {       // 32 scores
+          uint32_t w[16];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
-#pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            const int at = h * 64 + 2 * k;
+          for (int k = 0; k < 16; ++k) {
+            const int at = q * 32 + 2 * k;
             const float2 x = unpair(fma2(pair(__uint_as_float(v[at]), __uint_as_float(v[at + 1])), mul, add));
-            const float e0 = ex2(x.x), e1 = ex2(x.y);
-            sums[k & 1] = add2(sums[k & 1], pair(e0, e1));
-            w[k] = pack_bf16(e0, e1);
+            const float2 e = make_float2(ex2(x.x), ex2(x.y));
+            sums[k & 1] = add2(sums[k & 1], pair(e.x, e.y));
+            w[k] = pack_bf16(e.x, e.y);
           }
-          tmem_st32(s_addr + h * 32, w);
-        }
+          tmem_st16(s_addr + q * 16, w);
+        };
+        weigh(0); weigh(1); weigh(2);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_half[tile]);      // the products with the first half of the values begin
+        weigh(3);
         const float2 both = unpair(add2(sums[0], sums[1]));
         l += both.x + both.y;
         tmem_wait_st();
@@ -470,11 +488,14 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
 #pragma unroll 1
         for (int t = 0; t <= two && ok; ++t) {
           if (u == pc.u0 && n_piece[t] > 0) ok = wait_piece(p, &sh.o_free[t], (n_piece[t] - 1) & 1, abort_flag);
-          ok = ok && mbar_wait_warp(&sh.p_full[t], n_it[t] & 1, abort_flag);
+          ok = ok && mbar_wait_warp(&sh.p_half[t], n_it[t] & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
           const uint64_t b = desc_mn(kv_addr + vs * kTileBytes);
           umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128, b, pv, u > pc.u0);
+          ok = mbar_wait_warp(&sh.p_full[t], n_it[t] & 1, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
           umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128 + 32, b + (64 * 128 >> 4), pv, true);
           if (more) {            // over the weights that the products before this one read: products run in the order of their issue
             if (t == 0) ok = wait_kv(pos + 1);
