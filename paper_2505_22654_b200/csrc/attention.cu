@@ -259,30 +259,15 @@ static size_t prompt_bytes(const PromptPlan& pl, int head_dim) {
   return kStatusBytes + prompt_flag_bytes(pl) + prompt_boundary_bytes(pl) + round_up(2 * static_cast<size_t>(pl.ctas) * partial_floats(pl.tile_rows, head_dim) * 4, 256);
 }
 
-// Boxes of 64 channels x `inner` x `outer` of q (heads of a group, tokens), k or v (rows, a head).  False where TMA does not take the strides: heads
-// or rows on top of each other, for one
-static bool rows_map(const vscan_attention_desc* d, const void* at, const int64_t (&sizes)[2], const int64_t (&steps)[2], int64_t seq_step, int inner,
-                     int outer, CUtensorMap* map) {
-  const auto encode = tc::encode_fn();
-  if (!encode) return false;
-  const int64_t all[3] = {sizes[0], sizes[1], d->padded ? d->batch : 1}, step[3] = {steps[0], steps[1], seq_step};
-  cuuint64_t dims[4] = {static_cast<cuuint64_t>(d->head_dim)}, strides[3];
-  for (int i = 0; i < 3; ++i) {
-    if (all[i] > 1 && step[i] == 0) return false;
-    dims[i + 1] = static_cast<cuuint64_t>(all[i]);
-    strides[i] = all[i] > 1 ? static_cast<cuuint64_t>(step[i]) * 2 : 16;
-  }
-  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(inner), static_cast<cuuint32_t>(outer), 1}, each[4] = {1, 1, 1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(at), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 struct PromptMaps { CUtensorMap q, k, v; };
 static bool prompt_maps(const vscan_attention_desc* d, PromptMaps& m) {
   const int group = d->q_heads / d->kv_heads;
   const int64_t q_sizes[2] = {d->q_heads, d->rows}, kv_sizes[2] = {d->kv_rows, d->kv_heads};
   const int64_t q_steps[2] = {d->q_stride[1], d->q_stride[2]}, k_steps[2] = {d->k_stride[2], d->k_stride[1]}, v_steps[2] = {d->v_stride[2], d->v_stride[1]};
-  return rows_map(d, d->q, q_sizes, q_steps, d->q_stride[0], group, 128 / group, &m.q) &&
-         rows_map(d, d->k, kv_sizes, k_steps, d->k_stride[0], kPtKeys, 1, &m.k) && rows_map(d, d->v, kv_sizes, v_steps, d->v_stride[0], kPtKeys, 1, &m.v);
+  const int batch = d->padded ? d->batch : 1;
+  return rows_map(d->q, d->head_dim, q_sizes, q_steps, batch, d->q_stride[0], group, 128 / group, &m.q) &&
+         rows_map(d->k, d->head_dim, kv_sizes, k_steps, batch, d->k_stride[0], kPtKeys, 1, &m.k) &&
+         rows_map(d->v, d->head_dim, kv_sizes, v_steps, batch, d->v_stride[0], kPtKeys, 1, &m.v);
 }
 
 template <int DP>

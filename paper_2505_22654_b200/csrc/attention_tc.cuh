@@ -25,11 +25,12 @@
 
 #include "attention_prompt.cuh"
 #include "kv_attention_tc.cuh"
+#include "tc_rows.cuh"
 
 namespace vscan {
 namespace kv {
 
-constexpr int kPtThreads = 512, kPtKeys = 128, kPtWhole = 4, kPtExtra = 1;
+constexpr int kPtThreads = 512, kPtKeys = 128, kPtWhole = 4, kPtExtra = 3;
 constexpr int kPtHelper = 8, kPtIssuer = 12, kPtLoader = 13, kPtPlanner = 14;   // first warp of each role
 constexpr int kPtStages = 4, kPtPlan = 4;
 constexpr int kPtReaders = 14;       // warps that read the plan
@@ -58,14 +59,6 @@ struct PtShared {
 };
 
 // ---------------------------------------------------------------------------------------------- instructions
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-      ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-      : "memory");
-}
-// bf16 x bf16 -> float32, M = 128; b_mn: the second operand MN-major
-__device__ __forceinline__ uint32_t idesc_bf16(int n, bool b_mn) { return idesc_f16(n, b_mn) | (1u << 7) | (1u << 10); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);

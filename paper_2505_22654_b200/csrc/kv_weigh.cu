@@ -3,52 +3,14 @@
 // exp(scale q k - lse) needs no maximum and no sum of its own: every token's sum over the query rows stands alone.  So the line of
 // (sequence, head, 64 tokens) is cut into equal stretches as for the attention over few rows, but nothing is joined afterwards, and a token's
 // weight is read and written once by the lane that owns it, in a fixed order of the rows.
-#include "kv_attention_mma.cuh"
+#include "kv_weigh_tc.cuh"
 
 namespace vscan {
 namespace kv {
 
-struct WeighParams : AttnParams {
-  float* weight;
-  float decay;
-  int window;
-};
-
-// One segment a KV head: rows of all tiles go to the same tokens
-__device__ __forceinline__ Sequence sequence_at(const WeighParams& p, int b) {
-  Sequence s;
-  row_span(p.row_offset, p.kv_len, b, p.rows, p.padded, s.first, s.n, s.start);
-  s.n = min(s.n, p.max_q_len);
-  s.len = min(max(p.kv_len[b], 0), p.max_blocks << p.shift);
-  s.tiles = s.n > 0 ? 1 : 0;
-  s.units = max(1, (s.len + kUnit - 1) / kUnit);
-  s.weight = static_cast<long long>(s.tiles) * p.kv_heads * s.units;
-  return s;
-}
-
-// Row r of the window's rows x heads of the group
-struct WindowRow { RowAt at; int seen; float lse; };   // seen: tokens, 0 where the row gives nothing; lse in base 2
-__device__ __forceinline__ WindowRow window_row(const WeighParams& p, const Sequence& s, int b, int head, int r) {
-  const int u = min(s.n, p.window), i = r / p.group;
-  WindowRow w = {{s.n - u, head * p.group}, 0, 0.f};
-  if (i >= u) return w;
-  w.at.i += i;
-  w.at.h += r - i * p.group;
-  const float lse = *lse_at(p, b, s.first, w.at);
-  w.lse = lse * 1.44269504088896341f;
-  if (lse != -INFINITY) w.seen = visible(p, s, w.at.i);
-  return w;
-}
-// Rows of a segment; no more than fit 32 bits, since rows x heads of the buffer do
-__device__ __forceinline__ int window_rows(const WeighParams& p, const Sequence& s) { return min(s.n, p.window) * p.group; }
-
-__device__ __forceinline__ float* weight_at(const WeighParams& p, int block, int head, int t) {
-  return p.weight + ((static_cast<size_t>(block) * p.kv_heads + head) << p.shift) + (t & (p.block_size - 1));
-}
-
 // ---------------------------------------------------------------------------------------------- bf16 queries, few rows
 // m16n8k16 products of 16 tokens x 8 rows as in the attention over few rows: codes from global memory straight into fragments.  More
-// rows than the 8 NT of a pass take more passes over the worker's tokens, which L2 holds by then.
+// rows than the 8 NT of a pass (heads of more than 128 channels) take more passes over the worker's tokens, which L2 holds by then.
 template <int KV, int DP, int NT, bool FULL>
 __global__ void __launch_bounds__(kMmaThreads, DP == 256 ? 3 : NT > 1 ? 4 : 6) weigh_mma_kernel(WeighParams p) {
   constexpr int R = 8 * NT, KS = DP / 16, kPieces = DP / 64;
@@ -336,10 +298,22 @@ static vscan_status launch_weigh_mma(const WeighParams& p, int rows, cudaStream_
   return VSCAN_OK;
 }
 
+template <int KV, int DP>
+static vscan_status launch_weigh_tc(const WeighParams& p, const CUtensorMap& q, cudaStream_t stream) {
+  constexpr size_t smem = 1024 + (2 + kWtStages) * static_cast<size_t>(DP / 64) * kChunk;
+  VSCAN_CUDA_TRY(allow_smem(weigh_tc_kernel<KV, DP>, smem));
+  prof_before("kv_weigh_tc", stream);
+  VSCAN_CUDA_TRY(launch_dependent(weigh_tc_kernel<KV, DP>, dim3(weigh_ctas(p, 1)), dim3(kWtThreads), smem, stream, p, q));
+  prof_after(stream);
+  VSCAN_AFTER_LAUNCH();
+  return VSCAN_OK;
+}
+
 template <int KV>
-static vscan_status launch_weigh(const WeighParams& p, int dtype, cudaStream_t stream) {
+static vscan_status launch_weigh(const WeighParams& p, int dtype, const CUtensorMap* q, cudaStream_t stream) {
   const int64_t used = p.max_q_len < p.window ? p.max_q_len : p.window;
   const int rows = static_cast<int>(used * p.group < (1 << 20) ? used * p.group : 1 << 20), d = p.head_dim;
+  if (q) return d <= 64 ? launch_weigh_tc<KV, 64>(p, *q, stream) : launch_weigh_tc<KV, 128>(p, *q, stream);
   if (dtype == VSCAN_BF16) {
     if (d == 64) return launch_weigh_mma<KV, 64, true>(p, rows, stream);
     if (d == 128) return launch_weigh_mma<KV, 128, true>(p, rows, stream);
@@ -381,5 +355,12 @@ extern "C" vscan_status vscan_kv_weigh(const vscan_kv_weigh_desc* d, void* strea
   const double factor = static_cast<double>(d->scale) * 1.4426950408889634074;
   p.scale_log2e = static_cast<float>(factor);
   p.scale_rest = static_cast<float>(factor - p.scale_log2e);
-  return d->kv_dtype == VSCAN_KV_E4M3 ? kv::launch_weigh<VSCAN_KV_E4M3>(p, d->dtype, stream) : kv::launch_weigh<VSCAN_KV_I8>(p, d->dtype, stream);
+  // 5th-generation tensor cores from 17 query rows of a sequence and KV head on, as in the attention, where TMA takes the rows
+  CUtensorMap map;
+  const int64_t used = d->max_q_len < d->window ? d->max_q_len : d->window;
+  const int64_t sizes[2] = {d->q_heads, d->rows}, steps[2] = {d->q_stride[1], d->q_stride[2]};
+  const bool tensor = d->dtype == VSCAN_BF16 && d->head_dim <= 128 && used * p.group > 16 &&
+                      kv::rows_map(d->q, d->head_dim, sizes, steps, d->padded ? d->batch : 1, d->q_stride[0], p.group, 128 / p.group, &map);
+  return d->kv_dtype == VSCAN_KV_E4M3 ? kv::launch_weigh<VSCAN_KV_E4M3>(p, d->dtype, tensor ? &map : nullptr, stream)
+                                      : kv::launch_weigh<VSCAN_KV_I8>(p, d->dtype, tensor ? &map : nullptr, stream);
 }

@@ -323,6 +323,32 @@ def test_weigh_windows_missing_blocks_and_empty_sequences(dtype, new):
     _weigh_case("i8", dtype, 2, 2, 64, 16, [30, 5], new, window=1, decay=0.0, seed=4)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weigh_of_more_rows_than_max_q_len_and_long_windows(dtype):
+    """Rows behind max_q_len are not there: tokens that only they would see get nothing."""
+    for hq, hk, d, past, new, top in ((4, 2, 64, [30, 0], [400, 300], 20), (7, 1, 128, [500, 3], [90, 200], 1000), (1, 1, 32, [600], [300], 1000)):
+        lens, off = [p + n for p, n in zip(past, new)], _offsets(new)
+        kind, codes, scale, dev = _random_cache("e4m3", hk, 16, d, sum(-(-n // 16) for n in lens) + 2, d)
+        table = _tables(lens, 16, -(-max(lens) // 16), len(codes[0]), np.random.default_rng(0))
+        q = torch.randn((off[-1], hq, d), generator=gen(d)).to(DT[dtype]).cuda()
+        lse = (5 + torch.rand((off[-1], hq), generator=gen(1))).cuda()
+        got = torch.full((len(codes[0]), hk, 16), 2.0, device="cuda")
+        vs.vscan_kv_weigh(q, lse, i32(lens), i32(off), i32(table), dev[0], dev[2], got, d ** -0.5, max_q_len=top, decay=0.5)
+        want = torch.full(got.shape, 2.0, dtype=torch.float64, device="cuda")
+        for b, T in enumerate(lens):
+            ids, n, rows = torch.tensor(table[b][:-(-T // 16)], device="cuda"), new[b], min(new[b], top)
+            k = (dev[0][ids].double() * dev[2][ids].double()[..., None, None]).transpose(0, 1).reshape(hk, -1, d)[:, :T]
+            x = q[off[b]:off[b] + rows].double().view(rows, hk, hq // hk, d)
+            s = d ** -0.5 * torch.einsum("nhgd,htd->hgnt", x, k) - lse[off[b]:off[b] + rows].double().view(rows, hk, -1).permute(1, 2, 0)[..., None]
+            s.masked_fill_(torch.arange(T, device="cuda") > T - n + torch.arange(rows, device="cuda")[:, None], -torch.inf)
+            w = torch.cat([torch.full((hk, T - n), 1.0, device="cuda", dtype=torch.float64), torch.zeros((hk, n), device="cuda", dtype=torch.float64)], 1)
+            w = torch.nn.functional.pad(w + s.exp().sum((1, 2)), (0, len(ids) * 16 - T), value=2.0)
+            want[ids] = w.view(hk, len(ids), 16).transpose(0, 1)
+        # scores of a few units at most: (head_dim + 8) 2^-24 (|s| + |lse|) below 136 x 2^-24 x 64 of a weight, and the sums
+        tol = (136 * 2.0 ** -24 * 64 + 2.0 ** -21 + (max(new) * hq / 4 + 16) * 2.0 ** -24) * want.abs()
+        assert ((got.double() - want).abs() <= tol).all(), float(((got.double() - want).abs() / tol).max())
+
+
 def test_weigh_over_many_short_and_one_long_sequence():
     _weigh_case("e4m3", "bf16", 2, 1, 64, 16, [3000] + [2] * 40, [1] * 41, seed=5)
     _weigh_case("e4m3", "bf16", 8, 8, 64, 16, [20] * 30, [1] * 30, seed=6)
