@@ -2,11 +2,11 @@
 //
 // A CTA takes 256 tokens of one KV head as two tiles of 128, turned from codes to bf16 (exactly) once, and runs over all query rows of the window,
 // a tile of up to 128 (whole tokens of the group's heads) at a time:
-//   warps 0-3, 4-7   tile 0, 1: a thread a token.  S^T [128 tokens x 128 rows] from tensor memory, exponentials, their sum in registers: nothing
-//                    goes back but one number a token at the end.  Before that, the tile's codes into shared memory
-//   warp 8           issues the products: two buffers of scores a tile, so that they run beside the exponentials
-//   warp 9           the rows' queries by TMA, a ring of four tiles
-//   warp 10          the rows' logarithms, beside them
+//   warps 0-7, 8-15  tile 0, 1: two threads a token, 64 of the rows each.  S^T [128 tokens x 128 rows] from tensor memory, exponentials, their sum
+//                    in registers: nothing goes back but one number a token at the end.  Before that, the tile's codes into shared memory
+//   warp 16          issues the products: two buffers of scores a tile, so that they run beside the exponentials
+//   warp 17          the rows' queries by TMA, a ring of four tiles
+//   warp 18          the rows' logarithms, beside them
 // Bound by the exponentials: 32,768 a tile of rows, 16 a cycle, twice what the products take.
 // Every wait is bounded; on expiry the CTA's tokens keep the weights that they had (there is no workspace to say so in).
 #pragma once
@@ -17,16 +17,17 @@
 namespace vscan {
 namespace kv {
 
-constexpr int kWtThreads = 384, kWtIssuer = 8, kWtLoader = 9, kWtLogs = 10;
+constexpr int kWtThreads = 640, kWtIssuer = 16, kWtLoader = 17, kWtLogs = 18;
 constexpr int kWtTokens = 256, kWtStages = 4;
 
 struct WtShared {
-  uint64_t k_full[2], s_full[2][2], s_empty[2][2];
+  uint64_t k_full[2], s_full[2][2], s_empty[2][2], other[2][4];   // other: of the two warps that share 32 tokens
   uint64_t q_full[kWtStages], q_empty[kWtStages], log_full[kWtStages], log_empty[kWtStages];
   uint32_t tmem_base;
   int abort_flag;
   alignas(16) float log[kWtStages][128];      // minus the rows' logarithms in base 2; -inf where a row gives nothing
   int silent[kWtStages];                      // some row of the tile gives nothing
+  float part[2][128];                         // sums of the second threads
   ScheduleShared sched;
 };
 
@@ -61,13 +62,20 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.k_full[i], 4);
-      for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[i][k], 1); mbar_init(&sh.s_empty[i][k], 4); }
+      mbar_init(&sh.k_full[i], 8);
+      for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[i][k], 1); mbar_init(&sh.s_empty[i][k], 8); }
+      for (int k = 0; k < 4; ++k) mbar_init(&sh.other[i][k], 1);
     }
-    for (int i = 0; i < kWtStages; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.log_full[i], 1); mbar_init(&sh.log_empty[i], 8); }
+    for (int i = 0; i < kWtStages; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.log_full[i], 1); mbar_init(&sh.log_empty[i], 16); }
     sh.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  // rows of a stage behind the whole tokens of a tile are never loaded: their scores have to be finite
+  for (int i = threadIdx.x; i < kWtStages * kDChunks * 128 * 8; i += kWtThreads) {
+    const int row = (i >> 3) & 127;
+    if (row >= 128 / p.group * p.group) *reinterpret_cast<uint4*>(q_sh + static_cast<size_t>(i >> 10) * kChunk + (i & 1023) * 16) = make_uint4(0, 0, 0, 0);
+  }
+  fence_async();
   if (warp == kWtIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "n"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -83,10 +91,10 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
   bool ok = true;
 
   if (warp < kWtIssuer) {
-    // ============================================================ a thread a token
-    const int tile = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    // ============================================================ two threads a token
+    const int tile = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    int n_it = 0, n_row = 0;                       // tiles of rows that this tile has had; of the CTA
+    int n_it = 0, n_row = 0, n_sum = 0;            // tiles of rows that this tile has had; of the CTA; sums told so far
     while (ok && next_piece(p, st, pc)) {
       const int stop = min(st.s.len, pc.u1 * kUnit);
       for (int t0 = pc.u0 * kUnit; t0 < stop && ok; t0 += kWtTokens) {
@@ -109,18 +117,18 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
         if (block >= 0) {
           factor = __ldg(p.k_scale + static_cast<size_t>(block) * p.kv_heads + st.head) * p.scale_log2e;
           weight = weight_at(p, block, st.head, t);
-          if (t < st.s.start) sum = p.decay * *weight;
+          if (half == 0 && t < st.s.start) sum = p.decay * *weight;
         }
         if (c.first == c.tiles) {                  // no row of the window sees any of the tokens (rows that are not there would)
-          if (weight) *weight = sum;
+          if (weight && half == 0) *weight = sum;
           continue;
         }
         // ---- codes to bf16 into the tile (whose products before are done: this warp has read their scores); rows of the group of
         // lanes that has a token's pieces in turn
         {
           constexpr int kPer = DP / 16;                                  // pieces of 16 codes of a token
-#pragma unroll 2
-          for (int i = lane; i < 32 * kPer; i += 32) {
+#pragma unroll
+          for (int i = half * 16 * kPer + lane; i < (half + 1) * 16 * kPer; i += 32) {
             const int row = i / kPer, piece = i % kPer, mine = quarter * 32 + row, tok = t0 + tile * 128 + mine;
             const int blk = __shfl_sync(0xffffffffu, block, row);
             uint4 raw = make_uint4(0, 0, 0, 0);
@@ -159,10 +167,10 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
           const int c0 = static_cast<int>(min(max(from - static_cast<long long>(j) * per_tile, 0ll), 128ll)) * p.group;
           const int c1 = min(c.rows - j * per_tile, per_tile) * p.group;
           const float* log = sh.log[stage];
-          const bool masked = __any_sync(0xffffffffu, c0 > 0) || c1 < 128 || sh.silent[stage];
+          const bool masked = __any_sync(0xffffffffu, c0 > 0) || c1 < per_tile * p.group || sh.silent[stage];
           const uint32_t s_addr = tmem + lanes + tile * 256 + buf * 128;
 #pragma unroll 1
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 2 * half; q < 2 * half + 2; ++q) {
             uint32_t v[32];
             tmem_read32(s_addr + q * 32, v);
             float e[32];
@@ -189,7 +197,16 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
           if (lane == 0) { mbar_arrive(&sh.s_empty[tile][buf]); mbar_arrive(&sh.log_empty[stage]); }
         }
         const float2 a = unpair(sums[0]), b = unpair(sums[1]);
-        if (ok && weight) *weight = sum + ((a.x + a.y) + (b.x + b.y));
+        sum += (a.x + a.y) + (b.x + b.y);
+        if (!ok) break;
+        if (half == 1) {
+          sh.part[tile][r] = sum;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.other[tile][quarter]);
+        } else {
+          ok = mbar_wait_warp(&sh.other[tile][quarter], n_sum++ & 1, abort_flag);
+          if (ok && weight) *weight = sum + sh.part[tile][r];
+        }
       }
     }
   } else if (warp == kWtIssuer) {
