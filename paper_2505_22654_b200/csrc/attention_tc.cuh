@@ -2,14 +2,14 @@
 //
 // A CTA takes up to 256 query rows (new rows x heads of a group) of one KV head as two tiles of up to 128 and runs over its stretch of the keys,
 // 128 at a time:
-//   warps 0-3, 4-7   tile 0, 1: a thread a query row.  Scores from tensor memory into registers, running maximum and sum, weights back to
-//                    tensor memory as bf16, over the scores that they come from
-//   warps 8-11       the results of both tiles: tensor memory to memory, while the others begin the next piece; and the values of a step
+//   warps 0-7, 8-15  tile 0, 1: a warp 16 query rows, four threads a row.  Scores from tensor memory into registers, running maximum and sum,
+//                    weights back to tensor memory as bf16, over the scores that they come from
+//   warps 16-19      the results of both tiles: tensor memory to memory, while the others begin the next piece; and the values of a step
 //                    that some row does not see in full (below)
-//   warp 12          issues the products: S[128 x 128] = Q K^T (operands in shared memory), O[128 x d] += P V with P read from tensor
+//   warp 20          issues the products: S[128 x 128] = Q K^T (operands in shared memory), O[128 x d] += P V with P read from tensor
 //                    memory and V, tokens down and channels across, as the MN-major operand
-//   warp 13          queries, K and V by TMA; K and V in a ring of four tiles of 128 rows
-//   warp 14          plans: what the next pieces of the stretch are, a few ahead of all others
+//   warp 21          queries, K and V by TMA; K and V in a ring of four tiles of 128 rows
+//   warp 22          plans: what the next pieces of the stretch are, a few ahead of all others
 // A tile of 128 rows has whole tokens of the group's heads (126 rows for groups of seven), so that TMA can bring them.
 // The two tiles take turns: while one's weights are made, the other's products run.  A step takes the tensor cores 2,048 cycles (32
 // products of 64) and the exponentials, 32,768 at 16 a cycle, as many.
@@ -30,11 +30,11 @@
 namespace vscan {
 namespace kv {
 
-constexpr int kPtThreads = 512, kPtKeys = 128, kPtWhole = 4, kPtExtra = 3;
-constexpr int kPtHelper = 8, kPtIssuer = 12, kPtLoader = 13, kPtPlanner = 14;   // first warp of each role
+constexpr int kPtThreads = 768, kPtKeys = 128, kPtWhole = 4, kPtExtra = 3;
+constexpr int kPtHelper = 16, kPtIssuer = 20, kPtLoader = 21, kPtPlanner = 22;   // first warp of each role
 constexpr int kPtStages = 4, kPtPlan = 4;
-constexpr int kPtReaders = 14;       // warps that read the plan
-// 512 threads start with 128 registers each: 256 x 192 + 128 x 72 + 128 x 56 = 512 x 128.
+constexpr int kPtReaders = 22;       // warps that read the plan
+// 768 threads start with 80 registers each: 512 x 88 + 256 x 64 = 768 x 80.
 using PtShape = TileShape<kPtThreads, 0, kPtKeys, kPtWhole, kPtExtra>;
 
 struct PtPiece {         // steps u0 .. u1 - 1 of a tile; u1 = 0: there is no more
@@ -63,20 +63,42 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
+// 16 lanes (rows) x 64 columns of tensor memory, with the wait: v[4 i + k] is row lane / 4 + 8 (k / 2), column 8 i + 2 (lane % 4) + k % 2
+__device__ __forceinline__ void tmem_read_rows(uint32_t taddr, uint32_t* v) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 "
-      "[%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(taddr),
-        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-        "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
-        "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-        "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+        "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr)
       : "memory");
 }
-
-
+// The same rows x 16 columns, read and written
+__device__ __forceinline__ void tmem_read_rows16(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_write_rows16(uint32_t taddr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+// The same rows x 32 columns written: v[2 i + k] is row lane / 4 + 8 k, column 4 i + lane % 4
+__device__ __forceinline__ void tmem_write_pairs(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
 // The largest of three; NaN if one is
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float r;
@@ -176,8 +198,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.p_half[i], 4); mbar_init(&sh.p_full[i], 4);
-      mbar_init(&sh.o_done[i], 1); mbar_init(&sh.o_free[i], 4); mbar_init(&sh.stat_full[i], 4);
+      mbar_init(&sh.p_half[i], 8); mbar_init(&sh.p_full[i], 8);
+      mbar_init(&sh.o_done[i], 1); mbar_init(&sh.o_free[i], 4); mbar_init(&sh.stat_full[i], 8);
       mbar_init(&sh.dirty[i], 1); mbar_init(&sh.clean[i], 4);
     }
     for (int i = 0; i < kPtStages; ++i) { mbar_init(&sh.kv_full[i], 1); mbar_init(&sh.kv_empty[i], 1); }
@@ -216,109 +238,119 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
   const int tokens = p.tile_rows / (2 * p.group), half = tokens * p.group;      // tokens and rows of a tile of 128
 
   if (warp < kPtHelper) {
-    // ============================================================ a thread a query row
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-    const int tile = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
-    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t s_addr = tmem + lanes + tile * 128;            // this row's scores, and its weights
+    // ============================================================ four threads a query row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
+    const int tile = warp >> 3, row0 = (warp & 3) * 32 + ((warp >> 2) & 1) * 16;
+    const uint32_t lanes = static_cast<uint32_t>(row0) << 16;
+    const uint32_t s_addr = tmem + lanes + tile * 128;            // these rows' scores, and their weights
     const uint32_t o_addr = tmem + lanes + 256 + tile * 128;
     const float factor = fmaxf(p.scale_log2e, 0x1p-126f);         // held above 0: a masked score stays -inf
     int n_it = 0, n_piece = 0;                                    // steps and pieces of this tile so far
     bool ok = true;
     while (ok && next()) {
       if (tile * half >= pc.n_rows) continue;
-      const int seen = r < half && tile * half + r < pc.n_rows ? keys_seen(p, pc, pc.token + tile * tokens + r / p.group) : 0;
-      float m = -INFINITY, l = 0.f;      // reference and sum of the weights, in units of 2^m
-      float minus_m = 0.f;               // what is added to a score; NaN where the reference is infinite
+      int seen[2];                       // of rows row0 + lane / 4 and 8 on, less this lane's first column
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = row0 + (lane >> 2) + 8 * i;
+        seen[i] = (r < half && tile * half + r < pc.n_rows ? keys_seen(p, pc, pc.token + tile * tokens + r / p.group) : 0) - 2 * (lane & 3);
+      }
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};      // reference, and this thread's sum of the weights, in units of 2^m
+      float minus_m[2] = {0.f, 0.f};     // what is added to a score; NaN where the reference is infinite
+      const bool sees_all = pc.partial >= pc.u1;
       for (int u = pc.u0; u < pc.u1; ++u, ++n_it) {
         ok = u == pc.u0 ? wait_piece(p, &sh.s_full[tile], n_it & 1, abort_flag) : mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        // a row that does not see all of the step: scores of -inf into tensor memory first, in a loop of its own (a body of 128 scores in two
-        // forms is more than the instruction cache holds)
-        const int vis = seen - u * kPtKeys;
-        const bool masked = __any_sync(0xffffffffu, vis < kPtKeys);
-        if (masked) {
-#pragma unroll 1
-          for (int q = 0; q < 4; ++q) {
-            uint32_t x[32];
-            tmem_read32(s_addr + q * 32, x);
+        uint32_t v[64];                  // v[4 i + k]: row k / 2, column 8 i + k % 2 from the lane's first
+        tmem_read_rows(s_addr, v);
+        tmem_read_rows(s_addr + 64, v + 32);
+        if (!sees_all && u >= pc.partial) {
+          const int vis[2] = {seen[0] - u * kPtKeys, seen[1] - u * kPtKeys};
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (q * 32 + k >= vis) x[k] = 0xff800000u;
-            tmem_st32(s_addr + q * 32, x);
-          }
-          tmem_wait_st();
+          for (int k = 0; k < 64; ++k)
+            if ((k >> 2) * 8 + (k & 1) >= vis[(k >> 1) & 1]) v[k] = 0xff800000u;      // -inf
         }
-        uint32_t v[128];
+        float top[2][2];
 #pragma unroll
-        for (int h = 0; h < 4; ++h) tmem_read32(s_addr + h * 32, v + h * 32);
-        float top[4];
+        for (int i = 0; i < 2; ++i) {
+          top[i][0] = __uint_as_float(v[2 * i]);
+          top[i][1] = __uint_as_float(v[2 * i + 1]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) top[k] = __uint_as_float(v[k]);
+          for (int k = 4; k < 60; k += 8) {
+            top[i][0] = max3_nan(top[i][0], __uint_as_float(v[2 * i + k]), __uint_as_float(v[2 * i + k + 4]));
+            top[i][1] = max3_nan(top[i][1], __uint_as_float(v[2 * i + k + 1]), __uint_as_float(v[2 * i + k + 5]));
+          }
+          top[i][0] = max_nan(max3_nan(top[i][0], __uint_as_float(v[2 * i + 60]), __uint_as_float(v[2 * i + 61])), top[i][1]);
+          top[i][0] = max_nan(top[i][0], __shfl_xor_sync(0xffffffffu, top[i][0], 1));
+          top[i][0] = max_nan(top[i][0], __shfl_xor_sync(0xffffffffu, top[i][0], 2)) * factor;      // NaN where a score is
+        }
+        if (__any_sync(0xffffffffu, !(top[0][0] <= m[0] + kLazy) || !(top[1][0] <= m[1] + kLazy))) {
+          float f[2];
 #pragma unroll
-        for (int k = 4; k < 124; k += 8)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) top[i] = max3_nan(top[i], __uint_as_float(v[k + i]), __uint_as_float(v[k + 4 + i]));
-        top[0] = max3_nan(top[0], __uint_as_float(v[124]), __uint_as_float(v[125]));
-        top[1] = max3_nan(top[1], __uint_as_float(v[126]), __uint_as_float(v[127]));
-        const float most = max_nan(max3_nan(top[0], top[1], top[2]), top[3]) * factor;     // NaN where a score is
-        if (__any_sync(0xffffffffu, !(most <= m + kLazy))) {
-          const float now = max_nan(m, most), f = now == m ? 1.f : ex2(m - now);
-          m = now;
-          minus_m = m == -INFINITY ? 0.f : m == INFINITY ? __uint_as_float(0x7fc00000u) : -m;
-          l *= f;
-          // (the products with V of the step before are done: this step's scores were issued after them)
-          if (u > pc.u0 && __any_sync(0xffffffffu, f != 1.f)) {
+          for (int i = 0; i < 2; ++i) {
+            const float now = max_nan(m[i], top[i][0]);
+            f[i] = now == m[i] ? 1.f : ex2(m[i] - now);
+            m[i] = now;
+            minus_m[i] = now == -INFINITY ? 0.f : now == INFINITY ? __uint_as_float(0x7fc00000u) : -now;
+            l[i] *= f[i];
+          }
+          if (u > pc.u0 && __any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
+            // (the products with V of the step before are done: this step's scores were issued after them)
 #pragma unroll 1
             for (int c = 0; c < DP; c += 16) {
-              uint32_t x[16];
-              tmem_read16(o_addr + c, x);
+              uint32_t x[8];
+              tmem_read_rows16(o_addr + c, x);
 #pragma unroll
-              for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
-              tmem_st16(o_addr + c, x);
+              for (int k = 0; k < 8; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f[(k >> 1) & 1]);
+              tmem_write_rows16(o_addr + c, x);
             }
           }
         }
-        const uint64_t mul = pair(factor, factor), add = pair(minus_m, minus_m);
+        const uint64_t mul = pair(factor, factor), add[2] = {pair(minus_m[0], minus_m[0]), pair(minus_m[1], minus_m[1])};
         uint64_t sums[2] = {0, 0};
-        auto weigh = [&](int q) {       // 32 scores
+        auto weigh = [&](int h) {        // 64 columns of both rows
           uint32_t w[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            const int at = q * 32 + 2 * k;
-            const float2 x = unpair(fma2(pair(__uint_as_float(v[at]), __uint_as_float(v[at + 1])), mul, add));
+            const int at = h * 32 + 2 * k;
+            const float2 x = unpair(fma2(pair(__uint_as_float(v[at]), __uint_as_float(v[at + 1])), mul, add[k & 1]));
             const float2 e = make_float2(ex2(x.x), ex2(x.y));
             sums[k & 1] = add2(sums[k & 1], pair(e.x, e.y));
             w[k] = pack_bf16(e.x, e.y);
           }
-          tmem_st16(s_addr + q * 16, w);
+          tmem_write_pairs(s_addr + h * 32, w);
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
         };
-        weigh(0); weigh(1); weigh(2);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
+        weigh(0);
         if (lane == 0) mbar_arrive(&sh.p_half[tile]);      // the products with the first half of the values begin
-        weigh(3);
-        const float2 both = unpair(add2(sums[0], sums[1]));
-        l += both.x + both.y;
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
+        weigh(1);
         if (lane == 0) mbar_arrive(&sh.p_full[tile]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 both = unpair(sums[i]);
+          l[i] += both.x + both.y;
+        }
       }
       if (!ok) break;
       // ---- reference and sum to the warps that write the results, which are done with those of the piece before
       if (n_piece > 0) ok = wait_piece(p, &sh.o_free[tile], (n_piece - 1) & 1, abort_flag);
       if (!ok) break;
-      sh.stat[tile][r] = make_float2(m, l);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+        if ((lane & 3) == 0) sh.stat[tile][row0 + (lane >> 2) + 8 * i] = make_float2(m[i], l[i]);
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.stat_full[tile]);
       ++n_piece;
     }
   } else if (warp < kPtIssuer) {
     // ============================================================ results; values of steps that are seen in part
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const int quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
     const int r_token = r / p.group, r_head = r - r_token * p.group;
@@ -405,23 +437,23 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
         float* part = p.partial + (static_cast<size_t>(blockIdx.x) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(p.tile_rows, D);
         char* out = out_at(p, pc.b, pc.first, at);
 #pragma unroll 1
-        for (int c = 0; c < DP; c += 32) {
-          uint32_t v[32];
-          tmem_read32(tmem + lanes + 256 + t * 128 + c, v);
+        for (int c = 0; c < DP; c += 16) {
+          uint32_t v[16];
+          tmem_read16(tmem + lanes + 256 + t * 128 + c, v);
           if (on && c < D) {
-          float x[32];
+          float x[16];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) x[k] = __uint_as_float(v[k]);
+          for (int k = 0; k < 16; ++k) x[k] = __uint_as_float(v[k]);
           if (odd) {
-            const uint32_t up = sh.odd[t][r][c >> 5], down = sh.odd[t][r][4 + (c >> 5)];
+            const uint32_t up = sh.odd[t][r][c >> 5] >> (c & 31), down = sh.odd[t][r][4 + (c >> 5)] >> (c & 31);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
+            for (int k = 0; k < 16; ++k) {
               if ((up >> k) & 1u) x[k] += INFINITY;
               if ((down >> k) & 1u) x[k] -= INFINITY;
             }
           }
 #pragma unroll
-          for (int k = 0; k < 32; k += 8) {
+          for (int k = 0; k < 16; k += 8) {
             if (c + k >= D) continue;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[k + i] *= mul;
@@ -446,7 +478,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
     }
   } else if (warp == kPtIssuer) {
     // ============================================================ products
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const uint32_t qk = idesc_bf16(kPtKeys, false), pv = idesc_bf16(DP, true);
     const uint32_t q_addr = smem_u32(q_sh), kv_addr = smem_u32(kv_sh);
     int pos = 0, n_partial = 0, n_it[2] = {0, 0}, n_piece[2] = {0, 0};
@@ -512,7 +544,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
     __syncwarp();
   } else if (warp == kPtLoader) {
     // ============================================================ queries, keys and values
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     int pos = 0, n_partial = 0, n_piece[2] = {0, 0};
     bool ok = true;
     while (ok && next()) {
@@ -549,7 +581,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
     __syncwarp();
   } else if (warp == kPtPlanner) {
     // ============================================================ what there is to do
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     PtPlanner plan = {st};
     bool ok = true, more = true;
     while (ok && more) {
@@ -568,7 +600,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       ++n_plan;
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   }
 
   // ------------------------------------------------------------ teardown
