@@ -43,9 +43,18 @@ __device__ __forceinline__ long long tiles_before(const AttnParams& p, const TcS
   return k < q.tiles ? sum : sum + max(q.base + q.rows, one);
 }
 
-// Quotient of numbers that nearly always fit 32 bits
+// Quotient of numbers that nearly always fit 32 bits; bit by bit where they do not (a division of 64 bits is 2 KB of instructions
+// wherever it stands, and the kernels that divide here have to stay in the instruction cache)
 __device__ __forceinline__ long long quotient(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? static_cast<unsigned>(a) / static_cast<unsigned>(b) : a / b;
+  if (((a | b) >> 32) == 0) return static_cast<unsigned>(a) / static_cast<unsigned>(b);
+  unsigned long long q = 0, r = 0;
+#pragma unroll 1
+  for (int i = 63; i >= 0; --i) {
+    r = r << 1 | (static_cast<unsigned long long>(a) >> i & 1);
+    q <<= 1;
+    if (r >= static_cast<unsigned long long>(b)) { r -= b; q |= 1; }
+  }
+  return static_cast<long long>(q);
 }
 
 template <typename S, typename P>
@@ -67,6 +76,7 @@ __device__ __forceinline__ TcStretch tc_locate(const P& p, DivisionShared& sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = (p.batch + S::kThreads - 1) / S::kThreads, b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
   long long sum = 0;
+#pragma unroll 1
   for (int b = b0; b < b1; ++b) sum += tc_sequence_at<S>(p, b).weight * p.kv_heads;
   long long incl = sum;
 #pragma unroll
@@ -89,6 +99,7 @@ __device__ __forceinline__ TcStretch tc_locate(const P& p, DivisionShared& sh) {
   st.end = min(st.begin + st.quota, total);
   long long at = before + incl - sum;
   if (at <= st.begin && st.begin < at + sum) {
+#pragma unroll 1
     for (int b = b0; b < b1; ++b) {
       const long long w = tc_sequence_at<S>(p, b).weight * p.kv_heads;
       if (st.begin < at + w) { sh.b = b; sh.seq0 = at; break; }
@@ -122,6 +133,7 @@ __device__ __forceinline__ bool tc_next(const P& p, TcStretch& st, TcPiece& pc) 
     if (st.begin >= st.seq0 + all) { st.seq0 += all; ++st.b; continue; }
     const long long head = quotient(st.begin - st.seq0, pc.q.weight), rel = st.begin - st.seq0 - head * pc.q.weight;
     int lo = 0, hi = pc.q.tiles;
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (tiles_before<S>(p, pc.q, mid) <= rel) lo = mid; else hi = mid;

@@ -30,7 +30,7 @@
 namespace vscan {
 namespace kv {
 
-constexpr int kPtThreads = 768, kPtKeys = 128, kPtWhole = 4, kPtExtra = 3;
+constexpr int kPtThreads = 768, kPtKeys = 128, kPtWhole = 8, kPtExtra = 4;
 constexpr int kPtHelper = 16, kPtIssuer = 20, kPtLoader = 21, kPtPlanner = 22;   // first warp of each role
 constexpr int kPtStages = 4, kPtPlan = 4;
 constexpr int kPtReaders = 22;       // warps that read the plan
@@ -105,19 +105,29 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// A wait that may last for all of a piece: the limit of the other waits, 4 s or some two million steps, is granted once more for every
-// 2^17 keys that there may be.  If another role gives up, so does this wait.
-__device__ __forceinline__ bool wait_piece(const PromptParams& p, uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  bool got = false;
-  for (int turn = p.kv_rows >> 17; turn >= 0 && !got && !*abort_flag; --turn)
-    for (uint32_t i = 0; i < tc::kSpinLimit && !got; ++i) {
-      got = tc::mbar_try_wait(bar, parity);
-      if ((i & 1023u) == 1023u && *abort_flag) break;
-    }
+// Bounded wait of a warp, in few instructions: this kernel's code has to stay in the instruction cache
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  bool got = tc::mbar_try_wait(bar, parity);
+#pragma unroll 1
+  for (uint32_t i = 0; i < tc::kSpinLimit && !got; ++i) {
+    if ((i & 1023u) == 1023u && *abort_flag) break;
+    got = tc::mbar_try_wait(bar, parity);
+  }
   if (!got) *abort_flag = 1;
   return __all_sync(0xffffffffu, got);
 }
-
+// A wait that may last for all of a piece: the limit of the other waits, 4 s or some two million steps, is granted once more for every
+// 2^17 keys that there may be.  If another role gives up, so does this wait.
+__device__ __forceinline__ bool wait_piece(const PromptParams& p, uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  bool got = tc::mbar_try_wait(bar, parity);
+#pragma unroll 1
+  for (unsigned long long i = 0, n = static_cast<unsigned long long>((p.kv_rows >> 17) + 1) * tc::kSpinLimit; i < n && !got; ++i) {
+    if ((i & 1023u) == 1023u && *abort_flag) break;
+    got = tc::mbar_try_wait(bar, parity);
+  }
+  if (!got) *abort_flag = 1;
+  return __all_sync(0xffffffffu, got);
+}
 // Keys that row `token` of a sequence sees
 __device__ __forceinline__ int keys_seen(const PromptParams& p, const PtPiece& pc, int token) {
   if (!p.causal) return pc.len;
@@ -259,7 +269,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       float minus_m[2] = {0.f, 0.f};     // what is added to a score; NaN where the reference is infinite
       const bool sees_all = pc.partial >= pc.u1;
       for (int u = pc.u0; u < pc.u1; ++u, ++n_it) {
-        ok = u == pc.u0 ? wait_piece(p, &sh.s_full[tile], n_it & 1, abort_flag) : mbar_wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
+        ok = u == pc.u0 ? wait_piece(p, &sh.s_full[tile], n_it & 1, abort_flag) : wait_warp(&sh.s_full[tile], n_it & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
         uint32_t v[64];                  // v[4 i + k]: row k / 2, column 8 i + k % 2 from the lane's first
@@ -366,7 +376,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       for (int u = pc.partial; u < pc.u1 && ok; ++u, ++n_partial) {
         const int at = pos + 1 + 2 * (u - pc.u0), s = at % kPtStages;
         ok = wait_piece(p, &sh.dirty[n_partial & 1], (n_partial >> 1) & 1, abort_flag) &&
-             mbar_wait_warp(&sh.kv_full[s], (at / kPtStages) & 1, abort_flag);
+             wait_warp(&sh.kv_full[s], (at / kPtStages) & 1, abort_flag);
         if (!ok) break;
         // a row of 64 channels is 128 bytes; 16-byte pieces of a row may be in any order
         unsigned char* tile = kv_sh + s * kTileBytes;
@@ -400,7 +410,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
         if (lane == 0) words[quarter] = mine;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.clean[n_partial & 1]);
-        ok = mbar_wait_warp(&sh.clean[n_partial & 1], (n_partial >> 1) & 1, abort_flag);    // the words of all four
+        ok = wait_warp(&sh.clean[n_partial & 1], (n_partial >> 1) & 1, abort_flag);    // the words of all four
         if (ok && (words[0] | words[1] | words[2] | words[3])) {   // rare: what those values give to the rows that see them, from memory
           if (!odd)
             for (int t = 0; t < 2; ++t)
@@ -488,10 +498,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
 #pragma unroll
       for (int c = 0; c < kDChunks; ++c) umma_f16_ss_x4(tmem + t * 128, a + c * (kChunk >> 4), b + c * (kChunk >> 4), qk, c > 0);
     };
-    auto wait_kv = [&](int at) { return mbar_wait_warp(&sh.kv_full[at % kPtStages], (at / kPtStages) & 1, abort_flag); };
+    auto wait_kv = [&](int at) { return wait_warp(&sh.kv_full[at % kPtStages], (at / kPtStages) & 1, abort_flag); };
     while (ok && next()) {
       const int two = pc.n_rows > half;
-      for (int t = 0; t <= two && ok; ++t) ok = mbar_wait_warp(&sh.q_full[t], n_piece[t] & 1, abort_flag);
+      for (int t = 0; t <= two && ok; ++t) ok = wait_warp(&sh.q_full[t], n_piece[t] & 1, abort_flag);
       ok = ok && wait_kv(pos);
       if (!ok) break;
       tc_fence_after();
@@ -507,18 +517,18 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
         const bool more = u + 1 < pc.u1;
         ok = wait_kv(pos);
         if (u >= pc.partial) {
-          ok = ok && mbar_wait_warp(&sh.clean[n_partial & 1], (n_partial >> 1) & 1, abort_flag);
+          ok = ok && wait_warp(&sh.clean[n_partial & 1], (n_partial >> 1) & 1, abort_flag);
           ++n_partial;
         }
 #pragma unroll 1
         for (int t = 0; t <= two && ok; ++t) {
           if (u == pc.u0 && n_piece[t] > 0) ok = wait_piece(p, &sh.o_free[t], (n_piece[t] - 1) & 1, abort_flag);
-          ok = ok && mbar_wait_warp(&sh.p_half[t], n_it[t] & 1, abort_flag);
+          ok = ok && wait_warp(&sh.p_half[t], n_it[t] & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
           const uint64_t b = desc_mn(kv_addr + vs * kTileBytes);
           umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128, b, pv, u > pc.u0);
-          ok = mbar_wait_warp(&sh.p_full[t], n_it[t] & 1, abort_flag);
+          ok = wait_warp(&sh.p_full[t], n_it[t] & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
           umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128 + 32, b + (64 * 128 >> 4), pv, true);
@@ -551,7 +561,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       const int seq = p.padded ? pc.b : 0, two = pc.n_rows > half;
       for (int i = 2 * pc.u0; i < 2 * pc.u1 && ok; ++i, ++pos) {
         const int s = pos % kPtStages, u = i >> 1;
-        if (pos >= kPtStages) ok = mbar_wait_warp(&sh.kv_empty[s], (pos / kPtStages - 1) & 1, abort_flag);
+        if (pos >= kPtStages) ok = wait_warp(&sh.kv_empty[s], (pos / kPtStages - 1) & 1, abort_flag);
         if (!ok) break;
         if (lane == 0) {
           mbar_arrive_expect_tx(&sh.kv_full[s], kTileBytes);
