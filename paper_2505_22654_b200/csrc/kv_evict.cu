@@ -1,12 +1,13 @@
 // vscan_kv_evict: the tokens that gathered least weight leave the paged 8-bit cache.
 //
 // Two launches.  rank_kernel: a CTA a (sequence, head), or a sequence where all heads keep the same tokens, finds the threshold of
-// the weights by an exact radix select and writes the places of the tokens that stay, ascending.  move_kernel: a group of warps a
-// (block of the result, head, K or V) gathers the block's codes from where they lie and writes them in place.
-//
-// In place: token j of the result comes from place src(j) >= j.  A unit holds all codes of its block in registers, says so in a
-// flag, and writes once every unit in front of it that reads from the block it will write has said so too.  Those units have begun
-// before it (units are handed out by a counter) and wait for nobody before they have read, so the waits end.
+// the weights by an exact radix select and writes the places of the tokens that stay, ascending.  Then the codes of each block of the
+// result are gathered from where they lie and written in place.  Token j of the result comes from place src(j) >= j, so
+//   sweep_kernel   a warp takes a head's K or V from the first block on: what it writes nobody reads any more.  Where there are enough
+//                  heads and sequences to fill the GPU with warps
+//   move_kernel    a group of warps a block.  A unit holds all codes of its block in registers, says so in a flag, and writes once every
+//                  unit in front of it that reads from the block it will write has said so too.  Those units have begun before it
+//                  (units are handed out by a counter) and wait for nobody before they have read, so the waits end
 #include "kv_common.cuh"
 #include "topk.cuh"
 
@@ -137,6 +138,20 @@ __device__ __forceinline__ uint4 recode(const uint4& old, float scale, float inv
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
+// The scale of a block from its peak, and its codes
+struct Fresh { float s, inv; bool nan; };
+template <int KV>
+__device__ __forceinline__ Fresh fresh_scale(uint32_t peak) {
+  const int e = scale_exponent<KV>(__uint_as_float(peak));
+  const bool nan = peak >= 0x7f800000u;
+  return {nan ? __uint_as_float(0x7fc00000u) : exp2_int(e), nan ? 0.f : exp2_int(-e), nan};
+}
+template <int KV>
+__device__ __forceinline__ uint4 moved(const uint4& old, float scale, const Fresh& f) {
+  if (f.nan) return make_uint4(0, 0, 0, 0);
+  return scale == f.s ? old : recode<KV>(old, scale, f.inv);
+}
+
 __host__ __device__ constexpr int move_threads(int w) { return w == 8 ? 256 : 128; }
 
 template <int KV, int W, int HELD>
@@ -251,22 +266,110 @@ __global__ void __launch_bounds__(move_threads(W)) move_kernel(EvictParams p) {
     if (in_group == 0) p.bad[b] = VSCAN_ERR_TIMEOUT;
     return;
   }
-  const float s = peak < 0x7f800000u ? exp2_int(scale_exponent<KV>(__uint_as_float(peak))) : __uint_as_float(0x7fc00000u);
-  const bool nan = s != s;
-  const float inv = nan ? 0.f : exp2_int(-scale_exponent<KV>(__uint_as_float(peak)));
+  const Fresh f = fresh_scale<KV>(peak);
   uint8_t* dst = p.cache[which] + (to << p.shift) * p.head_dim;
 #pragma unroll
   for (int k = 0; k < HELD; ++k) {
     const int c = in_group + k * 32 * W;
-    if (c < total) {
-      uint4 v = held[k];
-      if (nan) v = make_uint4(0, 0, 0, 0);
-      else if (scale[k] != s) v = recode<KV>(v, scale[k], inv);
-      st_16(dst + static_cast<size_t>(c) * 16, v);
-    }
+    if (c < total) st_16(dst + static_cast<size_t>(c) * 16, moved<KV>(held[k], scale[k], f));
   }
-  if (in_group == 0) p.scale[which][to] = s;
+  if (in_group == 0) p.scale[which][to] = f.s;
   store_weights();
+}
+
+// ---------------------------------------------------------------------------------------------- a warp a head's K or V
+// The next block's codes are on their way while one is coded and written.  Bound by DRAM once the loads of some 30 warps an SM are under way.
+constexpr int kSweepThreads = 128;
+
+template <int KV, int HELD>
+__global__ void __launch_bounds__(kSweepThreads, HELD > 4 ? 4 : 6) sweep_kernel(EvictParams p) {
+  constexpr int kWeights = 8;
+  grid_dependency_wait();
+  const int lane = threadIdx.x & 31;
+  const long long unit = static_cast<long long>(blockIdx.x) * (kSweepThreads / 32) + (threadIdx.x >> 5);
+  const int which = static_cast<int>(unit & 1);
+  const long long rest = unit >> 1;
+  const int h = static_cast<int>(rest % p.kv_heads);
+  if (rest / p.kv_heads >= p.batch) return;
+  const int b = static_cast<int>(rest / p.kv_heads);
+  const int2 stay = p.stay[b];
+  const bool moves_weights = which == 0 && p.weight_out && (stay.y || p.weight_out != p.weight);
+  if (stay.x <= 0 || (!stay.y && !moves_weights)) return;
+  const int32_t* table = p.block_table + static_cast<size_t>(b) * p.max_blocks;
+  const int32_t* src = p.kept + (static_cast<size_t>(b) * p.heads + (p.heads > 1 ? h : 0)) * p.max_keep;
+  const int mask = p.block_size - 1, cpr = p.head_dim / 16;
+  const uint8_t* codes = p.cache[which];
+  int row[HELD];                                     // of this lane's pieces within a block, and their bytes within a row
+  int col[HELD];
+#pragma unroll
+  for (int k = 0; k < HELD; ++k) {
+    const int c = lane + k * 32;
+    row[k] = c / cpr;
+    col[k] = (c - row[k] * cpr) * 16;
+  }
+  const int columns = ((stay.x - 1) >> p.shift) + 1;
+  uint4 held[HELD], next[HELD];
+  float scale[HELD], next_scale[HELD];
+  bool moves = false, next_moves;                    // a block of which some token does not stay in its place
+  auto load = [&](int j, uint4* v, float* sc) {
+    const int first = j << p.shift, n = min(stay.x - first, p.block_size);
+    const bool some = n > 0 && stay.y && src[first + max(n, 1) - 1] != first + n - 1;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+      v[k] = make_uint4(0, 0, 0, 0);
+      sc[k] = 0.f;
+      if (some && row[k] < n) {
+        const int t = src[first + row[k]];
+        const size_t from = static_cast<size_t>(table[t >> p.shift]) * p.kv_heads + h;
+        sc[k] = p.scale[which][from];
+        v[k] = *reinterpret_cast<const uint4*>(codes + ((from << p.shift) + (t & mask)) * p.head_dim + col[k]);
+      }
+    }
+    return some;
+  };
+  moves = load(0, held, scale);
+  for (int j = 0; j < columns; ++j) {
+    const int first = j << p.shift, n = min(stay.x - first, p.block_size);
+    const size_t to = static_cast<size_t>(table[j]) * p.kv_heads + h;
+    next_moves = j + 1 < columns && load(j + 1, next, next_scale);
+    if (moves_weights && (moves || p.weight_out != p.weight)) {
+      float w[kWeights];
+#pragma unroll
+      for (int k = 0; k < kWeights; ++k) {
+        const int r = lane + k * 32;
+        if (r < n) {
+          const int t = src[first + r];
+          w[k] = p.weight[((static_cast<size_t>(table[t >> p.shift]) * p.kv_heads + h) << p.shift) + (t & mask)];
+        }
+      }
+      __syncwarp();                                  // all of them are read before one is written
+#pragma unroll
+      for (int k = 0; k < kWeights; ++k) {
+        const int r = lane + k * 32;
+        if (r < n) p.weight_out[(to << p.shift) + r] = w[k];
+      }
+    }
+    if (moves) {
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < HELD; ++k) {
+        const float m = code_magnitude<KV>(peak_code<KV>(held[k])) * scale[k];
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(m)));
+      }
+      // (the reduction also has all lanes' codes read before one is written)
+      const uint32_t peak = __reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu);
+      const Fresh f = fresh_scale<KV>(peak);
+      uint8_t* dst = p.cache[which] + (to << p.shift) * p.head_dim;
+#pragma unroll
+      for (int k = 0; k < HELD; ++k)
+        if (row[k] < n) st_16(dst + static_cast<size_t>(lane + k * 32) * 16, moved<KV>(held[k], scale[k], f));
+      if (lane == 0) p.scale[which][to] = f.s;
+    }
+    __syncwarp();
+    moves = next_moves;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) { held[k] = next[k]; scale[k] = next_scale[k]; }
+  }
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -321,6 +424,8 @@ static EvictLayout layout_of(const vscan_kv_evict_desc* d) {
   return l;
 }
 
+constexpr int64_t kSweeps = 148 * 14;
+
 template <int KV>
 static vscan_status launch_evict(const EvictParams& p, cudaStream_t stream) {
   const int64_t room = static_cast<int64_t>(p.max_blocks) * p.block_size;
@@ -332,8 +437,19 @@ static vscan_status launch_evict(const EvictParams& p, cudaStream_t stream) {
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
   if (p.columns == 0) return VSCAN_OK;
+  const int chunks = p.block_size * p.head_dim / 16;
+  const int64_t sweeps = static_cast<int64_t>(p.batch) * p.kv_heads * 2;
+  if (chunks <= 256 && sweeps >= kSweeps) {
+    const dim3 grid(static_cast<unsigned>((sweeps + kSweepThreads / 32 - 1) / (kSweepThreads / 32)));
+    prof_before("kv_evict_sweep", stream);
+    VSCAN_CUDA_TRY(chunks <= 128 ? launch_dependent(sweep_kernel<KV, 4>, grid, dim3(kSweepThreads), 0, stream, p)
+                                 : launch_dependent(sweep_kernel<KV, 8>, grid, dim3(kSweepThreads), 0, stream, p));
+    prof_after(stream);
+    VSCAN_AFTER_LAUNCH();
+    return VSCAN_OK;
+  }
   // as many warps to a unit as keep its codes in registers
-  const int chunks = p.block_size * p.head_dim / 16, w = chunks <= 256 ? 1 : 8, groups = move_threads(w) / 32 / w;
+  const int w = chunks <= 256 ? 1 : 8, groups = move_threads(w) / 32 / w;
   const int64_t units = static_cast<int64_t>(p.batch) * p.kv_heads * 2 * p.columns;
   const dim3 grid(static_cast<unsigned>((units + groups - 1) / groups));
   prof_before("kv_evict_move", stream);

@@ -467,6 +467,21 @@ def test_evict_budgets_beyond_max_keep_and_sequences_out_of_order(per_head):
     _evict_case("e4m3", 2, 32, 16, [-3, 60], [50, 50], per_head=per_head)
 
 
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+@pytest.mark.parametrize("hk,d,bs", [(24, 32, 16), (32, 128, 32), (40, 16, 64), (26, 256, 16), (32, 48, 32)])
+def test_evict_of_many_heads(kv, hk, d, bs):
+    """Enough heads and sequences for a warp each."""
+    rng = np.random.default_rng(hk)
+    B = -(-1100 // hk)
+    lens = [int(n) for n in rng.integers(0, 5 * bs, size=B)]
+    budget = [int(rng.integers(0, n + 1)) for n in lens]
+
+    def spoil(table, weight, scale, codes):
+        scale[0][table[1][0], 3] = np.nan
+    for per_head, where in ((True, "other"), (True, "same"), (False, "none")):
+        _evict_case(kv, hk, d, bs, lens, budget, 2, 3, per_head, where=where, seed=d, spoil=spoil)
+
+
 @pytest.mark.parametrize("per_head", [True, False])
 @pytest.mark.parametrize("length,keep", [(5000, 1200), (20000, 9000), (20000, 19990)])
 def test_evict_long_sequences(per_head, length, keep):
