@@ -8,7 +8,7 @@
 //   move_kernel    a group of warps a block.  A unit holds all codes of its block in registers, says so in a flag, and writes once every
 //                  unit in front of it that reads from the block it will write has said so too.  Those units have begun before it
 //                  (units are handed out by a counter) and wait for nobody before they have read, so the waits end
-#include "kv_common.cuh"
+#include "kv_attention_mma.cuh"
 #include "topk.cuh"
 
 namespace vscan {
@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
     return;
   }
   uint32_t* keys = p.held >= len ? rank_smem : p.keys + (static_cast<size_t>(b) * p.heads + head) * room;
+#pragma unroll 4
   for (int t = threadIdx.x; t < len; t += blockDim.x) {
     const float* w = p.weight + (static_cast<size_t>(table[t >> p.shift]) * p.kv_heads << p.shift) + (t & (p.block_size - 1));
     float rank;
@@ -88,17 +89,28 @@ __global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
   uint32_t threshold;
   int need;
   block_radix_select(keys, nullptr, len, n, sc, threshold, need);
-  int above = 0, equal = 0;                          // of the tokens in front: over the threshold, and on it
-  for (int t0 = 0; t0 < len; t0 += blockDim.x) {
-    const int t = t0 + threadIdx.x;
-    const uint32_t key = t < len ? keys[t] : 0u;
-    const bool over = t < len && key > threshold, on = t < len && key == threshold;
-    int total;
-    const int before = block_exclusive_scan((over ? 1 << 16 : 0) + (on ? 1 : 0), sc.warp_sums, total);
-    const int e = equal + (before & 0xffff);
-    if (over || (on && e < need)) out[above + (before >> 16) + min(e, need)] = t;
-    above += total >> 16;
-    equal += total & 0xffff;
+  // each warp a run of the tokens: how many are over the threshold and on it, then their places behind those of the runs in front
+  __shared__ int over_of[32], on_of[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int run = ((len + warps - 1) / warps + 31) & ~31, begin = static_cast<int>(min(static_cast<long long>(warp) * run, static_cast<long long>(len)));
+  const int end = static_cast<int>(min(static_cast<long long>(begin) + run, static_cast<long long>(len)));
+  int over = 0, on = 0;
+  for (int t0 = begin; t0 < end; t0 += 32) {
+    const uint32_t key = t0 + lane < end ? keys[t0 + lane] : 0u;
+    over += __popc(__ballot_sync(0xffffffffu, t0 + lane < end && key > threshold));
+    on += __popc(__ballot_sync(0xffffffffu, t0 + lane < end && key == threshold));
+  }
+  if (lane == 0) { over_of[warp] = over; on_of[warp] = on; }
+  __syncthreads();
+  int above = __reduce_add_sync(0xffffffffu, lane < warp ? over_of[lane] : 0), equal = __reduce_add_sync(0xffffffffu, lane < warp ? on_of[lane] : 0);
+  for (int t0 = begin; t0 < end; t0 += 32) {
+    const uint32_t key = t0 + lane < end ? keys[t0 + lane] : 0u, before = (1u << lane) - 1u;
+    const unsigned overs = __ballot_sync(0xffffffffu, t0 + lane < end && key > threshold);
+    const unsigned ons = __ballot_sync(0xffffffffu, t0 + lane < end && key == threshold);
+    const int e = equal + __popc(ons & before);
+    if (((overs >> lane) & 1u) || (((ons >> lane) & 1u) && e < need)) out[above + __popc(overs & before) + min(e, need)] = t0 + lane;
+    above += __popc(overs);
+    equal += __popc(ons);
   }
 }
 
@@ -124,6 +136,30 @@ __device__ __forceinline__ float code_magnitude(uint32_t code) {
     return static_cast<float>(code);                 // 128 where the code is -128
   }
 }
+// 16 codes times a power of two between 2^-14 and 2^14 that fit the type afterwards, as codes: two at a time in f16.  Codes are exact there; so is the
+// product as far as a code's last bit goes; one rounding, to nearest, ties to even (I8: 1.5 x 2^10 + x is rounded to a whole number, whose
+// last byte is the code).
+template <int KV>
+__device__ __forceinline__ uint4 recode_half(const uint4& old, uint32_t ratio) {
+  const uint32_t w[4] = {old.x, old.y, old.z, old.w};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t lo, hi;
+    codes_to_f16<KV>(w[i], lo, hi);
+    if constexpr (KV == VSCAN_KV_E4M3) {
+      asm("{\n\t.reg .b16 a, b;\n\t.reg .b32 x, y;\n\t"
+          "mul.rn.f16x2 x, %1, %3;\n\tmul.rn.f16x2 y, %2, %3;\n\t"
+          "cvt.rn.satfinite.e4m3x2.f16x2 a, x;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, y;\n\t"
+          "mov.b32 %0, {a, b};\n\t}"
+          : "=r"(r[i]) : "r"(lo), "r"(hi), "r"(ratio));
+    } else {
+      asm("fma.rn.f16x2 %0, %0, %2, %3;\n\tfma.rn.f16x2 %1, %1, %2, %3;" : "+r"(lo), "+r"(hi) : "r"(ratio), "r"(0x66006600u));
+      r[i] = __byte_perm(lo, hi, 0x6420);
+    }
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
 // 16 codes of one scale as codes of another: the value, then its code
 template <int KV>
 __device__ __forceinline__ uint4 recode(const uint4& old, float scale, float inv) {
@@ -139,17 +175,20 @@ __device__ __forceinline__ uint4 recode(const uint4& old, float scale, float inv
 }
 
 // The scale of a block from its peak, and its codes
-struct Fresh { float s, inv; bool nan; };
+struct Fresh { float s, inv; bool nan, fits; };   // fits: no element is beyond the largest code
 template <int KV>
 __device__ __forceinline__ Fresh fresh_scale(uint32_t peak) {
   const int e = scale_exponent<KV>(__uint_as_float(peak));
   const bool nan = peak >= 0x7f800000u;
-  return {nan ? __uint_as_float(0x7fc00000u) : exp2_int(e), nan ? 0.f : exp2_int(-e), nan};
+  return {nan ? __uint_as_float(0x7fc00000u) : exp2_int(e), nan ? 0.f : exp2_int(-e), nan, e < kExpMax};
 }
 template <int KV>
 __device__ __forceinline__ uint4 moved(const uint4& old, float scale, const Fresh& f) {
   if (f.nan) return make_uint4(0, 0, 0, 0);
-  return scale == f.s ? old : recode<KV>(old, scale, f.inv);
+  if (scale == f.s) return old;
+  const uint32_t ratio = __float_as_uint(scale * f.inv), e = ratio >> 23;
+  if (!(ratio & 0x7fffffu) && e >= 127 - 14 && e <= 127 + 14 && f.fits) return recode_half<KV>(old, (e - 127 + 15) * 0x04000400u);
+  return recode<KV>(old, scale, f.inv);
 }
 
 __host__ __device__ constexpr int move_threads(int w) { return w == 8 ? 256 : 128; }
@@ -282,7 +321,7 @@ __global__ void __launch_bounds__(move_threads(W)) move_kernel(EvictParams p) {
 constexpr int kSweepThreads = 128;
 
 template <int KV, int HELD>
-__global__ void __launch_bounds__(kSweepThreads, HELD > 4 ? 4 : 6) sweep_kernel(EvictParams p) {
+__global__ void __launch_bounds__(kSweepThreads, HELD > 4 ? 4 : 5) sweep_kernel(EvictParams p) {
   constexpr int kWeights = 8;
   grid_dependency_wait();
   const int lane = threadIdx.x & 31;
@@ -429,7 +468,9 @@ constexpr int64_t kSweeps = 148 * 14;
 template <int KV>
 static vscan_status launch_evict(const EvictParams& p, cudaStream_t stream) {
   const int64_t room = static_cast<int64_t>(p.max_blocks) * p.block_size;
-  const int threads = room <= 1024 ? 128 : room <= 4096 ? 256 : 1024;
+  // many sequences of few tokens: small CTAs, several an SM; else as many threads as there are, latency counts
+  const bool few = static_cast<int64_t>(p.heads) * p.batch <= 2 * 148;
+  const int threads = room <= 512 ? 128 : room <= 1024 ? (few ? 512 : 128) : room <= 4096 ? (few ? 1024 : 256) : 1024;
   const size_t smem = static_cast<size_t>(p.held) * 4;
   VSCAN_CUDA_TRY(allow_smem(rank_kernel, smem));
   prof_before("kv_evict_rank", stream);
