@@ -537,3 +537,91 @@ def test_evict_in_a_graph_and_again():
         assert all(torch.equal(t.view(torch.uint8) if t.element_size() == 1 else t, u.view(torch.uint8) if u.element_size() == 1 else u)
                    for t, u in zip(dev, want))
     assert vs.vscan_check(ws) == 0
+
+
+# --------------------------------------------------------------------------- a run of them together
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("per_head", [True, False])
+def test_a_layer_from_prompts_to_evictions(kv, dtype, per_head):
+    """Prompts, decode steps, an eviction, decode steps, another one: each call's result against 64 bits from what the cache held before it."""
+    hq, hk, d, bs, B, cols = 6, 2, 64, 16, 3, 12
+    g, kind = gen(11), KV[kv][0]
+    c = vs.VScanCache(num_blocks=B * cols, block_size=bs, kv_heads=hk, head_dim=d, batch=B, max_blocks=cols, rows=500, kv_dtype=kv, weights=True)
+    rope, scale = vs.rope_table(d, [d // 2]), d ** -0.5
+    weight = np.zeros((B * cols, hk, bs))
+
+    def state():
+        return [t.view(torch.uint8).cpu().numpy() for t in (c.k, c.v)], [t.double().cpu().numpy() for t in (c.k_scale, c.v_scale)], c.block_table.tolist()
+
+    def sequence(codes, scales, table, i, b, T):
+        return co.gather(codes[i], scales[i], table[b], T, bs, kind)
+
+    def weights_follow(q, lse, new, lens, decay, window):
+        codes, scales, table = state()
+        slack = co.weigh(weight, [q[b, :, :n].transpose(0, 1).double().cpu().numpy() for b, n in enumerate(new)],
+                         [lse[b][:n] for b, n in enumerate(new)], codes[0], scales[0], lens, table, bs, kind, scale, decay, window)
+        # lse is that of 64 bits here: the calls' own is off by what test_attention allows, at most 1e-5 + (head_dim + 8) 2^-24 of the scores' size
+        tol = (2 * (d + 8) * 2.0 ** -24) * slack + (1e-5 + 2.0 ** -21 + (max(new) * 3 / 4 + 16) * 2.0 ** -24) * np.abs(weight)
+        got = c.weight.double().cpu().numpy()
+        for b, T in enumerate(lens):
+            for t in range(T):
+                at = (table[b][t // bs], slice(None), t % bs)
+                assert (np.abs(got[at] - weight[at]) <= tol[at] + 1e-30).all(), (b, t, got[at], weight[at])
+        weight[:] = got
+
+    new = [140, 17, 63]
+    q, k, v = (torch.randn((B, H, max(new), d), generator=g).to(DT[dtype]).cuda() for H in (hq, hk, hk))
+    pos = torch.arange(max(new), dtype=torch.int32, device="cuda").expand(1, B, -1).contiguous()
+    out = c.prompt(q, k, v, pos, rope, i32(new), scale, window=8)
+    tq, tk = vs.vscan_rope(q, k, pos, *rope)
+    lse = []
+    for b, n in enumerate(new):
+        x = [t[b, :, :n].transpose(0, 1) for t in (tq, tk, v)]
+        _, ref_lse, _, _ = plain_attention(*x, scale, True)
+        got_lse = ref_lse.float()                                       # its own check is in test_attention
+        check_attention(dtype, out[b, :, :n].transpose(0, 1), got_lse, *x, scale, True)
+        lse.append(ref_lse.cpu().numpy())
+    lens = list(new)
+    weights_follow(tq, lse, new, lens, 1.0, 8)
+    assert c.kv_len.tolist() == lens and c.check() == (0, 0)
+    where = [pos[0, b, :n].tolist() for b, n in enumerate(new)]
+    for turn in range(2):
+        for _ in range(3):
+            q, k, v = (torch.randn((B, H, 1, d), generator=g).to(DT[dtype]).cuda() for H in (hq, hk, hk))
+            at = torch.tensor([[[w[-1] + 1] for w in where]], dtype=torch.int32, device="cuda")
+            for w in where:
+                w.append(w[-1] + 1)
+            out = c.step(q, k, v, at, rope, i32([1] * B), scale, decay=0.75)
+            lens = [n + 1 for n in lens]
+            tq, _ = vs.vscan_rope(q, k, at, *rope)
+            codes, scales, table = state()
+            lse = []
+            for b, T in enumerate(lens):
+                (kk, there), (vv, _) = (sequence(codes, scales, table, i, b, T) for i in range(2))
+                ref, ref_lse, size, reach = co.attention(tq[b].transpose(0, 1).double().cpu().numpy(), kk, vv, there, scale, True, T - 1)
+                err = np.abs(out[b].transpose(0, 1).double().cpu().numpy() - ref)
+                e = (d + 8) * 2.0 ** -24 * reach
+                tol = (2 * e + 2.0 ** -21 + (2.0 ** -11 if dtype == "bf16" else 0) + (T / 4 + 16) * 2.0 ** -24)[..., None] * size + h(dtype) * np.abs(ref)
+                assert (err <= tol + T * 2.0 ** -29 * np.abs(vv).max()).all()
+                lse.append(ref_lse)
+            weights_follow(tq, lse, [1] * B, lens, 0.75, None)
+        codes, scales, table = state()
+        budget = [60, 40, 30 + turn]
+        ref, delta, moved, wrong = co.evict(codes, scales, weight.astype(np.float32), lens, budget, table, bs, kind, 64, 2, 5, per_head)
+        kept = torch.full((B, hk if per_head else 1, 64), -1, dtype=torch.int32, device="cuda")
+        assert c.evict(i32(budget), 64, keep_first=2, keep_last=5, per_head=per_head, kept=kept).tolist() == delta and not wrong
+        for b in range(B):
+            for i in range(kept.shape[1]):
+                assert kept[b, i, :lens[b] + delta[b]].tolist() == ref[b][i]
+        lens = [n + e for n, e in zip(lens, delta)]
+        assert c.kv_len.tolist() == lens and c.check() == (0, 0)
+        now, now_scales, _ = state()
+        for b, T in enumerate(lens):
+            for i in range(2):
+                want, got = sequence(codes, scales, table, i, b, T), sequence(now, now_scales, table, i, b, T)
+                np.testing.assert_array_equal(got[0], want[0])
+            for t in range(T):
+                weight[table[b][t // bs], :, t % bs] = [moved[table[b][t // bs], head, t % bs] for head in range(hk)]
+        free = int(c._plan["ring_state_out"][1] - c._plan["ring_state_out"][0])
+        assert free == B * cols - sum(-(-n // bs) for n in lens)
