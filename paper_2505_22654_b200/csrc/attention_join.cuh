@@ -149,15 +149,26 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int
         factor[i][in_slab] = f;
       }
       __syncthreads();
+      // half of a piece's loads on their way at once
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int idx = threadIdx.x + e * kJoinThreads;
-        if (idx < total) {
-          const int row = idx / per_row, c = (idx - row * per_row) * 4;
-          for (int i = 0; i < count; ++i) {
-            const float f = factor[i][row];
-            const float4 x = *reinterpret_cast<const float4*>(pc.at(first + i) + static_cast<size_t>(r0 + row) * D + c);
-            o[e].x = fmaf(f, x.x, o[e].x); o[e].y = fmaf(f, x.y, o[e].y); o[e].z = fmaf(f, x.z, o[e].z); o[e].w = fmaf(f, x.w, o[e].w);
+      for (int half = 0; half < kEach; half += kEach / 2) {
+        for (int i = 0; i < count; ++i) {
+          const float* part = pc.at(first + i) + static_cast<size_t>(r0) * D;
+          float4 x[kEach / 2];
+#pragma unroll
+          for (int e = 0; e < kEach / 2; ++e) {
+            const int idx = threadIdx.x + (half + e) * kJoinThreads;
+            x[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (idx < total) x[e] = *reinterpret_cast<const float4*>(part + static_cast<size_t>(idx) * 4);
+          }
+#pragma unroll
+          for (int e = 0; e < kEach / 2; ++e) {
+            const int idx = threadIdx.x + (half + e) * kJoinThreads;
+            if (idx < total) {
+              const float f = factor[i][idx / per_row];
+              float4& a = o[half + e];
+              a.x = fmaf(f, x[e].x, a.x); a.y = fmaf(f, x[e].y, a.y); a.z = fmaf(f, x[e].z, a.z); a.w = fmaf(f, x[e].w, a.w);
+            }
           }
         }
       }
@@ -176,8 +187,12 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int
         const RowAt at = row_at(p, bd.tile, bd.head, r0 + row);
         char* out = out_at(p, bd.b, bd.first, at);
         const float inv = d == 0.f ? 0.f : 1.f / d;
-        store_out<T>(out, c, o[e].x * inv); store_out<T>(out, c + 1, o[e].y * inv);
-        store_out<T>(out, c + 2, o[e].z * inv); store_out<T>(out, c + 3, o[e].w * inv);
+        if constexpr (sizeof(T) == 2) {
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(o[e].x * inv, o[e].y * inv), hi = __floats2bfloat162_rn(o[e].z * inv, o[e].w * inv);
+          *reinterpret_cast<uint2*>(out + c * 2) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        } else {
+          *reinterpret_cast<float4*>(out + c * 4) = make_float4(o[e].x * inv, o[e].y * inv, o[e].z * inv, o[e].w * inv);
+        }
       }
     }
     if (turn == 0 && on && p.lse) {

@@ -473,13 +473,30 @@ def test_evict_of_many_heads(kv, hk, d, bs):
     """Enough heads and sequences for a warp each."""
     rng = np.random.default_rng(hk)
     B = -(-1100 // hk)
-    lens = [int(n) for n in rng.integers(0, 5 * bs, size=B)]
+    lens = [int(n) for n in rng.integers(0, min(5 * bs, 400), size=B)]     # (tables of at most 512 tokens at blocks of 16 to 64)
     budget = [int(rng.integers(0, n + 1)) for n in lens]
 
     def spoil(table, weight, scale, codes):
         scale[0][table[1][0], 3] = np.nan
     for per_head, where in ((True, "other"), (True, "same"), (False, "none")):
-        _evict_case(kv, hk, d, bs, lens, budget, 2, 3, per_head, where=where, seed=d, spoil=spoil)
+        _evict_case(kv, hk, d, bs, lens, budget, 2, 3, per_head, where=where, seed=d, spoil=spoil, ties=where == "same")
+
+
+def test_evict_of_many_short_sequences_out_of_order_and_of_no_finite_rank():
+    rng = np.random.default_rng(5)
+    lens = [int(n) for n in rng.integers(-1, 200, size=310)]
+    budget = [int(n) for n in rng.integers(-2, 150, size=310)]
+
+    def spoil(table, weight, scale, codes):
+        weight[rng.random(weight.shape) < 0.3] = np.nan
+        weight[rng.random(weight.shape) < 0.3] = -np.inf
+        weight[rng.random(weight.shape) < 0.2] = np.inf
+        weight[rng.random(weight.shape) < 0.2] = -0.0
+        for b in range(0, 310, 9):
+            if lens[b] > 0:
+                table[b][(lens[b] - 1) // 16] = (-1, 10 ** 6)[b % 2]
+    for per_head in (True, False):
+        _evict_case("i8", 3, 16, 16, lens, budget, 1, 2, per_head, spoil=spoil, max_keep=120)
 
 
 @pytest.mark.parametrize("per_head", [True, False])
