@@ -20,7 +20,9 @@ constexpr size_t flat_smem() { return (static_cast<size_t>(kFlatRows) * (DP + 4)
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(PromptParams p) {
-  constexpr int kQ = DP + 4, kP = kFlatKeys + 4, kChunks = DP / 64;
+  // a thread's channels: 4 of every 64, or 2 of every 32 (heads of 72 to 96)
+  constexpr int kVec = DP == 96 ? 2 : 4, kChunks = DP / (16 * kVec), kChannels = kVec * kChunks;
+  constexpr int kQ = DP + 4, kP = kFlatKeys + 4;
   static_assert(kP <= kQ, "weights lie over the keys");
   extern __shared__ __align__(16) float flat_sh[];
   float* q_sh = flat_sh;                        // [rows][DP + 4]
@@ -63,14 +65,14 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
     __syncthreads();                            // the buffers of the piece before are done with
     fill(q_sh, kQ, pc.n_rows, [&](int r) { return q_at(p, pc.b, s.first, row_of(r)); });
     int seen[4];
-    float m[4], l[4], o[4][4 * kChunks];
+    float m[4], l[4], o[4][kChannels];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = y * 4 + i;
       seen[i] = r < pc.n_rows ? visible(p, s, row_of(r).i) : 0;
       m[i] = -INFINITY; l[i] = 0.f;
 #pragma unroll
-      for (int c = 0; c < 4 * kChunks; ++c) o[i][c] = 0.f;
+      for (int c = 0; c < kChannels; ++c) o[i][c] = 0.f;
     }
     for (int u = pc.u0; u < pc.u1; ++u) {
       const int t0 = u * kFlatKeys, there = min(pc.most - t0, kFlatKeys);
@@ -84,7 +86,7 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
 #pragma unroll
         for (int j = 0; j < 4; ++j) dot[i][j] = 0.f;
 #pragma unroll 4
-      for (int c = 0; c < DP; c += 4) {
+      for (int c = 0; c < D; c += 4) {
         float4 a[4], b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -115,7 +117,7 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
         if (top != m[i]) {
           l[i] *= f;
 #pragma unroll
-          for (int c = 0; c < 4 * kChunks; ++c) o[i][c] *= f;
+          for (int c = 0; c < kChannels; ++c) o[i][c] *= f;
           m[i] = top;
         }
 #pragma unroll
@@ -142,14 +144,20 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
-              const float4 f = *reinterpret_cast<const float4*>(v_sh + (t + j) * DP + c * 64 + x * 4);
+              float f[kVec];
+              const float* from = v_sh + (t + j) * DP + (c * 16 + x) * kVec;
+              if constexpr (kVec == 4) {
+                const float4 y = *reinterpret_cast<const float4*>(from);
+                f[0] = y.x; f[1] = y.y; f[2] = y.z; f[3] = y.w;
+              } else {
+                const float2 y = *reinterpret_cast<const float2*>(from);
+                f[0] = y.x; f[1] = y.y;
+              }
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 if (decltype(masked)::value && t0 + t + j >= seen[i]) continue;
-                o[i][4 * c] = fmaf(w[i][j], f.x, o[i][4 * c]);
-                o[i][4 * c + 1] = fmaf(w[i][j], f.y, o[i][4 * c + 1]);
-                o[i][4 * c + 2] = fmaf(w[i][j], f.z, o[i][4 * c + 2]);
-                o[i][4 * c + 3] = fmaf(w[i][j], f.w, o[i][4 * c + 3]);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) o[i][kVec * c + e] = fmaf(w[i][j], f[e], o[i][kVec * c + e]);
               }
             }
         }
@@ -170,13 +178,13 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
       char* out = out_at(p, pc.b, s.first, at);
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
-        const int ch = c * 64 + x * 4;
+        const int ch = (c * 16 + x) * kVec;
         if (ch >= D) continue;
-        if (complete) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) store_out<T>(out, ch + j, sum == 0.f ? 0.f : o[i][4 * c + j] / sum);
-        } else {
-          *reinterpret_cast<float4*>(part + static_cast<size_t>(r) * D + ch) = make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
+        for (int e = 0; e < kVec; ++e) {
+          const float v = o[i][kVec * c + e];
+          if (complete) store_out<T>(out, ch + e, sum == 0.f ? 0.f : v / sum);
+          else part[static_cast<size_t>(r) * D + ch + e] = v;
         }
       }
       if (x == 0) {
@@ -294,7 +302,7 @@ static vscan_status launch_flat(const PromptParams& p, const PromptPlan& pl, cud
 
 template <typename T>
 static vscan_status launch_flats(const PromptParams& p, const PromptPlan& pl, cudaStream_t stream) {
-  return p.head_dim <= 64 ? launch_flat<T, 64>(p, pl, stream) : p.head_dim <= 128 ? launch_flat<T, 128>(p, pl, stream) : launch_flat<T, 256>(p, pl, stream);
+  return p.head_dim <= 64 ? launch_flat<T, 64>(p, pl, stream) : p.head_dim <= 96 ? launch_flat<T, 96>(p, pl, stream) : p.head_dim <= 128 ? launch_flat<T, 128>(p, pl, stream) : launch_flat<T, 256>(p, pl, stream);
 }
 
 template <typename T>
