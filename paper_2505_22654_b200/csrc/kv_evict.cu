@@ -70,20 +70,32 @@ __global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
     return;
   }
   uint32_t* keys = p.held >= len ? rank_smem : p.keys + (static_cast<size_t>(b) * p.heads + head) * room;
-#pragma unroll 4
-  for (int t = threadIdx.x; t < len; t += blockDim.x) {
-    const float* w = p.weight + (static_cast<size_t>(table[t >> p.shift]) * p.kv_heads << p.shift) + (t & (p.block_size - 1));
-    float rank;
-    if (t < p.keep_first || t >= static_cast<long long>(len) - p.keep_last) {
-      rank = INFINITY;
-    } else if (p.heads > 1 || p.kv_heads == 1) {
-      rank = __ldg(w + (static_cast<size_t>(head) << p.shift));
-    } else {
-      double sum = 0.;
-      for (int h = 0; h < p.kv_heads; ++h) sum += __ldg(w + (static_cast<size_t>(h) << p.shift));
-      rank = static_cast<float>(sum);
+  constexpr int kAhead = 4;                          // tokens of a thread whose loads are on their way at once
+  const bool one_head = p.heads > 1 || p.kv_heads == 1;
+  for (long long t0 = threadIdx.x; t0 < len; t0 += kAhead * blockDim.x) {
+    const float* w[kAhead];
+    float rank[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int t = static_cast<int>(min(t0 + u * static_cast<long long>(blockDim.x), static_cast<long long>(len) - 1));
+      w[u] = p.weight + (static_cast<size_t>(table[t >> p.shift]) * p.kv_heads << p.shift) + (t & (p.block_size - 1));
     }
-    keys[t] = rank_key(rank);
+    if (one_head) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) rank[u] = __ldg(w[u] + (static_cast<size_t>(head) << p.shift));
+    } else {
+      double sum[kAhead] = {};
+      for (int h = 0; h < p.kv_heads; ++h)
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) sum[u] += __ldg(w[u] + (static_cast<size_t>(h) << p.shift));
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) rank[u] = static_cast<float>(sum[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const long long t = t0 + u * static_cast<long long>(blockDim.x);
+      if (t < len) keys[t] = rank_key(t < p.keep_first || t >= static_cast<long long>(len) - p.keep_last ? INFINITY : rank[u]);
+    }
   }
   __syncthreads();
   uint32_t threshold;
@@ -271,6 +283,13 @@ __device__ __forceinline__ uint4 moved(const uint4& old, float scale, const Fres
   return recode<KV>(old, scale, f.inv);
 }
 
+// A load that stands where it is written
+__device__ __forceinline__ int load_now(const int32_t* at) {
+  int v;
+  asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(at) : "memory");
+  return v;
+}
+
 __host__ __device__ constexpr int move_threads(int w) { return w == 8 ? 256 : 128; }
 
 template <int KV, int W, int HELD>
@@ -289,18 +308,26 @@ __global__ void __launch_bounds__(move_threads(W)) move_kernel(EvictParams p) {
   const int h = static_cast<int>(rest % p.kv_heads);
   rest /= p.kv_heads;
   const int b = static_cast<int>(rest % p.batch), j = static_cast<int>(rest / p.batch);
-  if (j >= p.columns) return;                        // (a group of eight warps is its whole CTA)
+  if (j >= p.columns) return;                        // (a group of several warps is its whole CTA)
+  const int32_t* table = p.block_table + static_cast<size_t>(b) * p.max_blocks;
+  const int32_t* src = p.kept + (static_cast<size_t>(b) * p.heads + (p.heads > 1 ? h : 0)) * p.max_keep;
+  const int first = j << p.shift, mask = p.block_size - 1, cpr = p.head_dim / 16;
+  // places of this thread's pieces, as far as the list goes, beside the loads that say how far it counts
+  int from[HELD];
+#pragma unroll
+  for (int k = 0; k < HELD; ++k) {
+    const int r = (in_group + k * 32 * W) / cpr;
+    from[k] = load_now(src + min(first + min(r, mask), p.max_keep - 1));
+  }
+  const int ahead = j - 1 - lane >= 0 ? load_now(src + ((j - 1 - lane) << p.shift) + mask) : -1;   // last token of a unit in front
   const int2 stay = p.stay[b];
-  const int first = j << p.shift, n = min(stay.x - first, p.block_size);
+  const int n = min(stay.x - first, p.block_size);
   if (n <= 0) return;
   const bool moves_weights = which == 0 && p.weight_out && (stay.y || p.weight_out != p.weight);
   if (!stay.y && !moves_weights) return;
-  const int32_t* table = p.block_table + static_cast<size_t>(b) * p.max_blocks;
-  const int32_t* src = p.kept + (static_cast<size_t>(b) * p.heads + (p.heads > 1 ? h : 0)) * p.max_keep;
   const size_t to = static_cast<size_t>(table[j]) * p.kv_heads + h;
   const int last = src[first + n - 1];
   const bool stays = last == first + n - 1;          // places ascend and none is below its number: then all of the block's tokens stay
-  const int mask = p.block_size - 1;
 
   float w[kWeights];
   if (moves_weights) {
@@ -327,7 +354,7 @@ __global__ void __launch_bounds__(move_threads(W)) move_kernel(EvictParams p) {
     return;
   }
 
-  const int cpr = p.head_dim / 16, total = n * cpr;
+  const int total = n * cpr;
   const uint8_t* codes = p.cache[which];
   uint4 held[HELD];
   float scale[HELD];
@@ -338,10 +365,10 @@ __global__ void __launch_bounds__(move_threads(W)) move_kernel(EvictParams p) {
     held[k] = make_uint4(0, 0, 0, 0);
     scale[k] = 0.f;
     if (c < total) {
-      const int r = c / cpr, t = src[first + r];
-      const size_t from = static_cast<size_t>(table[t >> p.shift]) * p.kv_heads + h;
-      scale[k] = p.scale[which][from];
-      held[k] = *reinterpret_cast<const uint4*>(codes + ((from << p.shift) + (t & mask)) * p.head_dim + (c - r * cpr) * 16);
+      const int r = c / cpr, t = from[k];
+      const size_t cell = static_cast<size_t>(table[t >> p.shift]) * p.kv_heads + h;
+      scale[k] = p.scale[which][cell];
+      held[k] = *reinterpret_cast<const uint4*>(codes + ((cell << p.shift) + (t & mask)) * p.head_dim + (c - r * cpr) * 16);
     }
   }
 #pragma unroll
@@ -365,7 +392,8 @@ __global__ void __launch_bounds__(move_threads(W)) move_kernel(EvictParams p) {
     if (lane == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(read + j) : "memory");
     for (int c0 = j - 1; c0 >= 0; c0 -= 32) {
       const int c = c0 - lane;
-      const bool reads = c >= 0 && src[(c << p.shift) + mask] >= first;     // its last token comes from this block or from behind it
+      // its last token comes from this block or from behind it
+      const bool reads = c >= 0 && (c0 == j - 1 ? ahead : src[(c << p.shift) + mask]) >= first;
       unsigned polls = 0;
       uint32_t done = !reads;
       while (!done && polls < kEvictPolls) {
@@ -560,12 +588,13 @@ static vscan_status launch_moves(const EvictParams& p, cudaStream_t stream) {
     return VSCAN_OK;
   }
   // as many warps to a unit as keep its codes in registers
-  const int w = chunks <= 256 ? 1 : 8, groups = move_threads(w) / 32 / w;
+  const int w = chunks <= 256 ? 1 : chunks <= 512 ? 4 : 8, groups = move_threads(w) / 32 / w;
   const int64_t units = static_cast<int64_t>(p.batch) * p.kv_heads * 2 * p.columns;
   const dim3 grid(static_cast<unsigned>((units + groups - 1) / groups));
   prof_before("kv_evict_move", stream);
   VSCAN_CUDA_TRY(chunks <= 128 ? launch_dependent(move_kernel<KV, 1, 4>, grid, dim3(move_threads(1)), 0, stream, p)
                  : chunks <= 256 ? launch_dependent(move_kernel<KV, 1, 8>, grid, dim3(move_threads(1)), 0, stream, p)
+                 : chunks <= 512 ? launch_dependent(move_kernel<KV, 4, 4>, grid, dim3(move_threads(4)), 0, stream, p)
                  : chunks <= 1024 ? launch_dependent(move_kernel<KV, 8, 4>, grid, dim3(move_threads(8)), 0, stream, p)
                  : chunks <= 2048 ? launch_dependent(move_kernel<KV, 8, 8>, grid, dim3(move_threads(8)), 0, stream, p)
                                   : launch_dependent(move_kernel<KV, 8, 16>, grid, dim3(move_threads(8)), 0, stream, p));
