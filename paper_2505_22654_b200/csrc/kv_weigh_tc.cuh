@@ -244,7 +244,12 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
     __syncwarp();
   } else if (warp == kWtLoader || warp == kWtLogs) {
     // ============================================================ queries; logarithms
-    int n_row = 0;
+    int n_row = 0, token_of[4], head_of[4];        // of rows lane, lane + 32, ... of a tile
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      token_of[i] = (i * 32 + lane) / p.group;
+      head_of[i] = i * 32 + lane - token_of[i] * p.group;
+    }
     while (ok && next_piece(p, st, pc)) {
       const int stop = min(st.s.len, pc.u1 * kUnit);
       for (int t0 = pc.u0 * kUnit; t0 < stop && ok; t0 += kWtTokens) {
@@ -263,14 +268,17 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
             }
           } else {
             bool silent = false;
-            for (int i = lane; i < 128; i += 32) {
-              const int k = i / p.group, h = i - k * p.group;
-              float x = -INFINITY;
-              if (k < per_tile && j * per_tile + k < c.rows) {
-                x = *lse_at(p, st.b, st.s.first, RowAt{token + k, st.head * p.group + h}) * -1.44269504088896341f;
-                if (x == INFINITY) { x = -INFINITY; silent = true; }
-              }
-              sh.log[stage][i] = x;
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              x[i] = INFINITY;
+              if (token_of[i] < per_tile && j * per_tile + token_of[i] < c.rows)
+                x[i] = __ldg(lse_at(p, st.b, st.s.first, RowAt{token + token_of[i], st.head * p.group + head_of[i]}));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (x[i] == -INFINITY) { x[i] = INFINITY; silent = true; }
+              sh.log[stage][i * 32 + lane] = x[i] * -1.44269504088896341f;
             }
             silent = __any_sync(0xffffffffu, silent);
             if (lane == 0) { sh.silent[stage] = silent; mbar_arrive(&sh.log_full[stage]); }
