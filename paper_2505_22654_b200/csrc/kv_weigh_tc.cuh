@@ -155,19 +155,20 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
         }
         // ---- rows that see the token: from this one of the window on
         const long long from = p.causal ? max(t - st.s.start - c.row0, 0ll) : 0;
+        // tiles of rows from this one on see all of the warp's tokens, up to the last one, which may have fewer rows
+        const int clear = __reduce_max_sync(0xffffffffu, static_cast<int>(min((from + per_tile - 1) / per_tile, static_cast<long long>(c.tiles))));
+        const int full = c.rows / per_tile;
         uint64_t sums[2] = {0, 0};
         const uint64_t mul = pair(factor, factor);
+#pragma unroll 1
         for (int j = c.first; j < c.tiles && ok; ++j, ++n_it, ++n_row) {
           const int stage = n_row % kWtStages, buf = n_it & 1;
           ok = mbar_wait_warp(&sh.log_full[stage], (n_row / kWtStages) & 1, abort_flag) &&
                mbar_wait_warp(&sh.s_full[tile][buf], (n_it >> 1) & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
-          // columns of the tile that count
-          const int c0 = static_cast<int>(min(max(from - static_cast<long long>(j) * per_tile, 0ll), 128ll)) * p.group;
-          const int c1 = min(c.rows - j * per_tile, per_tile) * p.group;
           const float* log = sh.log[stage];
-          const bool masked = __any_sync(0xffffffffu, c0 > 0) || c1 < per_tile * p.group || sh.silent[stage];
+          const bool masked = j < clear || j >= full || sh.silent[stage];
           const uint32_t s_addr = tmem + lanes + tile * 256 + buf * 128;
 #pragma unroll 1
           for (int q = 2 * half; q < 2 * half + 2; ++q) {
@@ -181,7 +182,9 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
               const float2 b = unpair(fma2(pair(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])), mul, pair(z.z, z.w)));
               e[k] = ex2(a.x); e[k + 1] = ex2(a.y); e[k + 2] = ex2(b.x); e[k + 3] = ex2(b.y);
             }
-            if (masked) {
+            if (masked) {                            // columns of the tile that count
+              const int c0 = static_cast<int>(min(max(from - static_cast<long long>(j) * per_tile, 0ll), 128ll)) * p.group;
+              const int c1 = min(c.rows - j * per_tile, per_tile) * p.group;
 #pragma unroll
               for (int k = 0; k < 32; ++k)
                 if (q * 32 + k < c0 || q * 32 + k >= c1 || log[q * 32 + k] == -INFINITY) e[k] = 0.f;
