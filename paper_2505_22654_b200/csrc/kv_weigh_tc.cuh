@@ -7,7 +7,9 @@
 //   warp 16          issues the products: two buffers of scores a tile, so that they run beside the exponentials
 //   warp 17          the rows' queries by TMA, a ring of four tiles
 //   warp 18          the rows' logarithms, beside them
-// Bound by the exponentials: 32,768 a tile of rows, 16 a cycle, twice what the products take.
+// Bound by the exponentials: 32,768 a tile of rows, 16 a cycle, twice what the products take.  Two prompts' windows of 512 rows of 900 to 1,024
+// behind 15,000 to 16,000 tokens, 28 / 4 heads of 128 (118 GFLOP, 102 us of exponentials): 214 us (351 with a thread a token and masks
+// everywhere; 1,857 as m16n8k16 products in passes of 16 rows).
 // Every wait is bounded; on expiry the CTA's tokens keep the weights that they had (there is no workspace to say so in).
 #pragma once
 
@@ -284,6 +286,7 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
               sh.log[stage][i * 32 + lane] = x[i] * -1.44269504088896341f;
             }
             silent = __any_sync(0xffffffffu, silent);
+            __syncwarp();
             if (lane == 0) { sh.silent[stage] = silent; mbar_arrive(&sh.log_full[stage]); }
           }
           __syncwarp();
