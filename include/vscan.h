@@ -544,7 +544,7 @@ vscan_status vscan_kv_attention(const vscan_kv_attention_desc* desc, void* works
  *   max_q_len no sequence has more query rows than this (rows behind it are left as they were)
  * Rows and keys that lie outside the buffers are not there.  Rows that no sequence owns are left as they were.  Elements of out, and
  * of lse, must not overlap each other.
- * Scores, softmax statistics and sums are float32.  For bf16 with head_dim up to 128 the weights are rounded to bf16 before they meet V.
+ * Scores, softmax statistics and sums are float32.  For bf16 the weights may be rounded to bf16 before they meet V.
  * Workspace: vscan_attention_workspace_bytes(desc), which reads the sizes only.  Calls that may run at the same time (on two streams,
  * or in two graphs) need a workspace each.
  * head_dim: a multiple of 8, at most 256; strides multiples of 16 bytes.  Limits of this build: q_heads / kv_heads <= 64; batch <= 8192;

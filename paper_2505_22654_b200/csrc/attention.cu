@@ -11,7 +11,7 @@ namespace vscan {
 namespace kv {
 
 // ---------------------------------------------------------------------------------------------- products on the CUDA cores
-// float32 queries (no rounding of queries or weights to 16 bits), and bf16 heads of more than 128 channels.  A CTA takes 64 query rows and
+// float32 queries (no rounding of queries or weights to 16 bits), and bf16 where the other kernel does not go.  A CTA takes 64 query rows and
 // 64 keys a step; a thread 4 x 4 scores, then 4 rows x DP / 16 channels of the sums.  Keys and weights take turns in one buffer.
 // Bound by what lies between the products of a step (loads, exponentials, barriers), with two CTAs an SM to fill it: 3 x 250 to 1,030 rows,
 // 16 heads of 80, float32, 4.1 GFLOP: 192 us, 21 TFLOP/s of 74 (246 with the sums in tiles of 128 channels).
@@ -243,12 +243,12 @@ static vscan_status validate_prompt(const vscan_attention_desc* d) {
 struct PromptPlan { int tile_rows, keys, whole; unsigned ctas; };
 
 // (a negative factor would turn the masks around: no model has one)
-static bool prompt_tensor(const vscan_attention_desc* d) { return d->dtype == VSCAN_BF16 && d->head_dim <= 128 && d->kv_rows > 0 && d->scale >= 0.f; }
+static bool prompt_tensor(const vscan_attention_desc* d) { return d->dtype == VSCAN_BF16 && d->kv_rows > 0 && d->scale >= 0.f; }
 
 static PromptPlan plan_prompt(const vscan_attention_desc* d, bool tensor) {
   PromptPlan pl;
   const int group = d->q_heads / d->kv_heads;
-  pl.tile_rows = tensor ? 2 * (128 / group) * group : kFlatRows;      // whole tokens of the group's heads
+  pl.tile_rows = tensor ? pt_tiles(d->head_dim) * (128 / group) * group : kFlatRows;      // whole tokens of the group's heads
   pl.keys = tensor ? kPtKeys : kFlatKeys;
   pl.whole = tensor ? kPtWhole : kFlatWhole;
   const int64_t resident = tensor || d->head_dim > 128 ? 1 : 2;
@@ -282,13 +282,18 @@ static bool prompt_maps(const vscan_attention_desc* d, PromptMaps& m) {
 
 template <int DP>
 static vscan_status launch_prompt_tc(const PromptParams& p, const PromptPlan& pl, const PromptMaps& m, cudaStream_t stream) {
-  constexpr size_t smem = 1024 + (2 + kPtStages) * static_cast<size_t>(DP / 64) * kChunk;
+  constexpr size_t smem = 1024 + (pt_tiles(DP) + pt_stages(DP)) * static_cast<size_t>(DP / 64) * kChunk;
   VSCAN_CUDA_TRY(allow_smem(prompt_tc_kernel<DP>, smem));
   prof_before("attention_tc", stream);
   VSCAN_CUDA_TRY(launch_dependent(prompt_tc_kernel<DP>, dim3(pl.ctas), dim3(kPtThreads), smem, stream, p, m.q, m.k, m.v));
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
   return VSCAN_OK;
+}
+
+static vscan_status launch_prompt_tcs(const PromptParams& p, const PromptPlan& pl, const PromptMaps& m, cudaStream_t stream) {
+  return p.head_dim <= 64 ? launch_prompt_tc<64>(p, pl, m, stream) : p.head_dim <= 128 ? launch_prompt_tc<128>(p, pl, m, stream)
+         : p.head_dim <= 192 ? launch_prompt_tc<192>(p, pl, m, stream) : launch_prompt_tc<256>(p, pl, m, stream);
 }
 
 template <typename T, int DP>
@@ -312,7 +317,8 @@ static vscan_status launch_prompt_join(const PromptParams& p, const PromptPlan& 
   // nothing can have been cut when no sequence has more keys than a tile that stays whole, or when one CTA did it all
   if (p.kv_rows <= pl.whole * pl.keys || pl.ctas == 1) return VSCAN_OK;
   prof_before("attention_join", stream);
-  const dim3 grid(pl.ctas, (pl.tile_rows + kJoinRows - 1) / kJoinRows);
+  const int rows = join_rows(p.head_dim);
+  const dim3 grid(pl.ctas, (pl.tile_rows + rows - 1) / rows);
   VSCAN_CUDA_TRY(launch_dependent(join_kernel<T>, grid, dim3(kJoinThreads), 0, stream, static_cast<const AttnParams&>(p), static_cast<int>(pl.ctas)));
   prof_after(stream);
   VSCAN_AFTER_LAUNCH();
@@ -329,7 +335,7 @@ extern "C" size_t vscan_attention_workspace_bytes(const vscan_attention_desc* d)
       d->q_heads / d->kv_heads > 64 || d->kv_rows < 0)
     return kStatusBytes;
   const size_t flat = kv::prompt_bytes(kv::plan_prompt(d, false), d->head_dim);      // strides decide between the two
-  const size_t tensor = d->dtype == VSCAN_BF16 && d->head_dim <= 128 ? kv::prompt_bytes(kv::plan_prompt(d, true), d->head_dim) : 0;
+  const size_t tensor = d->dtype == VSCAN_BF16 ? kv::prompt_bytes(kv::plan_prompt(d, true), d->head_dim) : 0;
   return flat > tensor ? flat : tensor;
 }
 
@@ -368,7 +374,7 @@ extern "C" vscan_status vscan_attention(const vscan_attention_desc* d, void* wor
   ws += kv::prompt_flag_bytes(pl);
   p.boundary = reinterpret_cast<kv::Boundary*>(ws);
   p.partial = reinterpret_cast<float*>(ws + kv::prompt_boundary_bytes(pl));
-  const vscan_status done = tensor ? (d->head_dim <= 64 ? kv::launch_prompt_tc<64>(p, pl, maps, stream) : kv::launch_prompt_tc<128>(p, pl, maps, stream))
+  const vscan_status done = tensor ? kv::launch_prompt_tcs(p, pl, maps, stream)
                             : d->dtype == VSCAN_F32 ? kv::launch_flats<float>(p, pl, stream) : kv::launch_flats<__nv_bfloat16>(p, pl, stream);
   if (done != VSCAN_OK) return done;
   return d->dtype == VSCAN_F32 ? kv::launch_prompt_join<float>(p, pl, stream) : kv::launch_prompt_join<__nv_bfloat16>(p, pl, stream);

@@ -6,7 +6,7 @@
 //   few rows, workers are CTAs    a few segments in many pieces: a CTA looks at kJoinLook boundaries, its warps share the rows and
 //                                 pieces of a segment that is cut there
 //   few rows, workers are warps   many segments in two pieces or three: a warp takes a boundary
-//   256 rows a tile               a CTA takes kJoinRows rows: their factors first, then all their channels side by side
+//   tiles of 64 to 256 rows       a CTA takes join_rows of them: their factors first, then all their channels side by side
 #pragma once
 
 #include "kv_attention.cuh"
@@ -17,6 +17,8 @@ namespace kv {
 constexpr int kJoinThreads = 512;
 constexpr int kJoinWarps = kJoinThreads / 32;
 constexpr int kJoinRows = 128;    // of a tile of 256: two CTAs a cut, all resident at once (32 rows: 28 us for 147 cuts)
+// of more than 128 channels half as many rows: a CTA holds as much
+__host__ __device__ constexpr int join_rows(int head_dim) { return head_dim > 128 ? kJoinRows / 2 : kJoinRows; }
 constexpr int kJoinLook = 4;      // so that all CTAs of the launch are resident at once
 
 struct Pieces {          // of one segment
@@ -118,7 +120,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int
     float (*factor)[kJoinRows] = dens + kTurns;
     static_assert((2 * kTurns + kBatch) * kJoinRows <= kJoinWarps * 256, "fits the sums");
     if (!cut_at(p, blockIdx.x, bd, pc)) return;
-    const int R = p.tile_rows, r0 = blockIdx.y * kJoinRows, n_rows = min(kJoinRows, bd.rows - r0);
+    const int R = p.tile_rows, r0 = blockIdx.y * join_rows(D), n_rows = min(join_rows(D), bd.rows - r0);
     if (n_rows <= 0) return;
     const int in_slab = warp % kSlabs * 32 + lane, mine = r0 + in_slab, turn = warp / kSlabs;
     const bool on = in_slab < n_rows;
@@ -131,8 +133,8 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(AttnParams p, int
     for (int w = 0; w < kTurns; ++w) top = fmaxf(top, tops[w][in_slab]);
     const float base = top == -INFINITY ? 0.f : top;
     den = 0.f;
-    constexpr int kEach = 8;                                      // 128 rows x 128 channels at most, four at a time
-    static_assert(kEach * kJoinThreads * 4 >= kJoinRows * 128, "tiles of 256 rows have up to 128 channels");
+    constexpr int kEach = 8;                                      // 128 rows x 128 channels or 64 x 256, four at a time
+    static_assert(kEach * kJoinThreads * 4 >= join_rows(128) * 128 && kEach * kJoinThreads * 4 >= join_rows(256) * 256, "a CTA's rows fit");
     const int per_row = D / 4, total = n_rows * per_row;
     float4 o[kEach];
 #pragma unroll

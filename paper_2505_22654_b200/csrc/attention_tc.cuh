@@ -1,4 +1,4 @@
-// Attention over whole prompts for bf16 on the 5th-generation tensor cores, head_dim up to 128.
+// Attention over whole prompts for bf16 on the 5th-generation tensor cores.
 //
 // A CTA takes up to 256 query rows (new rows x heads of a group) of one KV head as two tiles of up to 128 and runs over its stretch of the keys,
 // 128 at a time:
@@ -11,6 +11,9 @@
 //   warp 21          queries, K and V by TMA; K and V in a ring of four tiles of 128 rows
 //   warp 22          plans: what the next pieces of the stretch are, a few ahead of all others
 // A tile of 128 rows has whole tokens of the group's heads (126 rows for groups of seven), so that TMA can bring them.
+// Heads of more than 128 channels: one tile a CTA, whose sums take the tensor memory of both (warps 8-15 have nothing to do), and fewer, larger
+// tiles of K and V in the ring.  4 prompts of 1,700 to 2,176 rows, 28 / 4 heads of 256, 0.20 TFLOP: 312 us; 2 x
+// 9,000 to 12,200 rows: 0.91 PFLOP/s.
 // The two tiles take turns: while one's weights are made, the other's products run.  A step takes the tensor cores 2,048 cycles at 128 channels
 // (32 products of 64) and the exponentials, 32,768 at 16 a cycle, as many; it takes some 3,900: a tile's next scores wait for the products of
 // its weights, since tensor memory is full (two tiles of scores and two of sums, 128 columns each) and the weights lie over their scores.
@@ -39,6 +42,9 @@ namespace kv {
 constexpr int kPtThreads = 768, kPtKeys = 128, kPtWhole = 8, kPtExtra = 4;
 constexpr int kPtHelper = 16, kPtIssuer = 20, kPtLoader = 21, kPtPlanner = 22;   // first warp of each role
 constexpr int kPtStages = 4, kPtPlan = 4;
+// Tiles of a CTA, and of K and V in the ring: what 512 columns of tensor memory and 192 KB hold
+__host__ __device__ constexpr int pt_tiles(int dp) { return dp > 128 ? 1 : 2; }
+__host__ __device__ constexpr int pt_stages(int dp) { return dp > 192 ? 2 : dp > 128 ? 3 : kPtStages; }
 constexpr int kPtReaders = 22;       // warps that read the plan
 // 768 threads start with 80 registers each: 512 x 88 + 256 x 64 = 768 x 80.
 using PtShape = TileShape<kPtThreads, 0, kPtKeys, kPtWhole, kPtExtra>;
@@ -57,7 +63,7 @@ struct PtShared {
   uint32_t tmem_base;
   int abort_flag;
   float2 stat[2][128];                        // [tile][row]: reference and sum
-  uint32_t odd[2][128][8];                    // [tile][row]: channels that get +inf (4 words) and -inf
+  uint32_t odd[2 * 128 * 8];                  // [tile][row]: channels that get +inf (a bit each) and -inf
   uint32_t found[2][4];                       // of a step that is seen in part: keys whose values are not all finite, a word of each warp
   uint64_t plan_full[kPtPlan], plan_empty[kPtPlan];
   PtPiece plan[kPtPlan];
@@ -201,12 +207,12 @@ template <int DP>
 __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p, const __grid_constant__ CUtensorMap q_map,
                                                                   const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using namespace tc;
-  constexpr int kDChunks = DP / 64, kTileBytes = kDChunks * kChunk;
+  constexpr int kDChunks = DP / 64, kTileBytes = kDChunks * kChunk, kTiles = pt_tiles(DP), kStages = pt_stages(DP), kOddWords = kTiles == 1 ? 8 : 4;
   extern __shared__ unsigned char smem_dyn[];
   __shared__ PtShared sh;
   unsigned char* base = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
-  unsigned char* q_sh = base;                      // [2 tiles]
-  unsigned char* kv_sh = q_sh + 2 * kTileBytes;    // [stages]
+  unsigned char* q_sh = base;                      // [tiles]
+  unsigned char* kv_sh = q_sh + kTiles * kTileBytes;    // [stages]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int D = p.head_dim;
   volatile int* abort_flag = &sh.abort_flag;
@@ -218,7 +224,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       mbar_init(&sh.o_done[i], 1); mbar_init(&sh.o_free[i], 4); mbar_init(&sh.stat_full[i], 8);
       mbar_init(&sh.dirty[i], 1); mbar_init(&sh.clean[i], 4);
     }
-    for (int i = 0; i < kPtStages; ++i) { mbar_init(&sh.kv_full[i], 1); mbar_init(&sh.kv_empty[i], 1); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&sh.kv_full[i], 1); mbar_init(&sh.kv_empty[i], 1); }
     for (int i = 0; i < kPtPlan; ++i) { mbar_init(&sh.plan_full[i], 1); mbar_init(&sh.plan_empty[i], kPtReaders); }
     sh.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -251,7 +257,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
     ++n_plan;
     return pc.u1 > 0;
   };
-  const int tokens = p.tile_rows / (2 * p.group), half = tokens * p.group;      // tokens and rows of a tile of 128
+  const int tokens = p.tile_rows / (kTiles * p.group), half = tokens * p.group;      // tokens and rows of a tile of 128
 
   if (warp < kPtHelper) {
     // ============================================================ four threads a query row
@@ -380,9 +386,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
 #pragma unroll
       for (int t = 0; t < 2; ++t) seen[t] = r < half && t * half + r < pc.n_rows ? keys_seen(p, pc, pc.token + t * tokens + r_token) : 0;
       for (int u = pc.partial; u < pc.u1 && ok; ++u, ++n_partial) {
-        const int at = pos + 1 + 2 * (u - pc.u0), s = at % kPtStages;
+        const int at = pos + 1 + 2 * (u - pc.u0), s = at % kStages;
         ok = wait_piece(p, &sh.dirty[n_partial & 1], (n_partial >> 1) & 1, abort_flag) &&
-             wait_warp(&sh.kv_full[s], (at / kPtStages) & 1, abort_flag);
+             wait_warp(&sh.kv_full[s], (at / kStages) & 1, abort_flag);
         if (!ok) break;
         // a row of 64 channels is 128 bytes; 16-byte pieces of a row may be in any order
         unsigned char* tile = kv_sh + s * kTileBytes;
@@ -419,8 +425,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
         ok = wait_warp(&sh.clean[n_partial & 1], (n_partial >> 1) & 1, abort_flag);    // the words of all four
         if (ok && (words[0] | words[1] | words[2] | words[3])) {   // rare: what those values give to the rows that see them, from memory
           if (!odd)
-            for (int t = 0; t < 2; ++t)
-              for (int i = 0; i < 8; ++i) sh.odd[t][r][i] = 0;
+            for (int t = 0; t < kTiles; ++t)
+              for (int i = 0; i < 2 * kOddWords; ++i) sh.odd[(t * 128 + r) * 2 * kOddWords + i] = 0;
           odd = true;
           const char* v = p.v + (p.padded ? pc.b * p.v_seq : pc.key0 * p.v_row) + pc.head * p.v_head;
           const int t1 = min(max(seen[0], seen[1]), (u + 1) * kPtKeys);
@@ -429,10 +435,11 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
             for (int c = 0; c < D; ++c) {
               const float x = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(v + t * p.v_row)[c]);
               if (x - x == 0.f) continue;
-              for (int i = 0; i < 2; ++i) {
+              for (int i = 0; i < kTiles; ++i) {
                 if (t >= seen[i]) continue;
-                if (!(x < 0.f)) sh.odd[i][r][c >> 5] |= 1u << (c & 31);
-                if (!(x > 0.f)) sh.odd[i][r][4 + (c >> 5)] |= 1u << (c & 31);
+                uint32_t* odds = sh.odd + (i * 128 + r) * 2 * kOddWords + (c >> 5);
+                if (!(x < 0.f)) odds[0] |= 1u << (c & 31);
+                if (!(x > 0.f)) odds[kOddWords] |= 1u << (c & 31);
               }
             }
           }
@@ -461,7 +468,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
 #pragma unroll
           for (int k = 0; k < 16; ++k) x[k] = __uint_as_float(v[k]);
           if (odd) {
-            const uint32_t up = sh.odd[t][r][c >> 5] >> (c & 31), down = sh.odd[t][r][4 + (c >> 5)] >> (c & 31);
+            const uint32_t* odds = sh.odd + (t * 128 + r) * 2 * kOddWords + (c >> 5);
+            const uint32_t up = odds[0] >> (c & 31), down = odds[kOddWords] >> (c & 31);
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
               if ((up >> k) & 1u) x[k] += INFINITY;
@@ -504,7 +512,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
 #pragma unroll
       for (int c = 0; c < kDChunks; ++c) umma_f16_ss_x4(tmem + t * 128, a + c * (kChunk >> 4), b + c * (kChunk >> 4), qk, c > 0);
     };
-    auto wait_kv = [&](int at) { return wait_warp(&sh.kv_full[at % kPtStages], (at / kPtStages) & 1, abort_flag); };
+    auto wait_kv = [&](int at) { return wait_warp(&sh.kv_full[at % kStages], (at / kStages) & 1, abort_flag); };
     while (ok && next()) {
       const int two = pc.n_rows > half;
       for (int t = 0; t <= two && ok; ++t) ok = wait_warp(&sh.q_full[t], n_piece[t] & 1, abort_flag);
@@ -512,14 +520,14 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
       if (!ok) break;
       tc_fence_after();
       for (int t = 0; t <= two; ++t) {
-        scores(t, pos % kPtStages);
+        scores(t, pos % kStages);
         umma_commit_warp(&sh.s_full[t]);
         if (pc.u0 + 1 == pc.u1) umma_commit_warp(&sh.q_empty[t]);
       }
-      umma_commit_warp(&sh.kv_empty[pos % kPtStages]);
+      umma_commit_warp(&sh.kv_empty[pos % kStages]);
       ++pos;
       for (int u = pc.u0; u < pc.u1 && ok; ++u) {
-        const int vs = pos % kPtStages, ks = (pos + 1) % kPtStages;
+        const int vs = pos % kStages, ks = (pos + 1) % kStages;
         const bool more = u + 1 < pc.u1;
         ok = wait_kv(pos);
         if (u >= pc.partial) {
@@ -538,6 +546,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
           if (!ok) break;
           tc_fence_after();
           umma_f16_ts_x4(tmem + 256 + t * 128, tmem + t * 128 + 32, b + (64 * 128 >> 4), pv, true);
+          if constexpr (kTiles == 1) umma_commit_warp(&sh.kv_empty[vs]);      // the next values do not wait for the scores
           if (more) {            // over the weights that the products before this one read: products run in the order of their issue
             if (t == 0) ok = wait_kv(pos + 1);
             if (!ok) break;
@@ -551,7 +560,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
           ++n_it[t];
         }
         if (!ok) break;
-        umma_commit_warp(&sh.kv_empty[vs]);
+        if constexpr (kTiles > 1) umma_commit_warp(&sh.kv_empty[vs]);
         if (more) umma_commit_warp(&sh.kv_empty[ks]);
         pos += more ? 2 : 1;
       }
@@ -566,8 +575,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(PromptParams p
     while (ok && next()) {
       const int seq = p.padded ? pc.b : 0, two = pc.n_rows > half;
       for (int i = 2 * pc.u0; i < 2 * pc.u1 && ok; ++i, ++pos) {
-        const int s = pos % kPtStages, u = i >> 1;
-        if (pos >= kPtStages) ok = wait_warp(&sh.kv_empty[s], (pos / kPtStages - 1) & 1, abort_flag);
+        const int s = pos % kStages, u = i >> 1;
+        if (pos >= kStages) ok = wait_warp(&sh.kv_empty[s], (pos / kStages - 1) & 1, abort_flag);
         if (!ok) break;
         if (lane == 0) {
           mbar_arrive_expect_tx(&sh.kv_full[s], kTileBytes);

@@ -166,6 +166,28 @@ def test_attention_what_is_not_finite_reaches_those_who_see_it(dtype, d):
     run_attention(dtype, 4, 2, d, [0, 10], [300, 290], True, padded=True, touch=touch)
 
 
+@pytest.mark.parametrize("hq,hk,d,past,new", [
+    (1, 1, 192, [0], [1]), (2, 2, 256, [0, 0, 700], [129, 128, 1]), (7, 1, 256, [0, 40], [300, 18]), (4, 2, 136, [0, 5, 0], [127, 130, 0]),
+    (64, 1, 200, [3], [9]), (1, 1, 256, [9000], [200]), (14, 2, 192, [2500, 0], [90, 1400]), (3, 3, 248, [-1, -40, 9], [1, 200, 1]),
+    (40, 1, 184, [600], [17]), (2, 1, 256, [0, -200], [577, 300])])
+def test_attention_wide_heads(hq, hk, d, past, new):
+    for causal in (True, False):
+        run_attention("bf16", hq, hk, d, past, new, causal, padded=len(new) % 2 == 0, seed=hq + d)
+
+
+@pytest.mark.parametrize("d", [136, 192, 256])
+def test_attention_wide_heads_what_is_not_finite_reaches_those_who_see_it(d):
+    inf, nan = float("inf"), float("nan")
+
+    def touch(b, q, k, v):
+        v[40, 0, 3], v[40, 1, d - 6], v[70, 0, 3] = inf, -inf, -inf
+        v[len(v) - 1, 1, d - 1] = nan
+        v[130, :, 130] = -inf
+        k[-2] = nan
+    run_attention("bf16", 4, 2, d, [0, 10], [300, 290], True, padded=False, touch=touch)
+    run_attention("bf16", 2, 2, d, [0, 10], [300, 290], True, padded=True, touch=touch)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_large_scores_and_one_hot_rows(dtype):
     """Scores of hundreds, whose running maximum is raised many times over: each row's weights are nearly one key's alone."""
