@@ -301,7 +301,7 @@ static vscan_status launch_weigh_mma(const WeighParams& p, int rows, cudaStream_
 
 template <int KV, int DP>
 static vscan_status launch_weigh_tc(const WeighParams& p, const CUtensorMap& q, cudaStream_t stream) {
-  constexpr size_t smem = 1024 + (2 + kWtStages) * static_cast<size_t>(DP / 64) * kChunk;
+  constexpr size_t smem = 1024 + (wt_tiles(DP) + wt_stages(DP)) * static_cast<size_t>(DP / 64) * kChunk;
   VSCAN_CUDA_TRY(allow_smem(weigh_tc_kernel<KV, DP>, smem));
   prof_before("kv_weigh_tc", stream);
   VSCAN_CUDA_TRY(launch_dependent(weigh_tc_kernel<KV, DP>, dim3(weigh_ctas(p, 1)), dim3(kWtThreads), smem, stream, p, q));
@@ -314,7 +314,9 @@ template <int KV>
 static vscan_status launch_weigh(const WeighParams& p, int dtype, const CUtensorMap* q, cudaStream_t stream) {
   const int64_t used = p.max_q_len < p.window ? p.max_q_len : p.window;
   const int rows = static_cast<int>(used * p.group < (1 << 20) ? used * p.group : 1 << 20), d = p.head_dim;
-  if (q) return d <= 64 ? launch_weigh_tc<KV, 64>(p, *q, stream) : launch_weigh_tc<KV, 128>(p, *q, stream);
+  if (q)
+    return d <= 64 ? launch_weigh_tc<KV, 64>(p, *q, stream) : d <= 128 ? launch_weigh_tc<KV, 128>(p, *q, stream)
+           : d <= 192 ? launch_weigh_tc<KV, 192>(p, *q, stream) : launch_weigh_tc<KV, 256>(p, *q, stream);
   if (dtype == VSCAN_BF16) {
     if (d == 64) return launch_weigh_mma<KV, 64, true>(p, rows, stream);
     if (d == 128) return launch_weigh_mma<KV, 128, true>(p, rows, stream);
@@ -361,7 +363,7 @@ extern "C" vscan_status vscan_kv_weigh(const vscan_kv_weigh_desc* d, void* strea
   CUtensorMap map;
   const int64_t used = d->max_q_len < d->window ? d->max_q_len : d->window;
   const int64_t sizes[2] = {d->q_heads, d->rows}, steps[2] = {d->q_stride[1], d->q_stride[2]};
-  const bool tensor = d->dtype == VSCAN_BF16 && d->head_dim <= 128 && used * p.group > 16 &&
+  const bool tensor = d->dtype == VSCAN_BF16 && used * p.group > 16 &&
                       kv::rows_map(d->q, d->head_dim, sizes, steps, d->padded ? d->batch : 1, d->q_stride[0], p.group, 128 / p.group, &map);
   return d->kv_dtype == VSCAN_KV_E4M3 ? kv::launch_weigh<VSCAN_KV_E4M3>(p, d->dtype, tensor ? &map : nullptr, stream)
                                       : kv::launch_weigh<VSCAN_KV_I8>(p, d->dtype, tensor ? &map : nullptr, stream);

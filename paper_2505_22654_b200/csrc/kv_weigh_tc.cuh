@@ -10,6 +10,7 @@
 // Bound by the exponentials: 32,768 a tile of rows, 16 a cycle, twice what the products take.  Two prompts' windows of 512 rows of 900 to 1,024
 // behind 15,000 to 16,000 tokens, 28 / 4 heads of 128 (118 GFLOP, 102 us of exponentials): 214 us (351 with a thread a token and masks
 // everywhere; 1,857 as m16n8k16 products in passes of 16 rows).
+// Heads of more than 128 channels: one tile of tokens, and fewer tiles of queries in the ring.  The same windows at 256 channels: 334 us.
 // Every wait is bounded; on expiry the CTA's tokens keep the weights that they had (there is no workspace to say so in).
 #pragma once
 
@@ -20,7 +21,10 @@ namespace vscan {
 namespace kv {
 
 constexpr int kWtThreads = 640, kWtIssuer = 16, kWtLoader = 17, kWtLogs = 18;
-constexpr int kWtTokens = 256, kWtStages = 4;
+constexpr int kWtStages = 4;
+// Tiles of tokens of a CTA, and of queries in the ring: what 192 KB hold
+__host__ __device__ constexpr int wt_tiles(int dp) { return dp > 128 ? 1 : 2; }
+__host__ __device__ constexpr int wt_stages(int dp) { return dp > 192 ? 2 : dp > 128 ? 3 : kWtStages; }
 
 struct WtShared {
   uint64_t k_full[2], s_full[2][2], s_empty[2][2], other[2][4];   // other: of the two warps that share 32 tokens
@@ -33,13 +37,13 @@ struct WtShared {
   ScheduleShared sched;
 };
 
-// What a piece of a stretch is cut into: 256 tokens from t0 on, against the rows' tiles first .. tiles - 1
+// What a piece of a stretch is cut into: the CTA's 256 (or 128) tokens from t0 on, against the rows' tiles first .. tiles - 1
 struct WtChunk { int t0, n, first, tiles, row0, rows; };      // row0, rows: tokens of the window, the first as a row of the sequence
 
-__device__ __forceinline__ WtChunk wt_chunk(const WeighParams& p, const Sequence& s, int t0, int stop, int per_tile) {
+__device__ __forceinline__ WtChunk wt_chunk(const WeighParams& p, const Sequence& s, int t0, int stop, int per_tile, int tokens) {
   WtChunk c;
   c.t0 = t0;
-  c.n = min(stop - t0, kWtTokens);
+  c.n = min(stop - t0, tokens);
   c.rows = min(s.n, p.window);
   c.row0 = s.n - c.rows;
   c.tiles = (c.rows + per_tile - 1) / per_tile;
@@ -52,12 +56,12 @@ __device__ __forceinline__ WtChunk wt_chunk(const WeighParams& p, const Sequence
 template <int KV, int DP>
 __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, const __grid_constant__ CUtensorMap q_map) {
   using namespace tc;
-  constexpr int kDChunks = DP / 64, kTileBytes = kDChunks * kChunk;
+  constexpr int kDChunks = DP / 64, kTileBytes = kDChunks * kChunk, kTiles = wt_tiles(DP), kTokens = kTiles * 128, kStages = wt_stages(DP);
   extern __shared__ unsigned char smem_dyn[];
   __shared__ WtShared sh;
   unsigned char* base = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
-  unsigned char* k_sh = base;                      // [2 tiles]
-  unsigned char* q_sh = k_sh + 2 * kTileBytes;     // [stages]
+  unsigned char* k_sh = base;                      // [tiles]
+  unsigned char* q_sh = k_sh + kTiles * kTileBytes;     // [stages]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int D = p.head_dim;
   volatile int* abort_flag = &sh.abort_flag;
@@ -68,12 +72,12 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
       for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[i][k], 1); mbar_init(&sh.s_empty[i][k], 8); }
       for (int k = 0; k < 4; ++k) mbar_init(&sh.other[i][k], 1);
     }
-    for (int i = 0; i < kWtStages; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.log_full[i], 1); mbar_init(&sh.log_empty[i], 16); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.log_full[i], 1); mbar_init(&sh.log_empty[i], 16); }
     sh.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // rows of a stage behind the whole tokens of a tile are never loaded: their scores have to be finite
-  for (int i = threadIdx.x; i < kWtStages * kDChunks * 128 * 8; i += kWtThreads) {
+  for (int i = threadIdx.x; i < kStages * kDChunks * 128 * 8; i += kWtThreads) {
     const int row = (i >> 3) & 127;
     if (row >= 128 / p.group * p.group) *reinterpret_cast<uint4*>(q_sh + static_cast<size_t>(i >> 10) * kChunk + (i & 1023) * 16) = make_uint4(0, 0, 0, 0);
   }
@@ -99,12 +103,12 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
     int n_it = 0, n_row = 0, n_sum = 0;            // tiles of rows that this tile has had; of the CTA; sums told so far
     while (ok && next_piece(p, st, pc)) {
       const int stop = min(st.s.len, pc.u1 * kUnit);
-      for (int t0 = pc.u0 * kUnit; t0 < stop && ok; t0 += kWtTokens) {
-        const WtChunk c = wt_chunk(p, st.s, t0, stop, per_tile);
+      for (int t0 = pc.u0 * kUnit; t0 < stop && ok; t0 += kTokens) {
+        const WtChunk c = wt_chunk(p, st.s, t0, stop, per_tile, kTokens);
         if (tile * 128 >= c.n) {                   // nothing for this tile
           for (int j = c.first; j < c.tiles && ok; ++j, ++n_row) {
-            ok = mbar_wait_warp(&sh.log_full[n_row % kWtStages], (n_row / kWtStages) & 1, abort_flag);
-            if (ok && lane == 0) mbar_arrive(&sh.log_empty[n_row % kWtStages]);
+            ok = mbar_wait_warp(&sh.log_full[n_row % kStages], (n_row / kStages) & 1, abort_flag);
+            if (ok && lane == 0) mbar_arrive(&sh.log_empty[n_row % kStages]);
           }
           continue;
         }
@@ -164,8 +168,8 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
         const uint64_t mul = pair(factor, factor);
 #pragma unroll 1
         for (int j = c.first; j < c.tiles && ok; ++j, ++n_it, ++n_row) {
-          const int stage = n_row % kWtStages, buf = n_it & 1;
-          ok = mbar_wait_warp(&sh.log_full[stage], (n_row / kWtStages) & 1, abort_flag) &&
+          const int stage = n_row % kStages, buf = n_it & 1;
+          ok = mbar_wait_warp(&sh.log_full[stage], (n_row / kStages) & 1, abort_flag) &&
                mbar_wait_warp(&sh.s_full[tile][buf], (n_it >> 1) & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
@@ -220,15 +224,15 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
     int n_it[2] = {0, 0}, n_chunk[2] = {0, 0}, n_row = 0;
     while (ok && next_piece(p, st, pc)) {
       const int stop = min(st.s.len, pc.u1 * kUnit);
-      for (int t0 = pc.u0 * kUnit; t0 < stop && ok; t0 += kWtTokens) {
-        const WtChunk c = wt_chunk(p, st.s, t0, stop, per_tile);
-        const int two = c.n > 128;
+      for (int t0 = pc.u0 * kUnit; t0 < stop && ok; t0 += kTokens) {
+        const WtChunk c = wt_chunk(p, st.s, t0, stop, per_tile, kTokens);
+        const int two = c.n > 128;                 // never where a CTA has one tile
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           if (t <= two && c.first < c.tiles && ok) ok = mbar_wait_warp(&sh.k_full[t], n_chunk[t]++ & 1, abort_flag);
         for (int j = c.first; j < c.tiles && ok; ++j, ++n_row) {
-          const int stage = n_row % kWtStages;
-          ok = mbar_wait_warp(&sh.q_full[stage], (n_row / kWtStages) & 1, abort_flag);
+          const int stage = n_row % kStages;
+          ok = mbar_wait_warp(&sh.q_full[stage], (n_row / kStages) & 1, abort_flag);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             if (t > two || !ok) continue;
@@ -257,12 +261,12 @@ __global__ void __launch_bounds__(kWtThreads, 1) weigh_tc_kernel(WeighParams p, 
     }
     while (ok && next_piece(p, st, pc)) {
       const int stop = min(st.s.len, pc.u1 * kUnit);
-      for (int t0 = pc.u0 * kUnit; t0 < stop && ok; t0 += kWtTokens) {
-        const WtChunk c = wt_chunk(p, st.s, t0, stop, per_tile);
+      for (int t0 = pc.u0 * kUnit; t0 < stop && ok; t0 += kTokens) {
+        const WtChunk c = wt_chunk(p, st.s, t0, stop, per_tile, kTokens);
         for (int j = c.first; j < c.tiles && ok; ++j, ++n_row) {
-          const int stage = n_row % kWtStages, token = c.row0 + j * per_tile;
+          const int stage = n_row % kStages, token = c.row0 + j * per_tile;
           uint64_t* empty = warp == kWtLoader ? &sh.q_empty[stage] : &sh.log_empty[stage];
-          if (n_row >= kWtStages) ok = mbar_wait_warp(empty, (n_row / kWtStages - 1) & 1, abort_flag);
+          if (n_row >= kStages) ok = mbar_wait_warp(empty, (n_row / kStages - 1) & 1, abort_flag);
           if (!ok) break;
           if (warp == kWtLoader) {
             if (lane == 0) {

@@ -376,6 +376,14 @@ def test_weigh_over_many_short_and_one_long_sequence():
     _weigh_case("e4m3", "bf16", 8, 8, 64, 16, [20] * 30, [1] * 30, seed=6)
 
 
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+@pytest.mark.parametrize("hq,hk,d,bs,past,new,window,causal,padded", [
+    (2, 1, 256, 16, [300, 0], [40, 200], None, True, False), (7, 1, 192, 64, [100, 513], [64, 3], 20, True, True), (4, 4, 144, 32, [500], [129], None, False, False),
+    (40, 1, 224, 128, [90, 7], [5, 30], 17, True, False), (64, 2, 256, 16, [130], [9], None, True, True), (3, 3, 240, 256, [0, 1000, 20], [300, 0, 257], 250, True, False)])
+def test_weigh_windows_of_wide_heads(kv, hq, hk, d, bs, past, new, window, causal, padded):
+    _weigh_case(kv, "bf16", hq, hk, d, bs, past, new, causal=causal, padded=padded, window=window, decay=0.5, seed=hq + d, missing=[(0, 1)] if past[0] else ())
+
+
 def test_weigh_rows_that_see_nothing_give_nothing_and_nan_reaches_its_own():
     c, n = Cache("i8", 2, 16, 32, 4, 0), 3
     q = torch.randn((n, 2, 32), generator=gen(2)).to(torch.bfloat16).cuda()
