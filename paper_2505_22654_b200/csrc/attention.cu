@@ -12,24 +12,35 @@ namespace kv {
 
 // ---------------------------------------------------------------------------------------------- products on the CUDA cores
 // float32 queries (no rounding of queries or weights to 16 bits), and bf16 where the other kernel does not go.  A CTA takes 64 query rows and
-// 64 keys a step; a thread 4 x 4 scores, then 4 rows x DP / 16 channels of the sums.  Keys and weights take turns in one buffer.
-// Bound by what lies between the products of a step (loads, exponentials, barriers), with two CTAs an SM to fill it: 3 x 250 to 1,030 rows,
-// 16 heads of 80, float32, 4.1 GFLOP: 192 us, 21 TFLOP/s of 74 (246 with the sums in tiles of 128 channels).
+// 64 keys a step; a thread 4 x 4 scores, then 4 rows x DP / 16 channels of the sums.  The next step's keys are on
+// their way while the weights meet the values, and the values while the scores are made.  Weights pass between the 16 threads of a row only.
+// Four floats that lie together stay together; which four of a row lie where depends on the row, so that the rows that a warp reads at
+// once lie in different banks, and two CTAs of 128 channels fit an SM.
+// Bound by the instructions of the products and their operands from shared memory, which do not overlap in full with two CTAs an SM: 3 x 250 to
+// 1,030 rows, 16 heads of 80, 4.1 GFLOP: 185 us; 1,500 to 2,000 rows: 28 TFLOP/s of 74 (23 without copies in the background).  8 rows a thread,
+// or two sums to an instruction, gave the same.
 constexpr int kFlatThreads = 256, kFlatRows = 64, kFlatKeys = 64, kFlatWhole = 4;
 using FlatShape = TileShape<kFlatThreads, kFlatRows, kFlatKeys, kFlatWhole>;
 template <int DP>
-constexpr size_t flat_smem() { return (static_cast<size_t>(kFlatRows) * (DP + 4) + static_cast<size_t>(kFlatKeys) * (DP + 4) + static_cast<size_t>(kFlatKeys) * DP) * 4; }
+constexpr size_t flat_smem() { return (static_cast<size_t>(kFlatRows + 2 * kFlatKeys) * DP + kFlatRows * kFlatKeys) * 4; }
+
+__device__ __forceinline__ void copy_16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All copies have arrived but those of the last N groups
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(PromptParams p) {
   // a thread's channels: 4 of every 64, or 2 of every 32 (heads of 72 to 96)
-  constexpr int kVec = DP == 96 ? 2 : 4, kChunks = DP / (16 * kVec), kChannels = kVec * kChunks;
-  constexpr int kQ = DP + 4, kP = kFlatKeys + 4;
-  static_assert(kP <= kQ, "weights lie over the keys");
+  constexpr int kVec = DP == 96 ? 2 : 4, kChunks = DP / (16 * kVec), kEach = kFlatRows * 16 / kFlatThreads;   // kEach: rows of a thread
   extern __shared__ __align__(16) float flat_sh[];
-  float* q_sh = flat_sh;                        // [rows][DP + 4]
-  float* k_sh = q_sh + kFlatRows * kQ;          // [keys][DP + 4]; weights [rows][keys + 4]
-  float* v_sh = k_sh + kFlatKeys * kQ;          // [keys][DP]
+  float* q_sh = flat_sh;                        // [rows][DP]
+  float* k_sh = q_sh + kFlatRows * DP;          // [keys][DP]
+  float* v_sh = k_sh + kFlatKeys * DP;          // [keys][DP]
+  float* w_sh = v_sh + kFlatKeys * DP;          // [rows][keys]
   __shared__ DivisionShared division;
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4, D = p.head_dim;
   grid_dependency_wait();
@@ -40,18 +51,27 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
     p.flags[blockIdx.x] = 0;
   }
   TcPiece pc;
-  // Rows of a buffer as floats into shared memory, zeros beyond `there` rows and D channels
-  auto fill = [&](float* dst, int pitch, int there, auto at) {
+  // Rows of a buffer as floats into shared memory, zeros beyond `there` rows; turn(r): what the places of a row's fours are xored with
+  auto fill = [&](float* dst, int there, auto turn, auto at) {
     constexpr int kElems = Vec16<T>::kElems, kVecs = DP / kElems;
     for (int i = tid; i < 64 * kVecs; i += kFlatThreads) {
       const int r = i / kVecs, c = (i - r * kVecs) * kElems;
-      float f[kElems];
+      if (c >= D) continue;
+      float* row = dst + r * DP;
+      if constexpr (sizeof(T) == 4) {
+        float* to = row + (c ^ turn(r) * 4);
+        if (r < there) copy_16(to, at(r) + c * 4);
+        else *reinterpret_cast<float4*>(to) = make_float4(0.f, 0.f, 0.f, 0.f);
+      } else {
+        float f[kElems];
 #pragma unroll
-      for (int j = 0; j < kElems; ++j) f[j] = 0.f;
-      if (r < there && c < D) Vec16<T>::unpack(ld_nc_16(at(r) + c * static_cast<int>(sizeof(T))), f);
+        for (int j = 0; j < kElems; ++j) f[j] = 0.f;
+        if (r < there) Vec16<T>::unpack(ld_nc_16(at(r) + c * static_cast<int>(sizeof(T))), f);
 #pragma unroll
-      for (int j = 0; j < kElems; j += 4) *reinterpret_cast<float4*>(dst + r * pitch + c + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+        for (int j = 0; j < kElems; j += 4) *reinterpret_cast<float4*>(row + ((c + j) ^ turn(r) * 4)) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+      }
     }
+    copy_commit();
   };
   while (tc_next<FlatShape>(p, st, pc)) {
     const Sequence& s = pc.q.s;
@@ -64,54 +84,64 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
       const int flat = pc.tile * kFlatRows + r, i = flat / p.group;
       return RowAt{i, pc.head * p.group + flat - i * p.group};
     };
+    auto fill_keys = [&](int u) {
+      fill(k_sh, min(pc.most - u * kFlatKeys, kFlatKeys), [](int r) { return r & 7; }, [&](int r) { return k + (u * kFlatKeys + r) * p.k_row; });
+    };
     __syncthreads();                            // the buffers of the piece before are done with
-    fill(q_sh, kQ, pc.n_rows, [&](int r) { return q_at(p, pc.b, s.first, row_of(r)); });
-    int seen[4];
-    float m[4], l[4], o[4][kChannels];
+    fill(q_sh, pc.n_rows, [](int r) { return r / kEach & 7; }, [&](int r) { return q_at(p, pc.b, s.first, row_of(r)); });
+    fill_keys(pc.u0);
+    int seen[kEach];
+    float m[kEach], l[kEach];
+    float o[kEach][kChunks * kVec];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = y * 4 + i;
+    for (int i = 0; i < kEach; ++i) {
+      const int r = y * kEach + i;
       seen[i] = r < pc.n_rows ? visible(p, s, row_of(r).i) : 0;
       m[i] = -INFINITY; l[i] = 0.f;
 #pragma unroll
-      for (int c = 0; c < kChannels; ++c) o[i][c] = 0.f;
+      for (int c = 0; c < kChunks * kVec; ++c) o[i][c] = 0.f;
     }
     for (int u = pc.u0; u < pc.u1; ++u) {
       const int t0 = u * kFlatKeys, there = min(pc.most - t0, kFlatKeys);
-      __syncthreads();                          // weights and values of the step before are done with
-      fill(k_sh, kQ, there, [&](int r) { return k + (t0 + r) * p.k_row; });
-      fill(v_sh, DP, there, [&](int r) { return v + (t0 + r) * p.v_row; });
-      __syncthreads();
-      float dot[4][4];                          // rows 4 y + i, keys x + 16 j
+      copy_wait<0>();
+      __syncthreads();                          // queries and keys are there; values of the step before are done with
+      fill(v_sh, there, [](int) { return 0; }, [&](int r) { return v + (t0 + r) * p.v_row; });
+      float dot[kEach][4];                      // rows kEach y + i, keys x + 16 j
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < kEach; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) dot[i][j] = 0.f;
-#pragma unroll 4
+#pragma unroll 2
       for (int c = 0; c < D; c += 4) {
-        float4 a[4], b[4];
+        float4 b[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          a[i] = *reinterpret_cast<const float4*>(q_sh + (y * 4 + i) * kQ + c);
-          b[i] = *reinterpret_cast<const float4*>(k_sh + (x + 16 * i) * kQ + c);
+        for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4*>(k_sh + (x + 16 * j) * DP + (c ^ (x & 7) * 4));
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const float4 a = *reinterpret_cast<const float4*>(q_sh + (y * kEach + i) * DP + (c ^ (y & 7) * 4));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dot[i][j] = fmaf(a.x, b[j].x, dot[i][j]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dot[i][j] = fmaf(a.y, b[j].y, dot[i][j]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dot[i][j] = fmaf(a.z, b[j].z, dot[i][j]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dot[i][j] = fmaf(a.w, b[j].w, dot[i][j]);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            dot[i][j] = fmaf(a[i].x, b[j].x, fmaf(a[i].y, b[j].y, fmaf(a[i].z, b[j].z, fmaf(a[i].w, b[j].w, dot[i][j]))));
       }
-      __syncthreads();                          // keys are done with: weights take their place
-      float e[4][4];
+      __syncthreads();                          // keys are done with
+      if (u + 1 < pc.u1) fill_keys(u + 1);
+      else copy_commit();
+      float* w_row = w_sh + y * kEach * kFlatKeys;      // of the thread's rows; places xored with w_turn
+      const int w_turn = (y & 1) * 16;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kEach; ++i) {
         // the factor in two floats and the maximum taken off before the rounding: a weight near 1 is off by the exponential's error and
         // the dot product's, not by the rounding of a large score
         float top = m[i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bool on = t0 + x + 16 * j < seen[i];
-          if (on) top = fmaxf(top, fmaf(dot[i][j], p.scale_log2e, dot[i][j] * p.scale_rest));
+          if (t0 + x + 16 * j < seen[i]) top = fmaxf(top, fmaf(dot[i][j], p.scale_log2e, dot[i][j] * p.scale_rest));
         }
 #pragma unroll
         for (int off = 1; off < 16; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -119,49 +149,54 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
         if (top != m[i]) {
           l[i] *= f;
 #pragma unroll
-          for (int c = 0; c < kChannels; ++c) o[i][c] *= f;
+          for (int c = 0; c < kChunks * kVec; ++c) o[i][c] *= f;
           m[i] = top;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const bool on = t0 + x + 16 * j < seen[i];
-          e[i][j] = on ? ex2(fmaf(dot[i][j], p.scale_log2e, fmaf(dot[i][j], p.scale_rest, -base))) : 0.f;
-          l[i] += e[i][j];
-          k_sh[(y * 4 + i) * kP + x + 16 * j] = e[i][j];
+          const float e = on ? ex2(fmaf(dot[i][j], p.scale_log2e, fmaf(dot[i][j], p.scale_rest, -base))) : 0.f;
+          l[i] += e;
+          w_row[i * kFlatKeys + ((x + 16 * j) ^ w_turn)] = e;
         }
       }
-      __syncthreads();
+      copy_wait<1>();
+      __syncthreads();                          // values are there, and the weights
       // a row's own keys only: what lies in the others may be infinite
-      const int fewest = min(min(seen[0], seen[1]), min(seen[2], seen[3])) - t0;
+      int fewest = seen[0];
+#pragma unroll
+      for (int i = 1; i < kEach; ++i) fewest = min(fewest, seen[i]);
+      fewest -= t0;
       auto add = [&](auto masked) {
 #pragma unroll 2
         for (int t = 0; t < there; t += 4) {
-          float w[4][4];
+          float w[kEach][4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 f = *reinterpret_cast<const float4*>(k_sh + (y * 4 + i) * kP + t);
+          for (int i = 0; i < kEach; ++i) {
+            const float4 f = *reinterpret_cast<const float4*>(w_row + i * kFlatKeys + (t ^ w_turn));
             w[i][0] = f.x; w[i][1] = f.y; w[i][2] = f.z; w[i][3] = f.w;
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 4; ++j) {
+            float f[kChunks * kVec];
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
-              float f[kVec];
               const float* from = v_sh + (t + j) * DP + (c * 16 + x) * kVec;
               if constexpr (kVec == 4) {
-                const float4 y = *reinterpret_cast<const float4*>(from);
-                f[0] = y.x; f[1] = y.y; f[2] = y.z; f[3] = y.w;
+                const float4 four = *reinterpret_cast<const float4*>(from);
+                f[4 * c] = four.x; f[4 * c + 1] = four.y; f[4 * c + 2] = four.z; f[4 * c + 3] = four.w;
               } else {
-                const float2 y = *reinterpret_cast<const float2*>(from);
-                f[0] = y.x; f[1] = y.y;
-              }
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                if (decltype(masked)::value && t0 + t + j >= seen[i]) continue;
-#pragma unroll
-                for (int e = 0; e < kVec; ++e) o[i][kVec * c + e] = fmaf(w[i][j], f[e], o[i][kVec * c + e]);
+                const float2 two = *reinterpret_cast<const float2*>(from);
+                f[2 * c] = two.x; f[2 * c + 1] = two.y;
               }
             }
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+              if (decltype(masked)::value && t0 + t + j >= seen[i]) continue;
+#pragma unroll
+              for (int c = 0; c < kChunks * kVec; ++c) o[i][c] = fmaf(w[i][j], f[c], o[i][c]);
+            }
+          }
         }
       };
       if (fewest >= there) add(std::false_type{});
@@ -170,11 +205,11 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
     const bool complete = pc.u0 == 0 && pc.u1 == pc.units;
     float* part = p.partial + (static_cast<size_t>(blockIdx.x) * 2 + (pc.u0 == 0 ? 1 : 0)) * partial_floats(kFlatRows, D);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kEach; ++i) {
       float sum = l[i];
 #pragma unroll
       for (int off = 1; off < 16; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-      const int r = y * 4 + i;
+      const int r = y * kEach + i;
       if (r >= pc.n_rows) continue;
       const RowAt at = row_of(r);
       char* out = out_at(p, pc.b, s.first, at);
@@ -183,10 +218,14 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
         const int ch = (c * 16 + x) * kVec;
         if (ch >= D) continue;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float v = o[i][kVec * c + e];
-          if (complete) store_out<T>(out, ch + e, sum == 0.f ? 0.f : v / sum);
-          else part[static_cast<size_t>(r) * D + ch + e] = v;
+        for (int e = 0; e < kVec / 2; ++e) {
+          const float2 both = make_float2(o[i][kVec * c + 2 * e], o[i][kVec * c + 2 * e + 1]);
+          if (complete) {
+            store_out<T>(out, ch + 2 * e, sum == 0.f ? 0.f : both.x / sum);
+            store_out<T>(out, ch + 2 * e + 1, sum == 0.f ? 0.f : both.y / sum);
+          } else {
+            *reinterpret_cast<float2*>(part + static_cast<size_t>(r) * D + ch + 2 * e) = both;
+          }
         }
       }
       if (x == 0) {
