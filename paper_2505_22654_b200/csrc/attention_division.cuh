@@ -11,7 +11,7 @@ namespace kv {
 template <int THREADS, int ROWS, int KEYS, int WHOLE, int EXTRA = 0>
 struct TileShape {
   static constexpr int kThreads = THREADS, kKeys = KEYS, kWhole = WHOLE, kExtra = EXTRA;
-  __device__ __forceinline__ static int rows(const AttnParams& p) { return ROWS > 0 ? ROWS : p.tile_rows; }
+  __host__ __device__ __forceinline__ static int rows(const AttnParams& p) { return ROWS > 0 ? ROWS : p.tile_rows; }
 };
 
 struct DivisionShared {
@@ -22,7 +22,8 @@ struct DivisionShared {
 
 // As for few rows, but a place on the line is a key seen by a query row, so that the triangle of a causal prompt is divided
 // evenly: tile k of a causal sequence weighs group * start + min(kRows (k + 1), rows), at least one step, which has a closed
-// prefix sum.
+// prefix sum.  The sum is exact whatever the rows of a tile are (125 for groups of five above 128 channels): a stretch that finds its start
+// by it and one that gets there tile by tile have to agree on every place.
 struct TcSequence {
   Sequence s;
   long long base;       // what every tile sees at least
@@ -32,20 +33,27 @@ struct TcSequence {
 };
 
 template <typename S>
-__device__ __forceinline__ long long step_weight(const AttnParams& p) { return static_cast<long long>(S::kKeys) * p.group; }
+__host__ __device__ __forceinline__ long long step_weight(const AttnParams& p) { return static_cast<long long>(S::kKeys) * p.group; }
 
+// What tile k weighs, and the k tiles in front of it
 template <typename S>
-__device__ __forceinline__ long long tiles_before(const AttnParams& p, const TcSequence& q, long long k) {
-  const long long one = step_weight<S>(p), extra = k * one * S::kExtra;
-  if (!p.causal) return k * max(q.base, one) + extra;
+__host__ __device__ __forceinline__ long long tile_weight(const AttnParams& p, const TcSequence& q, int k) {
+  const long long one = step_weight<S>(p);
+  const long long seen = !p.causal ? q.base : q.base + (k + 1 < q.tiles ? static_cast<long long>(S::rows(p)) * (k + 1) : q.rows);
+  return max(seen, one) + S::kExtra * one;
+}
+template <typename S>
+__host__ __device__ __forceinline__ long long tiles_before(const AttnParams& p, const TcSequence& q, long long k) {
+  if (!p.causal) return k * tile_weight<S>(p, q, 0);
+  const long long one = step_weight<S>(p);
   const long long n = min(k, static_cast<long long>(q.tiles - 1)), m = min(n, static_cast<long long>(q.light));
-  const long long sum = m * one + (n - m) * q.base + (n * (n + 1) - m * (m + 1)) * (S::rows(p) / 2) + extra;
-  return k < q.tiles ? sum : sum + max(q.base + q.rows, one);
+  const long long sum = m * one + (n - m) * q.base + ((n * (n + 1) - m * (m + 1)) >> 1) * S::rows(p) + n * one * S::kExtra;
+  return k < q.tiles ? sum : sum + tile_weight<S>(p, q, q.tiles - 1);
 }
 
 // Quotient of numbers that nearly always fit 32 bits; bit by bit where they do not (a division of 64 bits is 2 KB of instructions
 // wherever it stands, and the kernels that divide here have to stay in the instruction cache)
-__device__ __forceinline__ long long quotient(long long a, long long b) {
+__host__ __device__ __forceinline__ long long quotient(long long a, long long b) {
   if (((a | b) >> 32) == 0) return static_cast<unsigned>(a) / static_cast<unsigned>(b);
   unsigned long long q = 0, r = 0;
 #pragma unroll 1
@@ -58,7 +66,7 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
 }
 
 template <typename S, typename P>
-__device__ __forceinline__ TcSequence tc_sequence_at(const P& p, int b) {
+__host__ __device__ __forceinline__ TcSequence tc_sequence_at(const P& p, int b) {
   TcSequence q;
   q.s = sequence_at(p, b);
   q.rows = static_cast<long long>(q.s.n) * p.group;
@@ -70,6 +78,17 @@ __device__ __forceinline__ TcSequence tc_sequence_at(const P& p, int b) {
 }
 
 struct TcStretch { long long begin, end, quota, seq0; int b; };
+
+// Stretch k of `ctas` on a line of `total`; which sequence it starts in is another question
+template <typename S>
+__host__ __device__ __forceinline__ TcStretch stretch_of(const AttnParams& p, long long total, unsigned ctas, unsigned k) {
+  TcStretch st = {};
+  // a stretch is at least a step long, so that no two cuts fall into one step
+  st.quota = max(quotient(total + ctas - 1, ctas), step_weight<S>(p) * (1 + S::kExtra));
+  st.begin = min(k * st.quota, total);
+  st.end = min(st.begin + st.quota, total);
+  return st;
+}
 
 template <typename S, typename P>
 __device__ __forceinline__ TcStretch tc_locate(const P& p, DivisionShared& sh) {
@@ -92,11 +111,7 @@ __device__ __forceinline__ TcStretch tc_locate(const P& p, DivisionShared& sh) {
     if (w < warp) before += sh.weight[w];
     total += sh.weight[w];
   }
-  TcStretch st;
-  // a stretch is at least a step long, so that no two cuts fall into one step
-  st.quota = max(quotient(total + gridDim.x - 1, gridDim.x), step_weight<S>(p) * (1 + S::kExtra));
-  st.begin = min(blockIdx.x * st.quota, total);
-  st.end = min(st.begin + st.quota, total);
+  TcStretch st = stretch_of<S>(p, total, gridDim.x, blockIdx.x);
   long long at = before + incl - sum;
   if (at <= st.begin && st.begin < at + sum) {
 #pragma unroll 1
@@ -114,7 +129,7 @@ __device__ __forceinline__ TcStretch tc_locate(const P& p, DivisionShared& sh) {
 
 // The step of a tile that place x of its weight falls into; what a tile weighs beside its steps lies in front of them
 template <typename S>
-__device__ __forceinline__ int step_at(long long x, long long per_unit, int units) {
+__host__ __device__ __forceinline__ int step_at(long long x, long long per_unit, int units) {
   if (S::kExtra > 0) x = max(x - S::kExtra * per_unit, 0ll);
   return static_cast<int>(min(quotient(x, per_unit), static_cast<long long>(units)));
 }
@@ -126,7 +141,7 @@ struct TcPiece {
 };
 
 template <typename S, typename P>
-__device__ __forceinline__ bool tc_next(const P& p, TcStretch& st, TcPiece& pc) {
+__host__ __device__ __forceinline__ bool tc_next(const P& p, TcStretch& st, TcPiece& pc) {
   while (st.begin < st.end) {
     pc.q = tc_sequence_at<S>(p, st.b);
     const long long all = pc.q.weight * p.kv_heads;

@@ -25,10 +25,10 @@ struct Pieces {          // of one segment
   const float* first;
   size_t stride;
   int n;
-  __device__ __forceinline__ const float* at(int i) const { return first + (i == 0 ? 0 : 2 * i - 1) * stride; }
+  __host__ __device__ __forceinline__ const float* at(int i) const { return first + (i == 0 ? 0 : 2 * i - 1) * stride; }
 };
 
-__device__ __forceinline__ bool cut_at(const AttnParams& p, int k, Boundary& bd, Pieces& pc) {
+__host__ __device__ __forceinline__ bool cut_at(const AttnParams& p, int k, Boundary& bd, Pieces& pc) {
   if (k == 0) return false;
   bd = p.boundary[k];
   const Boundary before = p.boundary[k - 1];

@@ -15,14 +15,14 @@ struct PromptParams : AttnParams {
 };
 
 // First key row of sequence b in the buffer (padded: 0), and its keys, held inside the buffer
-__device__ __forceinline__ void key_span(const PromptParams& p, int b, int& first, int& n) {
+__host__ __device__ __forceinline__ void key_span(const PromptParams& p, int b, int& first, int& n) {
   const long long lo = p.kv_offset[b], given = max(p.kv_offset[b + 1] - lo, 0ll);
   first = p.padded ? 0 : static_cast<int>(lo);
   const long long room = p.padded ? p.kv_rows : lo < 0 ? 0 : max(p.kv_rows - lo, 0ll);
   n = static_cast<int>(min(given, room));
 }
 
-__device__ __forceinline__ Sequence sequence_at(const PromptParams& p, int b) {
+__host__ __device__ __forceinline__ Sequence sequence_at(const PromptParams& p, int b) {
   Sequence s;
   const long long lo = p.row_offset[b], given = max(p.row_offset[b + 1] - lo, 0ll);
   s.first = p.padded ? 0 : static_cast<int>(lo);

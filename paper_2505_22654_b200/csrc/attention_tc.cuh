@@ -141,7 +141,7 @@ __device__ __forceinline__ bool wait_piece(const PromptParams& p, uint64_t* bar,
   return __all_sync(0xffffffffu, got);
 }
 // Keys that row `token` of a sequence sees
-__device__ __forceinline__ int keys_seen(const PromptParams& p, const PtPiece& pc, int token) {
+__host__ __device__ __forceinline__ int keys_seen(const PromptParams& p, const PtPiece& pc, int token) {
   if (!p.causal) return pc.len;
   return static_cast<int>(min(max(pc.start + token + 1, 0ll), static_cast<long long>(pc.len)));
 }
@@ -154,13 +154,13 @@ struct PtPlanner {
   int key0, head, tile;
   bool inside;
 
-  __device__ __forceinline__ void enter(const PromptParams& p, int b) {
+  __host__ __device__ __forceinline__ void enter(const PromptParams& p, int b) {
     st.b = b;
     q = tc_sequence_at<PtShape>(p, b);
     int keys;
     key_span(p, b, key0, keys);
   }
-  __device__ __forceinline__ bool next(const PromptParams& p, PtPiece& pc, Boundary& cut) {
+  __host__ __device__ __forceinline__ bool next(const PromptParams& p, PtPiece& pc, Boundary& cut) {
     const long long one = step_weight<PtShape>(p);
     while (st.begin < st.end) {
       if (!inside) {                                     // the stretch's first tile takes a search
@@ -182,8 +182,7 @@ struct PtPlanner {
           do enter(p, st.b + 1); while (q.tiles == 0);   // there is one: the stretch goes on
         }
       }
-      const long long mine = !p.causal ? q.base : q.base + (tile + 1 < q.tiles ? static_cast<long long>(p.tile_rows) * (tile + 1) : q.rows);
-      const long long seg_end = seg0 + max(mine, one) + kPtExtra * one;
+      const long long seg_end = seg0 + tile_weight<PtShape>(p, q, tile);
       pc.b = st.b; pc.head = head; pc.tile = tile; pc.first = q.s.first; pc.key0 = key0; pc.len = q.s.len; pc.start = q.s.start;
       const int tokens = p.tile_rows / p.group;
       pc.token = tile * tokens;

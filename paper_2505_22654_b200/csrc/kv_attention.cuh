@@ -50,7 +50,7 @@ struct Sequence {       // of one sequence: new rows, keys, tiles, units of a se
   long long start, weight;
 };
 
-__device__ __forceinline__ Sequence sequence_at(const AttnParams& p, int b) {
+__host__ __device__ __forceinline__ Sequence sequence_at(const AttnParams& p, int b) {
   Sequence s;
   row_span(p.row_offset, p.kv_len, b, p.rows, p.padded, s.first, s.n, s.start);
   s.n = min(s.n, p.max_q_len);
@@ -206,7 +206,7 @@ __device__ __forceinline__ const char* q_at(const AttnParams& p, int b, int firs
   return p.q + (p.padded ? b * p.q_seq : first * p.q_row) + r.i * p.q_row + r.h * p.q_head;
 }
 // Tokens that new row i sees
-__device__ __forceinline__ int visible(const AttnParams& p, const Sequence& s, int i) {
+__host__ __device__ __forceinline__ int visible(const AttnParams& p, const Sequence& s, int i) {
   if (!p.causal) return s.len;
   return static_cast<int>(min(max(s.start + i + 1, 0ll), static_cast<long long>(s.len)));
 }

@@ -73,7 +73,7 @@ __device__ __forceinline__ void decode4(uint32_t w, float* out) {
 
 // New rows of sequence b, held inside the `rows` of the buffer: first packed row (0: padded), count, and the position of the
 // first in the sequence (below zero where kv_len is less than the rows)
-__device__ __forceinline__ void row_span(const int32_t* row_offset, const int32_t* kv_len, int b, int rows, bool padded,
+__host__ __device__ __forceinline__ void row_span(const int32_t* row_offset, const int32_t* kv_len, int b, int rows, bool padded,
                                          int& first, int& n, long long& start) {
   const long long lo = row_offset[b], given = max(row_offset[b + 1] - lo, 0ll);
   start = kv_len[b] - given;
