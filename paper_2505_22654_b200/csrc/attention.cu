@@ -371,7 +371,7 @@ using namespace vscan;
 
 extern "C" size_t vscan_attention_workspace_bytes(const vscan_attention_desc* d) {
   if (!d || d->batch <= 0 || d->rows <= 0 || d->max_q_len <= 0 || d->q_heads <= 0 || d->kv_heads <= 0 || d->head_dim <= 0 || d->head_dim > 256 ||
-      d->q_heads / d->kv_heads > 64 || d->kv_rows < 0)
+      d->q_heads % d->kv_heads || d->q_heads / d->kv_heads > 64 || d->kv_rows < 0)      // (sizes that the call refuses; a plan divides by the group)
     return kStatusBytes;
   const size_t flat = kv::prompt_bytes(kv::plan_prompt(d, false), d->head_dim);      // strides decide between the two
   const size_t tensor = d->dtype == VSCAN_BF16 ? kv::prompt_bytes(kv::plan_prompt(d, true), d->head_dim) : 0;

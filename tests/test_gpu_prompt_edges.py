@@ -28,3 +28,9 @@ def test_attention_of_groups_whose_tiles_have_an_odd_number_of_rows(group, d, ro
                 j = min(i + 1500, n)
                 mine, keys = slice(off[b] + i, off[b] + j), slice(off[b], off[b] + j)
                 check_attention("bf16", out[mine, heads], lse[mine, heads], q[mine, heads], k[keys, h:h + 1], v[keys, h:h + 1], scale, True)
+
+
+def test_attention_of_queries_and_keys_in_each_others_place_is_refused():
+    q, k = torch.zeros((5, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((5, 2, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(vs.VScanError, match="vscan_attention"):
+        vs.vscan_attention(k, q, q, i32([0, 5]), 0.1, 5)
