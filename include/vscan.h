@@ -535,7 +535,7 @@ vscan_status vscan_kv_attention(const vscan_kv_attention_desc* desc, void* works
  *   row_offset [batch + 1] int32, from 0, not falling: sequence b has n_b = row_offset[b + 1] - row_offset[b] query rows
  *   kv_offset  optional [batch + 1] int32, likewise for keys: m_b.  NULL: row_offset serves both
  *   causal != 0: row i of the n_b stands at m_b - n_b + i and sees the keys up to itself; else every row sees all m_b.  A row
- *   that sees nothing gives 0 (and lse -inf).  What lies in keys and values that a row does not see never reaches it, infinities and
+ *   that sees nothing gives 0 (and lse -inf), and so does one whose scores are all -infinity.  What lies in keys and values that a row does not see never reaches it, infinities and
  *   NaN included.
  *   q, out    rows of q_heads x head_dim, k, v rows of kv_heads x head_dim, all of `dtype`, packed or padded as described at the
  *             paged cache: element (row, h, c) at (offset[b] + i) * stride[2] + h * stride[1] + c, or b * stride[0] + i * stride[2] +

@@ -50,6 +50,8 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
     p.boundary[blockIdx.x].seg1 = 0;
     p.flags[blockIdx.x] = 0;
   }
+  // A dot product whose score is -infinity, of weight 0 (the two parts of the factor would make a NaN of it where their signs differ or one is 0)
+  const float gone = p.scale_log2e > 0.f ? -INFINITY : p.scale_log2e < 0.f ? INFINITY : __uint_as_float(0x7fc00000u);
   TcPiece pc;
   // Rows of a buffer as floats into shared memory, zeros beyond `there` rows; turn(r): what the places of a row's fours are xored with
   auto fill = [&](float* dst, int there, auto turn, auto at) {
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(kFlatThreads, DP == 256 ? 1 : 2) flat_kernel(P
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bool on = t0 + x + 16 * j < seen[i];
+          const bool on = t0 + x + 16 * j < seen[i] && dot[i][j] != gone;
           const float e = on ? ex2(fmaf(dot[i][j], p.scale_log2e, fmaf(dot[i][j], p.scale_rest, -base))) : 0.f;
           l[i] += e;
           w_row[i * kFlatKeys + ((x + 16 * j) ^ w_turn)] = e;

@@ -1,5 +1,6 @@
 """vscan_attention, vscan_kv_weigh and vscan_kv_evict where they could go wrong beside what test_gpu_prompt_ops.py runs; tolerances are those of that
 file."""
+import numpy as np
 import pytest
 import torch
 
@@ -34,3 +35,55 @@ def test_attention_of_queries_and_keys_in_each_others_place_is_refused():
     q, k = torch.zeros((5, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((5, 2, 64), dtype=torch.bfloat16, device="cuda")
     with pytest.raises(vs.VScanError, match="vscan_attention"):
         vs.vscan_attention(k, q, q, i32([0, 5]), 0.1, 5)
+
+
+# --------------------------------------------------------------------------- attention: a visible score of -infinity
+def _rest(scale):
+    """What float32 leaves of scale * log2(e), as float32."""
+    factor = float(np.float32(scale)) * 1.4426950408889634
+    return float(np.float32(factor - float(np.float32(factor))))
+
+
+SCALES = (0.125, 0.3, 9e-39, 0.1, -0.125, -0.1)
+
+
+def test_the_scales_have_rests_of_every_sign():
+    rests = [_rest(s) for s in SCALES]
+    assert rests[0] > 0 and rests[2] == 0 and rests[3] < 0 and rests[4] < 0 < rests[5]
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("dtype,shared", [("f32", False), ("bf16", False), ("bf16", True), ("f32", True)])
+@pytest.mark.parametrize("d", [64, 80, 256])
+def test_attention_gives_no_weight_to_a_score_of_minus_infinity(dtype, shared, scale, d):
+    """Keys with a channel of -infinity (or infinity, for negative scales) that every query meets with a positive one: softmax gives them 0, the
+    others as if they were not there.
+    shared: the two heads of the keys are one (stride 0), which the CUDA cores take in bf16 too."""
+    g, n, m = gen(d), 70, 300
+    q, k, v = (torch.randn((rows, H, d), generator=g) for rows, H in ((n, 4), (m, 1 if shared else 2), (m, 2)))
+    q[..., 3] = q[..., 3].abs() + 0.5
+    gone = torch.zeros(m, dtype=torch.bool)
+    gone[[0, 5, 64, 127, 128, 200, 299]] = True
+    k[gone, :, 3] = float("-inf") if scale > 0 else float("inf")
+    q, k, v = (x.to(DT[dtype]).cuda() for x in (q, k, v))
+    k = k.expand(m, 2, d) if shared else k
+    stay = (~gone).cuda()
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    vs.vscan_attention(q, k, v, i32([0, n]), scale, n, kv_offset=i32([0, m]), causal=False, out=out, lse=lse)
+    check_attention(dtype, out, lse, q, k[stay], v[stay], scale, False)
+    # causal, rows and keys alike: row 0 sees nothing but such a key
+    gone[1:] = False
+    k = k.clone()
+    k[1:, :, 3] = 0.25
+    vs.vscan_attention(q, k, v, i32([0, n]), scale, n, out=out, lse=lse)
+    check_attention(dtype, out[1:], lse[1:], q[1:], k[1:n], v[1:n], scale, True)
+    assert (out[0] == 0).all() and torch.isneginf(lse[0]).all()
+
+
+def test_attention_gives_no_weight_to_a_score_that_leaves_float32():
+    q, k, v = torch.full((3, 1, 64), 1e19, device="cuda"), torch.full((5, 1, 64), 1e-19, device="cuda"), torch.randn((5, 1, 64), device="cuda")
+    k[2] = -1e19                                             # a sum of -6.4e39
+    lse = torch.empty((3, 1), device="cuda")
+    out = vs.vscan_attention(q, k, v, i32([0, 3]), 0.125, 3, kv_offset=i32([0, 5]), causal=False, lse=lse)
+    stay = [0, 1, 3, 4]
+    check_attention("f32", out, lse, q, k[stay], v[stay], 0.125, False)
