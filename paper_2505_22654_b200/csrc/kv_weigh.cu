@@ -238,7 +238,9 @@ __global__ void __launch_bounds__(128) weigh_fma_kernel(WeighParams p) {
         float gain = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const float sum = dot[r] + odd[r], hi = ks * p.scale_log2e, lo = sum * (ks * p.scale_rest);
+          const float sum = dot[r] + odd[r], hi = ks * p.scale_log2e;
+          // (infinity times a rest of the other sign, or of 0, would make a NaN of an infinite score)
+          const float lo = fabsf(sum) < INFINITY ? sum * (ks * p.scale_rest) : 0.f;
           if (t < seen[r]) gain += ex2(fmaf(sum, hi, lo - lse[r]));
         }
         *at = w + gain;

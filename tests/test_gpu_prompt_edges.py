@@ -5,8 +5,9 @@ import pytest
 import torch
 
 import paper_2505_22654_b200 as vs
+from oracle import cache_oracle as co
 from test_gpu_cache_ops import DT, _offsets, gen, i32
-from test_gpu_prompt_ops import check_attention
+from test_gpu_prompt_ops import _random_cache, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +88,25 @@ def test_attention_gives_no_weight_to_a_score_that_leaves_float32():
     out = vs.vscan_attention(q, k, v, i32([0, 3]), 0.125, 3, kv_offset=i32([0, 5]), causal=False, lse=lse)
     stay = [0, 1, 3, 4]
     check_attention("f32", out, lse, q, k[stay], v[stay], 0.125, False)
+
+
+# --------------------------------------------------------------------------- weigh: scores that leave float32
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+@pytest.mark.parametrize("scale", [0.125, 0.1, -0.125, -0.1])
+@pytest.mark.parametrize("rows", [1, 3])
+def test_weigh_of_scores_of_minus_infinity_gives_nothing(kv, scale, rows):
+    """float32 rows whose products with every key (codes above 0) sum to less than float32 holds: they add 0, the other row what it adds alone."""
+    hk, d, T = 2, 32, 40
+    kind, codes, sc, dev = _random_cache(kv, hk, 16, d, 4, 3)
+    codes[0][:] = codes[0] % 63 + 64                         # above 0; e4m3: 2 and more
+    dev[0].view(torch.uint8).copy_(torch.from_numpy(codes[0]))
+    table, q = [[2, 0, 3]], torch.randn((rows, hk, d), generator=gen(1))
+    q[-1] = -1e38 if scale > 0 else 1e38
+    q[rows // 2 + 1:] = q[-1]
+    lse = torch.full((rows, hk), 0.75)
+    w = torch.rand((4, hk, 16), generator=gen(2))
+    got, want = w.cuda(), w.double().numpy()
+    vs.vscan_kv_weigh(q.cuda(), lse.cuda(), i32([T]), i32([0, rows]), i32(table), dev[0], dev[2], got, scale, max_q_len=rows, decay=0.5, causal=False)
+    slack = co.weigh(want, [q.double().numpy()], [lse.double().numpy()], codes[0], sc[0], [T], table, 16, kind, float(np.float32(scale)), 0.5, None, False)
+    tol = (d + 8) * 2.0 ** -24 * slack + (2.0 ** -21 + (rows / 4 + 16) * 2.0 ** -24 + 2.0 ** -23) * np.abs(want)
+    assert (np.abs(got.double().cpu().numpy() - want) <= tol).all() and np.isfinite(want).all()
