@@ -602,7 +602,7 @@ vscan_status vscan_kv_weigh(const vscan_kv_weigh_desc* desc, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
  * vscan_kv_evict: of each sequence the min(budget, kv_len) tokens that rank highest stay, the others leave the cache.
- *   rank      of token t: above all others if t < keep_first or t >= kv_len - keep_last; else its weight (see vscan_kv_weigh) for the
+ *   rank      of token t: above all others, infinite weights too, if t < keep_first or t >= kv_len - keep_last; else its weight (see vscan_kv_weigh) for the
  *             KV head (per_head != 0), or the sum of its weights over the heads, taken in 64 bits and rounded to float32, for all heads
  *             alike.  NaN ranks as -inf.  Equal ranks: the lowest t stays.
  *   budget    [batch] int32, less than 0 counts as 0; no budget is larger than max_keep (larger ones count as max_keep)

@@ -219,11 +219,12 @@ def evict(codes, scale, weight, kv_len, budget, table, block_size, kind, max_kee
         delta.append(n - T)
         where = [(row[t // block_size], t % block_size) for t in range(T)]
         w = np.array([[weight[blk, h, at] for blk, at in where] for h in range(H)], dtype=np.float64).reshape(H, T)
-        rank = w if per_head else w.sum(0, keepdims=True).astype(np.float32).astype(np.float64)
+        with np.errstate(over="ignore"):
+            rank = w if per_head else w.sum(0, keepdims=True).astype(np.float32).astype(np.float64)
         rank = np.where(np.isnan(rank), -np.inf, rank)
         mine = []
         for r in rank:
-            key = [(-np.inf if t < first or t >= T - last else -r[t], t) for t in range(T)]
+            key = [((1, -r[t]) if first <= t < T - last else (0, 0.0), t) for t in range(T)]       # protected ones in front of all others, whatever these weigh
             mine.append(sorted(t for _, t in sorted(key)[:n]))
         kept.append(mine)
         full = [[where[t] for t in range(T)]] * H

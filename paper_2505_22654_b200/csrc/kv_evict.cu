@@ -40,6 +40,7 @@ struct EvictParams {
 // Reads 4 bytes a token and head, once; everything after that is the latency of five passes over keys in shared memory.  8 sequences of 12,000
 // to 16,400 tokens, 8 heads of their own (64 CTAs): 25 us, of which a copy of the weights would be one.
 __device__ __forceinline__ uint32_t rank_key(float w) { return float_to_key(w == w ? w : -INFINITY); }
+constexpr uint32_t kProtected = 0xffffffffu;        // above the key of an infinite weight, or of a sum over the heads that is
 
 __global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
   extern __shared__ uint32_t rank_smem[];
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const long long t = t0 + u * static_cast<long long>(blockDim.x);
-      if (t < len) keys[t] = rank_key(t < p.keep_first || t >= static_cast<long long>(len) - p.keep_last ? INFINITY : rank[u]);
+      if (t < len) keys[t] = t < p.keep_first || t >= static_cast<long long>(len) - p.keep_last ? kProtected : rank_key(rank[u]);
     }
   }
   __syncthreads();
@@ -165,17 +166,15 @@ __global__ void __launch_bounds__(kRankThreads) rank_warp_kernel(EvictParams p) 
     key[i] = 0;                                      // less than any rank
     if (t < len) {
       const float* w = p.weight + (static_cast<size_t>(block) * p.kv_heads << p.shift) + (t & (p.block_size - 1));
-      float rank;
       if (t < p.keep_first || t >= static_cast<long long>(len) - p.keep_last) {
-        rank = INFINITY;
+        key[i] = kProtected;
       } else if (p.heads > 1 || p.kv_heads == 1) {
-        rank = __ldg(w + (static_cast<size_t>(head) << p.shift));
+        key[i] = rank_key(__ldg(w + (static_cast<size_t>(head) << p.shift)));
       } else {
         double sum = 0.;
         for (int h = 0; h < p.kv_heads; ++h) sum += __ldg(w + (static_cast<size_t>(h) << p.shift));
-        rank = static_cast<float>(sum);
+        key[i] = rank_key(static_cast<float>(sum));
       }
-      key[i] = rank_key(rank);
       any |= key[i];
       all &= key[i];
     }

@@ -7,7 +7,7 @@ import torch
 import paper_2505_22654_b200 as vs
 from oracle import cache_oracle as co
 from test_gpu_cache_ops import DT, _offsets, gen, i32
-from test_gpu_prompt_ops import _random_cache, check_attention
+from test_gpu_prompt_ops import _evict_case, _random_cache, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,23 @@ def test_weigh_of_scores_of_minus_infinity_gives_nothing(kv, scale, rows):
     slack = co.weigh(want, [q.double().numpy()], [lse.double().numpy()], codes[0], sc[0], [T], table, 16, kind, float(np.float32(scale)), 0.5, None, False)
     tol = (d + 8) * 2.0 ** -24 * slack + (2.0 ** -21 + (rows / 4 + 16) * 2.0 ** -24 + 2.0 ** -23) * np.abs(want)
     assert (np.abs(got.double().cpu().numpy() - want) <= tol).all() and np.isfinite(want).all()
+
+
+# --------------------------------------------------------------------------- evict: protected tokens and infinite weights
+@pytest.mark.parametrize("per_head", [True, False])
+@pytest.mark.parametrize("B,hk,bs,length", [(2, 2, 16, 120), (100, 4, 16, 100), (1, 2, 64, 1500), (1, 1, 16, 17000)])
+def test_evict_keeps_protected_tokens_in_front_of_infinite_weights(per_head, B, hk, bs, length):
+    """More tokens of infinite weight (or of weights whose sum over the heads is) than the budget; ranks by a CTA, by a warp, through memory."""
+    def spoil(table, weight, scale, codes):
+        weight[:] = np.inf
+        weight[table[0][0]] = 3e38
+    lens, budget = [length - b % 7 for b in range(B)], [(40, 11, 6, 3)[b % 4] for b in range(B)]
+    for first, last in ((3, 5), (0, 8), (2, 0)):
+        _evict_case("i8", hk, 16, bs, lens, budget, first, last, per_head, spoil=spoil)
+
+
+@pytest.mark.parametrize("B", [1, 160])
+def test_evict_sums_over_the_heads_that_leave_float32_rank_below_protected_tokens(B):
+    def spoil(table, weight, scale, codes):
+        weight[:] = 3e38
+    _evict_case("e4m3", 2, 16, 16, [90] * B, [20] * B, 1, 12, False, spoil=spoil)
