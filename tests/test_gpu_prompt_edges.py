@@ -130,3 +130,185 @@ def test_evict_sums_over_the_heads_that_leave_float32_rank_below_protected_token
     def spoil(table, weight, scale, codes):
         weight[:] = 3e38
     _evict_case("e4m3", 2, 16, 16, [90] * B, [20] * B, 1, 12, False, spoil=spoil)
+
+
+# --------------------------------------------------------------------------- offsets outside the buffers, streams, graphs
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("padded", [False, True])
+def test_attention_of_offsets_that_leave_the_buffers(dtype, padded):
+    """What is outside is not there, positions follow the offsets as given; rows that nobody owns hold what they held."""
+    g = gen(4)
+    q, k, v = (torch.randn((5, 1, 64), generator=g).to(DT[dtype]).cuda() for _ in range(3))
+    views = [x.transpose(0, 1)[None] if padded else x for x in (q, k, v)]
+
+    def call(off, koff, causal=True):
+        out = torch.full_like(views[0], 7.0)
+        lse = torch.full(out.shape[:-1], 7.0, device="cuda")
+        vs.vscan_attention(*views, i32(off), 0.2, 9, kv_offset=i32(koff), causal=causal, out=out, lse=lse)
+        return (out[0].transpose(0, 1), lse[0].T) if padded else (out, lse)
+
+    out, lse = call([0, 9], [0, 5])                          # rows 5 .. 8 are not there; row 4 is at 0
+    assert (out[:4] == 0).all() and torch.isneginf(lse[:4]).all()
+    check_attention(dtype, out[4:], lse[4:], q[4:], k[:1], v[:1], 0.2, True)
+    out, lse = call([0, 5], [0, 2 ** 31 - 1])                # rows stand behind all keys that there are
+    check_attention(dtype, out, lse, q, k, v, 0.2, False)
+    out, lse = call([0, 5], [5, 5])
+    assert (out == 0).all() and torch.isneginf(lse).all()
+    for off, koff in (([3, 1], [0, 5]),) + (() if padded else (([-2, 3], [-2, 3]), ([5, 9], [5, 9]))):
+        out, lse = call(off, koff)
+        assert (out == 7).all() and (lse == 7).all()
+    out, lse = call([0, 3], [0, 5], False)
+    check_attention(dtype, out[:3], lse[:3], q[:3], k, v, 0.2, False)
+    assert (out[3:] == 7).all() and (lse[3:] == 7).all()
+
+
+def test_attention_of_two_streams_at_once():
+    """A workspace each: results as one after the other."""
+    g = gen(22)
+    sets = [[torch.randn((1500, 2, 128), generator=g).to(torch.bfloat16).cuda() for _ in range(3)] for _ in range(2)]
+    off = i32([0, 700, 1500])
+    want = [vs.vscan_attention(*s, off, 0.1, 800) for s in sets]
+    for s, w in zip(sets, want):
+        check_attention("bf16", w[:700], vs_lse(s, off)[:700], s[0][:700], s[1][:700], s[2][:700], 0.1, True)
+    streams, spaces = [torch.cuda.Stream() for _ in sets], [vs.vscan_attention_workspace(s[0], s[1], off, 800) for s in sets]
+    outs = [[torch.zeros_like(s[0]) for _ in range(8)] for s in sets]
+    torch.cuda.synchronize()
+    for n in range(8):
+        for s, st, ws, out in zip(sets, streams, spaces, outs):
+            with torch.cuda.stream(st):
+                vs.vscan_attention(*s, off, 0.1, 800, out=out[n], workspace=ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for out, w in zip(outs, want) for o in out) and [vs.vscan_check(w) for w in spaces] == [0, 0]
+
+
+def vs_lse(s, off):
+    lse = torch.empty(s[0].shape[:2], device="cuda")
+    vs.vscan_attention(*s, off, 0.1, 800, lse=lse)
+    return lse
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_captured_step_with_weights_and_an_eviction(dtype):
+    """A decode step and an eviction of a cache in one graph, replayed: codes, weights and lengths as those of a cache that made the calls."""
+    hq, hk, d, B, g = 4, 2, 64, 3, gen(31)
+    rope, budget = vs.rope_table(d, [d // 2]), i32([20, 40, 9])
+    make = [vs.VScanCache(num_blocks=40, block_size=16, kv_heads=hk, head_dim=d, batch=B, max_blocks=8, rows=200, weights=True) for _ in range(2)]
+    q, k, v = (torch.randn((B, H, 60, d), generator=g).to(DT[dtype]).cuda() for H in (hq, hk, hk))
+    pos = torch.arange(60, dtype=torch.int32, device="cuda").expand(1, B, -1).contiguous()
+    for c in make:
+        c.prompt(q, k, v, pos, rope, i32([60, 33, 5]), d ** -0.5)
+    q1, k1, v1 = (torch.randn((B, H, 1, d), generator=g).to(DT[dtype]).cuda() for H in (hq, hk, hk))
+    at, one, kept = i32([[[60], [33], [5]]]), i32([1, 1, 1]), torch.full((B, hk, 64), -1, dtype=torch.int32, device="cuda")
+
+    def turn(c):
+        out = c.step(q1, k1, v1, at, rope, one, d ** -0.5, decay=0.5)
+        c.evict(budget, 64, 2, 3, kept=kept)
+        return out
+    plain, captured = make
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    spare = vs.VScanCache(num_blocks=40, block_size=16, kv_heads=hk, head_dim=d, batch=B, max_blocks=8, rows=200, weights=True)
+    with torch.cuda.stream(side):
+        turn(spare)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = turn(captured)
+    for n in range(4):
+        q1.copy_(torch.randn(q1.shape, generator=gen(n)))
+        k1.copy_(torch.randn(k1.shape, generator=gen(9 + n)))
+        want = turn(plain).clone()
+        want_kept = kept.clone()
+        graph.replay()
+        assert torch.equal(out, want) and torch.equal(kept, want_kept)
+        for a, b in ((plain.k_scale, captured.k_scale), (plain.v_scale, captured.v_scale), (plain.kv_len, captured.kv_len), (plain.weight, captured.weight),
+                     (plain.block_table, captured.block_table), (plain.k.view(torch.uint8), captured.k.view(torch.uint8)),
+                     (plain.v.view(torch.uint8), captured.v.view(torch.uint8))):
+            assert torch.equal(a, b)
+        assert plain.check() == captured.check() == (0, 0)
+
+
+# --------------------------------------------------------------------------- the most sequences, and what lies beyond 2^31 elements
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_most_sequences(dtype):
+    """8,192 sequences of 0 to 3 rows behind 0 to 20 tokens, through all three calls."""
+    B, hq, hk, d, g, rng = 8192, 2, 1, 32, gen(41), np.random.default_rng(3)
+    new = [int(n) for n in rng.integers(0, 4, size=B)]
+    keys = [n + int(p) for n, p in zip(new, rng.integers(0, 21, size=B))]
+    off, koff = _offsets(new), _offsets(keys)
+    q, k, v = (torch.randn((n, H, d), generator=g).to(DT[dtype]).cuda() for n, H in ((off[-1], hq), (koff[-1], hk), (koff[-1], hk)))
+    out, lse = torch.full_like(q, float("nan")), torch.full(q.shape[:2], float("nan"), device="cuda")
+    ws = vs.vscan_attention_workspace(q, k, i32(off), 3)
+    vs.vscan_attention(q, k, v, i32(off), 0.2, 3, kv_offset=i32(koff), out=out, lse=lse, workspace=ws)
+    assert vs.vscan_check(ws) == 0 and torch.isfinite(out).all() and torch.isfinite(lse).all()
+    for b in [0, 1, B - 2, B - 1] + [int(x) for x in rng.integers(0, B, size=60)]:
+        mine, theirs = slice(off[b], off[b + 1]), slice(koff[b], koff[b + 1])
+        if new[b]:
+            check_attention(dtype, out[mine], lse[mine], q[mine], k[theirs], v[theirs], 0.2, True)
+    # each sequence has two blocks: the weights of its tokens, and of those 7 stay
+    table = torch.randperm(2 * B, generator=g).view(B, 2).int().cuda()
+    codes = torch.randint(-100, 101, (2, 2 * B, hk, 16, d), generator=g).to(torch.int8).cuda()
+    scale = torch.full((2, 2 * B, hk), 2.0 ** -7, device="cuda")
+    z = 2 + torch.rand(lse.shape, generator=g).cuda()
+    w = torch.full((2 * B, hk, 16), 0.5, device="cuda")
+    vs.vscan_kv_weigh(q, z, i32(keys), i32(off), table, codes[0], scale[0], w, 0.2, max_q_len=3, decay=0.5)
+    first = codes.clone()
+    ws = vs.vscan_kv_evict_workspace(table, codes[0], 7)
+    kept = torch.full((B, hk, 7), -1, dtype=torch.int32, device="cuda")
+    delta = vs.vscan_kv_evict(i32(keys), i32([7] * B), table, w, codes[0], codes[1], scale[0], scale[1], 7, 1, 1, kept=kept, workspace=ws)
+    assert vs.vscan_check(ws) == 0 and delta.tolist() == [min(7, m) - m for m in keys]
+    for b in [0, B - 1] + [int(x) for x in rng.integers(0, B, size=60)]:
+        m, n = keys[b], new[b]
+        ids = table[b].long()
+        kk = first[0][ids].double().reshape(32, d)[:m] / 128
+        got = w[ids].reshape(32)[:m].double()
+        x, zz = q[off[b]:off[b] + n].double(), z[off[b]:off[b] + n].double()
+        s = 0.2 * torch.einsum("nhd,td->hnt", x, kk) - zz.T[..., None]
+        s.masked_fill_(torch.arange(m, device="cuda") > m - n + torch.arange(n, device="cuda")[:, None], -torch.inf)
+        want = torch.where(torch.arange(m, device="cuda") < m - n, 0.25 if n else 0.5, 0.0).double() + s.exp().sum((0, 1))
+        # scores of some ten units at most
+        assert ((got - want).abs() <= (40 * 2.0 ** -24 * 64 + 2.0 ** -21 + 20 * 2.0 ** -24) * want).all()
+        rank = got.clone()
+        rank[:1] = rank[max(m - 1, 0):] = torch.inf
+        stay = torch.sort(torch.sort(rank, descending=True, stable=True)[1][:7])[0]
+        assert kept[b, 0].tolist() == stay.tolist() + [-1] * (7 - len(stay))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_keys_beyond_two_to_the_31_elements(dtype):
+    """A sequence whose keys and values begin 2.2 x 10^9 elements into their buffers, behind one that has no rows."""
+    far, n, m, hk, d, g = 2_200_000, 20, 333, 8, 128, gen(51)
+    q = torch.randn((n, 16, d), generator=g).to(DT[dtype]).cuda()
+    k, v = (torch.zeros((far + m, hk, d), dtype=DT[dtype], device="cuda") for _ in range(2))
+    for t in (k, v):
+        t[far:] = torch.randn((m, hk, d), generator=g).to(DT[dtype]).cuda()
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    vs.vscan_attention(q, k, v, i32([0, 0, n]), 0.1, n, kv_offset=i32([0, far, far + m]), out=out, lse=lse)
+    check_attention(dtype, out, lse, q, k[far:], v[far:], 0.1, True)
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 1), ("bf16", 40), ("f32", 2)])
+def test_weights_and_evictions_of_blocks_beyond_two_to_the_31_elements(dtype, rows):
+    """Blocks that begin 2.3 x 10^9 codes into the cache."""
+    blocks, hk, bs, d, T, g = 70_000, 8, 32, 128, 100, gen(52)
+    k, v = (torch.zeros((blocks, hk, bs, d), dtype=torch.int8, device="cuda") for _ in range(2))
+    ks, vsc, w = torch.full((blocks, hk), 2.0 ** -7, device="cuda"), torch.full((blocks, hk), 2.0 ** -7, device="cuda"), torch.full((blocks, hk, bs), 0.5, device="cuda")
+    ids = torch.tensor([blocks - 1, blocks - 4, blocks - 2, blocks - 3], device="cuda")
+    for t in (k, v):
+        t[ids] = torch.randint(-100, 101, (4, hk, bs, d), generator=g).to(torch.int8).cuda()
+    before = [t[ids].clone() for t in (k, v)]
+    q, lse = torch.randn((rows, hk, d), generator=g).to(DT[dtype]).cuda(), 2 + torch.rand((rows, hk), generator=g).cuda()
+    table = ids.int()[None]
+    vs.vscan_kv_weigh(q, lse, i32([T]), i32([0, rows]), table, k, ks, w, 0.1, max_q_len=rows, causal=False)
+    kk = before[0].double().transpose(0, 1).reshape(hk, -1, d)[:, :T] / 128
+    want = torch.where(torch.arange(T, device="cuda") < T - rows, 0.5, 0.0) + (0.1 * torch.einsum("nhd,htd->hnt", q.double(), kk) - lse.double().T[..., None]).exp().sum(1)
+    got = w[ids].transpose(0, 1).reshape(hk, -1)[:, :T].double()
+    assert ((got - want).abs() <= (136 * 2.0 ** -24 * 64 + 2.0 ** -21 + (rows / 4 + 16) * 2.0 ** -24) * want).all()
+    kept = torch.zeros((1, hk, 50), dtype=torch.int32, device="cuda")
+    assert vs.vscan_kv_evict(i32([T]), i32([50]), table, w, k, v, ks, vsc, 50, kept=kept).tolist() == [50 - T]
+    src = torch.sort(torch.sort(got.float(), dim=-1, descending=True, stable=True)[1][:, :50], dim=-1)[0]
+    assert torch.equal(kept[0].long(), src)
+    for now, sc, old in ((k, ks, before[0]), (v, vsc, before[1])):
+        flat = lambda x: x.transpose(0, 1).reshape(hk, -1, d)  # noqa: E731
+        values = flat(now[ids].double() * sc[ids][..., None, None].double())[:, :50]
+        assert torch.equal(values, flat(old).double().gather(1, src[..., None].expand(hk, 50, d)) / 128)
