@@ -360,12 +360,17 @@ extern "C" vscan_status vscan_kv_weigh(const vscan_kv_weigh_desc* d, void* strea
   const double factor = static_cast<double>(d->scale) * 1.4426950408889634074;
   p.scale_log2e = static_cast<float>(factor);
   p.scale_rest = static_cast<float>(factor - p.scale_log2e);
-  // 5th-generation tensor cores from 17 query rows of a sequence and KV head on, where TMA takes the rows: up to 16 are one pass of the other
-  // kernel, which reads the codes once and computes less than it reads; from two passes on that one falls behind (1,857 us against 214 at 3,584 rows)
+  // 5th-generation tensor cores from 65 query rows of a sequence and KV head on (49 above 128 channels), where TMA takes the rows: a tile of that
+  // kernel costs the same with 17 rows as with 128, while the other one takes a pass of 16 rows (8 above 128 channels) after the other over
+  // codes that L2 holds after the first.  Microseconds, passes / tiles, 28 / 4 heads of 128: 16 x 2,000 tokens: 16 / 41 at 28 rows, 28 / 41 at 49,
+  // 34 / 42 at 70, 47 / 42 at 98, 59 / 48 at 133, 109 / 56 at 259; 256 x 300: 36 / 125 at 28, 80 / 125 at 70, 110 / 126 at 98, 257 / 176 at 259; one
+  // of 1,000: 9 / 11 at 28, 14 / 11 at 49, 18 / 11 at 70, 53 / 15 at 259.  32 heads, 16,000 tokens: 80 / 139 at 64, 152 / 126 at 128; 256 x 300: 330 /
+  // 959 at 64, 651 / 900 at 128, 1,302 / 1,044 at 256 (short sequences of many heads would cross later than this, one short one earlier).  14 / 2 heads
+  // of 256, 16 x 2,000: 35 / 50 at 35, 47 / 50 at 49, 60 / 50 at 70.  Windows of 3,584 rows, twice: 1,857 / 214.
   CUtensorMap map;
   const int64_t used = d->max_q_len < d->window ? d->max_q_len : d->window;
   const int64_t sizes[2] = {d->q_heads, d->rows}, steps[2] = {d->q_stride[1], d->q_stride[2]};
-  const bool tensor = d->dtype == VSCAN_BF16 && used * p.group > 16 &&
+  const bool tensor = d->dtype == VSCAN_BF16 && used * p.group > (d->head_dim > 128 ? 48 : 64) &&
                       kv::rows_map(d->q, d->head_dim, sizes, steps, d->padded ? d->batch : 1, d->q_stride[0], p.group, 128 / p.group, &map);
   return d->kv_dtype == VSCAN_KV_E4M3 ? kv::launch_weigh<VSCAN_KV_E4M3>(p, d->dtype, tensor ? &map : nullptr, stream)
                                       : kv::launch_weigh<VSCAN_KV_I8>(p, d->dtype, tensor ? &map : nullptr, stream);

@@ -7,7 +7,7 @@ import torch
 import paper_2505_22654_b200 as vs
 from oracle import cache_oracle as co
 from test_gpu_cache_ops import DT, _offsets, gen, i32
-from test_gpu_prompt_ops import _evict_case, _random_cache, check_attention
+from test_gpu_prompt_ops import _evict_case, _random_cache, _weigh_case, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -312,3 +312,15 @@ def test_weights_and_evictions_of_blocks_beyond_two_to_the_31_elements(dtype, ro
         flat = lambda x: x.transpose(0, 1).reshape(hk, -1, d)  # noqa: E731
         values = flat(now[ids].double() * sc[ids][..., None, None].double())[:, :50]
         assert torch.equal(values, flat(old).double().gather(1, src[..., None].expand(hk, 50, d)) / 128)
+
+
+# --------------------------------------------------------------------------- weigh: on both sides of the choice of a kernel
+@pytest.mark.parametrize("hq,hk,d,new", [
+    (1, 1, 128, [17, 40, 0]), (1, 1, 128, [64, 3, 50]), (1, 1, 128, [65, 3, 64]), (2, 2, 64, [64, 20]), (2, 2, 64, [66, 1]), (7, 1, 96, [9, 2]), (7, 1, 96, [10, 9]),
+    (13, 1, 128, [5, 4]), (33, 1, 64, [2, 1]), (64, 1, 128, [1, 1]), (64, 1, 128, [2, 0]), (2, 1, 256, [24, 9]), (2, 1, 256, [25, 24]), (3, 1, 144, [16, 0]),
+    (3, 1, 192, [17, 5]), (1, 1, 48, [129, 65]), (5, 1, 240, [10, 11])])
+@pytest.mark.parametrize("kv", ["e4m3", "i8"])
+def test_weigh_where_the_kernel_changes(kv, hq, hk, d, new):
+    past = [150, 40, 7][:len(new)]
+    for window, causal in ((None, True), (60, True), (None, False)):
+        _weigh_case(kv, "bf16", hq, hk, d, 16, past, new, causal=causal, padded=len(new) % 2 == 1, window=window, decay=0.5, seed=d + hq, missing=[(0, 2), (1, 1)])
