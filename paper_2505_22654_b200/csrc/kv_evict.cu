@@ -616,9 +616,12 @@ static vscan_status launch_moves(const EvictParams& p, cudaStream_t stream) {
 template <int KV>
 static vscan_status launch_evict(const EvictParams& p, cudaStream_t stream) {
   const int64_t room = static_cast<int64_t>(p.max_blocks) * p.block_size;
-  // many sequences of few tokens: small CTAs, several an SM; else as many threads as there are, latency counts
+  // Where there are no more ranks than two CTAs an SM, the chain of passes counts: as many threads as there is work for.  Where there are more, small
+  // CTAs, several an SM, whose barriers hold up fewer.  Microseconds with 128 / 256 / 512 / 1,024 threads: 64 ranks of 1,000 tokens 12 / 10 / 10 / 11, of
+  // 2,000 18 / 14 / 12 / 12, of 4,000 28 / 18 / 14 / 14, of 16,000 87 / 51 / 33 / 26; 8,192 of 1,000 94 / 121 / 198 / 381, of 2,000 153 / 180 /
+  // 244 / 436, of 4,000 272 / 297 / 364 / 528, of 8,000 598 / 530 / 602 / 786; 1,024 of 2,000 26 / 28 / 37 / 59, of 16,000 312 / 178 / 149 / 168.
   const bool few = static_cast<int64_t>(p.heads) * p.batch <= 2 * 148;
-  const int threads = room <= 512 ? 256 : room <= 1024 ? (few ? 512 : 128) : room <= 4096 ? (few ? 1024 : 256) : 1024;
+  const int threads = room <= 512 ? 256 : room <= 1024 ? (few ? 512 : 128) : room <= 4096 ? (few ? 1024 : 256) : few ? 1024 : 512;
   const int64_t ranks = static_cast<int64_t>(p.heads) * p.batch;
   if (room <= 32 * kRankKeys && !few) {
     prof_before("kv_evict_rank", stream);

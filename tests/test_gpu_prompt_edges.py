@@ -324,3 +324,8 @@ def test_weigh_where_the_kernel_changes(kv, hq, hk, d, new):
     past = [150, 40, 7][:len(new)]
     for window, causal in ((None, True), (60, True), (None, False)):
         _weigh_case(kv, "bf16", hq, hk, d, 16, past, new, causal=causal, padded=len(new) % 2 == 1, window=window, decay=0.5, seed=d + hq, missing=[(0, 2), (1, 1)])
+
+
+def test_evict_of_more_long_tables_than_ctas_stay_resident():
+    """300 ranks of more than 4,096 tokens."""
+    _evict_case("i8", 100, 16, 64, [4200, 4100, 130], [900, 4099, 64], 2, 9, ties=True)
