@@ -544,7 +544,8 @@ vscan_status vscan_kv_attention(const vscan_kv_attention_desc* desc, void* works
  *   max_q_len no sequence has more query rows than this (rows behind it are left as they were)
  * Rows and keys that lie outside the buffers are not there.  Rows that no sequence owns are left as they were.  Elements of out, and
  * of lse, must not overlap each other.
- * Scores, softmax statistics and sums are float32.  For bf16 the weights may be rounded to bf16 before they meet V.
+ * Scores, softmax statistics and sums are float32.  For bf16 the weights may be rounded to bf16 before they meet V, and the factor of a score is
+ * one float32 (lse is off by 2^-23 of the largest score's size more).
  * Workspace: vscan_attention_workspace_bytes(desc), which reads the sizes only.  Calls that may run at the same time (on two streams,
  * or in two graphs) need a workspace each.
  * head_dim: a multiple of 8, at most 256; strides multiples of 16 bytes.  Limits of this build: q_heads / kv_heads <= 64; batch <= 8192;
@@ -577,6 +578,7 @@ vscan_status vscan_attention(const vscan_attention_desc* desc, void* workspace, 
  *   q, lse    of the new rows, in the layouts of vscan_kv_attention: what that call took and gave, or vscan_attention.  A row whose
  *             lse is -inf sees nothing and gives nothing.
  *   max_q_len no sequence has more new rows than this (rows behind it are not there; the launch is chosen from it)
+ * exp(s - lse) is taken in float32: a weight is off by 2^-23 (|s| + |lse|) of itself beside the error of the product.
  * Tokens in blocks whose table entry is not in [0, num_blocks), and behind the table's last column, are passed over.  Sums are float32,
  * in a fixed order.  No two sequences may hold the same block.  No workspace (so nothing tells of a bounded wait that ran out: the tokens
  * it concerned keep the weights that they had).  Limits as for vscan_kv_attention.

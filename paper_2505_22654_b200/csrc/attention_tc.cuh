@@ -18,14 +18,17 @@
 // (32 products of 64) and the exponentials, 32,768 at 16 a cycle, as many; it takes some 3,900: a tile's next scores wait for the products of
 // its weights, since tensor memory is full (two tiles of scores and two of sums, 128 columns each) and the weights lie over their scores.
 // The code of all roles together is more than the instruction cache holds, so what is written shorter here runs faster.
-// Measured: 2 x 9,000 to 12,200 rows, 28 / 4 heads of 128, 1.78 TFLOP: 1.57 to 1.72 ms; 160 x 577 rows, 16 heads of 64, 0.22 TFLOP: 520 us.
+// Measured: 2 x 9,000 to 12,200 rows, 28 / 4 heads of 128, 1.78 TFLOP: 1.56 to 1.84 ms from one GPU to the next; 160 x 577 rows, 16 heads of 64, 0.22
+// TFLOP: 514 to 535 us; 4 x 1,700 to 2,176 rows, 28 / 4 heads of 128: 164 to 172 us.
 // Tried and slower: weights through shared memory with the next scores made ahead (2.2 ms; products whose operands all lie in shared memory
 // take all of its bandwidth), the next scores ahead at 64 channels, where tensor memory has the room (760 us: more instruction cache
 // misses), exponentials on the FMA pipe (by a polynomial of degree 4: 1 to 25 % slower the more of them), one thread a row (1.78 ms, 600 us).
 //
 // The reference that is taken off a row's scores is raised only when a score is over it by 2^kLazy, so the sums are seldom rescaled; weights
-// are then up to 2^kLazy, which bf16 does not mind.  Weights are rounded to bf16, whose error (up to 2^-8 of each weight, of either sign) is
-// averaged over the keys and stays below the rounding of the result; their sum is taken before the rounding.
+// are then up to 2^kLazy, which bf16 does not mind.  Weights are rounded to bf16: both operands of a product have one type, and V in float16
+// would lose its range.  The error, up to 2^-8 of each weight and of either sign, is averaged over the keys and stays below the rounding of the
+// result; their sum is taken before the rounding.  scale log2(e) is one float32 here (two in the CUDA-core kernel), so a weight and lse are off by
+// 2^-24 of the score's size more.
 //
 // Masked weights are 0, but 0 times an infinity is not: in a step that some row does not see in full, values that are not finite are
 // made 0 in shared memory before the product, and what they give to the rows that do see them is put together beside it.
@@ -39,6 +42,9 @@
 namespace vscan {
 namespace kv {
 
+// kPtWhole, kPtExtra: steps up to which a tile is not cut, and what its start and end weigh beside its own steps.  This kernel, us, for 4 prompts of
+// 1,700 to 2,176 rows / encoder layers of 577 / 2 x 9,000 to 12,200 rows: 8 and 4: 154 / 532 / 1,559; 4 and 4: 151 / 543 and a join of 15 / 1,559;
+// 16 and 4: 163 / 532 / 1,560; 8 and 0: 209 / 530 / 1,825; 8 and 2: 166 / 532 / 1,609; 8 and 8: 167 / 532 / 1,610.
 constexpr int kPtThreads = 768, kPtKeys = 128, kPtWhole = 8, kPtExtra = 4;
 constexpr int kPtHelper = 16, kPtIssuer = 20, kPtLoader = 21, kPtPlanner = 22;   // first warp of each role
 constexpr int kPtStages = 4, kPtPlan = 4;

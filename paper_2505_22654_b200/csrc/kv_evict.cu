@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(1024) rank_kernel(EvictParams p) {
 }
 
 // Tables of up to 512 tokens: a warp a (sequence, head), 16 keys a lane in registers, the threshold bit by bit, until n
-// keys, no more, reach it.  8,192 of 240 to 300 tokens: 27 us (45 with a CTA each).  (For the larger tables of a CTA, whose every bit is a
+// keys, no more, reach it.  8,192 of 256 tokens: 26 us (53 with CTAs of 128 threads), of 512: 41 (65).  (For the larger tables of a CTA, whose every bit is a
 // barrier, the passes of the radix select take no longer.)
 constexpr int kRankThreads = 128, kRankKeys = 16;
 

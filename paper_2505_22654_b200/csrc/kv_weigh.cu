@@ -3,6 +3,8 @@
 // exp(scale q k - lse) needs no maximum and no sum of its own: every token's sum over the query rows stands alone.  So the line of
 // (sequence, head, 64 tokens) is cut into equal stretches as for the attention over few rows, but nothing is joined afterwards, and a token's
 // weight is read and written once by the lane that owns it, in a fixed order of the rows.
+// For bf16 queries scale log2(e) is one float32 (two for float32 queries), and lse log2(e) is for both: a weight is off by 2^-24 of the sizes of score
+// and lse, times itself, beside the error of the product.
 #include "kv_weigh_tc.cuh"
 
 namespace vscan {
@@ -175,7 +177,9 @@ __global__ void __launch_bounds__(kMmaThreads, DP == 256 ? 3 : NT > 1 ? 4 : 6) w
 }
 
 // ---------------------------------------------------------------------------------------------- float32 queries
-// Products on the CUDA cores, a lane a token, R rows a pass.
+// Products on the CUDA cores, a lane a token, R rows a pass; codes are read and decoded anew in each.  The exact kernel: for checking, and for models
+// that run in float32.  256 decode steps, 196 to 301 tokens, 32 heads of 128, 277 MB: 127 us, 2.2 TB/s, bound by instructions (a lane reads a
+// token's codes 16 bytes at a time); windows of 512 rows of 900 to 1,000 behind 15,000 tokens, twice, 28 / 4 heads (448 passes): 10.1 ms, 12 TFLOP/s.
 template <int KV, int R>
 __global__ void __launch_bounds__(128) weigh_fma_kernel(WeighParams p) {
   __shared__ __align__(16) float q_sh[R][256];
